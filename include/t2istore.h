@@ -373,6 +373,167 @@ t2i_status t2i_gather_noalloc(const void* pool_dev, uint64_t pool_bytes, uint64_
                               int device, void* cuda_stream);
 
 /* =========================================================================
+ * Keys and values in the store's pages. The paper has no counterpart: a text
+ * model that runs beside the store (a prompt rewriter, a text encoder) keeps
+ * its key/value cache in the same pool, in objects reserved with src = NULL
+ * and used in place, instead of in memory of its own.
+ *
+ * A page holds the rows of `page_tokens` consecutive tokens of one sequence:
+ * [layers][2][kv_heads][page_tokens][head_dim] elements of 16 bits from the
+ * page's start (2: keys, then values); what is left of the page is not used.
+ * A sequence's pages are listed, in token order, in its row of a page table
+ * in device memory. Slot j of a sequence is token j: row j % page_tokens of
+ * the page in column j / page_tokens.
+ *
+ * Every call enqueues its kernels on cuda_stream and returns. Host arguments
+ * and pointers are checked as in the calls above (INVALID, nothing
+ * enqueued). What lies in device memory cannot be: a page number outside the
+ * pool, or a slot behind a table row's end, is never written and reads as
+ * rows of zeros; a sequence whose bounds make no sense has no tokens.
+ * Order with other calls of the store comes from t2i_hold.
+ * ========================================================================= */
+
+#define T2I_BF16 0u
+#define T2I_F16 1u
+#define T2I_F32 2u
+
+/* Gives n objects' pages to cuda_stream, to read and write in place. The
+ * stream is made to wait for every earlier user of the pages (a view of
+ * reads alone needs only their writer: t2i_view). A later call on any stream
+ * that reads, reuses or moves the pages waits for everything cuda_stream was
+ * given up to that call. The hold lasts until the objects are freed, moved
+ * by a compaction (the new pages are not held), put over, or held for
+ * another stream, which then waits for this one. Before cuda_stream writes
+ * pages that another stream was let read (a get, a pull, a view), hold them
+ * again. A repeated id is accepted.
+ * NOT_FOUND / EVICTED for unknown or evicted ids; nothing is held then.      */
+t2i_status t2i_hold(t2i_store* store, const t2i_id* ids, uint32_t n, void* cuda_stream);
+
+typedef struct t2i_kv_layout {
+    uint32_t layers;   /* >= 1: the layers whose rows share a page            */
+    uint32_t kv_heads; /* >= 1                                                */
+    uint32_t head_dim; /* a multiple of 8, at most 128                        */
+    uint32_t dtype;    /* of the cache, and of q and out: T2I_BF16 or T2I_F16 */
+} t2i_kv_layout;
+
+/* Tokens of a page: the largest power of two whose rows fit page_bytes.
+ * INVALID for a bad layout, or if fewer than 8 tokens fit. Host only.        */
+t2i_status t2i_kv_page_tokens(uint64_t page_bytes, const t2i_kv_layout* layout, uint32_t* out);
+
+typedef struct t2i_kv t2i_kv; /* opaque: a layout over one store's pages     */
+
+/* The handle of the calls below: it holds no device memory and no pages.
+ * Destroy it before the store. NULL is accepted by destroy.                  */
+t2i_status t2i_kv_create(t2i_store* store, const t2i_kv_layout* layout, t2i_kv** out);
+t2i_status t2i_kv_destroy(t2i_kv* kv);
+
+/* The sequences of a call and their new tokens, packed: tokens
+ * starts[s] .. starts[s + 1] of the token arrays are sequence s's, its last
+ * ones: with m of them and lens[s] = L, token i is in slot L - m + i.       */
+typedef struct t2i_kv_batch {
+    const int32_t* table;   /* device, [n_seqs][table_stride]: page numbers  */
+    uint64_t table_stride;  /* entries between rows, >= table_pages          */
+    const int32_t* lens;    /* device, [n_seqs]: tokens with the new ones    */
+    const int32_t* starts;  /* device, [n_seqs + 1], not decreasing; NULL:
+                               n_tokens / n_seqs tokens of every sequence    */
+    uint32_t table_pages;   /* entries of a row                              */
+    uint32_t n_seqs;
+    uint32_t n_tokens;      /* rows of the token arrays                      */
+    uint32_t max_new;       /* no sequence has more new tokens (those beyond
+                               are not attended); 0: n_tokens / n_seqs,
+                               without starts                                */
+    uint32_t layer;         /* < layout.layers                               */
+    uint32_t reserved;      /* must be 0                                     */
+} t2i_kv_batch;
+
+/* Token arrays are [n_tokens][heads][head_dim], heads contiguous, *_stride
+ * elements from token to token: 16-byte aligned, strides multiples of 8.    */
+typedef struct t2i_kv_append_desc {
+    t2i_kv_batch batch;
+    const void* q;          /* NULL with q_out NULL: keys and values only    */
+    const void* k;
+    const void* v;
+    void* q_out;            /* of the layout's dtype; may be q itself, with
+                               the same dtype and stride                     */
+    uint64_t q_stride, k_stride, v_stride, q_out_stride;
+    const float* q_norm;    /* device, [head_dim]; NULL: no norm             */
+    const float* k_norm;
+    const float* cos_table; /* device, [n_positions][rotary_dim / 2]         */
+    const float* sin_table;
+    const int32_t* positions; /* device, [n_tokens]; NULL: the token's slot  */
+    uint32_t q_heads;
+    uint32_t in_dtype;      /* of q, k, v: T2I_BF16, T2I_F16 or T2I_F32      */
+    uint32_t rotary_dim;    /* even, <= head_dim: the first elements turn;
+                               0: no rotation                                */
+    uint32_t n_positions;   /* a position outside gives NaN                  */
+    uint32_t interleaved;   /* pairs (2i, 2i + 1); 0: (i, i + rotary_dim / 2) */
+    float eps;
+} t2i_kv_append_desc;
+
+/* Keys and values of new tokens to their slots, queries to q_out. For each
+ * head x of q and k: x * w / sqrt(mean(x^2) + eps) where a norm weight w is
+ * given; then a pair (a, b) turns to (a cos - b sin, b cos + a sin). In fp32,
+ * rounded once. Values are rounded only.                                    */
+t2i_status t2i_kv_append(t2i_kv* kv, const t2i_kv_append_desc* desc, void* cuda_stream);
+
+typedef struct t2i_kv_attend_desc {
+    t2i_kv_batch batch;
+    const void* q;          /* of the layout's dtype                         */
+    void* out;              /* likewise, [n_tokens][q_heads][head_dim]       */
+    float* lse;             /* device, [n_tokens][q_heads]; may be NULL      */
+    uint64_t q_stride, out_stride;
+    const float* slopes;    /* device, [q_heads]; NULL: no bias              */
+    const int32_t* spans;   /* device, [n_tokens][2], 8-byte aligned: slots
+                               first, last + 1 that a token sees; NULL       */
+    const uint64_t* tree;   /* device, [n_tokens]: ancestors of a drafted
+                               token (bit i: it sees new token i); NULL      */
+    uint32_t q_heads;       /* a multiple of kv_heads                        */
+    uint32_t window;        /* 0: none                                       */
+    uint32_t max_len;       /* the longest lens; it sets how work is split,
+                               never a result; 0: what the table holds       */
+    float scale;
+    float softcap;          /* 0: none                                       */
+    uint32_t reserved;      /* must be 0                                     */
+    void* workspace;        /* device, 256-byte aligned, zero before its first
+                               use; calls of one stream at a time share one  */
+    uint64_t workspace_bytes;
+} t2i_kv_attend_desc;
+
+/* Attention of new tokens over their sequences' slots, with q_heads /
+ * kv_heads queries to a key head. Scores s = scale q.k, capped to
+ * softcap * tanh(s / softcap), less slope[head] * |position - position of
+ * the key|. A token in slot p sees slots j <= p; with a window, j > p -
+ * window; with spans, first <= j < last (window must be 0). With a tree
+ * (max_new <= 64, no spans) it sees the slots before the sequence's new
+ * tokens and the new ones of its word, and a new token's position is the
+ * slot of the first one + the number of its ancestors (itself not counted).
+ * out = the softmax's mean of the values, lse = log(sum(exp(s))). A token
+ * that sees nothing has out 0 and lse -infinity. Keys and values that no
+ * token of a call's sequence sees may hold anything.                        */
+t2i_status t2i_kv_attend(t2i_kv* kv, const t2i_kv_attend_desc* desc, void* cuda_stream);
+
+/* Workspace bytes that t2i_kv_attend needs for such a batch at most.         */
+t2i_status t2i_kv_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads,
+                                  uint64_t* out);
+
+typedef struct t2i_kv_commit_desc {
+    const int32_t* table;   /* as in t2i_kv_batch                            */
+    uint64_t table_stride;
+    const int32_t* ctx;     /* device, [n_seqs]: slots before the draft      */
+    const int32_t* path;    /* device, [n_seqs][max_path]: accepted tokens of
+                               the draft, ascending                          */
+    const int32_t* counts;  /* device, [n_seqs]: entries of each path        */
+    uint32_t table_pages;
+    uint32_t n_seqs;
+    uint32_t max_path;
+    uint32_t reserved;      /* must be 0                                     */
+} t2i_kv_commit_desc;
+
+/* Keeps the accepted tokens of a draft: the rows of slot ctx + path[i] move
+ * to slot ctx + i, i < count, in every layer.                               */
+t2i_status t2i_kv_commit(t2i_kv* kv, const t2i_kv_commit_desc* desc, void* cuda_stream);
+
+/* =========================================================================
  * First-layer prefix caching (§5.1). A model of L layers keeps its first L_e
  * layers in the store and streams the rest from host memory while inference
  * runs; T_load / T_comp are one layer's load / inference time. Pure host

@@ -8,3 +8,11 @@ fails loudly if it has not been built.
 """
 from .store import (GET_DTYPE, MOVE_DTYPE, PUT_DTYPE, Ctl, Store, T2IError, e2e_latency, gather_noalloc,  # noqa: F401
                     get_descs, pipeline_latency, prefix_layers, prefix_layers_pipeline, put_descs)
+
+
+def __getattr__(name):
+    # the key/value cache works on torch tensors; the store alone does without torch
+    if name in ("KVCache", "page_tokens"):
+        from . import kv
+        return getattr(kv, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

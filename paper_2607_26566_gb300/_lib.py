@@ -55,6 +55,12 @@ class PagedObject(C.Structure):
     _fields_ = [("nbytes", C.c_uint64), ("pages", C.c_void_p), ("n_pages", C.c_uint32), ("dtype_tag", C.c_uint32)]
 
 
+class KvLayout(C.Structure):
+    _fields_ = [("layers", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("dtype", C.c_uint32)]
+
+
+BF16, F16, F32 = 0, 1, 2
+
 _P = C.c_void_p
 _S = C.c_int32
 _U32 = C.c_uint32
@@ -93,6 +99,14 @@ PROTOTYPES = {
     "t2i_ctl_stats": (_S, [_P, C.POINTER(Stats)]),
     "t2i_ctl_last_error": (C.c_char_p, [_P]),
     "t2i_gather_noalloc": (_S, [_P, _U64, _U64, _PU32, _U32, _U64, _P, _U64, _U32, C.c_int, _P]),
+    "t2i_hold": (_S, [_P, _P, _U32, _P]),
+    "t2i_kv_page_tokens": (_S, [_U64, C.POINTER(KvLayout), C.POINTER(_U32)]),
+    "t2i_kv_create": (_S, [_P, C.POINTER(KvLayout), C.POINTER(_P)]),
+    "t2i_kv_destroy": (_S, [_P]),
+    "t2i_kv_append": (_S, [_P, _P, _P]),
+    "t2i_kv_attend": (_S, [_P, _P, _P]),
+    "t2i_kv_workspace_bytes": (_S, [_P, _U32, _U32, _U32, _PU64]),
+    "t2i_kv_commit": (_S, [_P, _P, _P]),
     "t2i_e2e_latency": (_S, [_U32, _U32, C.c_double, C.c_double, C.POINTER(C.c_double)]),
     "t2i_prefix_layers": (_S, [_U32, C.c_double, C.c_double, _PU32]),
     "t2i_pipeline_latency": (_S, [C.POINTER(C.c_double), C.POINTER(C.c_double), _U32, _U32, C.POINTER(C.c_double)]),

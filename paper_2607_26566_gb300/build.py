@@ -24,11 +24,15 @@ LIB = os.path.join(PKG, "libt2istore.so")
 # against LIB
 PYCALL_SRC = "pycall.c"
 PYCALL = os.path.join(PKG, "_pycall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+# ... and for those of the key/value cache (csrc/kvcall.cpp), against torch's headers too
+KVCALL_SRC = "kvcall.cpp"
+KVCALL = os.path.join(PKG, "_kvcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CXX_SOURCES = ["control.cpp", "ctl_capi.cpp", "prefix.cpp"]
-CU_SOURCES = ["store.cu"]
-HEADERS = ["control.hpp", "common.hpp", "deps.hpp", "kernels.cuh", "launch.cuh", "exports.map"]
+CU_SOURCES = ["store.cu", "kv.cu", "kv_append.cu", "kv_attend.cu"]
+HEADERS = ["control.hpp", "common.hpp", "deps.hpp", "kernels.cuh", "launch.cuh", "store_access.hpp", "kv.hpp",
+           "kv_device.cuh", "exports.map"]
 
 
 def _cuda_home() -> str:
@@ -41,7 +45,7 @@ def _cuda_home() -> str:
 
 
 def _inputs() -> list[str]:
-    files = [os.path.join(CSRC, f) for f in CXX_SOURCES + CU_SOURCES + HEADERS + [PYCALL_SRC]]
+    files = [os.path.join(CSRC, f) for f in CXX_SOURCES + CU_SOURCES + HEADERS + [PYCALL_SRC, KVCALL_SRC]]
     return files + [os.path.join(INCLUDE, "t2istore.h"), os.path.abspath(__file__)]
 
 
@@ -62,7 +66,7 @@ def _have_python_h() -> bool:
 
 
 def is_stale() -> bool:
-    outs = [LIB] + ([PYCALL] if _have_python_h() else [])
+    outs = [LIB] + ([PYCALL, KVCALL] if _have_python_h() else [])
     if not all(os.path.exists(f) for f in outs):
         return True
     t = min(os.path.getmtime(f) for f in outs)
@@ -117,9 +121,10 @@ def build(verbose: bool = False, ptxas_info: bool = False, defines=(), out: str 
     if out is None:
         if _have_python_h():
             build_pycall(verbose)
+            build_kvcall(verbose)
         else:
-            # the ctypes binding serves every call; only its per-call cost is higher
-            sys.stderr.write("build: Python.h not found; the CPython binding (_pycall) is not built\n")
+            # the ctypes binding serves every call of the store; only its per-call cost is higher
+            sys.stderr.write("build: Python.h not found; the CPython bindings are not built (no KVCache)\n")
     return lib_path
 
 
@@ -139,6 +144,31 @@ def build_pycall(verbose: bool = False) -> str:
         raise RuntimeError("CPython binding build failed: " + " ".join(cmd))
     os.replace(tmp, PYCALL)
     return PYCALL
+
+
+def build_kvcall(verbose: bool = False) -> str:
+    """Compiles the CPython module of csrc/kvcall.cpp next to LIB, against the
+    installed torch's headers and libraries. Raises on failure."""
+    import importlib.util
+
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        raise RuntimeError("torch not found: the key/value cache's binding cannot be built")
+    torch_dir = os.path.dirname(spec.origin)
+    lib = os.path.join(torch_dir, "lib")
+    tmp = KVCALL + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", os.path.join(CSRC, KVCALL_SRC),
+           "-I" + INCLUDE, "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(torch_dir, "include"),
+           "-I" + os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+           "-I" + os.path.join(_cuda_home(), "include"), "-L" + PKG, "-lt2istore", "-L" + lib, "-ltorch_python", "-lc10",
+           "-lc10_cuda", "-Wl,-rpath,$ORIGIN:" + lib, "-o", tmp]
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if verbose or r.returncode:
+        sys.stderr.write(r.stdout)
+    if r.returncode:
+        raise RuntimeError("CPython binding build failed: " + " ".join(cmd))
+    os.replace(tmp, KVCALL)
+    return KVCALL
 
 
 def build_cdriver() -> str:

@@ -146,6 +146,18 @@ class StreamDeps {
         streams_[cur_].viewed = true;
     }
 
+    // The current stream reads and writes the page in place from now on, beyond
+    // its calls: later users on other streams wait for all it was given by then.
+    // (The caller has let it wait as for a write.)
+    void mark_hold(uint32_t page) {
+        PageDeps& d = pages_[page];
+        d.writer = {kOpen, static_cast<uint16_t>(cur_)};
+        d.readers[0] = d.readers[1] = Dep{};
+        d.more_readers = 0;
+        d.viewer = static_cast<uint16_t>(cur_ + 1);
+        streams_[cur_].viewed = true;
+    }
+
     // Waits on the host for everything every known stream has been given.
     void synchronize_all() {
         for (State& st : streams_) {

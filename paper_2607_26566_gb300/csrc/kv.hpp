@@ -1,0 +1,89 @@
+// The key/value cache in the store's pages: what its host side (kv.cu) and its
+// kernels (kv_append.cu, kv_attend.cu) share. The calls are described in
+// include/t2istore.h.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace t2i {
+
+// Where the rows of one layer lie.
+struct KvPages {
+    uint64_t pool;         // device address of page 0
+    uint64_t page_bytes;
+    uint32_t total_pages;
+    uint32_t token_shift;  // log2 of the tokens of a page
+    uint32_t kv_heads;
+    uint32_t head_dim;
+    uint32_t layers;
+    uint32_t layer;
+    const int32_t* table;
+    uint64_t table_stride;
+    uint32_t table_pages;
+};
+
+// A call's sequences and their new tokens.
+struct KvTokens {
+    const int32_t* lens;
+    const int32_t* starts;  // null: `each` tokens of every sequence
+    uint32_t each;
+    uint32_t n_seqs;
+    uint32_t n_tokens;
+    uint32_t max_new;
+};
+
+struct KvAppend {
+    KvPages pages;
+    KvTokens tok;
+    const void* q;
+    const void* k;
+    const void* v;
+    void* q_out;
+    uint64_t q_stride, k_stride, v_stride, q_out_stride;
+    const float* q_norm;
+    const float* k_norm;
+    const float* cos_table;
+    const float* sin_table;
+    const int32_t* positions;
+    uint32_t q_heads;  // 0: keys and values only
+    uint32_t rotary_dim;
+    uint32_t n_positions;
+    uint32_t interleaved;
+    float eps;
+};
+
+struct KvAttend {
+    KvPages pages;
+    KvTokens tok;
+    const void* q;
+    void* out;
+    float* lse;
+    uint64_t q_stride, out_stride;
+    const float* slopes;
+    const int32_t* spans;
+    const uint64_t* tree;
+    uint32_t q_heads;
+    uint32_t group;  // q_heads / kv_heads
+    uint32_t window;
+    uint32_t max_len;
+    float scale;
+    float softcap;
+};
+
+struct KvCommit {
+    KvPages pages;
+    const int32_t* ctx;
+    const int32_t* path;
+    const int32_t* counts;
+    uint32_t n_seqs;
+    uint32_t max_path;
+};
+
+// dtype and in_dtype: T2I_BF16, T2I_F16, T2I_F32
+cudaError_t launch_kv_append(const KvAppend& a, uint32_t dtype, uint32_t in_dtype, cudaStream_t stream);
+cudaError_t launch_kv_commit(const KvCommit& c, cudaStream_t stream);
+cudaError_t launch_kv_attend(const KvAttend& a, uint32_t dtype, cudaStream_t stream);
+
+}  // namespace t2i

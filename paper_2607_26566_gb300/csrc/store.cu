@@ -15,6 +15,7 @@
 #include "control.hpp"
 #include "deps.hpp"
 #include "kernels.cuh"
+#include "store_access.hpp"
 
 namespace t2i {
 namespace {
@@ -143,6 +144,13 @@ class Store {
     }
     t2i_status compact(uint64_t limit_bytes, cudaStream_t stream, uint64_t* moved);
     t2i_status view(t2i_id id, cudaStream_t stream, void** ptr, uint64_t* nbytes);
+    t2i_status hold(const t2i_id* ids, uint32_t n, cudaStream_t stream);
+    // for the calls that use pages in place (store_access.hpp)
+    StoreInfo info() const { return {pool_, ctl_.total_pages(), cfg_.page_bytes, device_}; }
+    void check_begin() { access_cache_ = Range{}; }
+    const char* check_access(const void* p, uint64_t n);
+    bool may_launch() { return !(launcher_.fail_countdown && --launcher_.fail_countdown == 0); }
+    void launched() { ctl_.counters().launches++; }
     t2i_status pull_from(Store& src, const t2i_id* ids, uint32_t n, uint32_t consumers, t2i_id* out_ids,
                          t2i_status* per_item, cudaStream_t stream);
     t2i_status pull_pages(const void* src_pool, uint64_t src_pool_bytes, const t2i_paged_object* objs, uint32_t n,
@@ -195,6 +203,7 @@ class Store {
     std::vector<uint8_t> use_ce_;      // 1: the copy engine moves it
     std::vector<Seg> segs_;
     std::vector<t2i_move> batch_;  // the moves of one compaction launch
+    Range access_cache_;           // the allocation that check_access saw last
     // moves per compaction launch: one 24-byte descriptor each
     static constexpr size_t kMovesPerLaunch = 1024;
 #ifndef T2I_TUNE_COMPACT_FIRST
@@ -541,6 +550,51 @@ t2i_status Store::view(t2i_id id, cudaStream_t stream, void** ptr, uint64_t* nby
     for (uint32_t pg : o->pages) deps_.mark_view(pg);
     *ptr = reinterpret_cast<void*>(pool_ + (uint64_t(o->pages[0]) << page_shift_));
     return T2I_OK;
+}
+
+t2i_status Store::hold(const t2i_id* ids, uint32_t n, cudaStream_t stream) {
+    if (n == 0) return T2I_OK;
+    if (!ids) {
+        err_ = "hold: null id array";
+        return T2I_ERR_INVALID;
+    }
+    objs_.resize(n);
+    for (uint32_t i = 0; i < n; ++i) {
+        objs_[i] = ctl_.find(ids[i]);
+        if (!objs_[i]) {
+            const bool gone = ctl_.is_evicted(ids[i]);
+            err_ = "hold: item " + std::to_string(i) + (gone ? ": id was evicted" : ": id not found");
+            return gone ? T2I_ERR_EVICTED : T2I_ERR_NOT_FOUND;
+        }
+    }
+    DeviceGuard g(device_);
+    int si = 0;
+    const t2i_status st = stream_slot(stream, &si);
+    if (st != T2I_OK) return st;
+    deps_.begin(si);
+    for (uint32_t i = 0; i < n; ++i)
+        for (uint32_t pg : objs_[i]->pages) deps_.writes(pg);
+    const cudaError_t we = deps_.wait();
+    if (we != cudaSuccess) return cuda_fail("hold: cannot order after earlier calls", we);
+    for (uint32_t i = 0; i < n; ++i)
+        for (uint32_t pg : objs_[i]->pages) deps_.mark_hold(pg);
+    return T2I_OK;
+}
+
+const char* Store::check_access(const void* p, uint64_t n) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    if (n == 0) return nullptr;
+    if (!p) return "null buffer";
+    if (a + n < a) return "the range wraps around";
+    if (overlaps_pool(a, n)) return "it overlaps the store's pool";
+    if (!cfg_.check_pointers) return nullptr;
+    Range& r = access_cache_;
+    if (!(r.kind != MemKind::Unknown && a >= r.start && a + n <= r.end) && !query_range(p, &r))
+        return "the CUDA driver cannot describe the pointer";
+    if (r.kind != MemKind::Device && r.kind != MemKind::Managed) return "not device memory";
+    if (r.kind == MemKind::Device && r.device != device_) return "it lives on another device";
+    if (a + n > r.end) return "the range runs past the end of its allocation";
+    return nullptr;
 }
 
 // The consumer's store (this) allocates pages for the producer's objects and
@@ -934,6 +988,10 @@ t2i_status t2i_view(t2i_store* store, t2i_id id, void* cuda_stream, void** dev_p
     T2I_STORE_CALL(store, store->s->view(id, static_cast<cudaStream_t>(cuda_stream), dev_ptr, nbytes));
 }
 
+t2i_status t2i_hold(t2i_store* store, const t2i_id* ids, uint32_t n, void* cuda_stream) {
+    T2I_STORE_CALL(store, store->s->hold(ids, n, static_cast<cudaStream_t>(cuda_stream)));
+}
+
 t2i_status t2i_pull(t2i_store* dst, t2i_store* src, const t2i_id* src_ids, uint32_t n, uint32_t consumers,
                     t2i_id* out_ids, t2i_status* per_item, void* cuda_stream) {
     if (!dst || !src) return T2I_ERR_INVALID;
@@ -985,6 +1043,17 @@ const char* t2i_last_error(const t2i_store* store) {
 }
 
 }  // extern "C"
+
+// ============================================ for the other translation units
+namespace t2i {
+StoreInfo store_info(t2i_store* s) { return s->s->info(); }
+std::mutex& store_mutex(t2i_store* s) { return s->s->mu; }
+void store_set_error(t2i_store* s, std::string e) { s->s->set_error(std::move(e)); }
+void store_check_begin(t2i_store* s) { s->s->check_begin(); }
+const char* store_check(t2i_store* s, const void* p, uint64_t n) { return s->s->check_access(p, n); }
+bool store_may_launch(t2i_store* s) { return s->s->may_launch(); }
+void store_launched(t2i_store* s) { s->s->launched(); }
+}  // namespace t2i
 
 // ================================================= gather without allocation
 // t2i_gather_noalloc: the gather of one object's pages for callers that

@@ -359,6 +359,11 @@ class Store:
         st = self._lib.t2i_view(self._h, oid, _stream(stream), C.byref(ptr), C.byref(n))
         return st, int(ptr.value or 0), int(n.value)
 
+    def hold(self, ids, stream=None) -> int:
+        """t2i_hold: the objects' pages are ``stream``'s to read and write in place."""
+        ids = np.ascontiguousarray(ids, np.uint64)
+        return self._lib.t2i_hold(self._h, ids.ctypes.data, len(ids), _stream(stream))
+
     def tensor_view(self, oid: int, dtype=None, shape=None, stream=None):
         """The object as a tensor over the pool, without a copy (the pool must
         be a torch tensor): status, tensor (None on failure)."""
