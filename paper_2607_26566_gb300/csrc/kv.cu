@@ -1,9 +1,11 @@
 // The host side of the key/value cache in the store's pages: the t2i_kv_* C
 // ABI, its checks, and the launches.
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include <cmath>
+#include <memory>
 #include <string>
 
 #include "common.hpp"
@@ -16,6 +18,10 @@ struct t2i_kv {
     t2i::StoreInfo info;
     t2i_kv_layout layout;
     uint32_t token_shift;
+    uint32_t sms;
+    uint32_t* fault;       // pinned: a kernel's wait ran out
+    uint32_t* fault_dev;
+    CUtensorMap map;
 };
 
 namespace t2i {
@@ -164,6 +170,14 @@ t2i_status launch(t2i_kv* kv, const char* call, Launch&& go) {
     return T2I_OK;
 }
 
+// Reported once, by the first call after it: what the kernel wrote is not valid.
+t2i_status past_fault(t2i_kv* kv) {
+    if (*static_cast<volatile uint32_t*>(kv->fault) == 0) return T2I_OK;
+    *kv->fault = 0;
+    store_set_error(kv->store, "an earlier attention kernel gave up waiting for its own loads: its results are not valid");
+    return T2I_ERR_CUDA;
+}
+
 t2i_status append(t2i_kv* kv, const t2i_kv_append_desc& d, cudaStream_t stream) {
     Checks c(kv, "kv_append");
     const uint32_t K = kv->layout.kv_heads, D = kv->layout.head_dim;
@@ -216,7 +230,7 @@ t2i_status append(t2i_kv* kv, const t2i_kv_append_desc& d, cudaStream_t stream) 
     return launch(kv, "kv_append", [&] { return launch_kv_append(a, kv->layout.dtype, d.in_dtype, stream); });
 }
 
-uint64_t workspace_bytes(const t2i_kv*, uint32_t, uint32_t, uint32_t) { return 256; }
+uint64_t workspace_bytes(const t2i_kv* kv, uint32_t, uint32_t, uint32_t) { return kv_few_workspace(kv->sms); }
 
 t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) {
     Checks c(kv, "kv_attend");
@@ -228,6 +242,8 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     c.require(d.batch.max_new || !d.batch.starts, "with starts, max_new must be given");
     if (!c.batch(d.batch)) return c.ok() ? T2I_OK : T2I_ERR_INVALID;
     KvAttend a{};
+    const t2i_status past = past_fault(kv);
+    if (past != T2I_OK) return past;
     a.tok = tokens_of(d.batch);
     c.require(!d.tree || a.tok.max_new <= 64, "a tree has at most 64 tokens");
     const uint64_t n = d.batch.n_tokens;
@@ -254,7 +270,12 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     a.max_len = d.max_len;
     a.scale = d.scale;
     a.softcap = d.softcap;
-    return launch(kv, "kv_attend", [&] { return launch_kv_attend(a, kv->layout.dtype, stream); });
+    if (uint64_t(a.group) * a.tok.max_new > kFewRows)
+        return launch(kv, "kv_attend", [&] { return launch_kv_attend(a, kv->layout.dtype, stream); });
+    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms};
+    return launch(kv, "kv_attend", [&] {
+        return kv->layout.dtype == T2I_BF16 ? launch_kv_few_bf16(a, l, stream) : launch_kv_few_f16(a, l, stream);
+    });
 }
 
 t2i_status commit(t2i_kv* kv, const t2i_kv_commit_desc& d, cudaStream_t stream) {
@@ -274,6 +295,29 @@ t2i_status commit(t2i_kv* kv, const t2i_kv_commit_desc& d, cudaStream_t stream) 
     a.n_seqs = d.n_seqs;
     a.max_path = d.max_path;
     return launch(kv, "kv_commit", [&] { return launch_kv_commit(a, stream); });
+}
+
+using PFN_encodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                     const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                     CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The pool's pages for TMA (KvLaunch::map): null, or why not.
+const char* encode_map(t2i_kv* kv) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+        return "the driver has no tensor maps";
+    const t2i_kv_layout& l = kv->layout;
+    const cuuint64_t dims[3] = {l.head_dim, (cuuint64_t(l.layers) * 2 * l.kv_heads) << kv->token_shift, kv->info.total_pages};
+    const cuuint64_t strides[2] = {l.head_dim * 2u, kv->info.page_bytes};
+    const cuuint32_t box[3] = {64, kv->token_shift < 7 ? 1u << kv->token_shift : 128u, 1};
+    const cuuint32_t step[3] = {1, 1, 1};
+    const CUresult r = reinterpret_cast<PFN_encodeTiled>(p)(
+        &kv->map, l.dtype == T2I_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+        reinterpret_cast<void*>(kv->info.pool), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? nullptr : "the driver refuses a tensor map of the pool";
 }
 
 }  // namespace
@@ -318,7 +362,30 @@ t2i_status t2i_kv_create(t2i_store* store, const t2i_kv_layout* layout, t2i_kv**
     try {
         uint32_t shift = 0;
         while ((1u << shift) < tokens) ++shift;
-        *out = new t2i_kv{store, info, *layout, shift};
+        t2i::DeviceScope g(info.device);
+        std::unique_ptr<t2i_kv> kv(new t2i_kv{});
+        kv->store = store;
+        kv->info = info;
+        kv->layout = *layout;
+        kv->token_shift = shift;
+        int sms = 0;
+        cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, info.device);
+        kv->sms = uint32_t(sms);
+        if (const char* why = e == cudaSuccess ? t2i::encode_map(kv.get()) : "cannot query the device") {
+            t2i::set_thread_error(std::string("t2i_kv_create: ") + why);
+            return T2I_ERR_CUDA;
+        }
+        e = cudaHostAlloc(reinterpret_cast<void**>(&kv->fault), sizeof(uint32_t), cudaHostAllocMapped);
+        if (e == cudaSuccess) {
+            *kv->fault = 0;
+            e = cudaHostGetDevicePointer(reinterpret_cast<void**>(&kv->fault_dev), kv->fault, 0);
+            if (e != cudaSuccess) cudaFreeHost(kv->fault);
+        }
+        if (e != cudaSuccess) {
+            t2i::set_thread_error(std::string("t2i_kv_create: pinned host memory: ") + cudaGetErrorString(e));
+            return T2I_ERR_CUDA;
+        }
+        *out = kv.release();
     } catch (const std::exception& e) {
         t2i::set_thread_error(std::string("t2i_kv_create: host error: ") + e.what());
         return T2I_ERR_INVALID;
@@ -327,6 +394,9 @@ t2i_status t2i_kv_create(t2i_store* store, const t2i_kv_layout* layout, t2i_kv**
 }
 
 t2i_status t2i_kv_destroy(t2i_kv* kv) {
+    if (!kv) return T2I_OK;
+    t2i::DeviceScope g(kv->info.device);
+    cudaFreeHost(kv->fault);  // (waits for kernels that may write it)
     delete kv;
     return T2I_OK;
 }

@@ -3,6 +3,7 @@
 // include/t2istore.h.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -85,5 +86,20 @@ struct KvCommit {
 cudaError_t launch_kv_append(const KvAppend& a, uint32_t dtype, uint32_t in_dtype, cudaStream_t stream);
 cudaError_t launch_kv_commit(const KvCommit& c, cudaStream_t stream);
 cudaError_t launch_kv_attend(const KvAttend& a, uint32_t dtype, cudaStream_t stream);
+
+// What an attention launch needs beside its arguments.
+struct KvLaunch {
+    // the pool as [pages][rows of a page][head_dim], in boxes of 64 elements by
+    // min(page tokens, 128) rows, 128-byte swizzle; elements outside read as zeros
+    const CUtensorMap* map;
+    void* workspace;
+    uint32_t* fault;  // host memory that the device writes: not 0 after a wait that ran out
+    uint32_t sms;
+};
+// up to this many queries to a key head (new tokens of a sequence x heads of a group)
+constexpr uint32_t kFewRows = 64;
+cudaError_t launch_kv_few_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
+cudaError_t launch_kv_few_f16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
+uint64_t kv_few_workspace(uint32_t sms);
 
 }  // namespace t2i

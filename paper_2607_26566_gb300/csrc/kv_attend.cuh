@@ -1,0 +1,82 @@
+// What the attention kernels over the cache share: which slots a sequence's new
+// tokens see, and the scores.
+#pragma once
+
+#include "kv_device.cuh"
+#include "tc.cuh"
+
+namespace t2i {
+
+constexpr int kTileKeys = 128;       // keys of a tile
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Slots [lo, hi) outside which none of tokens [t0, t1) of sequence q sees anything,
+// and slots [all_lo, all_hi) that all of them see.
+struct KvSpan {
+    int32_t lo, hi, all_lo, all_hi;
+};
+__device__ __forceinline__ KvSpan kv_span(const KvAttend& a, const KvSeq& q, int32_t t0, int32_t t1) {
+    const int32_t ctx = q.len - q.n;
+    KvSpan r;
+    if (a.spans) {
+        r = {INT32_MAX, 0, 0, INT32_MAX};
+        for (int32_t i = t0; i < t1; ++i) {
+            const int2 s = reinterpret_cast<const int2*>(a.spans)[q.first + i];
+            const int32_t f = max(s.x, 0), l = min(s.y, q.len);
+            if (l > f) r.lo = min(r.lo, f), r.hi = max(r.hi, l);
+            r.all_lo = max(r.all_lo, f), r.all_hi = min(r.all_hi, l);
+        }
+        if (r.lo >= r.hi) r.lo = r.hi = 0;
+        return r;
+    }
+    const int64_t w = a.window ? int64_t(a.window) : int64_t(INT32_MAX);
+    if (a.tree) {
+        // positions lie between ctx - 1 (a word without bits) and ctx + n - 1
+        r.lo = int32_t(max(int64_t(0), ctx - w));
+        r.hi = q.len;
+        r.all_lo = a.window ? int32_t(max(int64_t(0), ctx + q.n - w)) : 0;
+        r.all_hi = ctx;
+        return r;
+    }
+    r.lo = int32_t(max(int64_t(0), ctx + t0 + 1 - w));
+    r.hi = ctx + t1;
+    r.all_lo = int32_t(max(int64_t(0), ctx + t1 - w));
+    r.all_hi = ctx + t0 + 1;
+    return r;
+}
+
+// One query: it sees the keys of slots below `last`, and of the drafted tokens in
+// `word`, whose position is `first` or above. pos: its own position.
+struct KvQuery {
+    int32_t first, last, pos;
+    uint64_t word;
+};
+__device__ __forceinline__ KvQuery kv_query(const KvAttend& a, const KvSeq& q, int32_t i) {
+    const int32_t ctx = q.len - q.n, t = q.first + i;
+    KvQuery r;
+    r.word = 0;
+    r.pos = ctx + i;
+    r.last = r.pos + 1;
+    if (a.tree) {
+        r.word = a.tree[t];
+        r.pos = ctx + __popcll(r.word) - 1;
+        r.last = ctx;
+    }
+    r.first = a.window ? int32_t(max(int64_t(0), int64_t(r.pos) + 1 - int64_t(a.window))) : 0;
+    if (a.spans) {
+        const int2 s = reinterpret_cast<const int2*>(a.spans)[t];
+        r.first = max(s.x, 0), r.last = min(s.y, q.len);
+    }
+    return r;
+}
+
+// A score in units of log2, from a raw product: scaled; MOD: capped and less the
+// distance's bias (slope and cap in log2 units; cap_in = scale / softcap).
+__device__ __forceinline__ float capped(float s, float cap_in, float cap) {
+    // tanh(y) = 1 - 2 / (exp(2y) + 1), within 2e-7
+    const float e = tc::exp2_approx(s * cap_in * (2.0f * kLog2e));
+    return cap - 2.0f * cap * tc::rcp_approx(e + 1.0f);
+}
+
+}  // namespace t2i

@@ -76,6 +76,7 @@ struct Kv16<__nv_bfloat16> {
         const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&r);
     }
+    static __device__ __forceinline__ __nv_bfloat16 from1(float a) { return __float2bfloat16_rn(a); }
 };
 template <>
 struct Kv16<__half> {
@@ -84,6 +85,7 @@ struct Kv16<__half> {
         const __half2 r = __floats2half2_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&r);
     }
+    static __device__ __forceinline__ __half from1(float a) { return __float2half_rn(a); }
 };
 
 // Eight consecutive elements as fp32, and back to 16 bits.

@@ -1,0 +1,674 @@
+// Attention of few new tokens a sequence (a decoding step, a drafted tree, a short
+// chunk): up to 64 queries to a key head.
+//
+// Such a call reads every key and value once and does little with it, so it is
+// bound by memory: the kernel's business is to keep loads in flight on every SM.
+// The products are turned round: S^T = K Q^T and O^T = V^T P^T, so that the 128
+// rows that a tensor core product has are keys (and dimensions of V), not padded
+// queries, and K and V go from memory (TMA) through shared memory to the tensor
+// cores without passing a register. A thread of the softmax warps is one key of a
+// 128-key tile, and, for the accumulators, one dimension.
+//
+// Work split: all tiles of all (sequence, key head) units, in order, are cut into
+// as many equal runs as there are SMs, whatever the lengths. A unit that lies in
+// several runs is joined by a second kernel from partial sums in the workspace,
+// in the order of the runs: results do not depend on timing.
+//
+// Softmax: the running maximum of a query is raised only when a score exceeds it by
+// 2^8 (the accumulators, in fp32, have the room), so most tiles need no exchange
+// between threads but one vote. Weights go to the product as two 16-bit numbers
+// (the rounded weight and what the rounding left): products are not what bounds
+// this kernel, and the weights keep 16 bits or more.
+#pragma once
+
+#include <atomic>
+#include <type_traits>
+
+#include "kv_attend.cuh"
+#include "t2istore.h"
+
+namespace t2i {
+namespace {
+
+using namespace tc;
+
+constexpr int kSoftThreads = 128;
+constexpr int kThreads = kSoftThreads + 64;  // + the loading warp and the product warp
+constexpr uint32_t kSlot = 16384;            // 128 rows of 64 elements
+constexpr float kRaise = 8.0f;
+
+template <int N, int NS>
+struct Shape {
+    // shared memory: ring of K and V tiles, queries, weights (and what stands in
+    // static shared memory: kFixed at most). A product over heads of 64 reads the
+    // 16 KiB behind its V tile too, for rows that nobody looks at.
+    static constexpr uint32_t kFixed = 2048 + 48 * N;
+    static constexpr uint32_t kPad = NS == 1 ? kSlot : 0;
+    static constexpr uint32_t kQ = N * 128 * NS;
+    static constexpr uint32_t kP = N * 512;  // two parts
+    static constexpr uint32_t kEntry = kSlot * NS;
+    static constexpr uint32_t kRoom = 227 * 1024 - 1024 - kFixed - kQ - kP - kPad;
+    static constexpr uint32_t kEntries = kRoom / kEntry < 12 ? kRoom / kEntry : 12;
+    static constexpr uint32_t kBytes = 1024 + kEntry * kEntries + kQ + kP + kPad;
+    static constexpr uint32_t kTmem = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;
+    static_assert(kEntries >= 2, "a tile of K and one of V");
+    static constexpr uint32_t kPart = N * (64 * NS) + 2 * N;  // floats of a part: O^T, maxima, sums
+};
+
+struct Shared {
+    uint64_t full[12], empty[12];
+    uint64_t s_full[2], p_full, pv_done, q_full;
+    uint32_t tmem, dead;
+    int32_t start_seq, start_rest;
+    int64_t sums[kThreads / 32];
+};
+
+// The run of tiles of one block, segment by segment (a segment: the tiles of the
+// run that lie in one unit). Every warp walks it on its own.
+struct Walk {
+    uint32_t s, h;
+    int64_t at, end;    // the next tile of all, and the end of the run
+    int64_t unit;       // the unit's first tile of all
+    int32_t tile, n, nt;  // the segment's first tile in the unit, its tiles, the unit's
+    KvSeq q;
+    KvSpan span;
+    int32_t rows;
+};
+
+// A unit in several runs, noted at the run that holds its second part: the runs
+// b0 to b1 hold it, the first as that block's part 0 or 1, the others as part 0.
+struct Join {
+    int32_t s, h, b0, b1, second, valid;
+};
+
+struct Few {
+    KvAttend a;
+    Join* join;        // [blocks]
+    float* part;       // [2 * blocks][kPart]
+    uint32_t* fault;   // host-mapped: set where a wait ran out
+};
+
+__device__ __forceinline__ int32_t unit_tiles(const KvAttend& a, const KvSeq& q, KvSpan& sp) {
+    if (q.n == 0) return 0;
+    sp = kv_span(a, q, 0, min(q.n, int32_t(a.tok.max_new)));
+    return max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
+}
+
+__device__ __forceinline__ void walk_seq(const KvAttend& a, Walk& w) {
+    w.nt = 0;
+    for (; w.s < a.tok.n_seqs; ++w.s) {
+        w.q = kv_seq(a.pages, a.tok, w.s);
+        w.nt = unit_tiles(a, w.q, w.span);
+        if (w.nt) break;
+    }
+    w.rows = min(w.q.n, int32_t(a.tok.max_new)) * int32_t(a.group);
+}
+__device__ __forceinline__ void walk_start(const KvAttend& a, Walk& w, uint32_t s, int32_t rest, int64_t at, int64_t end) {
+    w.s = s, w.at = at, w.end = end;
+    walk_seq(a, w);
+    const int32_t nt = max(w.nt, 1);
+    w.h = rest / nt;
+    w.tile = rest % nt;
+    w.unit = at - w.tile;
+    w.n = int32_t(min(int64_t(w.nt - w.tile), end - at));
+}
+__device__ __forceinline__ bool walk_next(const KvAttend& a, Walk& w) {
+    w.at += w.n;
+    if (w.at >= w.end) return false;
+    w.tile = 0;
+    w.unit = w.at;
+    if (++w.h == a.pages.kv_heads) {
+        w.h = 0;
+        ++w.s;
+        walk_seq(a, w);
+        if (w.nt == 0) return false;
+    }
+    w.n = int32_t(min(int64_t(w.nt), w.end - w.at));
+    return true;
+}
+// first slot of the unit's tile i
+__device__ __forceinline__ int32_t tile_slot(const Walk& w, int32_t i) { return (w.span.lo / kTileKeys + i) * kTileKeys; }
+
+// Sum or maximum over a warp's lanes of each of n = 16 or 32 columns: lane i gets
+// column i % n.
+template <int n, bool kMax>
+__device__ __forceinline__ float columns(float (&v)[n], uint32_t lane) {
+    auto join = [](float x, float y) { return kMax ? fmaxf(x, y) : x + y; };
+    if constexpr (n == 16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = join(v[i], __shfl_xor_sync(0xFFFFFFFFu, v[i], 16));
+    }
+#pragma unroll
+    for (int d = n / 2; d; d >>= 1) {
+        const bool up = lane & d;
+#pragma unroll
+        for (int i = 0; i < d; ++i) {
+            const float keep = up ? v[i + d] : v[i], send = up ? v[i] : v[i + d];
+            v[i] = join(keep, __shfl_xor_sync(0xFFFFFFFFu, send, d));
+        }
+    }
+    return v[0];
+}
+
+template <class T, int N, int NS, bool MOD>
+__global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant__ Few f, const __grid_constant__ CUtensorMap map) {
+    using Sh = Shape<N, NS>;
+    constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+    constexpr int C = N < 32 ? N : 32;  // columns at a time
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    uint8_t* const mem = raw + (base - smem_u32(raw));
+    const uint32_t ring = base, qs = ring + Sh::kEntry * Sh::kEntries, ps = qs + Sh::kQ;
+    __shared__ __align__(16) Shared sh;
+    __shared__ __align__(16) float top[N], scale_by[N], red[4][N];
+    __shared__ __align__(16) int32_t first[N], last[N], pos[N];
+    __shared__ __align__(16) uint64_t word[N];
+    __shared__ float slope[N];
+    const KvAttend& a = f.a;
+    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    volatile uint32_t* dead = &sh.dead;
+
+    auto bar = [&](const uint64_t& b) { return smem_u32(&b); };
+    if (tid == 0) {
+        for (uint32_t i = 0; i < Sh::kEntries; ++i) mbar_init(bar(sh.full[i]), 1), mbar_init(bar(sh.empty[i]), 1);
+        mbar_init(bar(sh.s_full[0]), 1), mbar_init(bar(sh.s_full[1]), 1);
+        mbar_init(bar(sh.p_full), kSoftThreads), mbar_init(bar(sh.pv_done), 1), mbar_init(bar(sh.q_full), kSoftThreads);
+        sh.dead = 0;
+        fence_mbar_init();
+        tma_prefetch_map(&map);
+    }
+    if (warp == 5) tmem_alloc(smem_u32(&sh.tmem), Sh::kTmem);
+    pdl_launch();
+    pdl_wait();
+
+    // the block's run of tiles
+    const int64_t K = a.pages.kv_heads;
+    const uint32_t per = (a.tok.n_seqs + kThreads - 1) / kThreads;
+    int64_t mine = 0;
+    for (uint32_t s = tid * per; s < min(a.tok.n_seqs, (tid + 1) * per); ++s) {
+        KvSpan sp;
+        mine += unit_tiles(a, kv_seq(a.pages, a.tok, s), sp);
+    }
+    // inclusive scan over the block's threads, in tiles of one key head
+    int64_t inc = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+        if (lane >= uint32_t(d)) inc += o;
+    }
+    if (lane == 31) sh.sums[warp] = inc;
+    fence_before();
+    __syncthreads();
+    fence_after();
+    int64_t before = 0, total = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kThreads / 32; ++i) {
+        if (i < warp) before += sh.sums[i];
+        total += sh.sums[i];
+    }
+    inc += before;
+    total *= K;
+    const int64_t blocks = min(int64_t(gridDim.x), total);
+    const int64_t run0 = blocks ? blockIdx.x * total / blocks : 0, run1 = blocks ? (blockIdx.x + 1) * total / blocks : 0;
+    const bool busy = blockIdx.x < blocks;
+    if (busy) {
+        const int64_t lo = (inc - mine) * K, hi = inc * K;
+        if (run0 >= lo && run0 < hi) {  // this thread's sequences hold the run's first tile
+            int64_t p = lo;
+            for (uint32_t s = tid * per;; ++s) {
+                KvSpan sp;
+                const int64_t n = unit_tiles(a, kv_seq(a.pages, a.tok, s), sp) * K;
+                if (run0 < p + n) {
+                    sh.start_seq = int32_t(s);
+                    sh.start_rest = int32_t(run0 - p);
+                    break;
+                }
+                p += n;
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t tmem = sh.tmem;
+
+    if (busy && warp == 4) {
+        // ---------------------------------------------------------- loads
+        Walk w;
+        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        const uint32_t shift = a.pages.token_shift;
+        const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
+        const uint32_t T_mask = (1u << shift) - 1;
+        uint32_t n = 0;
+        do {
+            const int32_t row_k = int32_t(((a.pages.layer * 2) * a.pages.kv_heads + w.h) << shift);
+            const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
+            const int32_t* table = a.pages.table + w.s * a.pages.table_stride;
+            for (int32_t i = 0; i < w.n; ++i) {
+                const uint32_t slot = uint32_t(tile_slot(w, w.tile + i)) + lane * box;
+                int32_t page = -1;
+                if (lane < boxes && slot < uint32_t(w.q.len)) page = table[slot >> shift];
+                // what the pool lacks, and what lies behind the sequence, is filled with zeros
+                const bool none = uint32_t(page) >= a.pages.total_pages;
+                const int32_t z = none ? int32_t(a.pages.total_pages) : page;
+                const int32_t y = int32_t(slot & T_mask);
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv, ++n) {
+                    const uint32_t e = n % Sh::kEntries;
+                    if (!mbar_wait(bar(sh.empty[e]), (n / Sh::kEntries & 1) ^ 1, dead)) goto loads_done;
+                    if (lane == 0) mbar_expect(bar(sh.full[e]), Sh::kEntry);
+                    __syncwarp();
+                    if (lane < boxes)
+                        for (int x = 0; x < NS; ++x)
+                            tma_load(ring + e * Sh::kEntry + x * kSlot + lane * box * 128, &map, x * 64,
+                                     (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
+                }
+            }
+        } while (walk_next(a, w));
+    loads_done:
+        __syncwarp();
+        if (*dead) {  // the copies in flight land before the block ends
+            uint32_t late = 0;
+            for (uint32_t k = n > Sh::kEntries ? n - Sh::kEntries : 0; k < n; ++k)
+                mbar_wait(bar(sh.full[k % Sh::kEntries]), k / Sh::kEntries & 1, &late);
+        }
+    } else if (busy && warp == 5) {
+        // ---------------------------------------------------------- products
+        Walk w;
+        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
+        constexpr uint32_t kPv = instr_desc(kBf16, true, true, 128, N);
+        const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
+        uint32_t n = 0, seg = 0;  // tile of the run
+        bool fresh_before = false;
+        auto pv = [&](uint32_t i, bool fresh) {
+            const uint32_t e = (2 * i + 1) % Sh::kEntries;
+            mbar_wait(bar(sh.p_full), i & 1, dead);
+            mbar_wait(bar(sh.full[e]), (2 * i + 1) / Sh::kEntries & 1, dead);
+            fence_after();
+            if (elect() && !*dead) {
+                const uint32_t v = ring + e * Sh::kEntry;
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        mma_ss(tmem + 2 * N, smem_desc(v + k * 2048, kSlot, 1024, 2),
+                               smem_desc(ps + part * (N * 256) + k * 256, 128, 2048, 0), kPv, !(fresh && part == 0 && k == 0));
+                mma_commit(bar(sh.empty[e]));
+                mma_commit(bar(sh.pv_done));
+            }
+            __syncwarp();
+        };
+        do {
+            for (int32_t i = 0; i < w.n; ++i, ++n) {
+                const bool fresh = i == 0;
+                if (fresh && n) pv(n - 1, fresh_before);
+                if (fresh) mbar_wait(bar(sh.q_full), seg++ & 1, dead);
+                const uint32_t e = (2 * n) % Sh::kEntries;
+                mbar_wait(bar(sh.full[e]), (2 * n) / Sh::kEntries & 1, dead);
+                fence_after();
+                if (elect() && !*dead) {
+                    const uint32_t k0 = ring + e * Sh::kEntry;
+                    for (uint32_t k = 0; k < ksteps; ++k)
+                        mma_ss(tmem + (n & 1) * N, smem_desc(k0 + (k / 4) * kSlot + (k % 4) * 32, 16, 1024, 2),
+                               smem_desc(qs + (k / 4) * (N * 128) + (k % 4) * 32, 16, 1024, 2), kQk, k != 0);
+                    mma_commit(bar(sh.empty[e]));
+                    mma_commit(bar(sh.s_full[n & 1]));
+                }
+                __syncwarp();
+                if (!fresh) pv(n - 1, fresh_before);
+                fresh_before = fresh;
+            }
+        } while (walk_next(a, w));
+        pv(n - 1, fresh_before);
+        if (*dead) {  // the products in flight end before the tensor memory is freed
+            const uint64_t t0 = now_ns();
+            while (now_ns() - t0 < 50000) {
+            }
+        }
+    } else if (busy) {
+        // ---------------------------------------------------------- softmax
+        Walk w;
+        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        const uint32_t D = a.pages.head_dim;
+        const uint32_t lanes = tmem + (warp << 21);  // this warp's 32 lanes
+        const float k2 = a.scale * kLog2e;
+        const float cap_in = MOD && a.softcap != 0.0f ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
+        if (tid == 0) {
+            // this run's note of a unit that began in the run before it
+            const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.nt) * blocks - 1) / total;
+            const bool here = w.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
+            f.join[blockIdx.x] = {int32_t(w.s), int32_t(w.h), int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
+        }
+        uint32_t n = 0;
+        do {
+            const int32_t ctx = w.q.len - w.q.n;
+            // the unit's queries: to shared memory, 64 dimensions at a time, 128-byte swizzle
+            for (uint32_t u = tid; u < N * NS * 8; u += kSoftThreads) {
+                const uint32_t c = u / (NS * 8), x = u % (NS * 8);
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (int32_t(c) < w.rows && x * 8 < D) {
+                    const uint32_t t = c / a.group, g = c % a.group;
+                    v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(w.q.first + t) * a.q_stride +
+                                                        uint64_t(w.h * a.group + g) * D + x * 8);
+                }
+                *reinterpret_cast<uint4*>(mem + (qs - base) + (x / 8) * (N * 128) + c * 128 + ((x % 8) ^ (c % 8)) * 16) = v;
+            }
+            if (tid < N) {
+                top[tid] = -INFINITY;
+                KvQuery q{0, INT32_MAX, 0, 0};
+                float sl = 0.0f;
+                if (int32_t(tid) < w.rows) {
+                    q = kv_query(a, w.q, tid / a.group);
+                    if (MOD && a.slopes) sl = a.slopes[w.h * a.group + tid % a.group] * kLog2e;
+                }
+                first[tid] = q.first, last[tid] = q.last, pos[tid] = q.pos, word[tid] = q.word;
+                slope[tid] = sl;
+            }
+            fence_async_smem();
+            mbar_arrive(bar(sh.q_full));
+            bar_sync<1, kSoftThreads>();
+
+            float sum[N];
+#pragma unroll
+            for (int c = 0; c < N; ++c) sum[c] = 0.0f;
+            for (int32_t i = 0; i < w.n; ++i, ++n) {
+                const int32_t slot0 = tile_slot(w, w.tile + i), key = slot0 + int32_t(tid);
+                const bool masked = slot0 < w.span.all_lo || slot0 + kTileKeys > w.span.all_hi;
+                // a drafted key's bit and position
+                uint64_t bit = 0;
+                int32_t kpos = key;
+                if (a.tree && key >= ctx && key < w.q.len && key - ctx < 64) {
+                    bit = uint64_t(1) << (key - ctx);
+                    kpos = ctx + __popcll(a.tree[w.q.first + key - ctx]) - 1;
+                }
+                const uint32_t s_at = lanes + (n & 1) * N;
+                mbar_wait(bar(sh.s_full[n & 1]), n >> 1 & 1, dead);
+                fence_after();
+                // scores of columns c0 .. c0 + C
+                auto scores = [&](int c0, float (&x)[C]) {
+                    if constexpr (C == 32)
+                        tmem_ld32(s_at + c0, x);
+                    else
+                        tmem_ld16(s_at + c0, x);
+                    wait_ld();
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        if (MOD) {
+                            x[c] = cap_in != 0.0f ? capped(x[c], cap_in, cap2) : x[c] * k2;
+                            x[c] -= slope[c0 + c] * fabsf(float(pos[c0 + c] - kpos));
+                        } else {
+                            x[c] *= k2;
+                        }
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int c = 0; c < C; ++c) {
+                            const bool see = kpos >= first[c0 + c] && (key < last[c0 + c] || (word[c0 + c] & bit));
+                            x[c] = see ? x[c] : -INFINITY;
+                        }
+                    }
+                };
+                float x[C];
+                bool over = false;
+#pragma unroll
+                for (int c0 = 0; c0 < N; c0 += C) {
+                    scores(c0, x);
+#pragma unroll
+                    for (int c = 0; c < C; ++c) over |= x[c] > top[c0 + c] + kRaise;
+                }
+                const bool raise = bar_any<1, kSoftThreads>(over);
+                if (n) mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
+                if (raise) {
+#pragma unroll
+                    for (int c0 = 0; c0 < N; c0 += C) {
+                        float y[C];
+                        if constexpr (N > C)
+                            scores(c0, y);
+                        else
+#pragma unroll
+                            for (int c = 0; c < C; ++c) y[c] = x[c];
+                        const float m = columns<C, true>(y, lane);
+                        if (lane < C) red[warp][c0 + lane] = m;
+                    }
+                    bar_sync<1, kSoftThreads>();
+                    if (tid < N) {
+                        const float was = top[tid];
+                        const float now = fmaxf(fmaxf(fmaxf(red[0][tid], red[1][tid]), fmaxf(red[2][tid], red[3][tid])), was);
+                        top[tid] = now;
+                        scale_by[tid] = was == now ? 1.0f : exp2_approx(was - now);
+                    }
+                    bar_sync<1, kSoftThreads>();
+                    if (i) {
+                        fence_after();
+#pragma unroll
+                        for (int c0 = 0; c0 < N; c0 += 16) {
+                            float o[16];
+                            tmem_ld16(lanes + 2 * N + c0, o);
+                            wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) o[c] *= scale_by[c0 + c], sum[c0 + c] *= scale_by[c0 + c];
+                            tmem_st16(lanes + 2 * N + c0, reinterpret_cast<uint32_t*>(o));
+                        }
+                        wait_st();
+                    }
+                }
+                // weights: rounded, and the rest, eight columns to a 16-byte row of the operand
+#pragma unroll
+                for (int c0 = 0; c0 < N; c0 += C) {
+                    if constexpr (N > C) scores(c0, x);
+#pragma unroll
+                    for (int c = 0; c < C; c += 8) {
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int j = 0; j < 8; j += 2) {
+                            float p[2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const float m = top[c0 + c + j + k];
+                                p[k] = exp2_approx(x[c + j + k] - (m == -INFINITY ? 0.0f : m));
+                                sum[c0 + c + j + k] += p[k];
+                            }
+                            hi[j / 2] = Kv16<T>::from2(p[0], p[1]);
+                            const float2 r = Kv16<T>::to2(hi[j / 2]);
+                            lo[j / 2] = Kv16<T>::from2(p[0] - r.x, p[1] - r.y);
+                        }
+                        uint8_t* at = mem + (ps - base) + (c0 + c) / 8 * 2048 + tid * 16;
+                        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        *reinterpret_cast<uint4*>(at + N * 256) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    }
+                }
+                // values that none of the unit's queries sees may be anything: zeros, as their weights are
+                if (slot0 < w.span.lo || slot0 + kTileKeys > w.span.hi) {
+                    const uint32_t e = (2 * n + 1) % Sh::kEntries;
+                    mbar_wait(bar(sh.full[e]), (2 * n + 1) / Sh::kEntries & 1, dead);
+                    if (key < w.span.lo || key >= w.span.hi) {
+#pragma unroll
+                        for (int k = 0; k < NS * 8; ++k)
+                            *reinterpret_cast<uint4*>(mem + e * Sh::kEntry + k / 8 * kSlot + tid * 128 + k % 8 * 16) =
+                                make_uint4(0, 0, 0, 0);
+                    }
+                }
+                fence_async_smem();
+                fence_before();
+                mbar_arrive(bar(sh.p_full));
+            }
+            // the segment's sums: over the keys' threads, then over the warps
+#pragma unroll
+            for (int c0 = 0; c0 < N; c0 += C) {
+                float y[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) y[c] = sum[c0 + c];
+                const float m = columns<C, false>(y, lane);
+                if (lane < C) red[warp][c0 + lane] = m;
+            }
+            mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
+            fence_after();
+            bar_sync<1, kSoftThreads>();
+            const bool whole = w.n == w.nt;
+            const uint32_t d = tid;
+            if (whole) {
+#pragma unroll
+                for (int c0 = 0; c0 < N; c0 += 16) {
+                    float o[16];
+                    tmem_ld16(lanes + 2 * N + c0, o);
+                    wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        const int col = c0 + c;
+                        if (col >= w.rows) break;
+                        const float l = red[0][col] + red[1][col] + red[2][col] + red[3][col];
+                        const uint32_t t = col / a.group, g = col % a.group;
+                        const uint64_t row = uint64_t(w.q.first + t);
+                        const float r = l == 0.0f ? 0.0f : 1.0f / l;
+                        if (d < D)
+                            static_cast<T*>(a.out)[row * a.out_stride + uint64_t(w.h * a.group + g) * D + d] =
+                                Kv16<T>::from1(o[c] * r);
+                        if (a.lse && d == 0)
+                            a.lse[row * a.q_heads + w.h * a.group + g] = l == 0.0f ? -INFINITY : (top[col] + log2f(l)) * kLn2;
+                    }
+                }
+            } else {
+                // a part of the unit: to the workspace
+                float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * Sh::kPart;
+#pragma unroll
+                for (int c0 = 0; c0 < N; c0 += 16) {
+                    float o[16];
+                    tmem_ld16(lanes + 2 * N + c0, o);
+                    wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        if (c0 + c < w.rows && d < 64 * NS) __stcg(part + (c0 + c) * (64 * NS) + d, o[c]);
+                }
+                if (tid < N) {
+                    __stcg(part + N * 64 * NS + tid, top[tid]);
+                    __stcg(part + N * 64 * NS + N + tid, red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]);
+                }
+            }
+            fence_before();
+            bar_sync<1, kSoftThreads>();  // red and top are read before the next segment writes them
+        } while (walk_next(a, w));
+    }
+    if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
+    __syncthreads();
+    if (tid == 0 && *dead) *f.fault = 1;
+    if (warp == 5) {
+        fence_after();
+        tmem_free(tmem, Sh::kTmem);
+    }
+}
+
+// Joins the units that lie in several runs: a block for each run's note, a warp
+// for each query.
+template <class T, int N, int NS>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Few f) {
+    using Sh = Shape<N, NS>;
+    using V = typename std::conditional<NS == 2, float4, float2>::type;
+    constexpr int kVec = 2 * NS;
+    const KvAttend& a = f.a;
+    pdl_launch();
+    pdl_wait();
+    const Join j = f.join[blockIdx.x];
+    if (!j.valid) return;
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, D = a.pages.head_dim;
+    const int32_t col = int32_t(blockIdx.y * 8 + warp);
+    const KvSeq q = kv_seq(a.pages, a.tok, uint32_t(j.s));
+    if (col >= min(q.n, int32_t(a.tok.max_new)) * int32_t(a.group)) return;
+    auto part = [&](int32_t b) { return f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * Sh::kPart; };
+    float top = -INFINITY;
+    for (int32_t b = j.b0 + int32_t(lane); b <= j.b1; b += 32) top = fmaxf(top, __ldcg(part(b) + N * 64 * NS + col));
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    float o[kVec] = {}, l = 0.0f;
+    for (int32_t b0 = j.b0; b0 <= j.b1; b0 += 32) {
+        const int32_t b = b0 + int32_t(lane);
+        float w = 0.0f;
+        if (b <= j.b1) {
+            const float m = __ldcg(part(b) + N * 64 * NS + col);
+            w = m == top ? 1.0f : exp2_approx(m - top);
+            l += w * __ldcg(part(b) + N * 64 * NS + N + col);
+        }
+        const int32_t n = min(32, j.b1 - b0 + 1);
+#pragma unroll 8
+        for (int32_t k = 0; k < n; ++k) {
+            const float wk = __shfl_sync(0xFFFFFFFFu, w, k);
+            const V v = __ldcg(reinterpret_cast<const V*>(part(b0 + k) + col * (64 * NS)) + lane);
+            const float* x = reinterpret_cast<const float*>(&v);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) o[e] += wk * x[e];
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+    const uint64_t row = uint64_t(q.first + col / int32_t(a.group));
+    const uint32_t head = uint32_t(j.h) * a.group + uint32_t(col) % a.group;
+    const float r = l == 0.0f ? 0.0f : 1.0f / l;
+    T* out = static_cast<T*>(a.out) + row * a.out_stride + uint64_t(head) * D + lane * kVec;
+    if (lane * kVec < D) {
+#pragma unroll
+        for (int e = 0; e < kVec; e += 2) reinterpret_cast<uint32_t*>(out)[e / 2] = Kv16<T>::from2(o[e] * r, o[e + 1] * r);
+    }
+    if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+}
+
+template <class... Args>
+cudaError_t launch_pdl(void (*kernel)(Args...), dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t stream,
+                       const typename std::common_type<Args>::type&... args) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, args...);
+}
+
+template <class T, int N, int NS, bool MOD>
+cudaError_t launch_as(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
+    constexpr uint32_t bytes = Shape<N, NS>::kBytes;
+    static std::atomic<uint64_t> ready{0};  // devices whose kernel may take this much shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !(ready.load() >> dev & 1)) {
+        e = cudaFuncSetAttribute(few_kernel<T, N, NS, MOD>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready |= uint64_t(1) << dev;
+    }
+    e = launch_pdl(few_kernel<T, N, NS, MOD>, dim3(sms), kThreads, bytes, stream, f, map);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(join_kernel<T, N, NS>, dim3(sms, (N + 7) / 8), 256, 0, stream, f);
+}
+
+template <class T, int N>
+cudaError_t launch_n(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
+    const bool mod = f.a.softcap != 0.0f || f.a.slopes;
+    if (f.a.pages.head_dim <= 64)
+        return mod ? launch_as<T, N, 1, true>(f, map, sms, stream) : launch_as<T, N, 1, false>(f, map, sms, stream);
+    return mod ? launch_as<T, N, 2, true>(f, map, sms, stream) : launch_as<T, N, 2, false>(f, map, sms, stream);
+}
+
+template <class T>
+cudaError_t launch_t(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
+    const uint32_t rows = f.a.group * f.a.tok.max_new;
+    return rows <= 16   ? launch_n<T, 16>(f, map, sms, stream)
+           : rows <= 32 ? launch_n<T, 32>(f, map, sms, stream)
+                        : launch_n<T, 64>(f, map, sms, stream);
+}
+
+constexpr uint64_t join_bytes(uint32_t sms) { return (uint64_t(sms) * sizeof(Join) + 255) / 256 * 256; }
+
+template <class T>
+cudaError_t launch_few(const KvAttend& a, const KvLaunch& l, cudaStream_t stream) {
+    Few f;
+    f.a = a;
+    f.join = static_cast<Join*>(l.workspace);
+    f.part = reinterpret_cast<float*>(static_cast<uint8_t*>(l.workspace) + join_bytes(l.sms));
+    f.fault = l.fault;
+    return launch_t<T>(f, *l.map, l.sms, stream);
+}
+
+}  // namespace
+}  // namespace t2i
