@@ -30,9 +30,10 @@ KVCALL = os.path.join(PKG, "_kvcall" + (sysconfig.get_config_var("EXT_SUFFIX") o
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CXX_SOURCES = ["control.cpp", "ctl_capi.cpp", "prefix.cpp"]
-CU_SOURCES = ["store.cu", "kv.cu", "kv_append.cu", "kv_attend.cu", "kv_few_bf16.cu", "kv_few_f16.cu"]
+CU_SOURCES = ["store.cu", "kv.cu", "kv_append.cu", "kv_few_bf16.cu", "kv_few_f16.cu", "kv_rows_bf16.cu",
+              "kv_rows_f16.cu"]
 HEADERS = ["control.hpp", "common.hpp", "deps.hpp", "kernels.cuh", "launch.cuh", "store_access.hpp", "kv.hpp",
-           "kv_device.cuh", "kv_attend.cuh", "kv_few.cuh", "tc.cuh", "exports.map"]
+           "kv_device.cuh", "kv_attend.cuh", "kv_few.cuh", "kv_rows.cuh", "tc.cuh", "exports.map"]
 
 
 def _cuda_home() -> str:

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <algorithm>
 #include <cmath>
 #include <memory>
 #include <string>
@@ -230,7 +231,9 @@ t2i_status append(t2i_kv* kv, const t2i_kv_append_desc& d, cudaStream_t stream) 
     return launch(kv, "kv_append", [&] { return launch_kv_append(a, kv->layout.dtype, d.in_dtype, stream); });
 }
 
-uint64_t workspace_bytes(const t2i_kv* kv, uint32_t, uint32_t, uint32_t) { return kv_few_workspace(kv->sms); }
+uint64_t workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads) {
+    return std::max(kv_few_workspace(kv->sms), kv_rows_workspace(kv->sms, n_seqs, n_tokens, q_heads / kv->layout.kv_heads));
+}
 
 t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) {
     Checks c(kv, "kv_attend");
@@ -270,11 +273,11 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     a.max_len = d.max_len;
     a.scale = d.scale;
     a.softcap = d.softcap;
-    if (uint64_t(a.group) * a.tok.max_new > kFewRows)
-        return launch(kv, "kv_attend", [&] { return launch_kv_attend(a, kv->layout.dtype, stream); });
     const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms};
+    const bool bf16 = kv->layout.dtype == T2I_BF16;
     return launch(kv, "kv_attend", [&] {
-        return kv->layout.dtype == T2I_BF16 ? launch_kv_few_bf16(a, l, stream) : launch_kv_few_f16(a, l, stream);
+        if (uint64_t(a.group) * a.tok.max_new <= kFewRows) return bf16 ? launch_kv_few_bf16(a, l, stream) : launch_kv_few_f16(a, l, stream);
+        return bf16 ? launch_kv_rows_bf16(a, l, stream) : launch_kv_rows_f16(a, l, stream);
     });
 }
 

@@ -1,5 +1,5 @@
 // The key/value cache in the store's pages: what its host side (kv.cu) and its
-// kernels (kv_append.cu, kv_attend.cu) share. The calls are described in
+// kernels (kv_append.cu, kv_few.cuh, kv_rows.cuh) share. The calls are described in
 // include/t2istore.h.
 #pragma once
 
@@ -85,7 +85,6 @@ struct KvCommit {
 // dtype and in_dtype: T2I_BF16, T2I_F16, T2I_F32
 cudaError_t launch_kv_append(const KvAppend& a, uint32_t dtype, uint32_t in_dtype, cudaStream_t stream);
 cudaError_t launch_kv_commit(const KvCommit& c, cudaStream_t stream);
-cudaError_t launch_kv_attend(const KvAttend& a, uint32_t dtype, cudaStream_t stream);
 
 // What an attention launch needs beside its arguments.
 struct KvLaunch {
@@ -101,5 +100,9 @@ constexpr uint32_t kFewRows = 64;
 cudaError_t launch_kv_few_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 cudaError_t launch_kv_few_f16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 uint64_t kv_few_workspace(uint32_t sms);
+// more of them
+cudaError_t launch_kv_rows_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
+cudaError_t launch_kv_rows_f16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
+uint64_t kv_rows_workspace(uint32_t sms, uint32_t n_seqs, uint32_t n_tokens, uint32_t group);
 
 }  // namespace t2i

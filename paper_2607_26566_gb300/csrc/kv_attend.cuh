@@ -2,6 +2,8 @@
 // tokens see, and the scores.
 #pragma once
 
+#include <type_traits>
+
 #include "kv_device.cuh"
 #include "tc.cuh"
 
@@ -77,6 +79,23 @@ __device__ __forceinline__ float capped(float s, float cap_in, float cap) {
     // tanh(y) = 1 - 2 / (exp(2y) + 1), within 2e-7
     const float e = tc::exp2_approx(s * cap_in * (2.0f * kLog2e));
     return cap - 2.0f * cap * tc::rcp_approx(e + 1.0f);
+}
+
+// A launch whose set-up overlaps the kernel before it on the stream.
+template <class... Args>
+inline cudaError_t launch_pdl(void (*kernel)(Args...), dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t stream,
+                       const typename std::common_type<Args>::type&... args) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, args...);
 }
 
 }  // namespace t2i

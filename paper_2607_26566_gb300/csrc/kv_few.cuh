@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                         tmem_ld32(s_at + c0, x);
                     else
                         tmem_ld16(s_at + c0, x);
-                    wait_ld();
+                    wait_ld(x);
 #pragma unroll
                     for (int c = 0; c < C; ++c) {
                         if (MOD) {
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                         for (int c0 = 0; c0 < N; c0 += 16) {
                             float o[16];
                             tmem_ld16(lanes + 2 * N + c0, o);
-                            wait_ld();
+                            wait_ld(o);
 #pragma unroll
                             for (int c = 0; c < 16; ++c) o[c] *= scale_by[c0 + c], sum[c0 + c] *= scale_by[c0 + c];
                             tmem_st16(lanes + 2 * N + c0, reinterpret_cast<uint32_t*>(o));
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                 for (int c0 = 0; c0 < N; c0 += 16) {
                     float o[16];
                     tmem_ld16(lanes + 2 * N + c0, o);
-                    wait_ld();
+                    wait_ld(o);
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
                         const int col = c0 + c;
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                 for (int c0 = 0; c0 < N; c0 += 16) {
                     float o[16];
                     tmem_ld16(lanes + 2 * N + c0, o);
-                    wait_ld();
+                    wait_ld(o);
 #pragma unroll
                     for (int c = 0; c < 16; ++c)
                         if (c0 + c < w.rows && d < 64 * NS) __stcg(part + (c0 + c) * (64 * NS) + d, o[c]);
@@ -607,22 +607,6 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Few f
         for (int e = 0; e < kVec; e += 2) reinterpret_cast<uint32_t*>(out)[e / 2] = Kv16<T>::from2(o[e] * r, o[e + 1] * r);
     }
     if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
-}
-
-template <class... Args>
-cudaError_t launch_pdl(void (*kernel)(Args...), dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t stream,
-                       const typename std::common_type<Args>::type&... args) {
-    cudaLaunchConfig_t c{};
-    c.gridDim = grid;
-    c.blockDim = dim3(threads);
-    c.dynamicSmemBytes = smem;
-    c.stream = stream;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = at;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, kernel, args...);
 }
 
 template <class T, int N, int NS, bool MOD>

@@ -1,0 +1,734 @@
+// Attention of many new tokens a sequence (prompts, chunks of them, large trees):
+// more than 64 queries to a key head.
+//
+// Bound by the tensor cores: 4 * 128 * head_dim operations for each query and 128-
+// key tile. A block takes 256 rows (a row: one query of one new token; the heads of
+// a group lie side by side, so shared keys are loaded once for all of them) as two
+// stages of 128. While one stage's four warps do the softmax of a tile, the other's
+// products run: S = Q K^T to tensor memory, a thread takes one row of S, writes
+// its weights over it (16 bits each), and O += P V reads them there. K and V come by
+// TMA; a row's maximum is raised only when a score exceeds it by 2^8, so most tiles
+// rescale nothing.
+//
+// Weights are rounded to the cache's type before the product (as accurate as the
+// values that they weigh: the output's own rounding is as large), the sums are not.
+//
+// Work split: a plan kernel lists the row tiles and the slots that each one sees;
+// all key tiles of all (sequence, key head, row tile) units, in order, are cut into
+// as many equal runs as there are SMs. A unit in several runs is joined by a third
+// kernel, in the order of the runs.
+#pragma once
+
+#include <atomic>
+
+#include "kv_attend.cuh"
+#include "t2istore.h"
+
+namespace t2i {
+namespace {
+
+using namespace tc;
+
+constexpr int kRows = 256;            // of a unit
+constexpr int kRowThreads = 320;         // two stages of 128, the loading warp, the product warp
+constexpr uint32_t kEntryBytes = 32768;  // a tile of K or V, 128 rows of 128 elements
+constexpr uint32_t kRowEntries = 4;
+constexpr uint32_t kRowSmem = 1024 + 2 * kEntryBytes + kRowEntries * kEntryBytes;
+constexpr uint32_t kRowPart = kRows * 128 + 2 * kRows;  // floats of a part: O, maxima, sums
+constexpr float kRowRaise = 8.0f;
+
+struct PlanTile {
+    int32_t s, m;       // the sequence, and which 256 rows of it
+    KvSpan span;
+    int32_t nt;         // key tiles
+    int32_t last;       // the sequence's last row tile
+    int64_t before;     // key tiles of the tiles before it
+    int64_t seq_before, seq_total;  // ... of the sequences before its own; of its own
+};
+struct PlanHead {
+    int64_t total;
+    int32_t tiles;
+};
+
+struct Join {
+    int32_t tile, h, b0, b1, second, valid;
+};
+
+struct Rows {
+    KvAttend a;
+    PlanHead* head;
+    int32_t* firsts;   // [n_seqs + 1]: each sequence's first tile
+    PlanTile* plan;
+    uint32_t most;     // entries of plan
+    Join* join;        // [blocks]
+    float* part;       // [2 * blocks][kRowPart]
+    uint32_t* fault;
+};
+
+__device__ __forceinline__ int32_t row_tiles(const KvAttend& a, const KvSeq& q) {
+    return int32_t((uint64_t(min(q.n, int32_t(a.tok.max_new))) * a.group + kRows - 1) / kRows);
+}
+
+// The span of a row tile, by a warp.
+__device__ __forceinline__ KvSpan tile_span(const KvAttend& a, const KvSeq& q, int32_t t0, int32_t t1, int32_t lane) {
+    if (!a.spans) return kv_span(a, q, t0, t1);
+    KvSpan r{INT32_MAX, 0, 0, INT32_MAX};
+    for (int32_t i = t0 + lane; i < t1; i += 32) {
+        const KvSpan x = kv_span(a, q, i, i + 1);
+        if (x.hi > x.lo) r.lo = min(r.lo, x.lo), r.hi = max(r.hi, x.hi);
+        r.all_lo = max(r.all_lo, x.all_lo), r.all_hi = min(r.all_hi, x.all_hi);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        r.lo = min(r.lo, __shfl_xor_sync(0xFFFFFFFFu, r.lo, d));
+        r.hi = max(r.hi, __shfl_xor_sync(0xFFFFFFFFu, r.hi, d));
+        r.all_lo = max(r.all_lo, __shfl_xor_sync(0xFFFFFFFFu, r.all_lo, d));
+        r.all_hi = min(r.all_hi, __shfl_xor_sync(0xFFFFFFFFu, r.all_hi, d));
+    }
+    if (r.lo >= r.hi) r.lo = r.hi = 0;
+    return r;
+}
+
+constexpr int kPlanThreads = 1024;
+// Exclusive scan of one number a thread over the block; *total: their sum.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* sums, int64_t* total) {
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int64_t inc = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+        if (lane >= uint32_t(d)) inc += o;
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp] = inc;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (uint32_t i = 0; i < kPlanThreads / 32; ++i) {
+        if (i < warp) before += sums[i];
+        all += sums[i];
+    }
+    *total = all;
+    return before + inc - v;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Rows f) {
+    __shared__ int64_t sums[kPlanThreads / 32];
+    const KvAttend& a = f.a;
+    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    pdl_launch();
+    pdl_wait();
+    // 1. each sequence's first tile
+    const uint32_t per = (a.tok.n_seqs + kPlanThreads - 1) / kPlanThreads;
+    const uint32_t s0 = tid * per, s1 = min(a.tok.n_seqs, s0 + per);
+    int64_t mine = 0, all;
+    for (uint32_t s = s0; s < s1; ++s) mine += row_tiles(a, kv_seq(a.pages, a.tok, s));
+    int64_t at = block_scan(mine, sums, &all);
+    for (uint32_t s = s0; s < s1; ++s) {
+        f.firsts[s] = int32_t(at);
+        at += row_tiles(a, kv_seq(a.pages, a.tok, s));
+    }
+    // more than the call's tokens make: starts that make no sense
+    const int32_t tiles = all > int64_t(f.most) ? 0 : int32_t(all);
+    if (tid == 0) f.firsts[a.tok.n_seqs] = tiles, f.head->tiles = tiles;
+    __syncthreads();
+    // 2. a warp a tile
+    KvTokens owner = a.tok;
+    owner.starts = f.firsts;
+    for (int32_t j = int32_t(warp); j < tiles; j += kPlanThreads / 32) {
+        const uint32_t s = kv_owner(owner, uint32_t(j));
+        const KvSeq q = kv_seq(a.pages, a.tok, s);
+        const int32_t m = j - f.firsts[s], G = int32_t(a.group);
+        const int32_t rows = int32_t(min(int64_t(min(q.n, int32_t(a.tok.max_new))) * G, (int64_t(m) + 1) * kRows));
+        const KvSpan sp = tile_span(a, q, m * kRows / G, (rows + G - 1) / G, int32_t(lane));
+        if (lane == 0) {
+            PlanTile& t = f.plan[j];
+            t.s = int32_t(s), t.m = m, t.span = sp;
+            t.nt = max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
+            t.last = j + 1 == f.firsts[s + 1];
+        }
+    }
+    __syncthreads();
+    // 3. key tiles before each tile, and of its sequence
+    const int32_t tper = (tiles + kPlanThreads - 1) / kPlanThreads;
+    const int32_t j0 = int32_t(tid) * tper, j1 = min(tiles, j0 + tper);
+    mine = 0;
+    for (int32_t j = j0; j < j1; ++j) mine += f.plan[j].nt;
+    at = block_scan(mine, sums, &all);
+    for (int32_t j = j0; j < j1; ++j) {
+        f.plan[j].before = at;
+        at += f.plan[j].nt;
+    }
+    if (tid == 0) f.head->total = all;
+    __syncthreads();
+    for (int32_t j = j0; j < j1; ++j) {
+        PlanTile& t = f.plan[j];
+        const int32_t a0 = f.firsts[t.s], a1 = f.firsts[t.s + 1];
+        t.seq_before = f.plan[a0].before;
+        t.seq_total = (a1 < tiles ? f.plan[a1].before : all) - t.seq_before;
+    }
+}
+
+// The run of one block, unit by unit: in a sequence, key head by key head, its row tiles.
+struct RowWalk {
+    int64_t at, end, unit;
+    int32_t j, h, tile, n;
+    PlanTile t;
+    KvSeq q;
+    int32_t rows;  // of the unit
+};
+__device__ __forceinline__ void walk_load(const Rows& f, RowWalk& w) {
+    w.t = f.plan[w.j];
+    w.q = kv_seq(f.a.pages, f.a.tok, uint32_t(w.t.s));
+    w.rows = int32_t(min(int64_t(min(w.q.n, int32_t(f.a.tok.max_new))) * f.a.group - int64_t(w.t.m) * kRows, int64_t(kRows)));
+}
+__device__ __forceinline__ void walk_start(const Rows& f, RowWalk& w, int32_t j, int32_t h, int32_t tile, int64_t at, int64_t end) {
+    w.at = at, w.end = end, w.j = j, w.h = h, w.tile = tile;
+    w.unit = at - tile;
+    walk_load(f, w);
+    w.n = int32_t(min(int64_t(w.t.nt - tile), end - at));
+}
+__device__ __forceinline__ bool walk_next(const Rows& f, RowWalk& w) {
+    w.at += w.n;
+    if (w.at >= w.end) return false;
+    w.tile = 0;
+    w.unit = w.at;
+    if (!w.t.last) {
+        ++w.j;
+    } else if (w.h + 1 < int32_t(f.a.pages.kv_heads)) {
+        ++w.h;
+        w.j -= w.t.m;
+    } else {
+        ++w.j;
+        w.h = 0;
+    }
+    walk_load(f, w);
+    w.n = int32_t(min(int64_t(w.t.nt), w.end - w.at));
+    return true;
+}
+__device__ __forceinline__ int32_t tile_slot(const RowWalk& w, int32_t i) { return (w.t.span.lo / kTileKeys + i) * kTileKeys; }
+
+struct RowShared {
+    uint64_t full[kRowEntries], empty[kRowEntries];
+    uint64_t s_full[2], p_full[2], pv_done[2], q_full[2];
+    uint32_t tmem, dead;
+    int32_t start_j, start_h, start_tile;
+    int32_t draft[2][64];  // positions of the unit's drafted tokens
+};
+
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+template <class T, bool MOD>
+__global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_constant__ Rows f, const __grid_constant__ CUtensorMap map) {
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    uint8_t* const mem = raw + (base - smem_u32(raw));
+    const uint32_t ring = base + 2 * kEntryBytes;  // behind the two stages' queries
+    __shared__ __align__(16) RowShared sh;
+    const KvAttend& a = f.a;
+    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const uint32_t D = a.pages.head_dim;
+    volatile uint32_t* dead = &sh.dead;
+
+    auto bar = [&](const uint64_t& b) { return smem_u32(&b); };
+    if (tid == 0) {
+        for (uint32_t i = 0; i < kRowEntries; ++i) mbar_init(bar(sh.full[i]), 1), mbar_init(bar(sh.empty[i]), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i]), 128);
+            mbar_init(bar(sh.pv_done[i]), 1), mbar_init(bar(sh.q_full[i]), 128);
+        }
+        sh.dead = 0;
+        fence_mbar_init();
+        tma_prefetch_map(&map);
+    }
+    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
+    pdl_launch();
+    pdl_wait();
+
+    const int64_t K = a.pages.kv_heads, total = f.head->total * K;
+    const int64_t blocks = min(int64_t(gridDim.x), total);
+    const bool busy = blockIdx.x < blocks;
+    const int64_t run0 = busy ? blockIdx.x * total / blocks : 0, run1 = busy ? (blockIdx.x + 1) * total / blocks : 0;
+    if (busy) {
+        const int32_t tiles = f.head->tiles;
+        for (int32_t j = int32_t(tid); j < tiles; j += kRowThreads) {
+            const PlanTile& t = f.plan[j];
+            const int64_t in = run0 - t.seq_before * K;
+            if (in < 0 || in >= t.seq_total * K) continue;
+            const int64_t r = in % t.seq_total - (t.before - t.seq_before);
+            if (r < 0 || r >= t.nt) continue;
+            sh.start_j = j, sh.start_h = int32_t(in / t.seq_total), sh.start_tile = int32_t(r);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sh.tmem;
+
+    if (busy && warp == 8) {
+        // ---------------------------------------------------------- loads
+        RowWalk w;
+        walk_start(f, w, sh.start_j, sh.start_h, sh.start_tile, run0, run1);
+        const uint32_t shift = a.pages.token_shift;
+        const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
+        const uint32_t mask = (1u << shift) - 1;
+        const int halves = D > 64 ? 2 : 1;
+        uint32_t n = 0;
+        do {
+            const int32_t row_k = int32_t((a.pages.layer * 2 * a.pages.kv_heads + w.h) << shift);
+            const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
+            const int32_t* table = a.pages.table + uint32_t(w.t.s) * a.pages.table_stride;
+            for (int32_t i = 0; i < w.n; ++i) {
+                const uint32_t slot = uint32_t(tile_slot(w, w.tile + i)) + lane * box;
+                int32_t page = -1;
+                if (lane < boxes && slot < uint32_t(w.q.len)) page = table[slot >> shift];
+                // what the pool lacks, and what lies behind the sequence, is filled with zeros
+                const int32_t z = uint32_t(page) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page;
+                const int32_t y = int32_t(slot & mask);
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv, ++n) {
+                    const uint32_t e = n % kRowEntries;
+                    if (!mbar_wait(bar(sh.empty[e]), (n / kRowEntries & 1) ^ 1, dead)) goto loads_done;
+                    if (lane == 0) mbar_expect(bar(sh.full[e]), uint32_t(halves) * 16384u);
+                    __syncwarp();
+                    if (lane < boxes)
+                        for (int x = 0; x < halves; ++x)
+                            tma_load(ring + e * kEntryBytes + x * 16384 + lane * box * 128, &map, x * 64,
+                                     (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
+                }
+            }
+        } while (walk_next(f, w));
+    loads_done:
+        __syncwarp();
+        if (*dead) {  // the copies in flight land before the block ends
+            uint32_t late = 0;
+            for (uint32_t k = n > kRowEntries ? n - kRowEntries : 0; k < n; ++k)
+                mbar_wait(bar(sh.full[k % kRowEntries]), k / kRowEntries & 1, &late);
+        }
+    } else if (busy && warp == 9) {
+        // ---------------------------------------------------------- products
+        RowWalk w;
+        walk_start(f, w, sh.start_j, sh.start_h, sh.start_tile, run0, run1);
+        const uint32_t dn = (D + 15) / 16;
+        constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, 128);
+        const uint32_t kPv = instr_desc(kBf16, false, true, 128, 0) | (dn * 2) << 17;
+        uint32_t units[2] = {0, 0}, cnt[2] = {0, 0};  // of each stage: units begun, tiles weighed
+        auto qk = [&](int st, uint32_t g, bool fresh, bool two) {
+            if (fresh) mbar_wait(bar(sh.q_full[st]), units[st]++ & 1, dead);
+            const uint32_t n = 2 * g, e = n % kRowEntries;
+            mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
+            fence_after();
+            if (elect() && !*dead) {
+                const uint32_t k0 = ring + e * kEntryBytes, q0 = base + st * kEntryBytes;
+                for (uint32_t k = 0; k < dn; ++k)
+                    mma_ss(tmem + st * 128, smem_desc(q0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2),
+                           smem_desc(k0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2), kQk, k != 0);
+                if (st || !two) mma_commit(bar(sh.empty[e]));
+                mma_commit(bar(sh.s_full[st]));
+            }
+            __syncwarp();
+        };
+        auto pv = [&](int st, uint32_t g, bool fresh, bool two) {
+            const uint32_t n = 2 * g + 1, e = n % kRowEntries;
+            mbar_wait(bar(sh.p_full[st]), cnt[st]++ & 1, dead);
+            mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
+            fence_after();
+            if (elect() && !*dead) {
+                const uint32_t v = ring + e * kEntryBytes;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, smem_desc(v + k * 2048, 16384, 1024, 2), kPv,
+                           !(fresh && k == 0));
+                if (st || !two) mma_commit(bar(sh.empty[e]));
+                mma_commit(bar(sh.pv_done[st]));
+            }
+            __syncwarp();
+        };
+        uint32_t g = 0;
+        int32_t i = 0;
+        bool two = w.rows > 128, fresh = true;
+        qk(0, 0, true, two);
+        if (two) qk(1, 0, true, two);
+        for (;;) {
+            // the next tile, whose scores are issued between this one's products
+            bool more = true, next_fresh = false, next_two = two;
+            if (++i == w.n) {
+                more = walk_next(f, w);
+                i = 0;
+                next_fresh = true;
+                next_two = w.rows > 128;
+            }
+            pv(0, g, fresh, two);
+            if (more && !next_fresh) qk(0, g + 1, false, next_two);
+            if (two) pv(1, g, fresh, two);
+            if (!more) break;
+            if (next_fresh) qk(0, g + 1, true, next_two);
+            if (next_two) qk(1, g + 1, next_fresh, next_two);
+            fresh = next_fresh, two = next_two;
+            ++g;
+        }
+        if (*dead) {  // the products in flight end before the tensor memory is freed
+            const uint64_t t0 = now_ns();
+            while (now_ns() - t0 < 50000) {
+            }
+        }
+    } else if (busy) {
+        // ---------------------------------------------------------- softmax
+        const int st = warp / 4;
+        const uint32_t r = tid % 128;  // the row of the stage
+        RowWalk w;
+        walk_start(f, w, sh.start_j, sh.start_h, sh.start_tile, run0, run1);
+        if (tid == 0) {
+            const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.t.nt) * blocks - 1) / total;
+            const bool here = w.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
+            f.join[blockIdx.x] = {w.j, w.h, int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
+        }
+        const uint32_t lanes = tmem + ((warp % 4) << 21), s_at = lanes + st * 128, o_at = lanes + 256 + st * 128;
+        // a negative scale turns the queries' signs, so that the largest product is the largest score
+        const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+        const float k2 = fabsf(a.scale) * kLog2e;
+        const float cap_in = MOD && a.softcap != 0.0f ? fabsf(a.scale) / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
+        // a unit's queries to shared memory, 64 dimensions at a time, 128-byte swizzle
+        auto load_q = [&](const RowWalk& u) {
+            const uint32_t row0 = uint32_t(u.t.m) * kRows + st * 128;
+            for (uint32_t k = r; k < 128 * 16; k += 128) {
+                const uint32_t c = k / 16, x = k % 16;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (int32_t(st * 128 + c) < u.rows && x * 8 < D) {
+                    const uint32_t t = (row0 + c) / a.group, g = (row0 + c) % a.group;
+                    v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(u.q.first + t) * a.q_stride +
+                                                        uint64_t(u.h * a.group + g) * D + x * 8);
+                    v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+                }
+                *reinterpret_cast<uint4*>(mem + st * kEntryBytes + (x / 8) * 16384 + c * 128 + ((x % 8) ^ (c % 8)) * 16) = v;
+            }
+            fence_async_smem();
+            mbar_arrive(bar(sh.q_full[st]));
+        };
+        if (st == 0 || w.rows > 128) load_q(w);
+        uint32_t n = 0;  // tiles of this stage
+        bool more = true;
+        while (more) {
+            RowWalk next;
+            const bool on = st == 0 || w.rows > 128;
+            if (on) {
+                const int32_t ctx = w.q.len - w.q.n;
+                const uint32_t row = uint32_t(w.t.m) * kRows + st * 128 + r;
+                const bool real = int32_t(st * 128 + r) < w.rows;
+                const uint32_t tok = real ? row / a.group : 0, gh = row % a.group;
+                KvQuery qy{0, INT32_MAX, 0, 0};
+                float slope = 0.0f;
+                if (real) {
+                    qy = kv_query(a, w.q, int32_t(tok));
+                    if (MOD && a.slopes) slope = a.slopes[w.h * a.group + gh] * kLog2e;
+                }
+                if (a.tree) {
+                    if (r < 64) {
+                        const bool drafted = int32_t(r) < w.q.n;
+                        sh.draft[st][r] = drafted ? ctx + __popcll(a.tree[w.q.first + int32_t(r)]) - 1 : 0;
+                    }
+                    if (st)
+                        bar_sync<2, 128>();
+                    else
+                        bar_sync<1, 128>();
+                }
+                float ref = -INFINITY, sum = 0.0f;
+                for (int32_t i = 0; i < w.n; ++i, ++n) {
+                    const int32_t slot0 = tile_slot(w, w.tile + i);
+                    const bool masked = slot0 < w.t.span.all_lo || slot0 + kTileKeys > w.t.span.all_hi;
+                    const bool drafts = a.tree && slot0 + kTileKeys > ctx;
+                    mbar_wait(bar(sh.s_full[st]), n & 1, dead);
+                    fence_after();
+                    if (MOD || masked) {
+                        // caps, biases and masks, 32 keys at a time, back to tensor memory: what follows
+                        // holds all 128 scores in registers
+                        const int32_t d = ctx - slot0;  // the drafted tokens' bits, from this tile's first key on
+                        uint64_t w0 = 0, w1 = 0;
+                        if (drafts) {
+                            w0 = d >= 64 ? 0 : d >= 0 ? qy.word << d : d > -64 ? qy.word >> -d : 0;
+                            w1 = d >= 128 ? 0 : d >= 64 ? qy.word << (d - 64) : d > 0 ? qy.word >> (64 - d) : 0;
+                        }
+#pragma unroll 1
+                        for (int c0 = 0; c0 < 128; c0 += 32) {
+                            float y[32];
+                            tmem_ld32(s_at + c0, y);
+                            wait_ld(y);
+                            const uint32_t bits = uint32_t((c0 < 64 ? w0 : w1) >> (c0 & 32));
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                const int32_t key = slot0 + c0 + c;
+                                int32_t kp = key;
+                                if (drafts && key >= ctx) kp = sh.draft[st][min(key - ctx, 63)];
+                                if (MOD) {
+                                    y[c] = cap_in != 0.0f ? capped(y[c], cap_in, cap2) : y[c] * k2;
+                                    y[c] -= slope * fabsf(float(qy.pos - kp));
+                                }
+                                const bool see = kp >= qy.first && (key < qy.last || (bits >> c & 1 && key < w.q.len));
+                                if (masked && !see) y[c] = -INFINITY;
+                            }
+                            tmem_st16(s_at + c0, reinterpret_cast<uint32_t*>(y));
+                            tmem_st16(s_at + c0 + 16, reinterpret_cast<uint32_t*>(y) + 16);
+                        }
+                        wait_st();
+                    }
+                    // the row's maximum, then its weights, 32 keys at a time with the next 32 on the way
+                    float m = -INFINITY;
+                    float xa[32], xb[32];
+                    auto peak = [&](const float (&x)[32]) {
+                        float m0 = fmaxf(x[0], x[1]), m1 = fmaxf(x[2], x[3]);
+#pragma unroll
+                        for (int c = 4; c < 32; c += 4) {
+                            m0 = fmaxf(m0, fmaxf(x[c], x[c + 1]));
+                            m1 = fmaxf(m1, fmaxf(x[c + 2], x[c + 3]));
+                        }
+                        m = fmaxf(m, fmaxf(m0, m1));
+                    };
+                    tmem_ld32(s_at, xa);
+                    wait_ld(xa);
+                    tmem_ld32(s_at + 32, xb);
+                    peak(xa);
+                    wait_ld(xb);
+                    tmem_ld32(s_at + 64, xa);
+                    peak(xb);
+                    wait_ld(xa);
+                    tmem_ld32(s_at + 96, xb);
+                    peak(xa);
+                    wait_ld(xb);
+                    tmem_ld32(s_at, xa);
+                    peak(xb);
+                    if (!MOD) m *= k2;
+                    const bool up = m > ref + kRowRaise;
+                    if (__any_sync(0xFFFFFFFFu, up)) {
+                        float by = 1.0f;
+                        if (up) {
+                            by = exp2_approx(ref - m);
+                            ref = m;
+                        }
+                        sum *= by;
+                        if (i) {
+                            mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
+                            fence_after();
+                            for (uint32_t c0 = 0; c0 < D; c0 += 16) {
+                                float o[16];
+                                tmem_ld16(o_at + c0, o);
+                                wait_ld(o);
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) o[c] *= by;
+                                tmem_st16(o_at + c0, reinterpret_cast<uint32_t*>(o));
+                            }
+                            wait_st();
+                        }
+                    }
+                    const float off = ref == -INFINITY ? 0.0f : -ref;
+                    const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
+                    uint64_t sum2 = 0, sum3 = 0;
+                    auto weigh = [&](const float (&x)[32], uint32_t (&p)[16]) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) {
+                            float u0, u1, u2, u3;
+                            unpack2(fma2(pack2(x[c], x[c + 1]), by2, off2), u0, u1);
+                            unpack2(fma2(pack2(x[c + 2], x[c + 3]), by2, off2), u2, u3);
+                            u0 = exp2_approx(u0), u1 = exp2_approx(u1), u2 = exp2_approx(u2), u3 = exp2_approx(u3);
+                            sum2 = add2(sum2, pack2(u0, u1));
+                            sum3 = add2(sum3, pack2(u2, u3));
+                            p[c / 2] = Kv16<T>::from2(u0, u1);
+                            p[c / 2 + 1] = Kv16<T>::from2(u2, u3);
+                        }
+                    };
+                    // weights 2c and 2c + 1 to column c: behind the scores that are still to be read
+                    uint32_t p[16];
+                    wait_ld(xa);
+                    tmem_ld32(s_at + 32, xb);
+                    weigh(xa, p);
+                    wait_ld(xb);
+                    tmem_ld32(s_at + 64, xa);
+                    tmem_st16(s_at, p);
+                    weigh(xb, p);
+                    wait_ld(xa);
+                    tmem_ld32(s_at + 96, xb);
+                    tmem_st16(s_at + 16, p);
+                    weigh(xa, p);
+                    wait_ld(xb);
+                    tmem_st16(s_at + 32, p);
+                    weigh(xb, p);
+                    tmem_st16(s_at + 48, p);
+                    float u0, u1;
+                    unpack2(add2(sum2, sum3), u0, u1);
+                    sum += u0 + u1;
+                    if (st == 0 && (slot0 < w.t.span.lo || slot0 + kTileKeys > w.t.span.hi)) {
+                        // values that none of the unit's queries sees may be anything: zeros, as their weights are
+                        const uint32_t e = (2 * n + 1) % kRowEntries;
+                        mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
+                        const int32_t key = slot0 + int32_t(r);
+                        if (key < w.t.span.lo || key >= w.t.span.hi) {
+#pragma unroll
+                            for (int k = 0; k < 16; ++k)
+                                if (k < 8 || D > 64)
+                                    *reinterpret_cast<uint4*>(mem + 2 * kEntryBytes + e * kEntryBytes + k / 8 * 16384 + r * 128 +
+                                                              k % 8 * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_smem();
+                    }
+                    wait_st();
+                    fence_before();
+                    mbar_arrive(bar(sh.p_full[st]));
+                }
+                next = w;
+                more = walk_next(f, next);
+                if (more && (st == 0 || next.rows > 128)) load_q(next);  // its scores start while this unit is written
+                mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
+                fence_after();
+                if (w.n == w.t.nt) {
+                    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    const uint64_t orow = uint64_t(w.q.first) + tok;
+                    T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(w.h * a.group + gh) * D;
+                    for (uint32_t c0 = 0; c0 < D; c0 += 16) {
+                        float o[16];
+                        tmem_ld16(o_at + c0, o);
+                        wait_ld(o);
+                        if (!real) continue;
+#pragma unroll
+                        for (int c = 0; c < 16; c += 8) {
+                            if (c0 + c >= D) break;
+                            float y[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) y[k] = o[c + k] * by;
+                            kv_store8(out + c0 + c, y);
+                        }
+                    }
+                    if (real && a.lse) a.lse[orow * a.q_heads + w.h * a.group + gh] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+                } else {
+                    // a part of the unit: [head_dim / 4][256 rows] of four, maxima, sums
+                    float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * kRowPart;
+                    const uint32_t pr = st * 128 + r;
+                    for (uint32_t c0 = 0; c0 < D; c0 += 16) {
+                        float o[16];
+                        tmem_ld16(o_at + c0, o);
+                        wait_ld(o);
+#pragma unroll
+                        for (int c = 0; c < 16; c += 4)
+                            __stcg(reinterpret_cast<float4*>(part) + (c0 + c) / 4 * kRows + pr,
+                                   make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]));
+                    }
+                    __stcg(part + kRows * 128 + pr, ref);
+                    __stcg(part + kRows * 128 + kRows + pr, sum);
+                }
+                fence_before();
+            } else {
+                next = w;
+                more = walk_next(f, next);
+                if (more && next.rows > 128) load_q(next);
+            }
+            w = next;
+        }
+    }
+    if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
+    __syncthreads();
+    if (tid == 0 && *dead) *f.fault = 1;
+    if (warp == 9) {
+        fence_after();
+        tmem_free(tmem, 512);
+    }
+}
+
+// Joins the units that lie in several runs: a block for 32 rows of a run's note, a
+// lane a row.
+template <class T>
+__global__ void __launch_bounds__(256) rows_join_kernel(const __grid_constant__ Rows f) {
+    const KvAttend& a = f.a;
+    pdl_launch();
+    pdl_wait();
+    const Join j = f.join[blockIdx.x];
+    if (!j.valid) return;
+    RowWalk w;
+    w.j = j.tile;
+    walk_load(f, w);
+    const uint32_t warp = threadIdx.x / 32, D = a.pages.head_dim;
+    const int32_t r = int32_t(blockIdx.y * 32 + threadIdx.x % 32);
+    if (r >= w.rows) return;
+    auto part = [&](int32_t b) { return f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * kRowPart; };
+    float top = -INFINITY, l = 0.0f;
+    for (int32_t b = j.b0; b <= j.b1; ++b) top = fmaxf(top, __ldcg(part(b) + kRows * 128 + r));
+    float4 o[4] = {};
+#pragma unroll 2
+    for (int32_t b = j.b0; b <= j.b1; ++b) {
+        const float* p = part(b);
+        const float m = __ldcg(p + kRows * 128 + r), x = m == top ? 1.0f : exp2_approx(m - top);
+        l += x * __ldcg(p + kRows * 128 + kRows + r);
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+            if ((warp + 8 * k) * 4 >= D) break;
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + (warp + 8 * k) * kRows + r);
+            o[k].x += x * v.x, o[k].y += x * v.y, o[k].z += x * v.z, o[k].w += x * v.w;
+        }
+    }
+    const uint32_t row = uint32_t(w.t.m) * kRows + uint32_t(r), head = uint32_t(j.h) * a.group + row % a.group;
+    const uint64_t orow = uint64_t(w.q.first) + row / a.group;
+    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D;
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+        const uint32_t d = (warp + 8 * k) * 4;
+        if (d >= D) break;
+        *reinterpret_cast<uint2*>(out + d) = make_uint2(Kv16<T>::from2(o[k].x * by, o[k].y * by), Kv16<T>::from2(o[k].z * by, o[k].w * by));
+    }
+    if (a.lse && warp == 0) a.lse[orow * a.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+}
+
+constexpr uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
+// the parts of the workspace, in order: head, notes, firsts, plan, parts
+uint64_t plan_tiles(uint64_t n_seqs, uint64_t n_tokens, uint64_t group) { return n_tokens * group / kRows + n_seqs + 1; }
+
+template <class T, bool MOD>
+cudaError_t launch_rows_as(const Rows& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
+    static std::atomic<uint64_t> ready{0};  // devices whose kernel may take this much shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !(ready.load() >> dev & 1)) {
+        e = cudaFuncSetAttribute(rows_kernel<T, MOD>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kRowSmem));
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready |= uint64_t(1) << dev;
+    }
+    if ((e = launch_pdl(plan_kernel, dim3(1), kPlanThreads, 0, stream, f)) != cudaSuccess) return e;
+    if ((e = launch_pdl(rows_kernel<T, MOD>, dim3(sms), kRowThreads, kRowSmem, stream, f, map)) != cudaSuccess) return e;
+    return launch_pdl(rows_join_kernel<T>, dim3(sms, kRows / 32), 256, 0, stream, f);
+}
+
+template <class T>
+cudaError_t launch_rows(const KvAttend& a, const KvLaunch& l, cudaStream_t stream) {
+    Rows f;
+    f.a = a;
+    uint8_t* p = static_cast<uint8_t*>(l.workspace);
+    f.head = reinterpret_cast<PlanHead*>(p);
+    p += 256;
+    f.join = reinterpret_cast<Join*>(p);
+    p += up256(l.sms * sizeof(Join));
+    f.firsts = reinterpret_cast<int32_t*>(p);
+    p += up256((uint64_t(a.tok.n_seqs) + 1) * 4);
+    f.plan = reinterpret_cast<PlanTile*>(p);
+    f.most = uint32_t(plan_tiles(a.tok.n_seqs, a.tok.n_tokens, a.group));
+    p += up256(uint64_t(f.most) * sizeof(PlanTile));
+    f.part = reinterpret_cast<float*>(p);
+    f.fault = l.fault;
+    return a.softcap != 0.0f || a.slopes ? launch_rows_as<T, true>(f, *l.map, l.sms, stream)
+                                         : launch_rows_as<T, false>(f, *l.map, l.sms, stream);
+}
+
+}  // namespace
+}  // namespace t2i

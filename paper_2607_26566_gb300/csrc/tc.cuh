@@ -44,23 +44,22 @@ __device__ __forceinline__ uint64_t now_ns() {
 }
 // Every wait ends: after a second the block is marked dead and all of its waits
 // return at once.
+// (Inline: a call here would have its caller save its registers.)
 constexpr uint64_t kWaitNs = 1000000000ull;
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-    const uint64_t t0 = now_ns();
-    while (!mbar_try(bar, parity)) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
+    uint64_t t0 = 0;
+#pragma unroll 1
+    for (uint32_t n = 1; !mbar_try(bar, parity); ++n) {
+        if (n % 16) continue;
         if (*dead) return false;
-        if (now_ns() - t0 > kWaitNs) {
+        const uint64_t t = now_ns();
+        if (t0 == 0) t0 = t;
+        if (t - t0 > kWaitNs) {
             *dead = 1;
             return false;
         }
     }
     return true;
-}
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-#pragma unroll 1
-    for (int i = 0; i < 32; ++i)
-        if (mbar_try(bar, parity)) return true;
-    return mbar_wait_slow(bar, parity, dead);
 }
 
 // ---- TMA
@@ -92,7 +91,14 @@ __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t cols) {
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for the loads so far; v's values are those loaded from here on (nothing
+// that uses them moves up past the wait).
+template <int N>
+__device__ __forceinline__ void wait_ld(float (&v)[N]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
+}
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Sixteen consecutive columns of the warp's 32 lanes, one lane a thread.
