@@ -30,7 +30,12 @@ namespace {
 using namespace tc;
 
 constexpr int kRows = 256;            // of a unit
-constexpr int kRowThreads = 320;         // two stages of 128, the loading warp, the product warp
+// Two stages of 128 threads, and 128 more: the loading warp, the product warp and two
+// that idle, so that registers can be shared out by groups of four warps (a softmax
+// thread holds its row's 128 scores).
+constexpr int kRowThreads = 384;
+constexpr int kRowRegs = 168, kSoftRegs = 208, kOtherRegs = 88;
+static_assert(kSoftRegs * 256 + kOtherRegs * 128 <= kRowRegs * kRowThreads, "what a block was launched with");
 constexpr uint32_t kEntryBytes = 32768;  // a tile of K or V, 128 rows of 128 elements
 constexpr uint32_t kRowEntries = 4;
 constexpr uint32_t kRowSmem = 1024 + 2 * kEntryBytes + kRowEntries * kEntryBytes;
@@ -40,6 +45,8 @@ constexpr float kRowRaise = 8.0f;
 struct PlanTile {
     int32_t s, m;       // the sequence, and which 256 rows of it
     KvSpan span;
+    KvSeq q;
+    int32_t rows;       // of the tile
     int32_t nt;         // key tiles
     int32_t last;       // the sequence's last row tile
     int64_t before;     // key tiles of the tiles before it
@@ -50,8 +57,11 @@ struct PlanHead {
     int32_t tiles;
 };
 
+// A unit in several runs, noted at the run that holds its second part: the runs
+// b0 to b1 hold it, the first as that block's part 0 or 1, the others as part 0.
 struct Join {
-    int32_t tile, h, b0, b1, second, valid;
+    int32_t first, m, rows, h;  // the sequence's first token, the unit's row tile, its rows, its key head
+    int32_t b0, b1, second, valid;
 };
 
 struct Rows {
@@ -117,34 +127,40 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     pdl_launch();
     pdl_wait();
+    // A few sequences' and tiles' numbers stay in shared memory.
+    __shared__ int32_t few_firsts[kPlanThreads + 1], few_nt[kPlanThreads];
+    const bool in_smem = a.tok.n_seqs <= kPlanThreads;
+    int32_t* const firsts = in_smem ? few_firsts : f.firsts;
     // 1. each sequence's first tile
     const uint32_t per = (a.tok.n_seqs + kPlanThreads - 1) / kPlanThreads;
     const uint32_t s0 = tid * per, s1 = min(a.tok.n_seqs, s0 + per);
     int64_t mine = 0, all;
     for (uint32_t s = s0; s < s1; ++s) mine += row_tiles(a, kv_seq(a.pages, a.tok, s));
     int64_t at = block_scan(mine, sums, &all);
-    for (uint32_t s = s0; s < s1; ++s) {
-        f.firsts[s] = int32_t(at);
-        at += row_tiles(a, kv_seq(a.pages, a.tok, s));
-    }
     // more than the call's tokens make: starts that make no sense
     const int32_t tiles = all > int64_t(f.most) ? 0 : int32_t(all);
-    if (tid == 0) f.firsts[a.tok.n_seqs] = tiles, f.head->tiles = tiles;
+    for (uint32_t s = s0; s < s1; ++s) {
+        firsts[s] = int32_t(at);
+        if (s + 1 < s1) at += row_tiles(a, kv_seq(a.pages, a.tok, s));
+    }
+    if (tid == 0) firsts[a.tok.n_seqs] = tiles, f.head->tiles = tiles;
     __syncthreads();
     // 2. a warp a tile
     KvTokens owner = a.tok;
-    owner.starts = f.firsts;
+    owner.starts = firsts;
     for (int32_t j = int32_t(warp); j < tiles; j += kPlanThreads / 32) {
         const uint32_t s = kv_owner(owner, uint32_t(j));
         const KvSeq q = kv_seq(a.pages, a.tok, s);
-        const int32_t m = j - f.firsts[s], G = int32_t(a.group);
-        const int32_t rows = int32_t(min(int64_t(min(q.n, int32_t(a.tok.max_new))) * G, (int64_t(m) + 1) * kRows));
-        const KvSpan sp = tile_span(a, q, m * kRows / G, (rows + G - 1) / G, int32_t(lane));
+        const int32_t j0 = firsts[s], m = j - j0, G = int32_t(a.group);
+        const int32_t end = int32_t(min(int64_t(min(q.n, int32_t(a.tok.max_new))) * G, (int64_t(m) + 1) * kRows));
+        const KvSpan sp = tile_span(a, q, m * kRows / G, (end + G - 1) / G, int32_t(lane));
         if (lane == 0) {
             PlanTile& t = f.plan[j];
-            t.s = int32_t(s), t.m = m, t.span = sp;
-            t.nt = max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
-            t.last = j + 1 == f.firsts[s + 1];
+            t.s = int32_t(s), t.m = m, t.span = sp, t.q = q, t.rows = end - m * kRows;
+            const int32_t nt = max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
+            t.nt = nt;
+            if (j < kPlanThreads) few_nt[j] = nt;
+            t.last = j + 1 == firsts[s + 1];
         }
     }
     __syncthreads();
@@ -152,46 +168,45 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     const int32_t tper = (tiles + kPlanThreads - 1) / kPlanThreads;
     const int32_t j0 = int32_t(tid) * tper, j1 = min(tiles, j0 + tper);
     mine = 0;
-    for (int32_t j = j0; j < j1; ++j) mine += f.plan[j].nt;
+    for (int32_t j = j0; j < j1; ++j) mine += tper == 1 ? few_nt[j] : f.plan[j].nt;
     at = block_scan(mine, sums, &all);
+    __shared__ int64_t few_before[kPlanThreads];
     for (int32_t j = j0; j < j1; ++j) {
         f.plan[j].before = at;
-        at += f.plan[j].nt;
+        if (tper == 1) few_before[j] = at;
+        if (j + 1 < j1) at += f.plan[j].nt;
     }
     if (tid == 0) f.head->total = all;
     __syncthreads();
     for (int32_t j = j0; j < j1; ++j) {
         PlanTile& t = f.plan[j];
-        const int32_t a0 = f.firsts[t.s], a1 = f.firsts[t.s + 1];
-        t.seq_before = f.plan[a0].before;
-        t.seq_total = (a1 < tiles ? f.plan[a1].before : all) - t.seq_before;
+        const int32_t a0 = firsts[t.s], a1 = firsts[t.s + 1];
+        const int64_t b0 = tper == 1 ? few_before[a0] : f.plan[a0].before;
+        t.seq_before = b0;
+        t.seq_total = (a1 >= tiles ? all : tper == 1 ? few_before[a1] : f.plan[a1].before) - b0;
     }
 }
 
-// The run of one block, unit by unit: in a sequence, key head by key head, its row tiles.
+// The run of one block, unit by unit: in a sequence, key head by key head, its row
+// tiles. The loading warp walks it, one unit ahead of its loads, and leaves each
+// unit in shared memory for the others.
+struct Unit {
+    KvSpan span;
+    KvSeq q;
+    int32_t s, m, h, rows;
+    int32_t tile, n, nt;  // the segment's first key tile in the unit, its key tiles, the unit's
+    int32_t more;         // another unit follows
+    int64_t at;           // the segment's first tile of all
+};
 struct RowWalk {
-    int64_t at, end, unit;
+    int64_t at, end;
     int32_t j, h, tile, n;
     PlanTile t;
-    KvSeq q;
-    int32_t rows;  // of the unit
 };
-__device__ __forceinline__ void walk_load(const Rows& f, RowWalk& w) {
-    w.t = f.plan[w.j];
-    w.q = kv_seq(f.a.pages, f.a.tok, uint32_t(w.t.s));
-    w.rows = int32_t(min(int64_t(min(w.q.n, int32_t(f.a.tok.max_new))) * f.a.group - int64_t(w.t.m) * kRows, int64_t(kRows)));
-}
-__device__ __forceinline__ void walk_start(const Rows& f, RowWalk& w, int32_t j, int32_t h, int32_t tile, int64_t at, int64_t end) {
-    w.at = at, w.end = end, w.j = j, w.h = h, w.tile = tile;
-    w.unit = at - tile;
-    walk_load(f, w);
-    w.n = int32_t(min(int64_t(w.t.nt - tile), end - at));
-}
 __device__ __forceinline__ bool walk_next(const Rows& f, RowWalk& w) {
     w.at += w.n;
     if (w.at >= w.end) return false;
     w.tile = 0;
-    w.unit = w.at;
     if (!w.t.last) {
         ++w.j;
     } else if (w.h + 1 < int32_t(f.a.pages.kv_heads)) {
@@ -201,15 +216,21 @@ __device__ __forceinline__ bool walk_next(const Rows& f, RowWalk& w) {
         ++w.j;
         w.h = 0;
     }
-    walk_load(f, w);
+    w.t = f.plan[w.j];
     w.n = int32_t(min(int64_t(w.t.nt), w.end - w.at));
     return true;
 }
-__device__ __forceinline__ int32_t tile_slot(const RowWalk& w, int32_t i) { return (w.t.span.lo / kTileKeys + i) * kTileKeys; }
+__device__ __forceinline__ int32_t tile_slot(const KvSpan& s, int32_t i) { return (s.lo / kTileKeys + i) * kTileKeys; }
+
+// Units in shared memory at a time: the loading warp is at most two tiles ahead of
+// the products, which are at most one unit ahead of what softmax writes.
+constexpr uint32_t kUnits = 8;
 
 struct RowShared {
     uint64_t full[kRowEntries], empty[kRowEntries];
     uint64_t s_full[2], p_full[2], pv_done[2], q_full[2];
+    uint64_t unit_full[kUnits];
+    Unit unit[kUnits];
     uint32_t tmem, dead;
     int32_t start_j, start_h, start_tile;
     int32_t draft[2][64];  // positions of the unit's drafted tokens
@@ -252,6 +273,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i]), 128);
             mbar_init(bar(sh.pv_done[i]), 1), mbar_init(bar(sh.q_full[i]), 128);
         }
+        for (uint32_t i = 0; i < kUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1);
         sh.dead = 0;
         fence_mbar_init();
         tma_prefetch_map(&map);
@@ -280,361 +302,407 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     fence_after();
     const uint32_t tmem = sh.tmem;
 
-    if (busy && warp == 8) {
-        // ---------------------------------------------------------- loads
-        RowWalk w;
-        walk_start(f, w, sh.start_j, sh.start_h, sh.start_tile, run0, run1);
-        const uint32_t shift = a.pages.token_shift;
-        const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
-        const uint32_t mask = (1u << shift) - 1;
-        const int halves = D > 64 ? 2 : 1;
-        uint32_t n = 0;
-        do {
-            const int32_t row_k = int32_t((a.pages.layer * 2 * a.pages.kv_heads + w.h) << shift);
-            const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
-            const int32_t* table = a.pages.table + uint32_t(w.t.s) * a.pages.table_stride;
-            for (int32_t i = 0; i < w.n; ++i) {
-                const uint32_t slot = uint32_t(tile_slot(w, w.tile + i)) + lane * box;
-                int32_t page = -1;
-                if (lane < boxes && slot < uint32_t(w.q.len)) page = table[slot >> shift];
-                // what the pool lacks, and what lies behind the sequence, is filled with zeros
-                const int32_t z = uint32_t(page) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page;
-                const int32_t y = int32_t(slot & mask);
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv, ++n) {
-                    const uint32_t e = n % kRowEntries;
-                    if (!mbar_wait(bar(sh.empty[e]), (n / kRowEntries & 1) ^ 1, dead)) goto loads_done;
-                    if (lane == 0) mbar_expect(bar(sh.full[e]), uint32_t(halves) * 16384u);
-                    __syncwarp();
-                    if (lane < boxes)
-                        for (int x = 0; x < halves; ++x)
-                            tma_load(ring + e * kEntryBytes + x * 16384 + lane * box * 128, &map, x * 64,
-                                     (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
+    if (busy && warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == 8) {
+            // ---------------------------------------------------------- loads
+            RowWalk w;
+            w.at = run0, w.end = run1, w.j = sh.start_j, w.h = sh.start_h, w.tile = sh.start_tile;
+            w.t = f.plan[w.j];
+            w.n = int32_t(min(int64_t(w.t.nt - w.tile), run1 - run0));
+            uint32_t u = 0;  // units left in shared memory
+            auto publish = [&]() {
+                if (lane == 0) {
+                    Unit& o = sh.unit[u % kUnits];
+                    o.span = w.t.span, o.q = w.t.q, o.s = w.t.s, o.m = w.t.m, o.h = w.h, o.rows = w.t.rows;
+                    o.tile = w.tile, o.n = w.n, o.nt = w.t.nt, o.at = w.at, o.more = w.at + w.n < w.end;
+                    mbar_arrive(bar(sh.unit_full[u % kUnits]));
+                }
+                ++u;
+                __syncwarp();
+            };
+            publish();
+            const uint32_t shift = a.pages.token_shift;
+            const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
+            const uint32_t mask = (1u << shift) - 1;
+            const int halves = D > 64 ? 2 : 1;
+            uint32_t n = 0;
+            bool more = true;
+            while (more) {
+                const int32_t row_k = int32_t((a.pages.layer * 2 * a.pages.kv_heads + w.h) << shift);
+                const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
+                const int32_t* table = a.pages.table + uint32_t(w.t.s) * a.pages.table_stride;
+                const int32_t slot0 = tile_slot(w.t.span, w.tile), tiles = w.n, len = w.t.q.len;
+                for (int32_t i = 0; i < tiles; ++i) {
+                    const uint32_t slot = uint32_t(slot0 + i * kTileKeys) + lane * box;
+                    int32_t page = -1;
+                    if (lane < boxes && slot < uint32_t(len)) page = table[slot >> shift];
+                    // what the pool lacks, and what lies behind the sequence, is filled with zeros
+                    const int32_t z = uint32_t(page) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page;
+                    const int32_t y = int32_t(slot & mask);
+    #pragma unroll
+                    for (int kv = 0; kv < 2; ++kv, ++n) {
+                        const uint32_t e = n % kRowEntries;
+                        if (!mbar_wait(bar(sh.empty[e]), (n / kRowEntries & 1) ^ 1, dead)) goto loads_done;
+                        if (lane == 0) mbar_expect(bar(sh.full[e]), uint32_t(halves) * 16384u);
+                        __syncwarp();
+                        if (lane < boxes)
+                            for (int x = 0; x < halves; ++x)
+                                tma_load(ring + e * kEntryBytes + x * 16384 + lane * box * 128, &map, x * 64,
+                                         (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
+                    }
+                    if (i == 0) {  // the next unit, while this one's loads are under way
+                        more = walk_next(f, w);
+                        if (more) publish();
+                    }
                 }
             }
-        } while (walk_next(f, w));
-    loads_done:
-        __syncwarp();
-        if (*dead) {  // the copies in flight land before the block ends
-            uint32_t late = 0;
-            for (uint32_t k = n > kRowEntries ? n - kRowEntries : 0; k < n; ++k)
-                mbar_wait(bar(sh.full[k % kRowEntries]), k / kRowEntries & 1, &late);
-        }
-    } else if (busy && warp == 9) {
-        // ---------------------------------------------------------- products
-        RowWalk w;
-        walk_start(f, w, sh.start_j, sh.start_h, sh.start_tile, run0, run1);
-        const uint32_t dn = (D + 15) / 16;
-        constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, 128);
-        const uint32_t kPv = instr_desc(kBf16, false, true, 128, 0) | (dn * 2) << 17;
-        uint32_t units[2] = {0, 0}, cnt[2] = {0, 0};  // of each stage: units begun, tiles weighed
-        auto qk = [&](int st, uint32_t g, bool fresh, bool two) {
-            if (fresh) mbar_wait(bar(sh.q_full[st]), units[st]++ & 1, dead);
-            const uint32_t n = 2 * g, e = n % kRowEntries;
-            mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
-            fence_after();
-            if (elect() && !*dead) {
-                const uint32_t k0 = ring + e * kEntryBytes, q0 = base + st * kEntryBytes;
-                for (uint32_t k = 0; k < dn; ++k)
-                    mma_ss(tmem + st * 128, smem_desc(q0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2),
-                           smem_desc(k0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2), kQk, k != 0);
-                if (st || !two) mma_commit(bar(sh.empty[e]));
-                mma_commit(bar(sh.s_full[st]));
-            }
+        loads_done:
             __syncwarp();
-        };
-        auto pv = [&](int st, uint32_t g, bool fresh, bool two) {
-            const uint32_t n = 2 * g + 1, e = n % kRowEntries;
-            mbar_wait(bar(sh.p_full[st]), cnt[st]++ & 1, dead);
-            mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
-            fence_after();
-            if (elect() && !*dead) {
-                const uint32_t v = ring + e * kEntryBytes;
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, smem_desc(v + k * 2048, 16384, 1024, 2), kPv,
-                           !(fresh && k == 0));
-                if (st || !two) mma_commit(bar(sh.empty[e]));
-                mma_commit(bar(sh.pv_done[st]));
+            if (*dead) {  // the copies in flight land before the block ends
+                uint32_t late = 0;
+                for (uint32_t k = n > kRowEntries ? n - kRowEntries : 0; k < n; ++k)
+                    mbar_wait(bar(sh.full[k % kRowEntries]), k / kRowEntries & 1, &late);
             }
-            __syncwarp();
-        };
-        uint32_t g = 0;
-        int32_t i = 0;
-        bool two = w.rows > 128, fresh = true;
-        qk(0, 0, true, two);
-        if (two) qk(1, 0, true, two);
-        for (;;) {
-            // the next tile, whose scores are issued between this one's products
-            bool more = true, next_fresh = false, next_two = two;
-            if (++i == w.n) {
-                more = walk_next(f, w);
-                i = 0;
-                next_fresh = true;
-                next_two = w.rows > 128;
+        } else if (warp == 9) {
+            // ---------------------------------------------------------- products
+            const uint32_t dn = (D + 15) / 16;
+            constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, 128);
+            const uint32_t kPv = instr_desc(kBf16, false, true, 128, 0) | (dn * 2) << 17;
+            uint32_t units[2] = {0, 0}, cnt[2] = {0, 0};  // of each stage: units begun, tiles weighed
+            auto qk = [&](int st, uint32_t g, bool fresh, bool two) {
+                if (fresh) mbar_wait(bar(sh.q_full[st]), units[st]++ & 1, dead);
+                const uint32_t n = 2 * g, e = n % kRowEntries;
+                mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
+                fence_after();
+                if (elect() && !*dead) {
+                    const uint32_t k0 = ring + e * kEntryBytes, q0 = base + st * kEntryBytes;
+                    for (uint32_t k = 0; k < dn; ++k)
+                        mma_ss(tmem + st * 128, smem_desc(q0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2),
+                               smem_desc(k0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2), kQk, k != 0);
+                    if (st || !two) mma_commit(bar(sh.empty[e]));
+                    mma_commit(bar(sh.s_full[st]));
+                }
+                __syncwarp();
+            };
+            auto pv = [&](int st, uint32_t g, bool fresh, bool two) {
+                const uint32_t n = 2 * g + 1, e = n % kRowEntries;
+                mbar_wait(bar(sh.p_full[st]), cnt[st]++ & 1, dead);
+                mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
+                fence_after();
+                if (elect() && !*dead) {
+                    const uint32_t v = ring + e * kEntryBytes;
+    #pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, smem_desc(v + k * 2048, 16384, 1024, 2), kPv,
+                               !(fresh && k == 0));
+                    if (st || !two) mma_commit(bar(sh.empty[e]));
+                    mma_commit(bar(sh.pv_done[st]));
+                }
+                __syncwarp();
+            };
+            uint32_t g = 0, u = 0;
+            int32_t i = 0, n = 0;
+            bool two = false, follows = false, fresh = true;
+            auto unit = [&]() {
+                mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead);
+                const Unit& o = sh.unit[u % kUnits];
+                ++u;
+                n = o.n, follows = o.more;
+                if (o.rows <= 128) mbar_wait(bar(sh.q_full[1]), units[1]++ & 1, dead);
+                return o.rows > 128;
+            };
+            two = unit();
+            qk(0, 0, true, two);
+            if (two) qk(1, 0, true, two);
+            while (!*dead) {
+                // the next tile's scores are issued between this one's products
+                const bool same = ++i < n;
+                pv(0, g, fresh, two);
+                if (same) qk(0, g + 1, false, two);
+                if (two) pv(1, g, fresh, two);
+                if (same) {
+                    if (two) qk(1, g + 1, false, two);
+                } else {
+                    if (!follows) break;
+                    i = 0;
+                    two = unit();
+                    qk(0, g + 1, true, two);
+                    if (two) qk(1, g + 1, true, two);
+                }
+                fresh = !same;
+                ++g;
             }
-            pv(0, g, fresh, two);
-            if (more && !next_fresh) qk(0, g + 1, false, next_two);
-            if (two) pv(1, g, fresh, two);
-            if (!more) break;
-            if (next_fresh) qk(0, g + 1, true, next_two);
-            if (next_two) qk(1, g + 1, next_fresh, next_two);
-            fresh = next_fresh, two = next_two;
-            ++g;
-        }
-        if (*dead) {  // the products in flight end before the tensor memory is freed
-            const uint64_t t0 = now_ns();
-            while (now_ns() - t0 < 50000) {
+            if (*dead) {  // the products in flight end before the tensor memory is freed
+                const uint64_t t0 = now_ns();
+                while (now_ns() - t0 < 50000) {
+                }
             }
         }
     } else if (busy) {
         // ---------------------------------------------------------- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         const int st = warp / 4;
         const uint32_t r = tid % 128;  // the row of the stage
-        RowWalk w;
-        walk_start(f, w, sh.start_j, sh.start_h, sh.start_tile, run0, run1);
-        if (tid == 0) {
-            const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.t.nt) * blocks - 1) / total;
-            const bool here = w.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
-            f.join[blockIdx.x] = {w.j, w.h, int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
-        }
         const uint32_t lanes = tmem + ((warp % 4) << 21), s_at = lanes + st * 128, o_at = lanes + 256 + st * 128;
         // a negative scale turns the queries' signs, so that the largest product is the largest score
         const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
         const float k2 = fabsf(a.scale) * kLog2e;
-        const float cap_in = MOD && a.softcap != 0.0f ? fabsf(a.scale) / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
-        // a unit's queries to shared memory, 64 dimensions at a time, 128-byte swizzle
-        auto load_q = [&](const RowWalk& u) {
-            const uint32_t row0 = uint32_t(u.t.m) * kRows + st * 128;
-            for (uint32_t k = r; k < 128 * 16; k += 128) {
-                const uint32_t c = k / 16, x = k % 16;
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (int32_t(st * 128 + c) < u.rows && x * 8 < D) {
-                    const uint32_t t = (row0 + c) / a.group, g = (row0 + c) % a.group;
-                    v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(u.q.first + t) * a.q_stride +
-                                                        uint64_t(u.h * a.group + g) * D + x * 8);
-                    v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
-                }
-                *reinterpret_cast<uint4*>(mem + st * kEntryBytes + (x / 8) * 16384 + c * 128 + ((x % 8) ^ (c % 8)) * 16) = v;
+        const bool cap = MOD && a.softcap != 0.0f;
+        const float cap_in = cap ? fabsf(a.scale) / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
+        const float kk = cap ? 1.0f : k2;  // what is left to scale after the cap
+        auto unit = [&](uint32_t u) -> const Unit& {
+            mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead);
+            return sh.unit[u % kUnits];
+        };
+        // a row of a unit's queries to shared memory, 64 dimensions at a time, 128-byte swizzle
+        // (of a unit without a second stage, that stage only says that it has come by)
+        auto load_q = [&](const Unit& o) {
+            if (st && o.rows <= 128) {
+                mbar_arrive(bar(sh.q_full[st]));
+                return;
+            }
+            const uint32_t row = uint32_t(o.m) * kRows + st * 128 + r;
+            const bool real = int32_t(st * 128 + r) < o.rows;
+            const uint32_t t = row / a.group, g = row % a.group;
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(o.q.first + t) * a.q_stride +
+                                                              uint64_t(o.h * a.group + g) * D);
+            uint8_t* dst = mem + st * kEntryBytes + r * 128;
+#pragma unroll
+            for (uint32_t x0 = 0; x0 < 16; x0 += 8) {
+                uint4 v[8];
+#pragma unroll
+                for (uint32_t x = 0; x < 8; ++x) v[x] = real && (x0 + x) * 8 < D ? src[x0 + x] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (uint32_t x = 0; x < 8; ++x)
+                    *reinterpret_cast<uint4*>(dst + x0 / 8 * 16384 + (x ^ (r % 8)) * 16) =
+                        make_uint4(v[x].x ^ flip, v[x].y ^ flip, v[x].z ^ flip, v[x].w ^ flip);
             }
             fence_async_smem();
             mbar_arrive(bar(sh.q_full[st]));
         };
-        if (st == 0 || w.rows > 128) load_q(w);
+        {
+            const Unit& o = unit(0);
+            if (tid == 0) {
+                // this run's note of a unit that began in the run before it
+                const int64_t u0 = o.at - o.tile;
+                const int64_t b0 = ((u0 + 1) * blocks - 1) / total, b1 = ((u0 + o.nt) * blocks - 1) / total;
+                const bool here = o.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
+                f.join[blockIdx.x] = {o.q.first, o.m, o.rows, o.h, int32_t(b0), int32_t(b1), b0 * total / blocks != u0, here};
+            }
+            load_q(o);
+        }
         uint32_t n = 0;  // tiles of this stage
         bool more = true;
-        while (more) {
-            RowWalk next;
-            const bool on = st == 0 || w.rows > 128;
-            if (on) {
-                const int32_t ctx = w.q.len - w.q.n;
-                const uint32_t row = uint32_t(w.t.m) * kRows + st * 128 + r;
-                const bool real = int32_t(st * 128 + r) < w.rows;
-                const uint32_t tok = real ? row / a.group : 0, gh = row % a.group;
-                KvQuery qy{0, INT32_MAX, 0, 0};
-                float slope = 0.0f;
-                if (real) {
-                    qy = kv_query(a, w.q, int32_t(tok));
-                    if (MOD && a.slopes) slope = a.slopes[w.h * a.group + gh] * kLog2e;
-                }
-                if (a.tree) {
-                    if (r < 64) {
-                        const bool drafted = int32_t(r) < w.q.n;
-                        sh.draft[st][r] = drafted ? ctx + __popcll(a.tree[w.q.first + int32_t(r)]) - 1 : 0;
+        for (uint32_t u = 0; more; ++u) {
+            const Unit& o = unit(u);
+            more = o.more && !*dead;
+            if (st && o.rows <= 128) {
+                if (more) load_q(unit(u + 1));
+                continue;
+            }
+            const KvSpan span = o.span;
+            const int32_t ctx = o.q.len - o.q.n, tiles = o.n;
+            const bool real = int32_t(st * 128 + r) < o.rows;
+            KvQuery qy{0, INT32_MAX, 0, 0};
+            float slope = 0.0f;
+            if (real) {
+                const uint32_t row = uint32_t(o.m) * kRows + st * 128 + r;
+                qy = kv_query(a, o.q, int32_t(row / a.group));
+                if (MOD && a.slopes) slope = a.slopes[o.h * a.group + row % a.group] * kLog2e;
+            }
+            if (a.tree) {
+                if (st)  // (the unit before has been read)
+                    bar_sync<2, 128>();
+                else
+                    bar_sync<1, 128>();
+                if (r < 64) sh.draft[st][r] = int32_t(r) < o.q.n ? ctx + __popcll(a.tree[o.q.first + int32_t(r)]) - 1 : INT32_MIN;
+                if (st)
+                    bar_sync<2, 128>();
+                else
+                    bar_sync<1, 128>();
+                // of the drafted tokens, those that are there and inside the window
+                if (real)
+                    for (int b = 0; b < 64; ++b)
+                        if (sh.draft[st][b] < qy.first) qy.word &= ~(uint64_t(1) << b);
+            }
+            const float pos = float(qy.pos);
+            float ref = -INFINITY, sum = 0.0f;
+            for (int32_t i = 0; i < tiles; ++i, ++n) {
+                const int32_t slot0 = tile_slot(span, o.tile + i);
+                const bool masked = slot0 < span.all_lo || slot0 + kTileKeys > span.all_hi;
+                const bool drafts = a.tree && slot0 + kTileKeys > ctx;
+                // the row's visible keys of the tile, a bit each
+                uint32_t see[4] = {};
+                if (masked) {
+                    const int32_t d = ctx - slot0;
+                    uint64_t w0 = 0, w1 = 0;
+                    if (drafts) {
+                        w0 = d >= 64 ? 0 : d >= 0 ? qy.word << d : d > -64 ? qy.word >> -d : 0;
+                        w1 = d >= 128 ? 0 : d >= 64 ? qy.word << (d - 64) : d > 0 ? qy.word >> (64 - d) : 0;
                     }
-                    if (st)
-                        bar_sync<2, 128>();
-                    else
-                        bar_sync<1, 128>();
-                }
-                float ref = -INFINITY, sum = 0.0f;
-                for (int32_t i = 0; i < w.n; ++i, ++n) {
-                    const int32_t slot0 = tile_slot(w, w.tile + i);
-                    const bool masked = slot0 < w.t.span.all_lo || slot0 + kTileKeys > w.t.span.all_hi;
-                    const bool drafts = a.tree && slot0 + kTileKeys > ctx;
-                    mbar_wait(bar(sh.s_full[st]), n & 1, dead);
-                    fence_after();
-                    if (MOD || masked) {
-                        // caps, biases and masks, 32 keys at a time, back to tensor memory: what follows
-                        // holds all 128 scores in registers
-                        const int32_t d = ctx - slot0;  // the drafted tokens' bits, from this tile's first key on
-                        uint64_t w0 = 0, w1 = 0;
-                        if (drafts) {
-                            w0 = d >= 64 ? 0 : d >= 0 ? qy.word << d : d > -64 ? qy.word >> -d : 0;
-                            w1 = d >= 128 ? 0 : d >= 64 ? qy.word << (d - 64) : d > 0 ? qy.word >> (64 - d) : 0;
-                        }
-#pragma unroll 1
-                        for (int c0 = 0; c0 < 128; c0 += 32) {
-                            float y[32];
-                            tmem_ld32(s_at + c0, y);
-                            wait_ld(y);
-                            const uint32_t bits = uint32_t((c0 < 64 ? w0 : w1) >> (c0 & 32));
+                    see[0] = uint32_t(w0), see[1] = uint32_t(w0 >> 32), see[2] = uint32_t(w1), see[3] = uint32_t(w1 >> 32);
+                    const int64_t f0 = int64_t(qy.first) - slot0, l0 = int64_t(qy.last) - slot0;
 #pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int32_t lo = int32_t(max(int64_t(0), min(int64_t(32), f0 - c * 32)));
+                        const int32_t hi = int32_t(max(int64_t(0), min(int64_t(32), l0 - c * 32)));
+                        const uint32_t below = hi == 32 ? 0xFFFFFFFFu : (1u << hi) - 1, under = lo == 32 ? 0xFFFFFFFFu : (1u << lo) - 1;
+                        see[c] |= below & ~under;
+                    }
+                }
+                mbar_wait(bar(sh.s_full[st]), n & 1, dead);
+                fence_after();
+                if (cap) {
+                    // the cap takes two special functions a score: once, back to tensor memory
+#pragma unroll 1
+                    for (int c0 = 0; c0 < 128; c0 += 32) {
+                        float y[32];
+                        tmem_ld32(s_at + c0, y);
+                        wait_ld(y);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) y[c] = capped(y[c], cap_in, cap2);
+                        tmem_st16(s_at + c0, reinterpret_cast<uint32_t*>(y));
+                        tmem_st16(s_at + c0 + 16, reinterpret_cast<uint32_t*>(y) + 16);
+                    }
+                    wait_st();
+                }
+                // bias (scores in units of log2 from here on, if MOD) and mask
+                const float ahead = pos - float(slot0);
+                auto shape = [&](float* x, int c0) {
+                    if (MOD) {
+                        if (drafts && a.slopes) {
                             for (int c = 0; c < 32; ++c) {
                                 const int32_t key = slot0 + c0 + c;
-                                int32_t kp = key;
-                                if (drafts && key >= ctx) kp = sh.draft[st][min(key - ctx, 63)];
-                                if (MOD) {
-                                    y[c] = cap_in != 0.0f ? capped(y[c], cap_in, cap2) : y[c] * k2;
-                                    y[c] -= slope * fabsf(float(qy.pos - kp));
-                                }
-                                const bool see = kp >= qy.first && (key < qy.last || (bits >> c & 1 && key < w.q.len));
-                                if (masked && !see) y[c] = -INFINITY;
+                                const float far = key >= ctx ? pos - float(sh.draft[st][min(key - ctx, 63)]) : ahead - float(c0 + c);
+                                x[c] = x[c] * kk - slope * fabsf(far);
                             }
-                            tmem_st16(s_at + c0, reinterpret_cast<uint32_t*>(y));
-                            tmem_st16(s_at + c0 + 16, reinterpret_cast<uint32_t*>(y) + 16);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) x[c] = x[c] * kk - slope * fabsf(ahead - float(c0 + c));
+                        }
+                    }
+                    if (masked) {
+                        const uint32_t bits = see[c0 / 32];
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) x[c] = bits & (1u << c) ? x[c] : -INFINITY;
+                    }
+                };
+                float x[128];
+                tmem_ld32(s_at, x), tmem_ld32(s_at + 32, x + 32), tmem_ld32(s_at + 64, x + 64), tmem_ld32(s_at + 96, x + 96);
+                wait_ld(x);
+                float m = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+                for (int c0 = 0; c0 < 128; c0 += 32) shape(x + c0, c0);
+#pragma unroll
+                for (int c = 0; c < 128; c += 4) {
+                    m = fmaxf(m, fmaxf(x[c], x[c + 1]));
+                    m1 = fmaxf(m1, fmaxf(x[c + 2], x[c + 3]));
+                }
+                m = fmaxf(m, m1);
+                if (!MOD) m *= k2;
+                const bool up = m > ref + kRowRaise;
+                if (__any_sync(0xFFFFFFFFu, up)) {
+                    float by = 1.0f;
+                    if (up) {
+                        by = exp2_approx(ref - m);
+                        ref = m;
+                    }
+                    sum *= by;
+                    if (i) {
+                        mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
+                        fence_after();
+                        for (uint32_t c0 = 0; c0 < D; c0 += 16) {
+                            float y[16];
+                            tmem_ld16(o_at + c0, y);
+                            wait_ld(y);
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) y[c] *= by;
+                            tmem_st16(o_at + c0, reinterpret_cast<uint32_t*>(y));
                         }
                         wait_st();
                     }
-                    // the row's maximum, then its weights, 32 keys at a time with the next 32 on the way
-                    float m = -INFINITY;
-                    float xa[32], xb[32];
-                    auto peak = [&](const float (&x)[32]) {
-                        float m0 = fmaxf(x[0], x[1]), m1 = fmaxf(x[2], x[3]);
+                }
+                const float off = ref == -INFINITY ? 0.0f : -ref;
+                const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
+                uint64_t sum2 = 0, sum3 = 0;
 #pragma unroll
-                        for (int c = 4; c < 32; c += 4) {
-                            m0 = fmaxf(m0, fmaxf(x[c], x[c + 1]));
-                            m1 = fmaxf(m1, fmaxf(x[c + 2], x[c + 3]));
-                        }
-                        m = fmaxf(m, fmaxf(m0, m1));
-                    };
-                    tmem_ld32(s_at, xa);
-                    wait_ld(xa);
-                    tmem_ld32(s_at + 32, xb);
-                    peak(xa);
-                    wait_ld(xb);
-                    tmem_ld32(s_at + 64, xa);
-                    peak(xb);
-                    wait_ld(xa);
-                    tmem_ld32(s_at + 96, xb);
-                    peak(xa);
-                    wait_ld(xb);
-                    tmem_ld32(s_at, xa);
-                    peak(xb);
-                    if (!MOD) m *= k2;
-                    const bool up = m > ref + kRowRaise;
-                    if (__any_sync(0xFFFFFFFFu, up)) {
-                        float by = 1.0f;
-                        if (up) {
-                            by = exp2_approx(ref - m);
-                            ref = m;
-                        }
-                        sum *= by;
-                        if (i) {
-                            mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
-                            fence_after();
-                            for (uint32_t c0 = 0; c0 < D; c0 += 16) {
-                                float o[16];
-                                tmem_ld16(o_at + c0, o);
-                                wait_ld(o);
-#pragma unroll
-                                for (int c = 0; c < 16; ++c) o[c] *= by;
-                                tmem_st16(o_at + c0, reinterpret_cast<uint32_t*>(o));
-                            }
-                            wait_st();
-                        }
-                    }
-                    const float off = ref == -INFINITY ? 0.0f : -ref;
-                    const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
-                    uint64_t sum2 = 0, sum3 = 0;
-                    auto weigh = [&](const float (&x)[32], uint32_t (&p)[16]) {
-#pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            float u0, u1, u2, u3;
-                            unpack2(fma2(pack2(x[c], x[c + 1]), by2, off2), u0, u1);
-                            unpack2(fma2(pack2(x[c + 2], x[c + 3]), by2, off2), u2, u3);
-                            u0 = exp2_approx(u0), u1 = exp2_approx(u1), u2 = exp2_approx(u2), u3 = exp2_approx(u3);
-                            sum2 = add2(sum2, pack2(u0, u1));
-                            sum3 = add2(sum3, pack2(u2, u3));
-                            p[c / 2] = Kv16<T>::from2(u0, u1);
-                            p[c / 2 + 1] = Kv16<T>::from2(u2, u3);
-                        }
-                    };
-                    // weights 2c and 2c + 1 to column c: behind the scores that are still to be read
+                for (int c0 = 0; c0 < 128; c0 += 32) {
                     uint32_t p[16];
-                    wait_ld(xa);
-                    tmem_ld32(s_at + 32, xb);
-                    weigh(xa, p);
-                    wait_ld(xb);
-                    tmem_ld32(s_at + 64, xa);
-                    tmem_st16(s_at, p);
-                    weigh(xb, p);
-                    wait_ld(xa);
-                    tmem_ld32(s_at + 96, xb);
-                    tmem_st16(s_at + 16, p);
-                    weigh(xa, p);
-                    wait_ld(xb);
-                    tmem_st16(s_at + 32, p);
-                    weigh(xb, p);
-                    tmem_st16(s_at + 48, p);
-                    float u0, u1;
-                    unpack2(add2(sum2, sum3), u0, u1);
-                    sum += u0 + u1;
-                    if (st == 0 && (slot0 < w.t.span.lo || slot0 + kTileKeys > w.t.span.hi)) {
-                        // values that none of the unit's queries sees may be anything: zeros, as their weights are
-                        const uint32_t e = (2 * n + 1) % kRowEntries;
-                        mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
-                        const int32_t key = slot0 + int32_t(r);
-                        if (key < w.t.span.lo || key >= w.t.span.hi) {
 #pragma unroll
-                            for (int k = 0; k < 16; ++k)
-                                if (k < 8 || D > 64)
-                                    *reinterpret_cast<uint4*>(mem + 2 * kEntryBytes + e * kEntryBytes + k / 8 * 16384 + r * 128 +
-                                                              k % 8 * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_smem();
+                    for (int c = 0; c < 32; c += 4) {
+                        float u0, u1, u2, u3;
+                        unpack2(fma2(pack2(x[c0 + c], x[c0 + c + 1]), by2, off2), u0, u1);
+                        unpack2(fma2(pack2(x[c0 + c + 2], x[c0 + c + 3]), by2, off2), u2, u3);
+                        u0 = exp2_approx(u0), u1 = exp2_approx(u1), u2 = exp2_approx(u2), u3 = exp2_approx(u3);
+                        sum2 = add2(sum2, pack2(u0, u1));
+                        sum3 = add2(sum3, pack2(u2, u3));
+                        p[c / 2] = Kv16<T>::from2(u0, u1);
+                        p[c / 2 + 1] = Kv16<T>::from2(u2, u3);
                     }
-                    wait_st();
-                    fence_before();
-                    mbar_arrive(bar(sh.p_full[st]));
+                    tmem_st16(s_at + c0 / 2, p);  // weights 2c and 2c + 1 in column c
                 }
-                next = w;
-                more = walk_next(f, next);
-                if (more && (st == 0 || next.rows > 128)) load_q(next);  // its scores start while this unit is written
-                mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
-                fence_after();
-                if (w.n == w.t.nt) {
-                    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    const uint64_t orow = uint64_t(w.q.first) + tok;
-                    T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(w.h * a.group + gh) * D;
-                    for (uint32_t c0 = 0; c0 < D; c0 += 16) {
-                        float o[16];
-                        tmem_ld16(o_at + c0, o);
-                        wait_ld(o);
-                        if (!real) continue;
+                float u0, u1;
+                unpack2(add2(sum2, sum3), u0, u1);
+                sum += u0 + u1;
+                if (st == 0 && (slot0 < span.lo || slot0 + kTileKeys > span.hi)) {
+                    // values that none of the unit's queries sees may be anything: zeros, as their weights are
+                    const uint32_t e = (2 * n + 1) % kRowEntries;
+                    mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
+                    const int32_t key = slot0 + int32_t(r);
+                    if (key < span.lo || key >= span.hi) {
 #pragma unroll
-                        for (int c = 0; c < 16; c += 8) {
-                            if (c0 + c >= D) break;
-                            float y[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) y[k] = o[c + k] * by;
-                            kv_store8(out + c0 + c, y);
-                        }
+                        for (int k = 0; k < 16; ++k)
+                            if (k < 8 || D > 64)
+                                *reinterpret_cast<uint4*>(mem + 2 * kEntryBytes + e * kEntryBytes + k / 8 * 16384 + r * 128 +
+                                                          k % 8 * 16) = make_uint4(0, 0, 0, 0);
                     }
-                    if (real && a.lse) a.lse[orow * a.q_heads + w.h * a.group + gh] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
-                } else {
-                    // a part of the unit: [head_dim / 4][256 rows] of four, maxima, sums
-                    float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * kRowPart;
-                    const uint32_t pr = st * 128 + r;
-                    for (uint32_t c0 = 0; c0 < D; c0 += 16) {
-                        float o[16];
-                        tmem_ld16(o_at + c0, o);
-                        wait_ld(o);
-#pragma unroll
-                        for (int c = 0; c < 16; c += 4)
-                            __stcg(reinterpret_cast<float4*>(part) + (c0 + c) / 4 * kRows + pr,
-                                   make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]));
-                    }
-                    __stcg(part + kRows * 128 + pr, ref);
-                    __stcg(part + kRows * 128 + kRows + pr, sum);
+                    fence_async_smem();
                 }
+                wait_st();
                 fence_before();
-            } else {
-                next = w;
-                more = walk_next(f, next);
-                if (more && next.rows > 128) load_q(next);
+                mbar_arrive(bar(sh.p_full[st]));
             }
-            w = next;
+            if (more) load_q(unit(u + 1));  // the next unit's scores start while this one is written
+            mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
+            fence_after();
+            if (tiles == o.nt) {
+                const uint32_t row = uint32_t(o.m) * kRows + st * 128 + r;
+                const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+                const uint64_t orow = uint64_t(o.q.first) + row / a.group;
+                const uint32_t head = o.h * a.group + row % a.group;
+                T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D;
+                for (uint32_t c0 = 0; c0 < D; c0 += 16) {
+                    float y[16];
+                    tmem_ld16(o_at + c0, y);
+                    wait_ld(y);
+#pragma unroll
+                    for (int c = 0; c < 16; c += 8) {
+                        if (!real || c0 + c >= D) continue;
+                        float z[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) z[k] = y[c + k] * by;
+                        kv_store8(out + c0 + c, z);
+                    }
+                }
+                if (real && a.lse) a.lse[orow * a.q_heads + head] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+            } else {
+                // a part of the unit: [head_dim / 4][256 rows] of four, maxima, sums
+                float* part = f.part + (uint64_t(blockIdx.x) * 2 + (o.at == run0 ? 0 : 1)) * kRowPart;
+                const uint32_t pr = st * 128 + r;
+                for (uint32_t c0 = 0; c0 < D; c0 += 16) {
+                    float y[16];
+                    tmem_ld16(o_at + c0, y);
+                    wait_ld(y);
+#pragma unroll
+                    for (int c = 0; c < 16; c += 4)
+                        __stcg(reinterpret_cast<float4*>(part) + (c0 + c) / 4 * kRows + pr,
+                               make_float4(y[c], y[c + 1], y[c + 2], y[c + 3]));
+                }
+                __stcg(part + kRows * 128 + pr, ref);
+                __stcg(part + kRows * 128 + kRows + pr, sum);
+            }
+            fence_before();
         }
     }
     if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
@@ -655,12 +723,9 @@ __global__ void __launch_bounds__(256) rows_join_kernel(const __grid_constant__ 
     pdl_wait();
     const Join j = f.join[blockIdx.x];
     if (!j.valid) return;
-    RowWalk w;
-    w.j = j.tile;
-    walk_load(f, w);
     const uint32_t warp = threadIdx.x / 32, D = a.pages.head_dim;
     const int32_t r = int32_t(blockIdx.y * 32 + threadIdx.x % 32);
-    if (r >= w.rows) return;
+    if (r >= j.rows) return;
     auto part = [&](int32_t b) { return f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * kRowPart; };
     float top = -INFINITY, l = 0.0f;
     for (int32_t b = j.b0; b <= j.b1; ++b) top = fmaxf(top, __ldcg(part(b) + kRows * 128 + r));
@@ -677,8 +742,8 @@ __global__ void __launch_bounds__(256) rows_join_kernel(const __grid_constant__ 
             o[k].x += x * v.x, o[k].y += x * v.y, o[k].z += x * v.z, o[k].w += x * v.w;
         }
     }
-    const uint32_t row = uint32_t(w.t.m) * kRows + uint32_t(r), head = uint32_t(j.h) * a.group + row % a.group;
-    const uint64_t orow = uint64_t(w.q.first) + row / a.group;
+    const uint32_t row = uint32_t(j.m) * kRows + uint32_t(r), head = uint32_t(j.h) * a.group + row % a.group;
+    const uint64_t orow = uint64_t(j.first) + row / a.group;
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
     T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D;
 #pragma unroll
