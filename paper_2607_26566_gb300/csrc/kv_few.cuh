@@ -277,6 +277,10 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
         constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
         constexpr uint32_t kPv = instr_desc(kBf16, true, true, 128, N);
         const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
+        // keys and queries: rows of 64 elements, swizzled; values: the same rows, read along the keys; weights:
+        // eight columns to 16 bytes, a key after the other
+        const uint64_t kd = smem_desc(ring, 16, 1024, 2), qd = smem_desc(qs, 16, 1024, 2), vd = smem_desc(ring, kSlot, 1024, 2);
+        const uint64_t pd = smem_desc(ps, 128, 2048, 0);
         uint32_t n = 0, seg = 0;  // tile of the run
         bool fresh_before = false;
         auto pv = [&](uint32_t i, bool fresh) {
@@ -285,13 +289,13 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
             mbar_wait(bar(sh.full[e]), (2 * i + 1) / Sh::kEntries & 1, dead);
             fence_after();
             if (elect() && !*dead) {
-                const uint32_t v = ring + e * Sh::kEntry;
+                const uint64_t v0 = desc_at(vd, e * Sh::kEntry);
 #pragma unroll
                 for (int part = 0; part < 2; ++part)
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        mma_ss(tmem + 2 * N, smem_desc(v + k * 2048, kSlot, 1024, 2),
-                               smem_desc(ps + part * (N * 256) + k * 256, 128, 2048, 0), kPv, !(fresh && part == 0 && k == 0));
+                        mma_ss(tmem + 2 * N, desc_at(v0, k * 2048), desc_at(pd, part * (N * 256) + k * 256), kPv,
+                               !(fresh && part == 0 && k == 0));
                 mma_commit(bar(sh.empty[e]));
                 mma_commit(bar(sh.pv_done));
             }
@@ -306,10 +310,13 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                 mbar_wait(bar(sh.full[e]), (2 * n) / Sh::kEntries & 1, dead);
                 fence_after();
                 if (elect() && !*dead) {
-                    const uint32_t k0 = ring + e * Sh::kEntry;
-                    for (uint32_t k = 0; k < ksteps; ++k)
-                        mma_ss(tmem + (n & 1) * N, smem_desc(k0 + (k / 4) * kSlot + (k % 4) * 32, 16, 1024, 2),
-                               smem_desc(qs + (k / 4) * (N * 128) + (k % 4) * 32, 16, 1024, 2), kQk, k != 0);
+                    const uint64_t k0 = desc_at(kd, e * Sh::kEntry);
+#pragma unroll
+                    for (uint32_t k = 0; k < 4 * NS; ++k) {
+                        if (k >= ksteps) break;
+                        mma_ss(tmem + (n & 1) * N, desc_at(k0, (k / 4) * kSlot + (k % 4) * 32),
+                               desc_at(qd, (k / 4) * (N * 128) + (k % 4) * 32), kQk, k != 0);
+                    }
                     mma_commit(bar(sh.empty[e]));
                     mma_commit(bar(sh.s_full[n & 1]));
                 }

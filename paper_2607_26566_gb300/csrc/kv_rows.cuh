@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                     // what the pool lacks, and what lies behind the sequence, is filled with zeros
                     const int32_t z = uint32_t(page) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page;
                     const int32_t y = int32_t(slot & mask);
-    #pragma unroll
+#pragma unroll
                     for (int kv = 0; kv < 2; ++kv, ++n) {
                         const uint32_t e = n % kRowEntries;
                         if (!mbar_wait(bar(sh.empty[e]), (n / kRowEntries & 1) ^ 1, dead)) goto loads_done;
@@ -369,66 +369,73 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             const uint32_t dn = (D + 15) / 16;
             constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, 128);
             const uint32_t kPv = instr_desc(kBf16, false, true, 128, 0) | (dn * 2) << 17;
-            uint32_t units[2] = {0, 0}, cnt[2] = {0, 0};  // of each stage: units begun, tiles weighed
-            auto qk = [&](int st, uint32_t g, bool fresh, bool two) {
-                if (fresh) mbar_wait(bar(sh.q_full[st]), units[st]++ & 1, dead);
+            // queries and keys: rows of 64 elements, swizzled; values: the same rows, read along the keys
+            const uint64_t qd = smem_desc(base, 16, 1024, 2), kd = smem_desc(ring, 16, 1024, 2), vd = smem_desc(ring, 16384, 1024, 2);
+            uint32_t cnt[2] = {0, 0};  // tiles weighed, of each stage
+            // Products run in the order of issue, and the queue in front of the tensor cores is short, so what
+            // stands between two products must be as well. Keys and values that the first stage has waited
+            // for, the second one need not.
+            auto qk = [&](int st, uint32_t g, bool two) {
                 const uint32_t n = 2 * g, e = n % kRowEntries;
-                mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
+                if (st == 0) mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
                 fence_after();
-                if (elect() && !*dead) {
-                    const uint32_t k0 = ring + e * kEntryBytes, q0 = base + st * kEntryBytes;
-                    for (uint32_t k = 0; k < dn; ++k)
-                        mma_ss(tmem + st * 128, smem_desc(q0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2),
-                               smem_desc(k0 + (k / 4) * 16384 + (k % 4) * 32, 16, 1024, 2), kQk, k != 0);
-                    if (st || !two) mma_commit(bar(sh.empty[e]));
+                const uint64_t k0 = desc_at(kd, e * kEntryBytes), q0 = desc_at(qd, st * kEntryBytes);
+                if (elect()) {
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k) {
+                        if (k >= dn) break;
+                        const uint32_t off = (k / 4) * 16384 + (k % 4) * 32;
+                        mma_ss(tmem + st * 128, desc_at(q0, off), desc_at(k0, off), kQk, k != 0);
+                    }
                     mma_commit(bar(sh.s_full[st]));
+                    if (st || !two) mma_commit(bar(sh.empty[e]));
                 }
                 __syncwarp();
             };
             auto pv = [&](int st, uint32_t g, bool fresh, bool two) {
                 const uint32_t n = 2 * g + 1, e = n % kRowEntries;
+                if (st == 0) mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
                 mbar_wait(bar(sh.p_full[st]), cnt[st]++ & 1, dead);
-                mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
                 fence_after();
-                if (elect() && !*dead) {
-                    const uint32_t v = ring + e * kEntryBytes;
-    #pragma unroll
+                const uint64_t v0 = desc_at(vd, e * kEntryBytes);
+                if (elect()) {
+#pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, smem_desc(v + k * 2048, 16384, 1024, 2), kPv,
-                               !(fresh && k == 0));
-                    if (st || !two) mma_commit(bar(sh.empty[e]));
+                        mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, desc_at(v0, k * 2048), kPv, !(fresh && k == 0));
                     mma_commit(bar(sh.pv_done[st]));
+                    if (st || !two) mma_commit(bar(sh.empty[e]));
                 }
                 __syncwarp();
             };
             uint32_t g = 0, u = 0;
             int32_t i = 0, n = 0;
             bool two = false, follows = false, fresh = true;
+            // the next unit: both stages' queries are there
             auto unit = [&]() {
                 mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead);
                 const Unit& o = sh.unit[u % kUnits];
+                n = o.n, follows = o.more, two = o.rows > 128;
+                mbar_wait(bar(sh.q_full[0]), u & 1, dead);
+                mbar_wait(bar(sh.q_full[1]), u & 1, dead);
                 ++u;
-                n = o.n, follows = o.more;
-                if (o.rows <= 128) mbar_wait(bar(sh.q_full[1]), units[1]++ & 1, dead);
-                return o.rows > 128;
             };
-            two = unit();
-            qk(0, 0, true, two);
-            if (two) qk(1, 0, true, two);
+            unit();
+            qk(0, 0, two);
+            if (two) qk(1, 0, two);
             while (!*dead) {
                 // the next tile's scores are issued between this one's products
                 const bool same = ++i < n;
                 pv(0, g, fresh, two);
-                if (same) qk(0, g + 1, false, two);
+                if (same) qk(0, g + 1, two);
                 if (two) pv(1, g, fresh, two);
                 if (same) {
-                    if (two) qk(1, g + 1, false, two);
+                    if (two) qk(1, g + 1, two);
                 } else {
                     if (!follows) break;
                     i = 0;
-                    two = unit();
-                    qk(0, g + 1, true, two);
-                    if (two) qk(1, g + 1, true, two);
+                    unit();
+                    qk(0, g + 1, two);
+                    if (two) qk(1, g + 1, two);
                 }
                 fresh = !same;
                 ++g;
@@ -591,15 +598,17 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 float x[128];
                 tmem_ld32(s_at, x), tmem_ld32(s_at + 32, x + 32), tmem_ld32(s_at + 64, x + 64), tmem_ld32(s_at + 96, x + 96);
                 wait_ld(x);
-                float m = -INFINITY, m1 = -INFINITY;
 #pragma unroll
                 for (int c0 = 0; c0 < 128; c0 += 32) shape(x + c0, c0);
+                float top[4];
 #pragma unroll
-                for (int c = 0; c < 128; c += 4) {
-                    m = fmaxf(m, fmaxf(x[c], x[c + 1]));
-                    m1 = fmaxf(m1, fmaxf(x[c + 2], x[c + 3]));
+                for (int c = 0; c < 4; ++c) top[c] = fmaxf(x[2 * c], x[2 * c + 1]);
+#pragma unroll
+                for (int c = 8; c < 128; c += 8) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], fmaxf(x[c + 2 * k], x[c + 2 * k + 1]));
                 }
-                m = fmaxf(m, m1);
+                float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 if (!MOD) m *= k2;
                 const bool up = m > ref + kRowRaise;
                 if (__any_sync(0xFFFFFFFFu, up)) {

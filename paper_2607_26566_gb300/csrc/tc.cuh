@@ -136,6 +136,11 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint3
     return uint64_t((addr & 0x3FFFFu) >> 4) | uint64_t((lbo & 0x3FFFFu) >> 4) << 16 | uint64_t((sbo & 0x3FFFFu) >> 4) << 32 |
            uint64_t(1) << 46 | uint64_t(layout) << 61;
 }
+// The descriptor `bytes` further on in shared memory (a multiple of 16; addresses
+// stay below 256 KiB, so only the low word changes).
+__device__ __forceinline__ uint64_t desc_at(uint64_t d, uint32_t bytes) {
+    return (d & 0xFFFFFFFF00000000ull) | (uint32_t(d) + bytes / 16);
+}
 // Instruction descriptor: fp32 accumulators, both operands bf16 or fp16.
 __host__ __device__ constexpr uint32_t instr_desc(bool bf16, bool a_mn, bool b_mn, uint32_t m, uint32_t n) {
     return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | (n / 8) << 17 |
