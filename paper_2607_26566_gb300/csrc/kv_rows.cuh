@@ -7,8 +7,9 @@
 // stages of 128. While one stage's four warps do the softmax of a tile, the other's
 // products run: S = Q K^T to tensor memory, a thread takes one row of S, writes
 // its weights over it (16 bits each), and O += P V reads them there. K and V come by
-// TMA; a row's maximum is raised only when a score exceeds it by 2^8, so most tiles
-// rescale nothing.
+// TMA. Scores are weighed against a reference that need not be the maximum so far: it
+// is raised only behind a tile whose weights add up to over 2^8, so most tiles look
+// for no maximum and rescale nothing.
 //
 // Weights are rounded to the cache's type before the product (as accurate as the
 // values that they weigh: the output's own rounding is as large), the sums are not.
@@ -30,17 +31,19 @@ namespace {
 using namespace tc;
 
 constexpr int kRows = 256;            // of a unit
-// Two stages of 128 threads, and 128 more: the loading warp, the product warp and two
-// that idle, so that registers can be shared out by groups of four warps (a softmax
-// thread holds its row's 128 scores).
-constexpr int kRowThreads = 384;
-constexpr int kRowRegs = 168, kSoftRegs = 208, kOtherRegs = 88;
-static_assert(kSoftRegs * 256 + kOtherRegs * 128 <= kRowRegs * kRowThreads, "what a block was launched with");
+constexpr int kRowThreads = 320;         // two stages of 128, the loading warp, the product warp
 constexpr uint32_t kEntryBytes = 32768;  // a tile of K or V, 128 rows of 128 elements
 constexpr uint32_t kRowEntries = 4;
 constexpr uint32_t kRowSmem = 1024 + 2 * kEntryBytes + kRowEntries * kEntryBytes;
 constexpr uint32_t kRowPart = kRows * 128 + 2 * kRows;  // floats of a part: O, maxima, sums
-constexpr float kRowRaise = 8.0f;
+// A row's scores are weighed against a reference: its first tile's maximum, raised
+// behind a tile whose weights add up to more than kRaise (the accumulators follow
+// in the next tile), and at once where a weight would exceed kFar.
+constexpr float kRaise = 256.0f;
+template <class T>
+constexpr float kFarOf = 0x1p64f;
+template <>
+constexpr float kFarOf<__half> = 0x1p12f;
 
 struct PlanTile {
     int32_t s, m;       // the sequence, and which 256 rows of it
@@ -197,6 +200,7 @@ struct Unit {
     int32_t tile, n, nt;  // the segment's first key tile in the unit, its key tiles, the unit's
     int32_t more;         // another unit follows
     int64_t at;           // the segment's first tile of all
+    int32_t draft[64];    // positions of the drafted tokens, if there is a tree
 };
 struct RowWalk {
     int64_t at, end;
@@ -222,18 +226,18 @@ __device__ __forceinline__ bool walk_next(const Rows& f, RowWalk& w) {
 }
 __device__ __forceinline__ int32_t tile_slot(const KvSpan& s, int32_t i) { return (s.lo / kTileKeys + i) * kTileKeys; }
 
-// Units in shared memory at a time: the loading warp is at most two tiles ahead of
-// the products, which are at most one unit ahead of what softmax writes.
-constexpr uint32_t kUnits = 8;
+constexpr uint32_t kUnits = 8;      // in shared memory at a time
+constexpr uint32_t kUnitReaders = 9;  // eight softmax warps and the product warp
 
 struct RowShared {
     uint64_t full[kRowEntries], empty[kRowEntries];
-    uint64_t s_full[2], p_full[2], pv_done[2], q_full[2];
-    uint64_t unit_full[kUnits];
+    uint64_t s_full[2], q_full[2];
+    uint64_t p_full[2][2];  // the weights of a tile's first 64 keys, and of the others
+    uint64_t pv_half[2], pv_done[2];  // the products with them
+    uint64_t unit_full[kUnits], unit_empty[kUnits];
     Unit unit[kUnits];
     uint32_t tmem, dead;
     int32_t start_j, start_h, start_tile;
-    int32_t draft[2][64];  // positions of the unit's drafted tokens
 };
 
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
@@ -247,15 +251,24 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 
+// a condition that seldom holds
+__device__ __forceinline__ bool rare(bool c) { return __builtin_expect(c, 0); }
+
 template <class T, bool MOD>
 __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_constant__ Rows f, const __grid_constant__ CUtensorMap map) {
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr float kFar = kFarOf<T>;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t* const mem = raw + (base - smem_u32(raw));
@@ -270,14 +283,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     if (tid == 0) {
         for (uint32_t i = 0; i < kRowEntries; ++i) mbar_init(bar(sh.full[i]), 1), mbar_init(bar(sh.empty[i]), 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i]), 128);
-            mbar_init(bar(sh.pv_done[i]), 1), mbar_init(bar(sh.q_full[i]), 128);
+            mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i][0]), 128), mbar_init(bar(sh.p_full[i][1]), 128);
+            mbar_init(bar(sh.pv_half[i]), 1), mbar_init(bar(sh.pv_done[i]), 1), mbar_init(bar(sh.q_full[i]), 128);
         }
-        for (uint32_t i = 0; i < kUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1);
+        for (uint32_t i = 0; i < kUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kUnitReaders);
         sh.dead = 0;
         fence_mbar_init();
         tma_prefetch_map(&map);
     }
+    // (a unit that was never handed out has no rows: what a warp meets whose wait ran out)
+    for (uint32_t i = tid; i < sizeof(sh.unit) / 4; i += kRowThreads) reinterpret_cast<uint32_t*>(sh.unit)[i] = 0;
     if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
     pdl_launch();
     pdl_wait();
@@ -303,7 +318,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     const uint32_t tmem = sh.tmem;
 
     if (busy && warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp == 8) {
             // ---------------------------------------------------------- loads
             RowWalk w;
@@ -311,15 +325,22 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             w.t = f.plan[w.j];
             w.n = int32_t(min(int64_t(w.t.nt - w.tile), run1 - run0));
             uint32_t u = 0;  // units left in shared memory
-            auto publish = [&]() {
+            auto publish = [&]() -> bool {
+                if (!mbar_wait(bar(sh.unit_empty[u % kUnits]), (u / kUnits & 1) ^ 1, dead)) return false;
+                Unit& o = sh.unit[u % kUnits];
                 if (lane == 0) {
-                    Unit& o = sh.unit[u % kUnits];
                     o.span = w.t.span, o.q = w.t.q, o.s = w.t.s, o.m = w.t.m, o.h = w.h, o.rows = w.t.rows;
                     o.tile = w.tile, o.n = w.n, o.nt = w.t.nt, o.at = w.at, o.more = w.at + w.n < w.end;
-                    mbar_arrive(bar(sh.unit_full[u % kUnits]));
                 }
-                ++u;
+                if (a.tree) {
+                    const int32_t ctx = w.t.q.len - w.t.q.n;
+                    for (int32_t b = int32_t(lane); b < 64; b += 32)
+                        o.draft[b] = b < w.t.q.n ? ctx + __popcll(a.tree[w.t.q.first + b]) - 1 : INT32_MIN;
+                }
                 __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.unit_full[u % kUnits]));
+                ++u;
+                return true;
             };
             publish();
             const uint32_t shift = a.pages.token_shift;
@@ -353,7 +374,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                     }
                     if (i == 0) {  // the next unit, while this one's loads are under way
                         more = walk_next(f, w);
-                        if (more) publish();
+                        if (more && !publish()) goto loads_done;
                     }
                 }
             }
@@ -371,10 +392,10 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             const uint32_t kPv = instr_desc(kBf16, false, true, 128, 0) | (dn * 2) << 17;
             // queries and keys: rows of 64 elements, swizzled; values: the same rows, read along the keys
             const uint64_t qd = smem_desc(base, 16, 1024, 2), kd = smem_desc(ring, 16, 1024, 2), vd = smem_desc(ring, 16384, 1024, 2);
-            uint32_t cnt[2] = {0, 0};  // tiles weighed, of each stage
             // Products run in the order of issue, and the queue in front of the tensor cores is short, so what
             // stands between two products must be as well. Keys and values that the first stage has waited
             // for, the second one need not.
+            uint32_t cnt[2] = {0, 0}, second = 0;  // tiles weighed, of each stage; units with a second stage
             auto qk = [&](int st, uint32_t g, bool two) {
                 const uint32_t n = 2 * g, e = n % kRowEntries;
                 if (st == 0) mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
@@ -395,17 +416,21 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             auto pv = [&](int st, uint32_t g, bool fresh, bool two) {
                 const uint32_t n = 2 * g + 1, e = n % kRowEntries;
                 if (st == 0) mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
-                mbar_wait(bar(sh.p_full[st]), cnt[st]++ & 1, dead);
-                fence_after();
                 const uint64_t v0 = desc_at(vd, e * kEntryBytes);
-                if (elect()) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, desc_at(v0, k * 2048), kPv, !(fresh && k == 0));
-                    mma_commit(bar(sh.pv_done[st]));
-                    if (st || !two) mma_commit(bar(sh.empty[e]));
+                for (int half = 0; half < 2; ++half) {
+                    mbar_wait(bar(sh.p_full[st][half]), cnt[st] & 1, dead);
+                    fence_after();
+                    if (elect()) {
+#pragma unroll
+                        for (int k = 4 * half; k < 4 * half + 4; ++k)
+                            mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, desc_at(v0, k * 2048), kPv, !(fresh && k == 0));
+                        mma_commit(bar(half ? sh.pv_done[st] : sh.pv_half[st]));
+                        if (half && (st || !two)) mma_commit(bar(sh.empty[e]));
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+                ++cnt[st];
             };
             uint32_t g = 0, u = 0;
             int32_t i = 0, n = 0;
@@ -415,8 +440,10 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead);
                 const Unit& o = sh.unit[u % kUnits];
                 n = o.n, follows = o.more, two = o.rows > 128;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kUnits]));
                 mbar_wait(bar(sh.q_full[0]), u & 1, dead);
-                mbar_wait(bar(sh.q_full[1]), u & 1, dead);
+                if (two) mbar_wait(bar(sh.q_full[1]), second++ & 1, dead);
                 ++u;
             };
             unit();
@@ -448,7 +475,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
         }
     } else if (busy) {
         // ---------------------------------------------------------- softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         const int st = warp / 4;
         const uint32_t r = tid % 128;  // the row of the stage
         const uint32_t lanes = tmem + ((warp % 4) << 21), s_at = lanes + st * 128, o_at = lanes + 256 + st * 128;
@@ -458,19 +484,20 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
         const bool cap = MOD && a.softcap != 0.0f;
         const float cap_in = cap ? fabsf(a.scale) / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
         const float kk = cap ? 1.0f : k2;  // what is left to scale after the cap
+        bool gone = false;  // a wait ran out: what lies in shared memory is not to be gone by
         auto unit = [&](uint32_t u) -> const Unit& {
-            mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead);
+            if (!mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead)) gone = true;
             return sh.unit[u % kUnits];
         };
+        auto done_with = [&](uint32_t u) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kUnits]));
+        };
         // a row of a unit's queries to shared memory, 64 dimensions at a time, 128-byte swizzle
-        // (of a unit without a second stage, that stage only says that it has come by)
         auto load_q = [&](const Unit& o) {
-            if (st && o.rows <= 128) {
-                mbar_arrive(bar(sh.q_full[st]));
-                return;
-            }
+            if (st && o.rows <= 128) return;  // no second stage
             const uint32_t row = uint32_t(o.m) * kRows + st * 128 + r;
-            const bool real = int32_t(st * 128 + r) < o.rows;
+            const bool real = int32_t(st * 128 + r) < o.rows && !gone;
             const uint32_t t = row / a.group, g = row % a.group;
             const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(o.q.first + t) * a.q_stride +
                                                               uint64_t(o.h * a.group + g) * D);
@@ -503,14 +530,15 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
         bool more = true;
         for (uint32_t u = 0; more; ++u) {
             const Unit& o = unit(u);
-            more = o.more && !*dead;
+            more = o.more && !gone;
             if (st && o.rows <= 128) {
                 if (more) load_q(unit(u + 1));
+                done_with(u);
                 continue;
             }
             const KvSpan span = o.span;
             const int32_t ctx = o.q.len - o.q.n, tiles = o.n;
-            const bool real = int32_t(st * 128 + r) < o.rows;
+            const bool real = int32_t(st * 128 + r) < o.rows && !gone;
             KvQuery qy{0, INT32_MAX, 0, 0};
             float slope = 0.0f;
             if (real) {
@@ -518,49 +546,32 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 qy = kv_query(a, o.q, int32_t(row / a.group));
                 if (MOD && a.slopes) slope = a.slopes[o.h * a.group + row % a.group] * kLog2e;
             }
-            if (a.tree) {
-                if (st)  // (the unit before has been read)
-                    bar_sync<2, 128>();
-                else
-                    bar_sync<1, 128>();
-                if (r < 64) sh.draft[st][r] = int32_t(r) < o.q.n ? ctx + __popcll(a.tree[o.q.first + int32_t(r)]) - 1 : INT32_MIN;
-                if (st)
-                    bar_sync<2, 128>();
-                else
-                    bar_sync<1, 128>();
-                // of the drafted tokens, those that are there and inside the window
-                if (real)
-                    for (int b = 0; b < 64; ++b)
-                        if (sh.draft[st][b] < qy.first) qy.word &= ~(uint64_t(1) << b);
-            }
+            if (a.tree && real)  // of the drafted tokens, those that are there and inside the window
+                for (int b = 0; b < 64; ++b)
+                    if (o.draft[b] < qy.first) qy.word &= ~(uint64_t(1) << b);
             const float pos = float(qy.pos);
-            float ref = -INFINITY, sum = 0.0f;
+            float ref = -INFINITY, sum = 0.0f, pend = 1.0f;  // pend: what O, once it is there, has to be scaled by
+            bool late = false;                               // ... of some row of the warp
             for (int32_t i = 0; i < tiles; ++i, ++n) {
                 const int32_t slot0 = tile_slot(span, o.tile + i);
                 const bool masked = slot0 < span.all_lo || slot0 + kTileKeys > span.all_hi;
                 const bool drafts = a.tree && slot0 + kTileKeys > ctx;
                 // the row's visible keys of the tile, a bit each
-                uint32_t see[4] = {};
-                if (masked) {
+                uint64_t see0 = 0, see1 = 0;
+                if (rare(masked)) {
                     const int32_t d = ctx - slot0;
-                    uint64_t w0 = 0, w1 = 0;
                     if (drafts) {
-                        w0 = d >= 64 ? 0 : d >= 0 ? qy.word << d : d > -64 ? qy.word >> -d : 0;
-                        w1 = d >= 128 ? 0 : d >= 64 ? qy.word << (d - 64) : d > 0 ? qy.word >> (64 - d) : 0;
+                        see0 = d >= 64 ? 0 : d >= 0 ? qy.word << d : d > -64 ? qy.word >> -d : 0;
+                        see1 = d >= 128 ? 0 : d >= 64 ? qy.word << (d - 64) : d > 0 ? qy.word >> (64 - d) : 0;
                     }
-                    see[0] = uint32_t(w0), see[1] = uint32_t(w0 >> 32), see[2] = uint32_t(w1), see[3] = uint32_t(w1 >> 32);
+                    auto below = [](int64_t n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
                     const int64_t f0 = int64_t(qy.first) - slot0, l0 = int64_t(qy.last) - slot0;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int32_t lo = int32_t(max(int64_t(0), min(int64_t(32), f0 - c * 32)));
-                        const int32_t hi = int32_t(max(int64_t(0), min(int64_t(32), l0 - c * 32)));
-                        const uint32_t below = hi == 32 ? 0xFFFFFFFFu : (1u << hi) - 1, under = lo == 32 ? 0xFFFFFFFFu : (1u << lo) - 1;
-                        see[c] |= below & ~under;
-                    }
+                    see0 |= below(l0) & ~below(f0);
+                    see1 |= below(l0 - 64) & ~below(f0 - 64);
                 }
                 mbar_wait(bar(sh.s_full[st]), n & 1, dead);
                 fence_after();
-                if (cap) {
+                if (rare(cap)) {
                     // the cap takes two special functions a score: once, back to tensor memory
 #pragma unroll 1
                     for (int c0 = 0; c0 < 128; c0 += 32) {
@@ -574,110 +585,129 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                     }
                     wait_st();
                 }
-                // bias (scores in units of log2 from here on, if MOD) and mask
                 const float ahead = pos - float(slot0);
-                auto shape = [&](float* x, int c0) {
+                // Sixty-four keys at a time: their product runs beside the weights of the next ones. (One copy
+                // of this code for both halves, and what is rare behind it: it has to stay in the
+                // instruction cache beside the other stage's.)
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    const int c0 = half * 64;
+                    float x[64];
+                    tmem_ld32(s_at + c0, x), tmem_ld32(s_at + c0 + 32, x + 32);
+                    wait_ld(x);
+                    // bias (scores in units of log2 from here on, if MOD) and mask
                     if (MOD) {
-                        if (drafts && a.slopes) {
-                            for (int c = 0; c < 32; ++c) {
+                        if (rare(drafts && a.slopes)) {
+#pragma unroll
+                            for (int c = 0; c < 64; ++c) {
                                 const int32_t key = slot0 + c0 + c;
-                                const float far = key >= ctx ? pos - float(sh.draft[st][min(key - ctx, 63)]) : ahead - float(c0 + c);
+                                const float far = key >= ctx ? pos - float(o.draft[min(key - ctx, 63)]) : pos - float(key);
                                 x[c] = x[c] * kk - slope * fabsf(far);
                             }
                         } else {
+                            const float from = ahead - float(c0);
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) x[c] = x[c] * kk - slope * fabsf(ahead - float(c0 + c));
+                            for (int c = 0; c < 64; ++c) x[c] = x[c] * kk - slope * fabsf(from - float(c));
                         }
                     }
-                    if (masked) {
-                        const uint32_t bits = see[c0 / 32];
+                    const uint64_t bits = !masked ? ~0ull : half ? see1 : see0;
+                    if (rare(masked)) {
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) x[c] = bits & (1u << c) ? x[c] : -INFINITY;
+                        for (int c = 0; c < 64; ++c) x[c] = bits >> c & 1 ? x[c] : -INFINITY;
                     }
-                };
-                float x[128];
-                tmem_ld32(s_at, x), tmem_ld32(s_at + 32, x + 32), tmem_ld32(s_at + 64, x + 64), tmem_ld32(s_at + 96, x + 96);
-                wait_ld(x);
+                    auto peak = [&]() {
+                        float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-                for (int c0 = 0; c0 < 128; c0 += 32) shape(x + c0, c0);
-                float top[4];
+                        for (int c = 0; c < 64; c += 4) t0 = max3(t0, x[c], x[c + 1]), t1 = max3(t1, x[c + 2], x[c + 3]);
+                        return fmaxf(t0, t1) * (MOD ? 1.0f : k2);
+                    };
+                    // weights against the reference so far; a row's first keys that it sees set it
+                    uint32_t p[32];
+                    float part;
+                    bool set = i == 0 && half == 0;
+#pragma unroll 1
+                    for (int pass = 0; pass < 2; ++pass) {
+                        if (rare(set)) {
+                            const float m = peak();
+                            if (m > ref) {
+                                const float by = i || half ? exp2_approx(ref - m) : 1.0f;  // at first there is nothing to scale
+                                ref = m, sum *= by, pend *= by;
+                            }
+                            late = i || half;
+                        }
+                        const float off = ref == -INFINITY ? 0.0f : -ref;
+                        const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
+                        uint64_t sum2 = 0, sum3 = 0;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) top[c] = fmaxf(x[2 * c], x[2 * c + 1]);
-#pragma unroll
-                for (int c = 8; c < 128; c += 8) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], fmaxf(x[c + 2 * k], x[c + 2 * k + 1]));
-                }
-                float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                if (!MOD) m *= k2;
-                const bool up = m > ref + kRowRaise;
-                if (__any_sync(0xFFFFFFFFu, up)) {
-                    float by = 1.0f;
-                    if (up) {
-                        by = exp2_approx(ref - m);
-                        ref = m;
+                        for (int c = 0; c < 64; c += 4) {
+                            float u0, u1, u2, u3;
+                            unpack2(fma2(pack2(x[c], x[c + 1]), by2, off2), u0, u1);
+                            unpack2(fma2(pack2(x[c + 2], x[c + 3]), by2, off2), u2, u3);
+                            u0 = exp2_approx(u0), u1 = exp2_approx(u1), u2 = exp2_approx(u2), u3 = exp2_approx(u3);
+                            sum2 = add2(sum2, pack2(u0, u1));
+                            sum3 = add2(sum3, pack2(u2, u3));
+                            p[c / 2] = Kv16<T>::from2(u0, u1);
+                            p[c / 2 + 1] = Kv16<T>::from2(u2, u3);
+                        }
+                        float u0, u1;
+                        unpack2(add2(sum2, sum3), u0, u1);
+                        part = u0 + u1;
+                        // too far above the reference for the weights' type, or the first that the row sees:
+                        // raised at once, and once more
+                        set = __any_sync(0xFFFFFFFFu, part > kFar || (ref == -INFINITY && bits));
+                        if (!rare(set)) break;
                     }
-                    sum *= by;
-                    if (i) {
-                        mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
+                    if (rare(late)) {
+                        // (the products of the tile before were complete before this one's scores)
+                        if (half) mbar_wait(bar(sh.pv_half[st]), n & 1, dead);
                         fence_after();
-                        for (uint32_t c0 = 0; c0 < D; c0 += 16) {
+#pragma unroll 1
+                        for (uint32_t d0 = 0; d0 < D; d0 += 16) {
                             float y[16];
-                            tmem_ld16(o_at + c0, y);
+                            tmem_ld16(o_at + d0, y);
                             wait_ld(y);
 #pragma unroll
-                            for (int c = 0; c < 16; ++c) y[c] *= by;
-                            tmem_st16(o_at + c0, reinterpret_cast<uint32_t*>(y));
+                            for (int c = 0; c < 16; ++c) y[c] *= pend;
+                            tmem_st16(o_at + d0, reinterpret_cast<uint32_t*>(y));
                         }
-                        wait_st();
+                        pend = 1.0f, late = false;
+                    }
+                    if (rare(half == 0 && st == 0 && (slot0 < span.lo || slot0 + kTileKeys > span.hi))) {
+                        // values that none of the unit's queries sees may be anything: zeros, as their weights are
+                        const uint32_t e = (2 * n + 1) % kRowEntries;
+                        mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
+                        const int32_t key = slot0 + int32_t(r);
+                        if (key < span.lo || key >= span.hi) {
+#pragma unroll 1
+                            for (int k = 0; k < 16; ++k)
+                                if (k < 8 || D > 64)
+                                    *reinterpret_cast<uint4*>(mem + 2 * kEntryBytes + e * kEntryBytes + k / 8 * 16384 + r * 128 +
+                                                              k % 8 * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_smem();
+                    }
+                    // weights 2c and 2c + 1 to column c, over scores that are read
+                    tmem_st16(s_at + c0 / 2, p), tmem_st16(s_at + c0 / 2 + 16, p + 16);
+                    wait_st();
+                    fence_before();
+                    mbar_arrive(bar(sh.p_full[st][half]));
+                    sum += part;
+                    // for what follows: the reference, and what the accumulators follow it by
+                    late = __any_sync(0xFFFFFFFFu, part > kRaise);
+                    if (rare(late) && part > kRaise) {
+                        ref += log2f(part);
+                        pend = 1.0f / part;
+                        sum *= pend;
                     }
                 }
-                const float off = ref == -INFINITY ? 0.0f : -ref;
-                const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
-                uint64_t sum2 = 0, sum3 = 0;
-#pragma unroll
-                for (int c0 = 0; c0 < 128; c0 += 32) {
-                    uint32_t p[16];
-#pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        float u0, u1, u2, u3;
-                        unpack2(fma2(pack2(x[c0 + c], x[c0 + c + 1]), by2, off2), u0, u1);
-                        unpack2(fma2(pack2(x[c0 + c + 2], x[c0 + c + 3]), by2, off2), u2, u3);
-                        u0 = exp2_approx(u0), u1 = exp2_approx(u1), u2 = exp2_approx(u2), u3 = exp2_approx(u3);
-                        sum2 = add2(sum2, pack2(u0, u1));
-                        sum3 = add2(sum3, pack2(u2, u3));
-                        p[c / 2] = Kv16<T>::from2(u0, u1);
-                        p[c / 2 + 1] = Kv16<T>::from2(u2, u3);
-                    }
-                    tmem_st16(s_at + c0 / 2, p);  // weights 2c and 2c + 1 in column c
-                }
-                float u0, u1;
-                unpack2(add2(sum2, sum3), u0, u1);
-                sum += u0 + u1;
-                if (st == 0 && (slot0 < span.lo || slot0 + kTileKeys > span.hi)) {
-                    // values that none of the unit's queries sees may be anything: zeros, as their weights are
-                    const uint32_t e = (2 * n + 1) % kRowEntries;
-                    mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
-                    const int32_t key = slot0 + int32_t(r);
-                    if (key < span.lo || key >= span.hi) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            if (k < 8 || D > 64)
-                                *reinterpret_cast<uint4*>(mem + 2 * kEntryBytes + e * kEntryBytes + k / 8 * 16384 + r * 128 +
-                                                          k % 8 * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async_smem();
-                }
-                wait_st();
-                fence_before();
-                mbar_arrive(bar(sh.p_full[st]));
             }
             if (more) load_q(unit(u + 1));  // the next unit's scores start while this one is written
             mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
             fence_after();
             if (tiles == o.nt) {
+                const bool real = int32_t(st * 128 + r) < o.rows && !gone;
                 const uint32_t row = uint32_t(o.m) * kRows + st * 128 + r;
-                const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+                const float by = sum == 0.0f ? 0.0f : pend / sum;
                 const uint64_t orow = uint64_t(o.q.first) + row / a.group;
                 const uint32_t head = o.h * a.group + row % a.group;
                 T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D;
@@ -706,12 +736,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
 #pragma unroll
                     for (int c = 0; c < 16; c += 4)
                         __stcg(reinterpret_cast<float4*>(part) + (c0 + c) / 4 * kRows + pr,
-                               make_float4(y[c], y[c + 1], y[c + 2], y[c + 3]));
+                               make_float4(y[c] * pend, y[c + 1] * pend, y[c + 2] * pend, y[c + 3] * pend));
                 }
                 __stcg(part + kRows * 128 + pr, ref);
                 __stcg(part + kRows * 128 + kRows + pr, sum);
             }
             fence_before();
+            done_with(u);
         }
     }
     if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;

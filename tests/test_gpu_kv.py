@@ -321,6 +321,20 @@ def test_pages_in_the_table_that_the_pool_lacks_read_as_zeros():
     assert (c.attend(q.to(DEV), ints(lens), table=table) == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rise", [3.0, 30.0, 200.0])
+@pytest.mark.parametrize("new,ctx", [([1], [900]), ([20], [700]), ([300], [600])])
+def test_scores_that_rise_from_tile_to_tile(dtype, rise, new, ctx):
+    """Each 128 keys score `rise` above the ones before, some rows fall instead."""
+    c, lens, kvs, q = case(dtype, 2, 1, 64, new, ctx, qs=1.0)
+    k, v = kvs[0]
+    k[:, :, :32] = (torch.arange(lens[0]) * (rise / 128 / 4)).to(dtype)[:, None, None] / 8
+    q[:, :, :32] = 1.0
+    q[::3, :, :32] = -1.0
+    write_rows(c, 0, 0, k.to(DEV), v.to(DEV))
+    check(c, lens, new, kvs, q, scale=1.0)
+
+
 def test_infinite_scores_give_nan_like_the_formula():
     c, lens, kvs, q = case(BF, 1, 1, 64, [1], [20])
     q[:] = 1.0
