@@ -21,6 +21,7 @@
 #pragma once
 
 #include <atomic>
+#include <type_traits>
 
 #include "kv_attend.cuh"
 #include "t2istore.h"
@@ -31,7 +32,12 @@ namespace {
 using namespace tc;
 
 constexpr int kRows = 256;            // of a unit
-constexpr int kRowThreads = 320;         // two stages of 128, the loading warp, the product warp
+// Two stages of 128 threads, and 128 more: the loading warp, the product warp and two
+// that idle, so that registers can be shared out by groups of four warps (a softmax
+// thread holds its row's 128 scores).
+constexpr int kRowThreads = 384;
+constexpr int kRowRegs = 168, kSoftRegs = 192, kOtherRegs = 120;
+static_assert(kSoftRegs * 256 + kOtherRegs * 128 <= kRowRegs * kRowThreads, "what a block was launched with");
 constexpr uint32_t kEntryBytes = 32768;  // a tile of K or V, 128 rows of 128 elements
 constexpr uint32_t kRowEntries = 4;
 constexpr uint32_t kRowSmem = 1024 + 2 * kEntryBytes + kRowEntries * kEntryBytes;
@@ -232,8 +238,7 @@ constexpr uint32_t kUnitReaders = 9;  // eight softmax warps and the product war
 struct RowShared {
     uint64_t full[kRowEntries], empty[kRowEntries];
     uint64_t s_full[2], q_full[2];
-    uint64_t p_full[2][2];  // the weights of a tile's first 64 keys, and of the others
-    uint64_t pv_half[2], pv_done[2];  // the products with them
+    uint64_t p_full[2], pv_done[2];
     uint64_t unit_full[kUnits], unit_empty[kUnits];
     Unit unit[kUnits];
     uint32_t tmem, dead;
@@ -283,8 +288,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     if (tid == 0) {
         for (uint32_t i = 0; i < kRowEntries; ++i) mbar_init(bar(sh.full[i]), 1), mbar_init(bar(sh.empty[i]), 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i][0]), 128), mbar_init(bar(sh.p_full[i][1]), 128);
-            mbar_init(bar(sh.pv_half[i]), 1), mbar_init(bar(sh.pv_done[i]), 1), mbar_init(bar(sh.q_full[i]), 128);
+            mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i]), 128);
+            mbar_init(bar(sh.pv_done[i]), 1), mbar_init(bar(sh.q_full[i]), 128);
         }
         for (uint32_t i = 0; i < kUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kUnitReaders);
         sh.dead = 0;
@@ -315,9 +320,10 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = 0;  // (all 512 columns are allocated)
 
     if (busy && warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp == 8) {
             // ---------------------------------------------------------- loads
             RowWalk w;
@@ -393,79 +399,87 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             // queries and keys: rows of 64 elements, swizzled; values: the same rows, read along the keys
             const uint64_t qd = smem_desc(base, 16, 1024, 2), kd = smem_desc(ring, 16, 1024, 2), vd = smem_desc(ring, 16384, 1024, 2);
             // Products run in the order of issue, and the queue in front of the tensor cores is short, so what
-            // stands between two products must be as well. Keys and values that the first stage has waited
-            // for, the second one need not.
-            uint32_t cnt[2] = {0, 0}, second = 0;  // tiles weighed, of each stage; units with a second stage
-            auto qk = [&](int st, uint32_t g, bool two) {
-                const uint32_t n = 2 * g, e = n % kRowEntries;
-                if (st == 0) mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
-                fence_after();
+            // stands between two products must be as well: the ring's entries are constants (ODD: the tile's
+            // parity), all of tensor memory is the block's and begins at column 0, and what the first stage
+            // has waited for the second one need not.
+            uint32_t units = 0, second = 0;   // units begun, and those with a second stage
+            uint32_t pp[2] = {0, 0}, kv = 0;  // parities of the next weights of each stage, and of the ring
+            int32_t left = 0;                 // tiles of the unit after this one
+            bool two = false, follows = false, fresh = true;
+            auto qk = [&](auto odd, int st) {
+                constexpr uint32_t e = decltype(odd)::value ? 2 : 0;
                 const uint64_t k0 = desc_at(kd, e * kEntryBytes), q0 = desc_at(qd, st * kEntryBytes);
                 if (elect()) {
 #pragma unroll
                     for (uint32_t k = 0; k < 8; ++k) {
                         if (k >= dn) break;
                         const uint32_t off = (k / 4) * 16384 + (k % 4) * 32;
-                        mma_ss(tmem + st * 128, desc_at(q0, off), desc_at(k0, off), kQk, k != 0);
+                        mma_ss(st * 128, desc_at(q0, off), desc_at(k0, off), kQk, k != 0);
                     }
                     mma_commit(bar(sh.s_full[st]));
+                }
+                __syncwarp();
+            };
+            // (One commit a batch, as far as that goes: each takes a place in the queue. So the tile's keys are
+            // handed back behind the first product with its values, and pv_done is for a unit's last tile.)
+            auto pv = [&](auto odd, int st, bool end) {
+                constexpr uint32_t e = decltype(odd)::value ? 3 : 1;
+                const uint64_t v0 = desc_at(vd, e * kEntryBytes);
+                mbar_wait(bar(sh.p_full[st]), pp[st], dead);
+                pp[st] ^= 1;
+                fence_after();
+                if (elect()) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        mma_ts(256 + st * 128, st * 128 + k * 8, desc_at(v0, k * 2048), kPv, !(fresh && k == 0));
+                    if (end) mma_commit(bar(sh.pv_done[st]));
+                    if (st == 0) mma_commit(bar(sh.empty[e - 1]));
                     if (st || !two) mma_commit(bar(sh.empty[e]));
                 }
                 __syncwarp();
             };
-            auto pv = [&](int st, uint32_t g, bool fresh, bool two) {
-                const uint32_t n = 2 * g + 1, e = n % kRowEntries;
-                if (st == 0) mbar_wait(bar(sh.full[e]), n / kRowEntries & 1, dead);
-                const uint64_t v0 = desc_at(vd, e * kEntryBytes);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    mbar_wait(bar(sh.p_full[st][half]), cnt[st] & 1, dead);
-                    fence_after();
-                    if (elect()) {
-#pragma unroll
-                        for (int k = 4 * half; k < 4 * half + 4; ++k)
-                            mma_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, desc_at(v0, k * 2048), kPv, !(fresh && k == 0));
-                        mma_commit(bar(half ? sh.pv_done[st] : sh.pv_half[st]));
-                        if (half && (st || !two)) mma_commit(bar(sh.empty[e]));
-                    }
-                    __syncwarp();
-                }
-                ++cnt[st];
-            };
-            uint32_t g = 0, u = 0;
-            int32_t i = 0, n = 0;
-            bool two = false, follows = false, fresh = true;
             // the next unit: both stages' queries are there
             auto unit = [&]() {
-                mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead);
-                const Unit& o = sh.unit[u % kUnits];
-                n = o.n, follows = o.more, two = o.rows > 128;
+                mbar_wait(bar(sh.unit_full[units % kUnits]), units / kUnits & 1, dead);
+                const Unit& o = sh.unit[units % kUnits];
+                left = o.n, follows = o.more, two = o.rows > 128;
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kUnits]));
-                mbar_wait(bar(sh.q_full[0]), u & 1, dead);
+                if (lane == 0) mbar_arrive(bar(sh.unit_empty[units % kUnits]));
+                mbar_wait(bar(sh.q_full[0]), units & 1, dead);
                 if (two) mbar_wait(bar(sh.q_full[1]), second++ & 1, dead);
-                ++u;
+                ++units;
+            };
+            // A tile (its values are there): its products with them, and between these the next tile's scores;
+            // false behind the last. Waits that seldom wait stand where products are queued.
+            auto tile = [&](auto odd) {
+                using Next = std::integral_constant<bool, !decltype(odd)::value>;
+                const bool same = --left > 0;
+                if (odd.value) kv ^= 1;
+                if (same) mbar_wait(bar(sh.full[odd.value ? 0 : 2]), kv, dead);
+                pv(odd, 0, !same);
+                if (same) qk(Next{}, 0);
+                if (two) pv(odd, 1, !same);
+                if (same) {
+                    const bool ok = mbar_wait(bar(sh.full[odd.value ? 1 : 3]), kv, dead);
+                    if (two) qk(Next{}, 1);
+                    fresh = false;
+                    return ok;
+                }
+                if (!follows || *dead) return false;
+                unit();
+                mbar_wait(bar(sh.full[odd.value ? 0 : 2]), kv, dead);
+                qk(Next{}, 0);
+                if (two) qk(Next{}, 1);
+                fresh = true;
+                return mbar_wait(bar(sh.full[odd.value ? 1 : 3]), kv, dead);
             };
             unit();
-            qk(0, 0, two);
-            if (two) qk(1, 0, two);
-            while (!*dead) {
-                // the next tile's scores are issued between this one's products
-                const bool same = ++i < n;
-                pv(0, g, fresh, two);
-                if (same) qk(0, g + 1, two);
-                if (two) pv(1, g, fresh, two);
-                if (same) {
-                    if (two) qk(1, g + 1, two);
-                } else {
-                    if (!follows) break;
-                    i = 0;
-                    unit();
-                    qk(0, g + 1, two);
-                    if (two) qk(1, g + 1, two);
-                }
-                fresh = !same;
-                ++g;
+            mbar_wait(bar(sh.full[0]), 0, dead);
+            fence_after();
+            qk(std::false_type{}, 0);
+            if (two) qk(std::false_type{}, 1);
+            mbar_wait(bar(sh.full[1]), 0, dead);
+            while (tile(std::false_type{}) && tile(std::true_type{})) {
             }
             if (*dead) {  // the products in flight end before the tensor memory is freed
                 const uint64_t t0 = now_ns();
@@ -475,6 +489,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
         }
     } else if (busy) {
         // ---------------------------------------------------------- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         const int st = warp / 4;
         const uint32_t r = tid % 128;  // the row of the stage
         const uint32_t lanes = tmem + ((warp % 4) << 21), s_at = lanes + st * 128, o_at = lanes + 256 + st * 128;
@@ -526,7 +541,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             }
             load_q(o);
         }
-        uint32_t n = 0;  // tiles of this stage
+        uint32_t n = 0, on = 0;  // tiles and units of this stage
         bool more = true;
         for (uint32_t u = 0; more; ++u) {
             const Unit& o = unit(u);
@@ -585,124 +600,113 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                     }
                     wait_st();
                 }
-                const float ahead = pos - float(slot0);
-                // Sixty-four keys at a time: their product runs beside the weights of the next ones. (One copy
-                // of this code for both halves, and what is rare behind it: it has to stay in the
-                // instruction cache beside the other stage's.)
-#pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
-                    const int c0 = half * 64;
-                    float x[64];
-                    tmem_ld32(s_at + c0, x), tmem_ld32(s_at + c0 + 32, x + 32);
-                    wait_ld(x);
-                    // bias (scores in units of log2 from here on, if MOD) and mask
-                    if (MOD) {
-                        if (rare(drafts && a.slopes)) {
+                float x[128];
+                tmem_ld32(s_at, x), tmem_ld32(s_at + 32, x + 32), tmem_ld32(s_at + 64, x + 64), tmem_ld32(s_at + 96, x + 96);
+                wait_ld(x);
+                // bias (scores in units of log2 from here on, if MOD) and mask
+                if (MOD) {
+                    const float ahead = pos - float(slot0);
+                    if (rare(drafts && a.slopes)) {
 #pragma unroll
-                            for (int c = 0; c < 64; ++c) {
-                                const int32_t key = slot0 + c0 + c;
-                                const float far = key >= ctx ? pos - float(o.draft[min(key - ctx, 63)]) : pos - float(key);
-                                x[c] = x[c] * kk - slope * fabsf(far);
-                            }
-                        } else {
-                            const float from = ahead - float(c0);
-#pragma unroll
-                            for (int c = 0; c < 64; ++c) x[c] = x[c] * kk - slope * fabsf(from - float(c));
+                        for (int c = 0; c < 128; ++c) {
+                            const int32_t key = slot0 + c;
+                            const float far = key >= ctx ? pos - float(o.draft[min(key - ctx, 63)]) : ahead - float(c);
+                            x[c] = x[c] * kk - slope * fabsf(far);
                         }
-                    }
-                    const uint64_t bits = !masked ? ~0ull : half ? see1 : see0;
-                    if (rare(masked)) {
+                    } else {
 #pragma unroll
-                        for (int c = 0; c < 64; ++c) x[c] = bits >> c & 1 ? x[c] : -INFINITY;
+                        for (int c = 0; c < 128; ++c) x[c] = x[c] * kk - slope * fabsf(ahead - float(c));
                     }
-                    auto peak = [&]() {
-                        float t0 = -INFINITY, t1 = -INFINITY;
+                }
+                if (rare(masked)) {
 #pragma unroll
-                        for (int c = 0; c < 64; c += 4) t0 = max3(t0, x[c], x[c + 1]), t1 = max3(t1, x[c + 2], x[c + 3]);
-                        return fmaxf(t0, t1) * (MOD ? 1.0f : k2);
-                    };
-                    // weights against the reference so far; a row's first keys that it sees set it
-                    uint32_t p[32];
-                    float part;
-                    bool set = i == 0 && half == 0;
+                    for (int c = 0; c < 128; ++c) x[c] = (c < 64 ? see0 >> c : see1 >> (c - 64)) & 1 ? x[c] : -INFINITY;
+                }
+                // weights against the reference so far; the first keys that a row sees set it
+                float part;
+                bool set = i == 0;
 #pragma unroll 1
-                    for (int pass = 0; pass < 2; ++pass) {
-                        if (rare(set)) {
-                            const float m = peak();
-                            if (m > ref) {
-                                const float by = i || half ? exp2_approx(ref - m) : 1.0f;  // at first there is nothing to scale
-                                ref = m, sum *= by, pend *= by;
-                            }
-                            late = i || half;
-                        }
-                        const float off = ref == -INFINITY ? 0.0f : -ref;
-                        const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
-                        uint64_t sum2 = 0, sum3 = 0;
+                for (int pass = 0; pass < 2; ++pass) {
+                    if (rare(set)) {
+                        float t0 = max3(x[0], x[1], x[2]), t1 = x[3];
 #pragma unroll
-                        for (int c = 0; c < 64; c += 4) {
+                        for (int c = 4; c < 128; c += 4) t0 = max3(t0, x[c], x[c + 1]), t1 = max3(t1, x[c + 2], x[c + 3]);
+                        const float m = fmaxf(t0, t1) * (MOD ? 1.0f : k2);
+                        if (m > ref) {
+                            const float by = i ? exp2_approx(ref - m) : 1.0f;  // at first there is nothing to scale
+                            ref = m, sum *= by, pend *= by;
+                        }
+                        late = i != 0;
+                    }
+                    const float off = ref == -INFINITY ? 0.0f : -ref;
+                    const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
+                    uint64_t sum2 = 0, sum3 = 0;
+#pragma unroll
+                    for (int c0 = 0; c0 < 128; c0 += 32) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) {
                             float u0, u1, u2, u3;
-                            unpack2(fma2(pack2(x[c], x[c + 1]), by2, off2), u0, u1);
-                            unpack2(fma2(pack2(x[c + 2], x[c + 3]), by2, off2), u2, u3);
+                            unpack2(fma2(pack2(x[c0 + c], x[c0 + c + 1]), by2, off2), u0, u1);
+                            unpack2(fma2(pack2(x[c0 + c + 2], x[c0 + c + 3]), by2, off2), u2, u3);
                             u0 = exp2_approx(u0), u1 = exp2_approx(u1), u2 = exp2_approx(u2), u3 = exp2_approx(u3);
                             sum2 = add2(sum2, pack2(u0, u1));
                             sum3 = add2(sum3, pack2(u2, u3));
                             p[c / 2] = Kv16<T>::from2(u0, u1);
                             p[c / 2 + 1] = Kv16<T>::from2(u2, u3);
                         }
-                        float u0, u1;
-                        unpack2(add2(sum2, sum3), u0, u1);
-                        part = u0 + u1;
-                        // too far above the reference for the weights' type, or the first that the row sees:
-                        // raised at once, and once more
-                        set = __any_sync(0xFFFFFFFFu, part > kFar || (ref == -INFINITY && bits));
-                        if (!rare(set)) break;
+                        tmem_st16(s_at + c0 / 2, p);  // weights 2c and 2c + 1 to column c, over scores that are read
                     }
-                    if (rare(late)) {
-                        // (the products of the tile before were complete before this one's scores)
-                        if (half) mbar_wait(bar(sh.pv_half[st]), n & 1, dead);
-                        fence_after();
-#pragma unroll 1
-                        for (uint32_t d0 = 0; d0 < D; d0 += 16) {
-                            float y[16];
-                            tmem_ld16(o_at + d0, y);
-                            wait_ld(y);
-#pragma unroll
-                            for (int c = 0; c < 16; ++c) y[c] *= pend;
-                            tmem_st16(o_at + d0, reinterpret_cast<uint32_t*>(y));
-                        }
-                        pend = 1.0f, late = false;
-                    }
-                    if (rare(half == 0 && st == 0 && (slot0 < span.lo || slot0 + kTileKeys > span.hi))) {
-                        // values that none of the unit's queries sees may be anything: zeros, as their weights are
-                        const uint32_t e = (2 * n + 1) % kRowEntries;
-                        mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
-                        const int32_t key = slot0 + int32_t(r);
-                        if (key < span.lo || key >= span.hi) {
-#pragma unroll 1
-                            for (int k = 0; k < 16; ++k)
-                                if (k < 8 || D > 64)
-                                    *reinterpret_cast<uint4*>(mem + 2 * kEntryBytes + e * kEntryBytes + k / 8 * 16384 + r * 128 +
-                                                              k % 8 * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_smem();
-                    }
-                    // weights 2c and 2c + 1 to column c, over scores that are read
-                    tmem_st16(s_at + c0 / 2, p), tmem_st16(s_at + c0 / 2 + 16, p + 16);
+                    float u0, u1;
+                    unpack2(add2(sum2, sum3), u0, u1);
+                    part = u0 + u1;
+                    // too far above the reference for the weights' type, or the first that the row sees:
+                    // raised at once, and once more
+                    set = __any_sync(0xFFFFFFFFu, part > kFar || (ref == -INFINITY && (!masked || (see0 | see1))));
+                    if (!rare(set)) break;
                     wait_st();
-                    fence_before();
-                    mbar_arrive(bar(sh.p_full[st][half]));
-                    sum += part;
-                    // for what follows: the reference, and what the accumulators follow it by
-                    late = __any_sync(0xFFFFFFFFu, part > kRaise);
-                    if (rare(late) && part > kRaise) {
-                        ref += log2f(part);
-                        pend = 1.0f / part;
-                        sum *= pend;
+                }
+                if (rare(late)) {
+                    // (the products of the tile before were complete before this one's scores)
+#pragma unroll 1
+                    for (uint32_t d0 = 0; d0 < D; d0 += 16) {
+                        float y[16];
+                        tmem_ld16(o_at + d0, y);
+                        wait_ld(y);
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) y[c] *= pend;
+                        tmem_st16(o_at + d0, reinterpret_cast<uint32_t*>(y));
                     }
+                    pend = 1.0f, late = false;
+                }
+                if (rare(st == 0 && (slot0 < span.lo || slot0 + kTileKeys > span.hi))) {
+                    // values that none of the unit's queries sees may be anything: zeros, as their weights are
+                    const uint32_t e = (2 * n + 1) % kRowEntries;
+                    mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
+                    const int32_t key = slot0 + int32_t(r);
+                    if (key < span.lo || key >= span.hi) {
+#pragma unroll 1
+                        for (int k = 0; k < 16; ++k)
+                            if (k < 8 || D > 64)
+                                *reinterpret_cast<uint4*>(mem + 2 * kEntryBytes + e * kEntryBytes + k / 8 * 16384 + r * 128 +
+                                                          k % 8 * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                }
+                wait_st();
+                fence_before();
+                mbar_arrive(bar(sh.p_full[st]));
+                sum += part;
+                // for the next tile: the reference, and what the accumulators follow it by
+                late = __any_sync(0xFFFFFFFFu, part > kRaise);
+                if (rare(late) && part > kRaise) {
+                    ref += log2f(part);
+                    pend = 1.0f / part;
+                    sum *= pend;
                 }
             }
             if (more) load_q(unit(u + 1));  // the next unit's scores start while this one is written
-            mbar_wait(bar(sh.pv_done[st]), (n - 1) & 1, dead);
+            mbar_wait(bar(sh.pv_done[st]), on++ & 1, dead);
             fence_after();
             if (tiles == o.nt) {
                 const bool real = int32_t(st * 128 + r) < o.rows && !gone;
@@ -750,7 +754,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     if (tid == 0 && *dead) *f.fault = 1;
     if (warp == 9) {
         fence_after();
-        tmem_free(tmem, 512);
+        tmem_free(sh.tmem, 512);
     }
 }
 

@@ -28,12 +28,16 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// (A try sleeps until the phase ends or this time is over. Without it tries came
+// back every few dozen cycles, and a warp's polling took a quarter of the issue slots
+// of the warps beside it.)
+constexpr uint32_t kTryNs = 100000;
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
-        : "r"(bar), "r"(parity)
+        : "r"(bar), "r"(parity), "n"(kTryNs)
         : "memory");
     return ok != 0;
 }
@@ -47,14 +51,12 @@ __device__ __forceinline__ uint64_t now_ns() {
 // (Inline: a call here would have its caller save its registers.)
 constexpr uint64_t kWaitNs = 1000000000ull;
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-    uint64_t t0 = 0;
+    if (mbar_try(bar, parity)) return true;
+    const uint64_t t0 = now_ns();
 #pragma unroll 1
-    for (uint32_t n = 1; !mbar_try(bar, parity); ++n) {
-        if (n % 16) continue;
+    while (!mbar_try(bar, parity)) {
         if (*dead) return false;
-        const uint64_t t = now_ns();
-        if (t0 == 0) t0 = t;
-        if (t - t0 > kWaitNs) {
+        if (now_ns() - t0 > kWaitNs) {
             *dead = 1;
             return false;
         }
