@@ -399,15 +399,15 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             // queries and keys: rows of 64 elements, swizzled; values: the same rows, read along the keys
             const uint64_t qd = smem_desc(base, 16, 1024, 2), kd = smem_desc(ring, 16, 1024, 2), vd = smem_desc(ring, 16384, 1024, 2);
             // Products run in the order of issue, and the queue in front of the tensor cores is short, so what
-            // stands between two products must be as well: the ring's entries are constants (ODD: the tile's
-            // parity), all of tensor memory is the block's and begins at column 0, and what the first stage
-            // has waited for the second one need not.
+            // stands between two products must be as well: all of tensor memory is the block's and begins at
+            // column 0, and what the first stage has waited for the second one need not. (odd: the tile's
+            // parity, whose entries of the ring are 2 odd and 2 odd + 1.)
             uint32_t units = 0, second = 0;   // units begun, and those with a second stage
             uint32_t pp[2] = {0, 0}, kv = 0;  // parities of the next weights of each stage, and of the ring
             int32_t left = 0;                 // tiles of the unit after this one
             bool two = false, follows = false, fresh = true;
-            auto qk = [&](auto odd, int st) {
-                constexpr uint32_t e = decltype(odd)::value ? 2 : 0;
+            auto qk = [&](uint32_t odd, int st) {
+                const uint32_t e = odd * 2;
                 const uint64_t k0 = desc_at(kd, e * kEntryBytes), q0 = desc_at(qd, st * kEntryBytes);
                 if (elect()) {
 #pragma unroll
@@ -422,8 +422,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             };
             // (One commit a batch, as far as that goes: each takes a place in the queue. So the tile's keys are
             // handed back behind the first product with its values, and pv_done is for a unit's last tile.)
-            auto pv = [&](auto odd, int st, bool end) {
-                constexpr uint32_t e = decltype(odd)::value ? 3 : 1;
+            auto pv = [&](uint32_t odd, int st, bool end) {
+                const uint32_t e = odd * 2 + 1;
                 const uint64_t v0 = desc_at(vd, e * kEntryBytes);
                 mbar_wait(bar(sh.p_full[st]), pp[st], dead);
                 pp[st] ^= 1;
@@ -451,35 +451,31 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             };
             // A tile (its values are there): its products with them, and between these the next tile's scores;
             // false behind the last. Waits that seldom wait stand where products are queued.
-            auto tile = [&](auto odd) {
-                using Next = std::integral_constant<bool, !decltype(odd)::value>;
+            auto tile = [&](uint32_t odd) {
                 const bool same = --left > 0;
-                if (odd.value) kv ^= 1;
-                if (same) mbar_wait(bar(sh.full[odd.value ? 0 : 2]), kv, dead);
+                kv ^= odd;
+                if (same) mbar_wait(bar(sh.full[2 - 2 * odd]), kv, dead);
                 pv(odd, 0, !same);
-                if (same) qk(Next{}, 0);
+                if (same) qk(odd ^ 1, 0);
                 if (two) pv(odd, 1, !same);
-                if (same) {
-                    const bool ok = mbar_wait(bar(sh.full[odd.value ? 1 : 3]), kv, dead);
-                    if (two) qk(Next{}, 1);
-                    fresh = false;
-                    return ok;
+                if (!same) {
+                    if (!follows || *dead) return false;
+                    unit();
+                    mbar_wait(bar(sh.full[2 - 2 * odd]), kv, dead);
+                    qk(odd ^ 1, 0);
                 }
-                if (!follows || *dead) return false;
-                unit();
-                mbar_wait(bar(sh.full[odd.value ? 0 : 2]), kv, dead);
-                qk(Next{}, 0);
-                if (two) qk(Next{}, 1);
-                fresh = true;
-                return mbar_wait(bar(sh.full[odd.value ? 1 : 3]), kv, dead);
+                const bool ok = mbar_wait(bar(sh.full[3 - 2 * odd]), kv, dead);
+                if (two) qk(odd ^ 1, 1);
+                fresh = !same;
+                return ok;
             };
             unit();
             mbar_wait(bar(sh.full[0]), 0, dead);
             fence_after();
-            qk(std::false_type{}, 0);
-            if (two) qk(std::false_type{}, 1);
+            qk(0, 0);
+            if (two) qk(0, 1);
             mbar_wait(bar(sh.full[1]), 0, dead);
-            while (tile(std::false_type{}) && tile(std::true_type{})) {
+            for (uint32_t odd = 0; tile(odd); odd ^= 1) {
             }
             if (*dead) {  // the products in flight end before the tensor memory is freed
                 const uint64_t t0 = now_ns();
