@@ -96,7 +96,7 @@ struct KvLaunch {
     uint32_t sms;
 };
 // up to this many queries to a key head (new tokens of a sequence x heads of a group)
-constexpr uint32_t kFewRows = 64;
+constexpr uint32_t kFewRows = 128;
 cudaError_t launch_kv_few_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 cudaError_t launch_kv_few_f16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 uint64_t kv_few_workspace(uint32_t sms);

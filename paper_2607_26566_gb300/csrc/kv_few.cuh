@@ -1,5 +1,5 @@
 // Attention of few new tokens a sequence (a decoding step, a drafted tree, a short
-// chunk): up to 64 queries to a key head.
+// chunk): up to 128 queries to a key head, 64 of them at a time.
 //
 // Such a call reads every key and value once and does little with it, so it is
 // bound by memory: the kernel's business is to keep loads in flight on every SM.
@@ -9,8 +9,8 @@
 // cores without passing a register. A thread of the softmax warps is one key of a
 // 128-key tile, and, for the accumulators, one dimension.
 //
-// Work split: all tiles of all (sequence, key head) units, in order, are cut into
-// as many equal runs as there are SMs, whatever the lengths. A unit that lies in
+// Work split: all tiles of all units (a sequence, a key head, up to 64 queries), in
+// order, are cut into equal runs, one or two an SM, whatever the lengths. A unit that lies in
 // several runs is joined by a second kernel from partial sums in the workspace,
 // in the order of the runs: results do not depend on timing.
 //
@@ -47,11 +47,14 @@ struct Shape {
     static constexpr uint32_t kQ = N * 128 * NS;
     static constexpr uint32_t kP = N * 512;  // two parts
     static constexpr uint32_t kEntry = kSlot * NS;
-    static constexpr uint32_t kRoom = 227 * 1024 - 1024 - kFixed - kQ - kP - kPad;
+    // Two blocks an SM where they fit: one's loads and products run beside the other's softmax.
+    static constexpr uint32_t kBlocks = N <= 32 ? 2 : 1;
+    static constexpr uint32_t kRoom = 228 * 1024 / kBlocks - 1024 - 1024 - kFixed - kQ - kP - kPad;
     static constexpr uint32_t kEntries = kRoom / kEntry < 12 ? kRoom / kEntry : 12;
     static constexpr uint32_t kBytes = 1024 + kEntry * kEntries + kQ + kP + kPad;
     static constexpr uint32_t kTmem = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;
     static_assert(kEntries >= 2, "a tile of K and one of V");
+    static_assert(kBlocks * N <= 64, "the workspace is laid out for one block of 64 rows an SM");
     static constexpr uint32_t kPart = N * (64 * NS) + 2 * N;  // floats of a part: O^T, maxima, sums
 };
 
@@ -67,6 +70,7 @@ struct Shared {
 // run that lie in one unit). Every warp walks it on its own.
 struct Walk {
     uint32_t s, h;
+    int32_t rb, rbs;    // which N rows (queries of a key head) of the sequence's, and of how many
     int64_t at, end;    // the next tile of all, and the end of the run
     int64_t unit;       // the unit's first tile of all
     int32_t tile, n, nt;  // the segment's first tile in the unit, its tiles, the unit's
@@ -78,7 +82,8 @@ struct Walk {
 // A unit in several runs, noted at the run that holds its second part: the runs
 // b0 to b1 hold it, the first as that block's part 0 or 1, the others as part 0.
 struct Join {
-    int32_t s, h, b0, b1, second, valid;
+    int32_t first, row0, rows, h;  // the sequence's first token, the unit's first row and its rows, its key head
+    int32_t b0, b1, second, valid;
 };
 
 struct Few {
@@ -88,12 +93,18 @@ struct Few {
     uint32_t* fault;   // host-mapped: set where a wait ran out
 };
 
+// The sequence's rows, in units of N.
+template <int N>
+__device__ __forceinline__ int32_t row_units(const KvAttend& a, const KvSeq& q) {
+    return (min(q.n, int32_t(a.tok.max_new)) * int32_t(a.group) + N - 1) / N;
+}
 __device__ __forceinline__ int32_t unit_tiles(const KvAttend& a, const KvSeq& q, KvSpan& sp) {
     if (q.n == 0) return 0;
     sp = kv_span(a, q, 0, min(q.n, int32_t(a.tok.max_new)));
     return max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
 }
 
+template <int N>
 __device__ __forceinline__ void walk_seq(const KvAttend& a, Walk& w) {
     w.nt = 0;
     for (; w.s < a.tok.n_seqs; ++w.s) {
@@ -101,29 +112,40 @@ __device__ __forceinline__ void walk_seq(const KvAttend& a, Walk& w) {
         w.nt = unit_tiles(a, w.q, w.span);
         if (w.nt) break;
     }
-    w.rows = min(w.q.n, int32_t(a.tok.max_new)) * int32_t(a.group);
+    w.rbs = max(1, row_units<N>(a, w.q));
 }
+template <int N>
+__device__ __forceinline__ void walk_unit(const KvAttend& a, Walk& w) {
+    w.rows = min(N, min(w.q.n, int32_t(a.tok.max_new)) * int32_t(a.group) - w.rb * N);
+    w.n = int32_t(min(int64_t(w.nt - w.tile), w.end - w.at));
+}
+template <int N>
 __device__ __forceinline__ void walk_start(const KvAttend& a, Walk& w, uint32_t s, int32_t rest, int64_t at, int64_t end) {
     w.s = s, w.at = at, w.end = end;
-    walk_seq(a, w);
+    walk_seq<N>(a, w);
     const int32_t nt = max(w.nt, 1);
-    w.h = rest / nt;
+    w.h = rest / nt / w.rbs;
+    w.rb = rest / nt % w.rbs;
     w.tile = rest % nt;
     w.unit = at - w.tile;
-    w.n = int32_t(min(int64_t(w.nt - w.tile), end - at));
+    walk_unit<N>(a, w);
 }
+template <int N>
 __device__ __forceinline__ bool walk_next(const KvAttend& a, Walk& w) {
     w.at += w.n;
     if (w.at >= w.end) return false;
     w.tile = 0;
     w.unit = w.at;
-    if (++w.h == a.pages.kv_heads) {
-        w.h = 0;
-        ++w.s;
-        walk_seq(a, w);
-        if (w.nt == 0) return false;
+    if (++w.rb == w.rbs) {
+        w.rb = 0;
+        if (++w.h == a.pages.kv_heads) {
+            w.h = 0;
+            ++w.s;
+            walk_seq<N>(a, w);
+            if (w.nt == 0) return false;
+        }
     }
-    w.n = int32_t(min(int64_t(w.nt), w.end - w.at));
+    walk_unit<N>(a, w);
     return true;
 }
 // first slot of the unit's tile i
@@ -151,7 +173,7 @@ __device__ __forceinline__ float columns(float (&v)[n], uint32_t lane) {
 }
 
 template <class T, int N, int NS, bool MOD>
-__global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant__ Few f, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(const __grid_constant__ Few f, const __grid_constant__ CUtensorMap map) {
     using Sh = Shape<N, NS>;
     constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
     constexpr int C = N < 32 ? N : 32;  // columns at a time
@@ -187,7 +209,8 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
     int64_t mine = 0;
     for (uint32_t s = tid * per; s < min(a.tok.n_seqs, (tid + 1) * per); ++s) {
         KvSpan sp;
-        mine += unit_tiles(a, kv_seq(a.pages, a.tok, s), sp);
+        const KvSeq q = kv_seq(a.pages, a.tok, s);
+        mine += unit_tiles(a, q, sp) * row_units<N>(a, q);
     }
     // inclusive scan over the block's threads, in tiles of one key head
     int64_t inc = mine;
@@ -217,7 +240,8 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
             int64_t p = lo;
             for (uint32_t s = tid * per;; ++s) {
                 KvSpan sp;
-                const int64_t n = unit_tiles(a, kv_seq(a.pages, a.tok, s), sp) * K;
+                const KvSeq q = kv_seq(a.pages, a.tok, s);
+                const int64_t n = int64_t(unit_tiles(a, q, sp)) * row_units<N>(a, q) * K;
                 if (run0 < p + n) {
                     sh.start_seq = int32_t(s);
                     sh.start_rest = int32_t(run0 - p);
@@ -233,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
     if (busy && warp == 4) {
         // ---------------------------------------------------------- loads
         Walk w;
-        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        walk_start<N>(a, w, sh.start_seq, sh.start_rest, run0, run1);
         const uint32_t shift = a.pages.token_shift;
         const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
         const uint32_t T_mask = (1u << shift) - 1;
@@ -262,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                                      (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
                 }
             }
-        } while (walk_next(a, w));
+        } while (walk_next<N>(a, w));
     loads_done:
         __syncwarp();
         if (*dead) {  // the copies in flight land before the block ends
@@ -273,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
     } else if (busy && warp == 5) {
         // ---------------------------------------------------------- products
         Walk w;
-        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        walk_start<N>(a, w, sh.start_seq, sh.start_rest, run0, run1);
         constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
         constexpr uint32_t kPv = instr_desc(kBf16, true, true, 128, N);
         const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
@@ -324,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                 if (!fresh) pv(n - 1, fresh_before);
                 fresh_before = fresh;
             }
-        } while (walk_next(a, w));
+        } while (walk_next<N>(a, w));
         pv(n - 1, fresh_before);
         if (*dead) {  // the products in flight end before the tensor memory is freed
             const uint64_t t0 = now_ns();
@@ -334,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
     } else if (busy) {
         // ---------------------------------------------------------- softmax
         Walk w;
-        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        walk_start<N>(a, w, sh.start_seq, sh.start_rest, run0, run1);
         const uint32_t D = a.pages.head_dim;
         const uint32_t lanes = tmem + (warp << 21);  // this warp's 32 lanes
         const float k2 = a.scale * kLog2e;
@@ -343,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
             // this run's note of a unit that began in the run before it
             const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.nt) * blocks - 1) / total;
             const bool here = w.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
-            f.join[blockIdx.x] = {int32_t(w.s), int32_t(w.h), int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
+            f.join[blockIdx.x] = {w.q.first, w.rb * N, w.rows, int32_t(w.h), int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
         }
         uint32_t n = 0;
         do {
@@ -353,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                 const uint32_t c = u / (NS * 8), x = u % (NS * 8);
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (int32_t(c) < w.rows && x * 8 < D) {
-                    const uint32_t t = c / a.group, g = c % a.group;
+                    const uint32_t t = (w.rb * N + c) / a.group, g = (w.rb * N + c) % a.group;
                     v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(w.q.first + t) * a.q_stride +
                                                         uint64_t(w.h * a.group + g) * D + x * 8);
                 }
@@ -364,8 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                 KvQuery q{0, INT32_MAX, 0, 0};
                 float sl = 0.0f;
                 if (int32_t(tid) < w.rows) {
-                    q = kv_query(a, w.q, tid / a.group);
-                    if (MOD && a.slopes) sl = a.slopes[w.h * a.group + tid % a.group] * kLog2e;
+                    q = kv_query(a, w.q, (w.rb * N + tid) / a.group);
+                    if (MOD && a.slopes) sl = a.slopes[w.h * a.group + (w.rb * N + tid) % a.group] * kLog2e;
                 }
                 first[tid] = q.first, last[tid] = q.last, pos[tid] = q.pos, word[tid] = q.word;
                 slope[tid] = sl;
@@ -523,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
                         const int col = c0 + c;
                         if (col >= w.rows) break;
                         const float l = red[0][col] + red[1][col] + red[2][col] + red[3][col];
-                        const uint32_t t = col / a.group, g = col % a.group;
+                        const uint32_t t = (w.rb * N + col) / a.group, g = (w.rb * N + col) % a.group;
                         const uint64_t row = uint64_t(w.q.first + t);
                         const float r = l == 0.0f ? 0.0f : 1.0f / l;
                         if (d < D)
@@ -552,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_kernel(const __grid_constant_
             }
             fence_before();
             bar_sync<1, kSoftThreads>();  // red and top are read before the next segment writes them
-        } while (walk_next(a, w));
+        } while (walk_next<N>(a, w));
     }
     if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
     __syncthreads();
@@ -577,8 +601,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Few f
     if (!j.valid) return;
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, D = a.pages.head_dim;
     const int32_t col = int32_t(blockIdx.y * 8 + warp);
-    const KvSeq q = kv_seq(a.pages, a.tok, uint32_t(j.s));
-    if (col >= min(q.n, int32_t(a.tok.max_new)) * int32_t(a.group)) return;
+    if (col >= j.rows) return;
     auto part = [&](int32_t b) { return f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * Sh::kPart; };
     float top = -INFINITY;
     for (int32_t b = j.b0 + int32_t(lane); b <= j.b1; b += 32) top = fmaxf(top, __ldcg(part(b) + N * 64 * NS + col));
@@ -605,8 +628,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Few f
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
-    const uint64_t row = uint64_t(q.first + col / int32_t(a.group));
-    const uint32_t head = uint32_t(j.h) * a.group + uint32_t(col) % a.group;
+    const uint64_t row = uint64_t(j.first + (j.row0 + col) / int32_t(a.group));
+    const uint32_t head = uint32_t(j.h) * a.group + uint32_t(j.row0 + col) % a.group;
     const float r = l == 0.0f ? 0.0f : 1.0f / l;
     T* out = static_cast<T*>(a.out) + row * a.out_stride + uint64_t(head) * D + lane * kVec;
     if (lane * kVec < D) {
@@ -628,9 +651,10 @@ cudaError_t launch_as(const Few& f, const CUtensorMap& map, uint32_t sms, cudaSt
         if (e != cudaSuccess) return e;
         if (dev < 64) ready |= uint64_t(1) << dev;
     }
-    e = launch_pdl(few_kernel<T, N, NS, MOD>, dim3(sms), kThreads, bytes, stream, f, map);
+    const uint32_t blocks = sms * Shape<N, NS>::kBlocks;
+    e = launch_pdl(few_kernel<T, N, NS, MOD>, dim3(blocks), kThreads, bytes, stream, f, map);
     if (e != cudaSuccess) return e;
-    return launch_pdl(join_kernel<T, N, NS>, dim3(sms, (N + 7) / 8), 256, 0, stream, f);
+    return launch_pdl(join_kernel<T, N, NS>, dim3(blocks, (N + 7) / 8), 256, 0, stream, f);
 }
 
 template <class T, int N>
@@ -649,7 +673,7 @@ cudaError_t launch_t(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStr
                         : launch_n<T, 64>(f, map, sms, stream);
 }
 
-constexpr uint64_t join_bytes(uint32_t sms) { return (uint64_t(sms) * sizeof(Join) + 255) / 256 * 256; }
+constexpr uint64_t join_bytes(uint32_t sms) { return (uint64_t(sms) * 2 * sizeof(Join) + 255) / 256 * 256; }  // two blocks an SM
 
 template <class T>
 cudaError_t launch_few(const KvAttend& a, const KvLaunch& l, cudaStream_t stream) {

@@ -757,41 +757,33 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
 // Joins the units that lie in several runs: a block for 32 rows of a run's note, a
 // lane a row.
 template <class T>
-__global__ void __launch_bounds__(256) rows_join_kernel(const __grid_constant__ Rows f) {
+__global__ void __launch_bounds__(1024) rows_join_kernel(const __grid_constant__ Rows f) {
     const KvAttend& a = f.a;
     pdl_launch();
     pdl_wait();
     const Join j = f.join[blockIdx.x];
     if (!j.valid) return;
-    const uint32_t warp = threadIdx.x / 32, D = a.pages.head_dim;
+    const uint32_t warp = threadIdx.x / 32, D = a.pages.head_dim;  // warp: which four dimensions
     const int32_t r = int32_t(blockIdx.y * 32 + threadIdx.x % 32);
-    if (r >= j.rows) return;
+    if (r >= j.rows || warp * 4 >= D) return;
     auto part = [&](int32_t b) { return f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * kRowPart; };
     float top = -INFINITY, l = 0.0f;
+#pragma unroll 8
     for (int32_t b = j.b0; b <= j.b1; ++b) top = fmaxf(top, __ldcg(part(b) + kRows * 128 + r));
-    float4 o[4] = {};
-#pragma unroll 2
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
     for (int32_t b = j.b0; b <= j.b1; ++b) {
         const float* p = part(b);
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + warp * kRows + r);
         const float m = __ldcg(p + kRows * 128 + r), x = m == top ? 1.0f : exp2_approx(m - top);
         l += x * __ldcg(p + kRows * 128 + kRows + r);
-#pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) {
-            if ((warp + 8 * k) * 4 >= D) break;
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + (warp + 8 * k) * kRows + r);
-            o[k].x += x * v.x, o[k].y += x * v.y, o[k].z += x * v.z, o[k].w += x * v.w;
-        }
+        o.x += x * v.x, o.y += x * v.y, o.z += x * v.z, o.w += x * v.w;
     }
     const uint32_t row = uint32_t(j.m) * kRows + uint32_t(r), head = uint32_t(j.h) * a.group + row % a.group;
     const uint64_t orow = uint64_t(j.first) + row / a.group;
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
-    T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D;
-#pragma unroll
-    for (uint32_t k = 0; k < 4; ++k) {
-        const uint32_t d = (warp + 8 * k) * 4;
-        if (d >= D) break;
-        *reinterpret_cast<uint2*>(out + d) = make_uint2(Kv16<T>::from2(o[k].x * by, o[k].y * by), Kv16<T>::from2(o[k].z * by, o[k].w * by));
-    }
+    T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D + warp * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(Kv16<T>::from2(o.x * by, o.y * by), Kv16<T>::from2(o.z * by, o.w * by));
     if (a.lse && warp == 0) a.lse[orow * a.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
 }
 
@@ -812,7 +804,7 @@ cudaError_t launch_rows_as(const Rows& f, const CUtensorMap& map, uint32_t sms, 
     }
     if ((e = launch_pdl(plan_kernel, dim3(1), kPlanThreads, 0, stream, f)) != cudaSuccess) return e;
     if ((e = launch_pdl(rows_kernel<T, MOD>, dim3(sms), kRowThreads, kRowSmem, stream, f, map)) != cudaSuccess) return e;
-    return launch_pdl(rows_join_kernel<T>, dim3(sms, kRows / 32), 256, 0, stream, f);
+    return launch_pdl(rows_join_kernel<T>, dim3(sms, kRows / 32), 1024, 0, stream, f);
 }
 
 template <class T>
