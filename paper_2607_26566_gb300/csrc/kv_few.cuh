@@ -14,9 +14,9 @@
 // several runs is joined by a second kernel from partial sums in the workspace,
 // in the order of the runs: results do not depend on timing.
 //
-// Softmax: the running maximum of a query is raised only when a score exceeds it by
-// 2^8 (the accumulators, in fp32, have the room), so most tiles need no exchange
-// between threads but one vote. Weights go to the product as two 16-bit numbers
+// Softmax: a query's scores are weighed against a reference, its first tile's
+// maximum, that is raised only when a score exceeds it by 2^8 (the accumulators, in
+// fp32, have the room), so most tiles need no exchange between threads but one vote. Weights go to the product as two 16-bit numbers
 // (the rounded weight and what the rounding left): products are not what bounds
 // this kernel, and the weights keep 16 bits or more.
 #pragma once
@@ -35,7 +35,7 @@ using namespace tc;
 constexpr int kSoftThreads = 128;
 constexpr int kThreads = kSoftThreads + 64;  // + the loading warp and the product warp
 constexpr uint32_t kSlot = 16384;            // 128 rows of 64 elements
-constexpr float kRaise = 8.0f;
+constexpr float kRaise = 8.0f;  // in units of log2
 
 template <int N, int NS>
 struct Shape {
@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     __shared__ __align__(16) float top[N], scale_by[N], red[4][N];
     __shared__ __align__(16) int32_t first[N], last[N], pos[N];
     __shared__ __align__(16) uint64_t word[N];
+    static_assert(N <= 64, "two columns of sums a lane");
     __shared__ float slope[N];
     const KvAttend& a = f.a;
     const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -398,9 +399,11 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             mbar_arrive(bar(sh.q_full));
             bar_sync<1, kSoftThreads>();
 
-            float sum[N];
-#pragma unroll
-            for (int c = 0; c < N; ++c) sum[c] = 0.0f;
+            // Sums of weights: up to 32 columns, each thread its key's; 64, of the warp's keys: lane i has columns
+            // i and i + 32 (a tile then adds up over its lanes; 64 registers less, and code that fits beside the rest).
+            constexpr bool kLanes = N > 32;
+            constexpr int S = kLanes ? N / 32 : N;
+            float sum[S] = {};
             for (int32_t i = 0; i < w.n; ++i, ++n) {
                 const int32_t slot0 = tile_slot(w, w.tile + i), key = slot0 + int32_t(tid);
                 const bool masked = slot0 < w.span.all_lo || slot0 + kTileKeys > w.span.all_hi;
@@ -415,7 +418,9 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 mbar_wait(bar(sh.s_full[n & 1]), n >> 1 & 1, dead);
                 fence_after();
                 // scores of columns c0 .. c0 + C
-                auto scores = [&](int c0, float (&x)[C]) {
+                float x[C];
+                static_assert(kLanes || C == N, "x holds every column's weight behind the pass");
+                auto scores = [&](int c0) {
                     if constexpr (C == 32)
                         tmem_ld32(s_at + c0, x);
                     else
@@ -431,35 +436,22 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                         }
                     }
                     if (masked) {
+                        uint32_t see = 0;
+#pragma unroll 4
+                        for (int c = 0; c < C; ++c)
+                            see |= uint32_t(kpos >= first[c0 + c] && (key < last[c0 + c] || (word[c0 + c] & bit))) << c;
 #pragma unroll
-                        for (int c = 0; c < C; ++c) {
-                            const bool see = kpos >= first[c0 + c] && (key < last[c0 + c] || (word[c0 + c] & bit));
-                            x[c] = see ? x[c] : -INFINITY;
-                        }
+                        for (int c = 0; c < C; ++c) x[c] = see & (1u << c) ? x[c] : -INFINITY;
                     }
                 };
-                float x[C];
-                bool over = false;
-#pragma unroll
-                for (int c0 = 0; c0 < N; c0 += C) {
-                    scores(c0, x);
-#pragma unroll
-                    for (int c = 0; c < C; ++c) over |= x[c] > top[c0 + c] + kRaise;
-                }
-                const bool raise = bar_any<1, kSoftThreads>(over);
-                if (n) mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
-                if (raise) {
-#pragma unroll
-                    for (int c0 = 0; c0 < N; c0 += C) {
-                        float y[C];
-                        if constexpr (N > C)
-                            scores(c0, y);
-                        else
-#pragma unroll
-                            for (int c = 0; c < C; ++c) y[c] = x[c];
-                        const float m = columns<C, true>(y, lane);
-                        if (lane < C) red[warp][c0 + lane] = m;
-                    }
+                // the product before this one is complete: its weights may be overwritten, its accumulators scaled
+                bool over_with = n == 0;
+                auto last_product = [&]() {
+                    if (!over_with) mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
+                    over_with = true;
+                };
+                // references become the tile's maxima (red: of each warp's keys)
+                auto raise = [&]() {
                     bar_sync<1, kSoftThreads>();
                     if (tid < N) {
                         const float was = top[tid];
@@ -469,50 +461,104 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                     }
                     bar_sync<1, kSoftThreads>();
                     if (i) {
+                        last_product();
                         fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int c0 = 0; c0 < N; c0 += 16) {
                             float o[16];
                             tmem_ld16(lanes + 2 * N + c0, o);
                             wait_ld(o);
 #pragma unroll
-                            for (int c = 0; c < 16; ++c) o[c] *= scale_by[c0 + c], sum[c0 + c] *= scale_by[c0 + c];
+                            for (int c = 0; c < 16; ++c) o[c] *= scale_by[c0 + c];
                             tmem_st16(lanes + 2 * N + c0, reinterpret_cast<uint32_t*>(o));
                         }
                         wait_st();
-                    }
-                }
-                // weights: rounded, and the rest, eight columns to a 16-byte row of the operand
 #pragma unroll
-                for (int c0 = 0; c0 < N; c0 += C) {
-                    if constexpr (N > C) scores(c0, x);
+                        for (int c = 0; c < S; ++c) sum[c] *= scale_by[kLanes ? c * 32 + int(lane) : c];
+                    }
+                };
+                // weights of columns c0 to c0 + C (in x afterwards): rounded, and the rest, eight columns to a 16-byte
+                // row of the operand
+                auto weigh = [&](int c0) {
+                    last_product();
 #pragma unroll
                     for (int c = 0; c < C; c += 8) {
                         uint32_t hi[4], lo[4];
 #pragma unroll
                         for (int j = 0; j < 8; j += 2) {
-                            float p[2];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
                                 const float m = top[c0 + c + j + k];
-                                p[k] = exp2_approx(x[c + j + k] - (m == -INFINITY ? 0.0f : m));
-                                sum[c0 + c + j + k] += p[k];
+                                x[c + j + k] = exp2_approx(x[c + j + k] - (m == -INFINITY ? 0.0f : m));
                             }
-                            hi[j / 2] = Kv16<T>::from2(p[0], p[1]);
+                            hi[j / 2] = Kv16<T>::from2(x[c + j], x[c + j + 1]);
                             const float2 r = Kv16<T>::to2(hi[j / 2]);
-                            lo[j / 2] = Kv16<T>::from2(p[0] - r.x, p[1] - r.y);
+                            lo[j / 2] = Kv16<T>::from2(x[c + j] - r.x, x[c + j + 1] - r.y);
                         }
                         uint8_t* at = mem + (ps - base) + (c0 + c) / 8 * 2048 + tid * 16;
                         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                         *reinterpret_cast<uint4*>(at + N * 256) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                     }
+                };
+                if constexpr (!kLanes) {
+                    // all columns at once: their scores are looked at while the product before this one runs
+                    scores(0);
+                    bool over = false;
+#pragma unroll
+                    for (int c = 0; c < C; ++c) over |= x[c] > top[c] + kRaise;
+                    if (bar_any<1, kSoftThreads>(over)) {
+                        float y[C];
+#pragma unroll
+                        for (int c = 0; c < C; ++c) y[c] = x[c];
+                        const float m = columns<C, true>(y, lane);
+                        if (lane < C) red[warp][lane] = m;
+                        raise();
+                    }
+                    weigh(0);
+#pragma unroll
+                    for (int c = 0; c < S; ++c) sum[c] += x[c % C];
+                } else {
+                    // 32 at a time, in code that is not repeated (a call of a few tiles waits for its instructions more
+                    // than for anything else): weighed against the references so far, and, where that will not do
+                    // or there is none yet, once more against the tile's maxima
+                    bool above = i == 0;
+                    float part[S];
+#pragma unroll 1
+                    for (int pass = 0; pass < 2; ++pass) {
+                        if (above) {
+#pragma unroll 1
+                            for (int c0 = 0; c0 < N; c0 += C) {
+                                scores(c0);
+                                const float m = columns<C, true>(x, lane);
+                                if (lane < C) red[warp][c0 + lane] = m;
+                            }
+                            raise();
+                        }
+                        bool over = false;
+#pragma unroll 1
+                        for (int c0 = 0; c0 < N; c0 += C) {
+                            scores(c0);
+#pragma unroll
+                            for (int c = 0; c < C; ++c) over |= x[c] > top[c0 + c] + kRaise;
+                            weigh(c0);
+                            const float all = columns<C, false>(x, lane);
+                            if (c0 == 0)
+                                part[0] = all;
+                            else
+                                part[S - 1] = all;
+                        }
+                        above = bar_any<1, kSoftThreads>(over);
+                        if (!above) break;
+                    }
+#pragma unroll
+                    for (int c = 0; c < S; ++c) sum[c] += part[c];
                 }
                 // values that none of the unit's queries sees may be anything: zeros, as their weights are
                 if (slot0 < w.span.lo || slot0 + kTileKeys > w.span.hi) {
                     const uint32_t e = (2 * n + 1) % Sh::kEntries;
                     mbar_wait(bar(sh.full[e]), (2 * n + 1) / Sh::kEntries & 1, dead);
                     if (key < w.span.lo || key >= w.span.hi) {
-#pragma unroll
+#pragma unroll 1
                         for (int k = 0; k < NS * 8; ++k)
                             *reinterpret_cast<uint4*>(mem + e * Sh::kEntry + k / 8 * kSlot + tid * 128 + k % 8 * 16) =
                                 make_uint4(0, 0, 0, 0);
@@ -522,57 +568,51 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 fence_before();
                 mbar_arrive(bar(sh.p_full));
             }
-            // the segment's sums: over the keys' threads, then over the warps
+            // the segment's sums over the warps
 #pragma unroll
-            for (int c0 = 0; c0 < N; c0 += C) {
-                float y[C];
-#pragma unroll
-                for (int c = 0; c < C; ++c) y[c] = sum[c0 + c];
-                const float m = columns<C, false>(y, lane);
-                if (lane < C) red[warp][c0 + lane] = m;
+            for (int c = 0; c < (kLanes ? S : 1); ++c) {
+                if constexpr (kLanes) {
+                    red[warp][c * 32 + lane] = sum[c];
+                } else {
+                    const float all = columns<N, false>(sum, lane);
+                    if (lane < N) red[warp][lane] = all;
+                }
             }
             mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
             fence_after();
             bar_sync<1, kSoftThreads>();
             const bool whole = w.n == w.nt;
             const uint32_t d = tid;
-            if (whole) {
+            float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * Sh::kPart;
+            uint32_t t = w.rb * N / a.group, g = w.rb * N % a.group;  // the column's token and head
+#pragma unroll 1
+            for (int c0 = 0; c0 < w.rows; c0 += 16) {
+                float o[16];
+                tmem_ld16(lanes + 2 * N + c0, o);
+                wait_ld(o);
 #pragma unroll
-                for (int c0 = 0; c0 < N; c0 += 16) {
-                    float o[16];
-                    tmem_ld16(lanes + 2 * N + c0, o);
-                    wait_ld(o);
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        const int col = c0 + c;
-                        if (col >= w.rows) break;
-                        const float l = red[0][col] + red[1][col] + red[2][col] + red[3][col];
-                        const uint32_t t = (w.rb * N + col) / a.group, g = (w.rb * N + col) % a.group;
-                        const uint64_t row = uint64_t(w.q.first + t);
-                        const float r = l == 0.0f ? 0.0f : 1.0f / l;
-                        if (d < D)
-                            static_cast<T*>(a.out)[row * a.out_stride + uint64_t(w.h * a.group + g) * D + d] =
-                                Kv16<T>::from1(o[c] * r);
-                        if (a.lse && d == 0)
-                            a.lse[row * a.q_heads + w.h * a.group + g] = l == 0.0f ? -INFINITY : (top[col] + log2f(l)) * kLn2;
+                for (int c = 0; c < 16; ++c) {
+                    const int col = c0 + c;
+                    if (col < w.rows) {
+                        if (whole) {
+                            const float l = red[0][col] + red[1][col] + red[2][col] + red[3][col];
+                            const uint64_t row = uint64_t(w.q.first + t);
+                            const float r = l == 0.0f ? 0.0f : 1.0f / l;
+                            if (d < D)
+                                static_cast<T*>(a.out)[row * a.out_stride + uint64_t(w.h * a.group + g) * D + d] =
+                                    Kv16<T>::from1(o[c] * r);
+                            if (a.lse && d == 0)
+                                a.lse[row * a.q_heads + w.h * a.group + g] = l == 0.0f ? -INFINITY : (top[col] + log2f(l)) * kLn2;
+                            if (++g == a.group) g = 0, ++t;
+                        } else if (d < 64 * NS) {  // a part of the unit: to the workspace
+                            __stcg(part + col * (64 * NS) + d, o[c]);
+                        }
                     }
                 }
-            } else {
-                // a part of the unit: to the workspace
-                float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * Sh::kPart;
-#pragma unroll
-                for (int c0 = 0; c0 < N; c0 += 16) {
-                    float o[16];
-                    tmem_ld16(lanes + 2 * N + c0, o);
-                    wait_ld(o);
-#pragma unroll
-                    for (int c = 0; c < 16; ++c)
-                        if (c0 + c < w.rows && d < 64 * NS) __stcg(part + (c0 + c) * (64 * NS) + d, o[c]);
-                }
-                if (tid < N) {
-                    __stcg(part + N * 64 * NS + tid, top[tid]);
-                    __stcg(part + N * 64 * NS + N + tid, red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]);
-                }
+            }
+            if (!whole && tid < N) {
+                __stcg(part + N * 64 * NS + tid, top[tid]);
+                __stcg(part + N * 64 * NS + N + tid, red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]);
             }
             fence_before();
             bar_sync<1, kSoftThreads>();  // red and top are read before the next segment writes them
