@@ -1,102 +1,159 @@
 // Appending keys and values to the cache (per-head RMS norm and rotation of
 // queries and keys on the way), and keeping the accepted rows of a draft.
-#include "kv_device.cuh"
+#include "kv_attend.cuh"
 #include "t2istore.h"
 
 namespace t2i {
 namespace {
 
-// Sixteen lanes hold a head's row, eight elements a lane.
+// Sixteen lanes hold a head's row, eight elements a lane, so that a row is one
+// 16-byte vector a lane and a norm's sum four shuffles. A block takes one token (or a
+// share of its heads): its cosines, sines, norm weights and place in the cache are
+// looked up once for all heads, and each group of sixteen lanes loads its next head
+// before it works on the one it has. Bound by memory at many tokens (each byte is
+// read and written once), by the chain of look-ups at few.
 constexpr uint32_t kLanes = 16;
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kGroups = kThreads / kLanes;
 
-// The rotation of a row that lies over sixteen lanes. c, s: the pair's cosine
-// and sine for each of the lane's eight elements.
-struct Turn {
-    float c[8], s[8];
+// How a pair's other element is reached: interleaved pairs lie in one lane; halves
+// that are multiples of eight elements lie at the same place in another lane; others
+// go through shared memory.
+enum Turn : int { kNone, kInLane, kAcross, kAnywhere };
+
+// Eight elements as they are loaded.
+template <class T>
+struct Raw {
+    uint4 v[sizeof(T) / 2];
 };
-
-// The lane's cosines and sines; NaN for a position that the tables lack.
-__device__ __forceinline__ void load_turn(const KvAppend& a, int32_t pos, uint32_t e0, Turn& t) {
-    const uint32_t half = a.rotary_dim / 2;
-    const bool known = pos >= 0 && pos < int64_t(a.n_positions);
-    const float* cs = a.cos_table + uint64_t(known ? pos : 0) * half;
-    const float* sn = a.sin_table + uint64_t(known ? pos : 0) * half;
+template <class T>
+__device__ __forceinline__ void unpack(const Raw<T>& r, float (&x)[8]) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t e = e0 + i;
-        t.c[i] = 1.0f;
-        t.s[i] = 0.0f;
-        if (e < a.rotary_dim) {
-            const uint32_t p = a.interleaved ? e / 2 : e < half ? e : e - half;
-            t.c[i] = known ? cs[p] : __int_as_float(0x7FC00000);
-            t.s[i] = known ? sn[p] : __int_as_float(0x7FC00000);
+        for (int i = 0; i < 2; ++i) {
+            x[4 * i] = __uint_as_float(r.v[i].x), x[4 * i + 1] = __uint_as_float(r.v[i].y);
+            x[4 * i + 2] = __uint_as_float(r.v[i].z), x[4 * i + 3] = __uint_as_float(r.v[i].w);
+        }
+    } else {
+        const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = Kv16<T>::to2(w[i]);
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
         }
     }
 }
 
-// Norm (w not null) and rotation of one row, in fp32. `row`: 128 floats of
-// shared memory of these sixteen lanes.
-__device__ __forceinline__ void norm_turn(const KvAppend& a, float (&x)[8], const float* w, const Turn& t, uint32_t e0,
-                                          float* row, uint32_t mask) {
-    if (w) {
-        float ss = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
-#pragma unroll
-        for (int d = 8; d; d >>= 1) ss += __shfl_xor_sync(mask, ss, d, kLanes);
-        const float r = 1.0f / sqrtf(ss / float(a.pages.head_dim) + a.eps);
-        if (e0 < a.pages.head_dim) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= r * w[e0 + i];
-        }
-    }
-    if (!a.rotary_dim) return;
-    const uint32_t half = a.rotary_dim / 2;
-    __syncwarp(mask);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) row[e0 + i] = x[i];
-    __syncwarp(mask);
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t e = e0 + i;
-        if (e < a.rotary_dim) {
-            const bool second = a.interleaved ? e & 1 : e >= half;
-            const uint32_t other = a.interleaved ? e ^ 1 : second ? e - half : e + half;
-            const float o = row[other];
-            x[i] = second ? x[i] * t.c[i] + o * t.s[i] : x[i] * t.c[i] - o * t.s[i];
-        }
-    }
-}
-
-template <class T, class TI>
+template <class T, class TI, int TURN>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ KvAppend a) {
-    __shared__ float rows[kGroups][128];
+    __shared__ float rows[TURN == kAnywhere ? kGroups : 1][128];
     const uint32_t g = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
     const uint32_t mask = 0xFFFFu << (threadIdx.x & 16u);
     const uint32_t t = blockIdx.x, e0 = lane * 8;
-    const bool mine = e0 < a.pages.head_dim;
+    const uint32_t K = a.pages.kv_heads, D = a.pages.head_dim, heads = a.q_heads + 2 * K, step = gridDim.y * kGroups;
+    const bool mine = e0 < D;
+    tc::pdl_launch();
+    tc::pdl_wait();
+    auto load = [&](uint32_t h) {  // queries, then keys, then values
+        Raw<TI> r{};
+        if (!mine) return r;
+        const uint32_t j = h - a.q_heads;
+        const TI* src = h < a.q_heads ? static_cast<const TI*>(a.q) + t * a.q_stride + uint64_t(h) * D
+                        : j < K       ? static_cast<const TI*>(a.k) + t * a.k_stride + uint64_t(j) * D
+                                      : static_cast<const TI*>(a.v) + t * a.v_stride + uint64_t(j - K) * D;
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(TI) / 2; ++i) r.v[i] = reinterpret_cast<const uint4*>(src + e0)[i];
+        return r;
+    };
+    uint32_t h = blockIdx.y * kGroups + g;
+    Raw<TI> next{};
+    if (h < heads) next = load(h);
+    float wq[8], wk[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        wq[i] = mine && a.q_norm ? a.q_norm[e0 + i] : 1.0f;
+        wk[i] = mine && a.k_norm ? a.k_norm[e0 + i] : 1.0f;
+    }
+
     const uint32_t seq = kv_owner(a.tok, t);
     const KvSeq s = kv_seq(a.pages, a.tok, seq);
     const int32_t i = int32_t(t) - s.first;
-    const bool real = i >= 0 && i < s.n;
-    const int64_t slot = real ? int64_t(s.len) - s.n + i : -1;
-    Turn turn;
-    load_turn(a, a.positions ? a.positions[t] : int32_t(slot), e0, turn);
-    const uint32_t K = a.pages.kv_heads, D = a.pages.head_dim;
-    for (uint32_t h = blockIdx.y * kGroups + g; h < a.q_heads + 2 * K; h += gridDim.y * kGroups) {
-        float x[8] = {};
-        const bool is_q = h < a.q_heads;
-        const uint32_t j = is_q ? h : h - a.q_heads;  // keys, then values
-        const bool is_v = !is_q && j >= K;
-        const TI* src = is_q   ? static_cast<const TI*>(a.q) + t * a.q_stride + uint64_t(h) * D
-                        : is_v ? static_cast<const TI*>(a.v) + t * a.v_stride + uint64_t(j - K) * D
-                               : static_cast<const TI*>(a.k) + t * a.k_stride + uint64_t(j) * D;
-        if (mine) kv_load8(src + e0, x);
-        if (!is_v) norm_turn(a, x, is_q ? a.q_norm : a.k_norm, turn, e0, rows[g], mask);
+    const int64_t slot = i >= 0 && i < s.n ? int64_t(s.len) - s.n + i : -1;
+    // the token's first row in the cache (key head 0 of the layer), and from head to head
+    uint8_t* const place = kv_row(a.pages, seq, slot, a.pages.layer, 0, 0);
+    const uint64_t apart = uint64_t(D * 2) << a.pages.token_shift;
+
+    // the pair's cosine and sine for each of the lane's elements; NaN for a position that the tables lack
+    float co[8], si[8];
+    const uint32_t half = a.rotary_dim / 2;
+    if (TURN != kNone) {
+        const int32_t pos = a.positions ? a.positions[t] : int32_t(slot);
+        const bool known = pos >= 0 && pos < int64_t(a.n_positions);
+        const float* cs = a.cos_table + uint64_t(known ? pos : 0) * half;
+        const float* sn = a.sin_table + uint64_t(known ? pos : 0) * half;
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+            const uint32_t e = e0 + k;
+            co[k] = 1.0f, si[k] = 0.0f;
+            if (e < a.rotary_dim) {
+                const uint32_t p = TURN == kInLane || a.interleaved ? e / 2 : e < half ? e : e - half;
+                co[k] = known ? cs[p] : __int_as_float(0x7FC00000);
+                si[k] = known ? sn[p] : __int_as_float(0x7FC00000);
+            }
+        }
+    }
+
+    for (; h < heads; h += step) {
+        const Raw<TI> raw = next;
+        if (h + step < heads) next = load(h + step);
+        float x[8];
+        unpack<TI>(raw, x);
+        const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + K;
+        if (!is_v && (is_q ? a.q_norm : a.k_norm)) {
+            float ss = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ss += x[k] * x[k];
+#pragma unroll
+            for (int d = 8; d; d >>= 1) ss += __shfl_xor_sync(mask, ss, d, kLanes);
+            const float r = 1.0f / sqrtf(ss / float(D) + a.eps);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] *= r * (is_q ? wq[k] : wk[k]);
+        }
+        if (TURN != kNone && !is_v) {
+            if (TURN == kInLane) {
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) {
+                    const float u = x[k], v = x[k + 1];
+                    x[k] = u * co[k] - v * si[k];
+                    x[k + 1] = v * co[k] + u * si[k];
+                }
+            } else if (TURN == kAcross) {
+                const bool turned = e0 < a.rotary_dim, second = e0 >= half;
+                const int from = int(lane) + (!turned ? 0 : second ? -int(half / 8) : int(half / 8));
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float o = __shfl_sync(mask, x[k], from, kLanes);
+                    if (turned) x[k] = second ? x[k] * co[k] + o * si[k] : x[k] * co[k] - o * si[k];
+                }
+            } else {
+                float* row = rows[g % (TURN == kAnywhere ? kGroups : 1)];
+                __syncwarp(mask);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) row[e0 + k] = x[k];
+                __syncwarp(mask);
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) {
+                    const uint32_t e = e0 + k;
+                    if (e < a.rotary_dim) {
+                        const bool second = a.interleaved ? e & 1 : e >= half;
+                        const float o = row[a.interleaved ? e ^ 1 : second ? e - half : e + half];
+                        x[k] = second ? x[k] * co[k] + o * si[k] : x[k] * co[k] - o * si[k];
+                    }
+                }
+            }
+        }
         T* dst = is_q ? static_cast<T*>(a.q_out) + t * a.q_out_stride + uint64_t(h) * D
-                      : reinterpret_cast<T*>(kv_row(a.pages, seq, slot, a.pages.layer, is_v, is_v ? j - K : j));
+                      : place ? reinterpret_cast<T*>(place + (h - a.q_heads) * apart) : nullptr;
         if (mine && dst) kv_store8(dst + e0, x);
     }
 }
@@ -106,6 +163,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 // row is overwritten before it was read.
 constexpr uint32_t kCommitThreads = 256;
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_constant__ KvCommit c) {
+    tc::pdl_launch();
+    tc::pdl_wait();
     const uint32_t s = blockIdx.x, per = c.pages.head_dim / 8;
     const uint32_t at = blockIdx.y * kCommitThreads + threadIdx.x;
     if (at >= c.pages.layers * 2 * c.pages.kv_heads * per) return;
@@ -138,9 +197,11 @@ template <class T, class TI>
 cudaError_t append_as(const KvAppend& a, cudaStream_t stream) {
     const uint32_t heads = a.q_heads + 2 * a.pages.kv_heads;
     // a few tokens: a head to a group, over as many blocks as that takes
-    const uint32_t y = a.tok.n_tokens >= 1024 ? 1 : (heads + kGroups - 1) / kGroups;
-    append_kernel<T, TI><<<dim3(a.tok.n_tokens, y), kThreads, 0, stream>>>(a);
-    return cudaGetLastError();
+    const dim3 grid(a.tok.n_tokens, a.tok.n_tokens >= 1024 ? 1 : (heads + kGroups - 1) / kGroups);
+    if (!a.rotary_dim) return launch_pdl(append_kernel<T, TI, kNone>, grid, kThreads, 0, stream, a);
+    if (a.interleaved && a.rotary_dim % 8 == 0) return launch_pdl(append_kernel<T, TI, kInLane>, grid, kThreads, 0, stream, a);
+    if (!a.interleaved && a.rotary_dim % 16 == 0) return launch_pdl(append_kernel<T, TI, kAcross>, grid, kThreads, 0, stream, a);
+    return launch_pdl(append_kernel<T, TI, kAnywhere>, grid, kThreads, 0, stream, a);
 }
 
 }  // namespace
@@ -158,8 +219,7 @@ cudaError_t launch_kv_append(const KvAppend& a, uint32_t dtype, uint32_t in_dtyp
 
 cudaError_t launch_kv_commit(const KvCommit& c, cudaStream_t stream) {
     const uint32_t cols = c.pages.layers * 2 * c.pages.kv_heads * (c.pages.head_dim / 8);
-    commit_kernel<<<dim3(c.n_seqs, (cols + kCommitThreads - 1) / kCommitThreads), kCommitThreads, 0, stream>>>(c);
-    return cudaGetLastError();
+    return launch_pdl(commit_kernel, dim3(c.n_seqs, (cols + kCommitThreads - 1) / kCommitThreads), kCommitThreads, 0, stream, c);
 }
 
 }  // namespace t2i

@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                     }
                     if (masked) {
                         uint32_t see = 0;
-#pragma unroll 4
+#pragma unroll(kLanes ? 4 : C)
                         for (int c = 0; c < C; ++c)
                             see |= uint32_t(kpos >= first[c0 + c] && (key < last[c0 + c] || (word[c0 + c] & bit))) << c;
 #pragma unroll
