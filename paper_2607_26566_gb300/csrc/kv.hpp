@@ -53,6 +53,7 @@ struct KvAppend {
     uint32_t n_positions;
     uint32_t interleaved;
     float eps;
+    uint32_t vectors;  // the launch's own: norm weights and tables may be read in 16 bytes
 };
 
 struct KvAttend {

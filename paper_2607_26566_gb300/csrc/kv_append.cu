@@ -13,7 +13,7 @@ namespace {
 // before it works on the one it has. Bound by memory at many tokens (each byte is
 // read and written once), by the chain of look-ups at few.
 constexpr uint32_t kLanes = 16;
-constexpr uint32_t kThreads = 256;
+constexpr uint32_t kThreads = 64;  // (of 256, 128, 64, 32: prompts of 8.7k tokens 63, 50, 49, 52 us)
 constexpr uint32_t kGroups = kThreads / kLanes;
 
 // How a pair's other element is reached: interleaved pairs lie in one lane; halves
@@ -44,6 +44,17 @@ __device__ __forceinline__ void unpack(const Raw<T>& r, float (&x)[8]) {
     }
 }
 
+// Eight floats, in two vectors where their address allows it.
+__device__ __forceinline__ void eight(const float* p, float (&x)[8], uint32_t vectors) {
+    if (vectors) {
+        const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
+        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = p[i];
+    }
+}
+
 template <class T, class TI, int TURN>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ KvAppend a) {
     __shared__ float rows[TURN == kAnywhere ? kGroups : 1][128];
@@ -54,26 +65,25 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     const bool mine = e0 < D;
     tc::pdl_launch();
     tc::pdl_wait();
-    auto load = [&](uint32_t h) {  // queries, then keys, then values
+    // the token's rows: head h of queries, then keys, then values lies h rows behind these
+    const uint32_t in_row = D * uint32_t(sizeof(TI)), QK = a.q_heads + K;
+    const uint8_t* const q0 = reinterpret_cast<const uint8_t*>(static_cast<const TI*>(a.q) + t * a.q_stride + e0);
+    const uint8_t* const k0 = reinterpret_cast<const uint8_t*>(static_cast<const TI*>(a.k) + t * a.k_stride + e0) - uint64_t(a.q_heads) * in_row;
+    const uint8_t* const v0 = reinterpret_cast<const uint8_t*>(static_cast<const TI*>(a.v) + t * a.v_stride + e0) - uint64_t(QK) * in_row;
+    auto load = [&](uint32_t h) {
         Raw<TI> r{};
         if (!mine) return r;
-        const uint32_t j = h - a.q_heads;
-        const TI* src = h < a.q_heads ? static_cast<const TI*>(a.q) + t * a.q_stride + uint64_t(h) * D
-                        : j < K       ? static_cast<const TI*>(a.k) + t * a.k_stride + uint64_t(j) * D
-                                      : static_cast<const TI*>(a.v) + t * a.v_stride + uint64_t(j - K) * D;
+        const uint8_t* src = (h < a.q_heads ? q0 : h < QK ? k0 : v0) + uint64_t(h) * in_row;
 #pragma unroll
-        for (uint32_t i = 0; i < sizeof(TI) / 2; ++i) r.v[i] = reinterpret_cast<const uint4*>(src + e0)[i];
+        for (uint32_t i = 0; i < sizeof(TI) / 2; ++i) r.v[i] = reinterpret_cast<const uint4*>(src)[i];
         return r;
     };
     uint32_t h = blockIdx.y * kGroups + g;
     Raw<TI> next{};
     if (h < heads) next = load(h);
-    float wq[8], wk[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        wq[i] = mine && a.q_norm ? a.q_norm[e0 + i] : 1.0f;
-        wk[i] = mine && a.k_norm ? a.k_norm[e0 + i] : 1.0f;
-    }
+    float wq[8] = {}, wk[8] = {};
+    if (mine && a.q_norm) eight(a.q_norm + e0, wq, a.vectors);
+    if (mine && a.k_norm) eight(a.k_norm + e0, wk, a.vectors);
 
     const uint32_t seq = kv_owner(a.tok, t);
     const KvSeq s = kv_seq(a.pages, a.tok, seq);
@@ -82,6 +92,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     // the token's first row in the cache (key head 0 of the layer), and from head to head
     uint8_t* const place = kv_row(a.pages, seq, slot, a.pages.layer, 0, 0);
     const uint64_t apart = uint64_t(D * 2) << a.pages.token_shift;
+    uint8_t* const cache0 = place + e0 * 2 - a.q_heads * apart;
+    uint8_t* const out0 = reinterpret_cast<uint8_t*>(static_cast<T*>(a.q_out) + t * a.q_out_stride + e0);
 
     // the pair's cosine and sine for each of the lane's elements; NaN for a position that the tables lack
     float co[8], si[8];
@@ -91,18 +103,29 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
         const bool known = pos >= 0 && pos < int64_t(a.n_positions);
         const float* cs = a.cos_table + uint64_t(known ? pos : 0) * half;
         const float* sn = a.sin_table + uint64_t(known ? pos : 0) * half;
+        if (TURN == kAcross && e0 < a.rotary_dim) {
+            const uint32_t p = e0 < half ? e0 : e0 - half;
+            eight(cs + p, co, a.vectors);
+            eight(sn + p, si, a.vectors);
+        } else {
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) {
-            const uint32_t e = e0 + k;
-            co[k] = 1.0f, si[k] = 0.0f;
-            if (e < a.rotary_dim) {
-                const uint32_t p = TURN == kInLane || a.interleaved ? e / 2 : e < half ? e : e - half;
-                co[k] = known ? cs[p] : __int_as_float(0x7FC00000);
-                si[k] = known ? sn[p] : __int_as_float(0x7FC00000);
+            for (uint32_t k = 0; k < 8; ++k) {
+                const uint32_t e = e0 + k;
+                co[k] = 1.0f, si[k] = 0.0f;
+                if (e < a.rotary_dim) {
+                    const uint32_t p = TURN == kInLane || a.interleaved ? e / 2 : e < half ? e : e - half;
+                    co[k] = cs[p], si[k] = sn[p];
+                }
             }
+        }
+        if (!known && e0 < a.rotary_dim) {
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+                if (e0 + k < a.rotary_dim) co[k] = si[k] = __int_as_float(0x7FC00000);
         }
     }
 
+    const float per_dim = 1.0f / float(D);
     for (; h < heads; h += step) {
         const Raw<TI> raw = next;
         if (h + step < heads) next = load(h + step);
@@ -115,7 +138,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
             for (int k = 0; k < 8; ++k) ss += x[k] * x[k];
 #pragma unroll
             for (int d = 8; d; d >>= 1) ss += __shfl_xor_sync(mask, ss, d, kLanes);
-            const float r = 1.0f / sqrtf(ss / float(D) + a.eps);
+            const float r = rsqrtf(ss * per_dim + a.eps);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] *= r * (is_q ? wq[k] : wk[k]);
         }
@@ -152,9 +175,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
                 }
             }
         }
-        T* dst = is_q ? static_cast<T*>(a.q_out) + t * a.q_out_stride + uint64_t(h) * D
-                      : place ? reinterpret_cast<T*>(place + (h - a.q_heads) * apart) : nullptr;
-        if (mine && dst) kv_store8(dst + e0, x);
+        uint8_t* const dst = is_q ? out0 + uint64_t(h) * (D * 2) : cache0 + uint64_t(h) * apart;
+        if (mine && (is_q || place)) kv_store8(reinterpret_cast<T*>(dst), x);
     }
 }
 
@@ -194,7 +216,11 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_con
 }
 
 template <class T, class TI>
-cudaError_t append_as(const KvAppend& a, cudaStream_t stream) {
+cudaError_t append_as(const KvAppend& args, cudaStream_t stream) {
+    KvAppend a = args;
+    const uint64_t at = reinterpret_cast<uint64_t>(a.cos_table) | reinterpret_cast<uint64_t>(a.sin_table) |
+                        reinterpret_cast<uint64_t>(a.q_norm) | reinterpret_cast<uint64_t>(a.k_norm);
+    a.vectors = at % 16 == 0 && a.rotary_dim % 8 == 0;  // (half a row of the tables: a multiple of four floats)
     const uint32_t heads = a.q_heads + 2 * a.pages.kv_heads;
     // a few tokens: a head to a group, over as many blocks as that takes
     const dim3 grid(a.tok.n_tokens, a.tok.n_tokens >= 1024 ? 1 : (heads + kGroups - 1) / kGroups);
