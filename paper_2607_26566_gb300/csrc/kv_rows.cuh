@@ -108,8 +108,8 @@ __device__ __forceinline__ KvSpan tile_span(const KvAttend& a, const KvSeq& q, i
     return r;
 }
 
-constexpr int kPlanThreads = 1024;
 // Exclusive scan of one number a thread over the block; *total: their sum.
+template <int THREADS>
 __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* sums, int64_t* total) {
     const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     int64_t inc = v;
@@ -122,7 +122,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* sums, int64_t*
     if (lane == 31) sums[warp] = inc;
     __syncthreads();
     int64_t before = 0, all = 0;
-    for (uint32_t i = 0; i < kPlanThreads / 32; ++i) {
+    for (uint32_t i = 0; i < THREADS / 32; ++i) {
         if (i < warp) before += sums[i];
         all += sums[i];
     }
@@ -130,71 +130,77 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* sums, int64_t*
     return before + inc - v;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Rows f) {
-    __shared__ int64_t sums[kPlanThreads / 32];
+// The plan, by a block: `firsts` [n_seqs + 1] and `plan` in global memory, or in
+// shared memory where they fit. Returns the row tiles; *total: key tiles of one head.
+template <int THREADS>
+__device__ __forceinline__ int32_t make_plan(const Rows& f, PlanTile* plan, int32_t* firsts, int64_t* sums, int64_t* total) {
     const KvAttend& a = f.a;
     const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    pdl_launch();
-    pdl_wait();
-    // A few sequences' and tiles' numbers stay in shared memory.
-    __shared__ int32_t few_firsts[kPlanThreads + 1], few_nt[kPlanThreads];
-    const bool in_smem = a.tok.n_seqs <= kPlanThreads;
-    int32_t* const firsts = in_smem ? few_firsts : f.firsts;
     // 1. each sequence's first tile
-    const uint32_t per = (a.tok.n_seqs + kPlanThreads - 1) / kPlanThreads;
+    const uint32_t per = (a.tok.n_seqs + THREADS - 1) / THREADS;
     const uint32_t s0 = tid * per, s1 = min(a.tok.n_seqs, s0 + per);
     int64_t mine = 0, all;
     for (uint32_t s = s0; s < s1; ++s) mine += row_tiles(a, kv_seq(a.pages, a.tok, s));
-    int64_t at = block_scan(mine, sums, &all);
+    int64_t at = block_scan<THREADS>(mine, sums, &all);
     // more than the call's tokens make: starts that make no sense
     const int32_t tiles = all > int64_t(f.most) ? 0 : int32_t(all);
     for (uint32_t s = s0; s < s1; ++s) {
         firsts[s] = int32_t(at);
         if (s + 1 < s1) at += row_tiles(a, kv_seq(a.pages, a.tok, s));
     }
-    if (tid == 0) firsts[a.tok.n_seqs] = tiles, f.head->tiles = tiles;
+    if (tid == 0) firsts[a.tok.n_seqs] = tiles;
     __syncthreads();
     // 2. a warp a tile
     KvTokens owner = a.tok;
     owner.starts = firsts;
-    for (int32_t j = int32_t(warp); j < tiles; j += kPlanThreads / 32) {
+    for (int32_t j = int32_t(warp); j < tiles; j += THREADS / 32) {
         const uint32_t s = kv_owner(owner, uint32_t(j));
         const KvSeq q = kv_seq(a.pages, a.tok, s);
-        const int32_t j0 = firsts[s], m = j - j0, G = int32_t(a.group);
+        const int32_t m = j - firsts[s], G = int32_t(a.group);
         const int32_t end = int32_t(min(int64_t(min(q.n, int32_t(a.tok.max_new))) * G, (int64_t(m) + 1) * kRows));
         const KvSpan sp = tile_span(a, q, m * kRows / G, (end + G - 1) / G, int32_t(lane));
         if (lane == 0) {
-            PlanTile& t = f.plan[j];
+            PlanTile& t = plan[j];
             t.s = int32_t(s), t.m = m, t.span = sp, t.q = q, t.rows = end - m * kRows;
-            const int32_t nt = max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
-            t.nt = nt;
-            if (j < kPlanThreads) few_nt[j] = nt;
+            t.nt = max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
             t.last = j + 1 == firsts[s + 1];
         }
     }
     __syncthreads();
     // 3. key tiles before each tile, and of its sequence
-    const int32_t tper = (tiles + kPlanThreads - 1) / kPlanThreads;
+    const int32_t tper = (tiles + THREADS - 1) / THREADS;
     const int32_t j0 = int32_t(tid) * tper, j1 = min(tiles, j0 + tper);
     mine = 0;
-    for (int32_t j = j0; j < j1; ++j) mine += tper == 1 ? few_nt[j] : f.plan[j].nt;
-    at = block_scan(mine, sums, &all);
-    __shared__ int64_t few_before[kPlanThreads];
+    for (int32_t j = j0; j < j1; ++j) mine += plan[j].nt;
+    at = block_scan<THREADS>(mine, sums, &all);
     for (int32_t j = j0; j < j1; ++j) {
-        f.plan[j].before = at;
-        if (tper == 1) few_before[j] = at;
-        if (j + 1 < j1) at += f.plan[j].nt;
+        plan[j].before = at;
+        at += plan[j].nt;
     }
-    if (tid == 0) f.head->total = all;
     __syncthreads();
     for (int32_t j = j0; j < j1; ++j) {
-        PlanTile& t = f.plan[j];
+        PlanTile& t = plan[j];
         const int32_t a0 = firsts[t.s], a1 = firsts[t.s + 1];
-        const int64_t b0 = tper == 1 ? few_before[a0] : f.plan[a0].before;
-        t.seq_before = b0;
-        t.seq_total = (a1 >= tiles ? all : tper == 1 ? few_before[a1] : f.plan[a1].before) - b0;
+        t.seq_before = plan[a0].before;
+        t.seq_total = (a1 < tiles ? plan[a1].before : all) - t.seq_before;
     }
+    *total = all;
+    return tiles;
 }
+
+constexpr int kPlanThreads = 1024;
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Rows f) {
+    __shared__ int64_t sums[kPlanThreads / 32];
+    pdl_launch();
+    pdl_wait();
+    int64_t total;
+    const int32_t tiles = make_plan<kPlanThreads>(f, f.plan, f.firsts, sums, &total);
+    if (threadIdx.x == 0) f.head->total = total, f.head->tiles = tiles;
+}
+
+// Up to so many row tiles (by their bound) every block makes the plan for itself, in
+// shared memory: it saves a kernel and its way through memory.
+constexpr uint32_t kOwnPlan = 64;
 
 // The run of one block, unit by unit: in a sequence, key head by key head, its row
 // tiles. The loading warp walks it, one unit ahead of its loads, and leaves each
@@ -213,7 +219,7 @@ struct RowWalk {
     int32_t j, h, tile, n;
     PlanTile t;
 };
-__device__ __forceinline__ bool walk_next(const Rows& f, RowWalk& w) {
+__device__ __forceinline__ bool walk_next(const Rows& f, const PlanTile* plan, RowWalk& w) {
     w.at += w.n;
     if (w.at >= w.end) return false;
     w.tile = 0;
@@ -226,7 +232,7 @@ __device__ __forceinline__ bool walk_next(const Rows& f, RowWalk& w) {
         ++w.j;
         w.h = 0;
     }
-    w.t = f.plan[w.j];
+    w.t = plan[w.j];
     w.n = int32_t(min(int64_t(w.t.nt), w.end - w.at));
     return true;
 }
@@ -243,6 +249,9 @@ struct RowShared {
     Unit unit[kUnits];
     uint32_t tmem, dead;
     int32_t start_j, start_h, start_tile;
+    int32_t firsts[kOwnPlan + 1];
+    int64_t sums[kRowThreads / 32];
+    PlanTile plan[kOwnPlan];
 };
 
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
@@ -302,14 +311,24 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     pdl_launch();
     pdl_wait();
 
-    const int64_t K = a.pages.kv_heads, total = f.head->total * K;
+    const bool own = f.most <= kOwnPlan;
+    const PlanTile* const plan = own ? sh.plan : f.plan;
+    int64_t total;
+    int32_t tiles;
+    if (own) {
+        tiles = make_plan<kRowThreads>(f, sh.plan, sh.firsts, sh.sums, &total);
+        __syncthreads();
+    } else {
+        total = f.head->total, tiles = f.head->tiles;
+    }
+    const int64_t K = a.pages.kv_heads;
+    total *= K;
     const int64_t blocks = min(int64_t(gridDim.x), total);
     const bool busy = blockIdx.x < blocks;
     const int64_t run0 = busy ? blockIdx.x * total / blocks : 0, run1 = busy ? (blockIdx.x + 1) * total / blocks : 0;
     if (busy) {
-        const int32_t tiles = f.head->tiles;
         for (int32_t j = int32_t(tid); j < tiles; j += kRowThreads) {
-            const PlanTile& t = f.plan[j];
+            const PlanTile& t = plan[j];
             const int64_t in = run0 - t.seq_before * K;
             if (in < 0 || in >= t.seq_total * K) continue;
             const int64_t r = in % t.seq_total - (t.before - t.seq_before);
@@ -328,7 +347,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             // ---------------------------------------------------------- loads
             RowWalk w;
             w.at = run0, w.end = run1, w.j = sh.start_j, w.h = sh.start_h, w.tile = sh.start_tile;
-            w.t = f.plan[w.j];
+            w.t = plan[w.j];
             w.n = int32_t(min(int64_t(w.t.nt - w.tile), run1 - run0));
             uint32_t u = 0;  // units left in shared memory
             auto publish = [&]() -> bool {
@@ -379,7 +398,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                                          (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
                     }
                     if (i == 0) {  // the next unit, while this one's loads are under way
-                        more = walk_next(f, w);
+                        more = walk_next(f, plan, w);
                         if (more && !publish()) goto loads_done;
                     }
                 }
@@ -757,33 +776,53 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
 // Joins the units that lie in several runs: a block for 32 rows of a run's note, a
 // lane a row.
 template <class T>
-__global__ void __launch_bounds__(1024) rows_join_kernel(const __grid_constant__ Rows f) {
+__global__ void __launch_bounds__(512) rows_join_kernel(const __grid_constant__ Rows f) {
     const KvAttend& a = f.a;
     pdl_launch();
     pdl_wait();
     const Join j = f.join[blockIdx.x];
     if (!j.valid) return;
-    const uint32_t warp = threadIdx.x / 32, D = a.pages.head_dim;  // warp: which four dimensions
+    const uint32_t warp = threadIdx.x / 32, D = a.pages.head_dim;  // warp: which four dimensions, and four more 64 on
     const int32_t r = int32_t(blockIdx.y * 32 + threadIdx.x % 32);
     if (r >= j.rows || warp * 4 >= D) return;
-    auto part = [&](int32_t b) { return f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * kRowPart; };
+    const bool more = warp * 4 + 64 < D;
     float top = -INFINITY, l = 0.0f;
-#pragma unroll 8
-    for (int32_t b = j.b0; b <= j.b1; ++b) top = fmaxf(top, __ldcg(part(b) + kRows * 128 + r));
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int32_t b = j.b0; b <= j.b1; ++b) {
-        const float* p = part(b);
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + warp * kRows + r);
-        const float m = __ldcg(p + kRows * 128 + r), x = m == top ? 1.0f : exp2_approx(m - top);
-        l += x * __ldcg(p + kRows * 128 + kRows + r);
-        o.x += x * v.x, o.y += x * v.y, o.z += x * v.z, o.w += x * v.w;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f), o1 = o;
+    auto add = [](float4& s, float x, const float4& v) { s.x += x * v.x, s.y += x * v.y, s.z += x * v.z, s.w += x * v.w; };
+    auto by = [](float4& s, float x) { s.x *= x, s.y *= x, s.z *= x, s.w *= x; };
+    for (int32_t b0 = j.b0; b0 <= j.b1; b0 += 4) {  // four parts' loads at a time
+        float m[4], s[4], now = top;
+        float4 v[4], v1[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int32_t b = b0 + k;
+            m[k] = -INFINITY, s[k] = 0.0f;
+            v[k] = v1[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (b > j.b1) continue;
+            const float* p = f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * kRowPart;
+            m[k] = __ldcg(p + kRows * 128 + r), s[k] = __ldcg(p + kRows * 128 + kRows + r);
+            v[k] = __ldcg(reinterpret_cast<const float4*>(p) + warp * kRows + r);
+            if (more) v1[k] = __ldcg(reinterpret_cast<const float4*>(p) + (warp + 16) * kRows + r);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) now = fmaxf(now, m[k]);
+        const float was = top == now ? 1.0f : exp2_approx(top - now);
+        l *= was, by(o, was), by(o1, was);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (b0 + k > j.b1) continue;
+            const float x = m[k] == now ? 1.0f : exp2_approx(m[k] - now);
+            l += x * s[k], add(o, x, v[k]), add(o1, x, v1[k]);
+        }
+        top = now;
     }
     const uint32_t row = uint32_t(j.m) * kRows + uint32_t(r), head = uint32_t(j.h) * a.group + row % a.group;
     const uint64_t orow = uint64_t(j.first) + row / a.group;
-    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    const float rl = l == 0.0f ? 0.0f : 1.0f / l;
     T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D + warp * 4;
-    *reinterpret_cast<uint2*>(out) = make_uint2(Kv16<T>::from2(o.x * by, o.y * by), Kv16<T>::from2(o.z * by, o.w * by));
+    by(o, rl), by(o1, rl);
+    *reinterpret_cast<uint2*>(out) = make_uint2(Kv16<T>::from2(o.x, o.y), Kv16<T>::from2(o.z, o.w));
+    if (more) *reinterpret_cast<uint2*>(out + 64) = make_uint2(Kv16<T>::from2(o1.x, o1.y), Kv16<T>::from2(o1.z, o1.w));
     if (a.lse && warp == 0) a.lse[orow * a.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
 }
 
@@ -802,9 +841,9 @@ cudaError_t launch_rows_as(const Rows& f, const CUtensorMap& map, uint32_t sms, 
         if (e != cudaSuccess) return e;
         if (dev < 64) ready |= uint64_t(1) << dev;
     }
-    if ((e = launch_pdl(plan_kernel, dim3(1), kPlanThreads, 0, stream, f)) != cudaSuccess) return e;
+    if (f.most > kOwnPlan && (e = launch_pdl(plan_kernel, dim3(1), kPlanThreads, 0, stream, f)) != cudaSuccess) return e;
     if ((e = launch_pdl(rows_kernel<T, MOD>, dim3(sms), kRowThreads, kRowSmem, stream, f, map)) != cudaSuccess) return e;
-    return launch_pdl(rows_join_kernel<T>, dim3(sms, kRows / 32), 1024, 0, stream, f);
+    return launch_pdl(rows_join_kernel<T>, dim3(sms, kRows / 32), 512, 0, stream, f);
 }
 
 template <class T>
