@@ -364,39 +364,44 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
         const uint32_t lanes = tmem + (warp << 21);  // this warp's 32 lanes
         const float k2 = a.scale * kLog2e;
         const float cap_in = MOD && a.softcap != 0.0f ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
-        if (tid == 0) {
-            // this run's note of a unit that began in the run before it
-            const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.nt) * blocks - 1) / total;
-            const bool here = w.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
-            f.join[blockIdx.x] = {w.q.first, w.rb * N, w.rows, int32_t(w.h), int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
-        }
         uint32_t n = 0;
         do {
             const int32_t ctx = w.q.len - w.q.n;
-            // the unit's queries: to shared memory, 64 dimensions at a time, 128-byte swizzle
-            for (uint32_t u = tid; u < N * NS * 8; u += kSoftThreads) {
-                const uint32_t c = u / (NS * 8), x = u % (NS * 8);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (int32_t(c) < w.rows && x * 8 < D) {
-                    const uint32_t t = (w.rb * N + c) / a.group, g = (w.rb * N + c) % a.group;
-                    v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(w.q.first + t) * a.q_stride +
-                                                        uint64_t(w.h * a.group + g) * D + x * 8);
-                }
-                *reinterpret_cast<uint4*>(mem + (qs - base) + (x / 8) * (N * 128) + c * 128 + ((x % 8) ^ (c % 8)) * 16) = v;
+            // the unit's queries: to shared memory, 64 dimensions at a time, 128-byte swizzle; kRowThreads threads
+            // a row, whose loads are all under way before the first is stored
+            constexpr uint32_t kRowThreads = kSoftThreads / N, kVecs = NS * 8 / kRowThreads;
+            const uint32_t c = tid / kRowThreads, x0 = tid % kRowThreads * kVecs;
+            const bool real = int32_t(c) < w.rows;
+            const uint32_t ct = (w.rb * N + c) / a.group, ch = w.h * a.group + (w.rb * N + c) % a.group;  // token and head
+            uint4 qv[kVecs];
+            {
+                const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(w.q.first + ct) * a.q_stride +
+                                                                  uint64_t(ch) * D) + x0;
+#pragma unroll
+                for (uint32_t x = 0; x < kVecs; ++x) qv[x] = real && (x0 + x) * 8 < D ? src[x] : make_uint4(0, 0, 0, 0);
             }
-            if (tid < N) {
-                top[tid] = -INFINITY;
+            if (tid % kRowThreads == 0) {
                 KvQuery q{0, INT32_MAX, 0, 0};
                 float sl = 0.0f;
-                if (int32_t(tid) < w.rows) {
-                    q = kv_query(a, w.q, (w.rb * N + tid) / a.group);
-                    if (MOD && a.slopes) sl = a.slopes[w.h * a.group + (w.rb * N + tid) % a.group] * kLog2e;
+                if (real) {
+                    q = kv_query(a, w.q, int32_t(ct));
+                    if (MOD && a.slopes) sl = a.slopes[ch] * kLog2e;
                 }
-                first[tid] = q.first, last[tid] = q.last, pos[tid] = q.pos, word[tid] = q.word;
-                slope[tid] = sl;
+                top[c] = -INFINITY;
+                first[c] = q.first, last[c] = q.last, pos[c] = q.pos, word[c] = q.word;
+                slope[c] = sl;
             }
+#pragma unroll
+            for (uint32_t x = 0; x < kVecs; ++x)
+                *reinterpret_cast<uint4*>(mem + (qs - base) + ((x0 + x) / 8) * (N * 128) + c * 128 + (((x0 + x) % 8) ^ (c % 8)) * 16) = qv[x];
             fence_async_smem();
             mbar_arrive(bar(sh.q_full));
+            if (tid == 0 && w.at == run0) {
+                // this run's note of a unit that began in the run before it
+                const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.nt) * blocks - 1) / total;
+                const bool here = w.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
+                f.join[blockIdx.x] = {w.q.first, w.rb * N, w.rows, int32_t(w.h), int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
+            }
             bar_sync<1, kSoftThreads>();
 
             // Sums of weights: up to 32 columns, each thread its key's; 64, of the warp's keys: lane i has columns
@@ -584,17 +589,17 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             const bool whole = w.n == w.nt;
             const uint32_t d = tid;
             float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * Sh::kPart;
-            uint32_t t = w.rb * N / a.group, g = w.rb * N % a.group;  // the column's token and head
+            if (whole) {
+                uint32_t t = w.rb * N / a.group, g = w.rb * N % a.group;  // the column's token and head
 #pragma unroll 1
-            for (int c0 = 0; c0 < w.rows; c0 += 16) {
-                float o[16];
-                tmem_ld16(lanes + 2 * N + c0, o);
-                wait_ld(o);
+                for (int c0 = 0; c0 < w.rows; c0 += 16) {
+                    float o[16];
+                    tmem_ld16(lanes + 2 * N + c0, o);
+                    wait_ld(o);
 #pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const int col = c0 + c;
-                    if (col < w.rows) {
-                        if (whole) {
+                    for (int c = 0; c < 16; ++c) {
+                        const int col = c0 + c;
+                        if (col < w.rows) {
                             const float l = red[0][col] + red[1][col] + red[2][col] + red[3][col];
                             const uint64_t row = uint64_t(w.q.first + t);
                             const float r = l == 0.0f ? 0.0f : 1.0f / l;
@@ -604,9 +609,19 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                             if (a.lse && d == 0)
                                 a.lse[row * a.q_heads + w.h * a.group + g] = l == 0.0f ? -INFINITY : (top[col] + log2f(l)) * kLn2;
                             if (++g == a.group) g = 0, ++t;
-                        } else if (d < 64 * NS) {  // a part of the unit: to the workspace
-                            __stcg(part + col * (64 * NS) + d, o[c]);
                         }
+                    }
+                }
+            } else {  // a part of the unit: to the workspace
+#pragma unroll 1
+                for (int c0 = 0; c0 < w.rows; c0 += 16) {
+                    float o[16];
+                    tmem_ld16(lanes + 2 * N + c0, o);
+                    wait_ld(o);
+                    if (d < 64 * NS) {
+                        float* at = part + c0 * (64 * NS) + d;
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) __stcg(at + c * (64 * NS), o[c]);
                     }
                 }
             }
