@@ -494,8 +494,8 @@ typedef struct t2i_kv_attend_desc {
     float scale;
     float softcap;          /* 0: none                                       */
     uint32_t reserved;      /* must be 0                                     */
-    void* workspace;        /* device, 256-byte aligned, zero before its first
-                               use; calls of one stream at a time share one  */
+    void* workspace;        /* device, 256-byte aligned, holding anything; calls
+                               on one stream share one, others need their own */
     uint64_t workspace_bytes;
 } t2i_kv_attend_desc;
 

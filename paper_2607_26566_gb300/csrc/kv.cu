@@ -270,7 +270,8 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     a.q_heads = d.q_heads;
     a.group = d.q_heads / K;
     a.window = d.window;
-    a.max_len = d.max_len;
+    // (what a row of the table holds, where the caller does not say)
+    a.max_len = d.max_len ? std::min(d.max_len, d.batch.table_pages << kv->token_shift) : d.batch.table_pages << kv->token_shift;
     a.scale = d.scale;
     a.softcap = d.softcap;
     const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms};

@@ -81,6 +81,13 @@ __device__ __forceinline__ float capped(float s, float cap_in, float cap) {
     return cap - 2.0f * cap * tc::rcp_approx(e + 1.0f);
 }
 
+// Blocks of an attention launch: no more than there are key tiles, going by max_len
+// (a block without any still takes its place on an SM and has to be waited for).
+inline uint32_t attend_blocks(const KvAttend& a, uint32_t most, uint64_t units) {
+    const uint64_t tiles = units * a.pages.kv_heads * (uint64_t(a.max_len) / kTileKeys + 1);
+    return uint32_t(tiles < most ? tiles : most);
+}
+
 // A launch whose set-up overlaps the kernel before it on the stream.
 template <class... Args>
 inline cudaError_t launch_pdl(void (*kernel)(Args...), dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t stream,

@@ -706,7 +706,8 @@ cudaError_t launch_as(const Few& f, const CUtensorMap& map, uint32_t sms, cudaSt
         if (e != cudaSuccess) return e;
         if (dev < 64) ready |= uint64_t(1) << dev;
     }
-    const uint32_t blocks = sms * Shape<N, NS>::kBlocks;
+    const uint64_t units = uint64_t(f.a.tok.n_seqs) * ((uint64_t(f.a.tok.max_new) * f.a.group + N - 1) / N);
+    const uint32_t blocks = attend_blocks(f.a, sms * Shape<N, NS>::kBlocks, units);
     e = launch_pdl(few_kernel<T, N, NS, MOD>, dim3(blocks), kThreads, bytes, stream, f, map);
     if (e != cudaSuccess) return e;
     return launch_pdl(join_kernel<T, N, NS>, dim3(blocks, (N + 7) / 8), 256, 0, stream, f);

@@ -842,8 +842,9 @@ cudaError_t launch_rows_as(const Rows& f, const CUtensorMap& map, uint32_t sms, 
         if (dev < 64) ready |= uint64_t(1) << dev;
     }
     if (f.most > kOwnPlan && (e = launch_pdl(plan_kernel, dim3(1), kPlanThreads, 0, stream, f)) != cudaSuccess) return e;
-    if ((e = launch_pdl(rows_kernel<T, MOD>, dim3(sms), kRowThreads, kRowSmem, stream, f, map)) != cudaSuccess) return e;
-    return launch_pdl(rows_join_kernel<T>, dim3(sms, kRows / 32), 512, 0, stream, f);
+    const uint32_t blocks = attend_blocks(f.a, sms, f.most);
+    if ((e = launch_pdl(rows_kernel<T, MOD>, dim3(blocks), kRowThreads, kRowSmem, stream, f, map)) != cudaSuccess) return e;
+    return launch_pdl(rows_join_kernel<T>, dim3(blocks, kRows / 32), 512, 0, stream, f);
 }
 
 template <class T>

@@ -29,7 +29,7 @@ struct Cache {
     at::ScalarType dtype;
     int64_t kv_heads, head_dim, max_seqs, max_pages;
     PyObject* table;                              // the cache's own page table
-    PyObject* grow;                               // (stream, bytes) -> a zeroed workspace tensor
+    PyObject* grow;                               // (stream, bytes) -> a workspace tensor
     std::vector<std::pair<void*, PyObject*>> work;  // stream -> workspace
 };
 

@@ -239,9 +239,9 @@ class KVCache:
 
 
 def _workspace_on(device):
-    """What the calls' workspaces come from: one a stream, zeroed on it."""
+    """Where the calls' workspaces come from: one a stream."""
     def grow(stream, nbytes):
         s = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
         with torch.cuda.stream(s):
-            return torch.zeros(nbytes, dtype=torch.uint8, device=device)
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
     return grow
