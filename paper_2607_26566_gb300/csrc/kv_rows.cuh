@@ -863,8 +863,9 @@ cudaError_t launch_rows(const KvAttend& a, const KvLaunch& l, cudaStream_t strea
     p += up256(uint64_t(f.most) * sizeof(PlanTile));
     f.part = reinterpret_cast<float*>(p);
     f.fault = l.fault;
-    return a.softcap != 0.0f || a.slopes ? launch_rows_as<T, true>(f, *l.map, l.sms, stream)
-                                         : launch_rows_as<T, false>(f, *l.map, l.sms, stream);
+    // (MOD scales before it masks: a scale of 0 would turn a masked -infinity into NaN)
+    return a.softcap != 0.0f || a.slopes || a.scale == 0.0f ? launch_rows_as<T, true>(f, *l.map, l.sms, stream)
+                                                            : launch_rows_as<T, false>(f, *l.map, l.sms, stream);
 }
 
 }  // namespace

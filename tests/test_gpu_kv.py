@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2607_26566_gb300 import put_descs
+from paper_2607_26566_gb300 import KVCache, Store, put_descs
 from kv_plain import (DEV, TINY, UNIT, attend64, make_cache, near_attend, read_rows, rows_of, turn64, words, write_rows)
 
 pytestmark = pytest.mark.gpu
@@ -276,6 +276,98 @@ def test_tree_words_that_see_nothing():
     want = attend64(q, *kvs[0], 0.125, tree=tree)
     near_attend(out, lse, *want, BF)
     assert (out[1] == 0).all() and (lse[1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("heads,kv", [(4, 2), (2, 2)])
+def test_many_short_sequences_beside_a_long_one(heads, kv):
+    new = [300] + [2, 0, 1] * 25 + [129]
+    ctx = [40] + [int(x) for x in np.random.default_rng(1).integers(0, 400, 75)] + [1]
+    c, lens, kvs, q = case(BF, heads, kv, 64, new, ctx)
+    check(c, lens, new, kvs, q)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [40, 3], [200, 30]])
+@pytest.mark.parametrize("max_len", [1, 700, 1 << 30])
+def test_a_wrong_max_len_changes_no_result(new, max_len):
+    c, lens, kvs, q = case(HF, 4, 2, 64, new, [600, 90])
+    check(c, lens, new, kvs, q, max_len=max_len)
+
+
+def test_a_negative_scale_and_none():
+    for new in ([1], [200]):
+        c, lens, kvs, q = case(BF, 2, 1, 64, new, [300])
+        check(c, lens, new, kvs, q, scale=-0.3)
+        check(c, lens, new, kvs, q, scale=0.0)
+        check(c, lens, new, kvs, q, scale=-0.2, softcap=3.0)
+
+
+def test_starts_that_make_no_sense_touch_nothing():
+    c, lens, kvs, q = case(BF, 2, 1, 64, [100, 100], [10, 10])
+    out = torch.full((200, 2, 64), 7.0, dtype=BF, device=DEV)
+    guard = torch.full((64,), 3.0, device=DEV)
+    before = c.store.pool.clone()
+    for starts in ([0, 200, 0], [500, 600, 700], [-50, -20, -10], [0, 1 << 30, 5]):
+        c.attend(q.to(DEV), ints([5, 5]), out=out, starts=ints(starts), max_new=100)      # fewer slots than new tokens
+        c.append(q[:, :1].contiguous().to(DEV), q[:, :1].contiguous().to(DEV), ints([5, 5]), starts=ints(starts), max_new=100)
+    many = ints([0, 200] * 40)
+    c2 = make_cache(1, 64, BF, [200] * 79, spare=0)
+    c2.attend(q.to(DEV), ints([200] * 79), out=torch.empty_like(out), starts=many, max_new=200)  # more tokens than there are
+    torch.cuda.synchronize()
+    assert (out == 7).all() and (guard == 3).all() and torch.equal(c.store.pool, before)
+
+
+def test_pages_beyond_4_gib():
+    """A cache at the end of a 6 GiB pool: offsets pass 32 bits."""
+    page = 1 << 20
+    st = Store(torch.empty(6 << 30, dtype=torch.uint8, device=DEV), page)
+    s, (filler,) = st.put_batch(put_descs([0], nbytes=[(6 << 30) - 4 * page]))
+    st.check(s)
+    c = KVCache(st, 2, 64, BF, max_seqs=2, max_tokens=3000)
+    c.reserve([2500, 1200])
+    assert min(c.pages(0) + c.pages(1)) >= 6 * 1024 - 4
+    g = gen(3)
+    q, k, v = (torch.randn(3700, h, 64, generator=g).to(BF) for h in (4, 2, 2))
+    new = [2500, 1200]
+    c.append(k.to(DEV), v.to(DEV), ints(new), starts=starts_of(new), max_new=2500)
+    for s, w in ((0, slice(0, 2500)), (1, slice(2500, 3700))):
+        assert torch.equal(read_rows(c, s, 0, new[s])[0].cpu(), k[w])
+    pick = [2499, 3699]
+    out = c.attend(q[pick].to(DEV), ints(new))
+    near_attend(out[:1], None, *attend64(q[2499:2500], k[:2500], v[:2500], 0.125), BF)
+    near_attend(out[1:], None, *attend64(q[3699:], k[2500:], v[2500:], 0.125), BF)
+    whole = c.attend(q.to(DEV), ints(new), starts=starts_of(new), max_new=2500)
+    near_attend(whole[2500:2600], None, *[x[:100] for x in attend64(q[2500:], k[2500:], v[2500:], 0.125)], BF)
+
+
+def test_two_streams_and_a_graph():
+    """Calls on two streams side by side have workspaces of their own; a graph of
+    calls gives what the calls give."""
+    c, lens, kvs, q = case(BF, 8, 2, 128, [1, 1, 1], [3000, 50, 1500])
+    c2, lens2, kvs2, q2 = case(HF, 4, 1, 64, [150, 9], [700, 2000], seed=1)
+    args, args2 = (q.to(DEV), ints(lens)), (q2.to(DEV), ints(lens2))
+    how2 = dict(starts=starts_of([150, 9]), max_new=150)
+    want, want2 = c.attend(*args), c2.attend(*args2, **how2)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got, got2 = [], []
+    for _ in range(20):
+        with torch.cuda.stream(a):
+            got.append(c.attend(*args))
+        with torch.cuda.stream(b):
+            got.append(c.attend(*args))
+            got2.append(c2.attend(*args2, **how2))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in got) and all(torch.equal(x, want2) for x in got2)
+    out, out2 = torch.zeros_like(want), torch.zeros_like(want2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attend(*args, out=out)
+        c2.attend(*args2, out=out2, **how2)
+    for _ in range(3):
+        out.zero_(), out2.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(out2, want2)
 
 
 @pytest.mark.parametrize("T", [8, 16, 128, 512])
