@@ -58,13 +58,20 @@ struct PlanTile {
     int32_t rows;       // of the tile
     int32_t nt;         // key tiles
     int32_t last;       // the sequence's last row tile
-    int64_t before;     // key tiles of the tiles before it
+    int64_t before;     // cost of the tiles before it: key tiles, and Rows::cost for each
     int64_t seq_before, seq_total;  // ... of the sequences before its own; of its own
 };
 struct PlanHead {
     int64_t total;
     int32_t tiles;
 };
+
+// What a unit costs beside its key tiles (its queries' way to shared memory, the first scores without a product
+// beside them, its output), in key tiles: it lies before its tiles when runs are cut. Measured with 0, 1, 2, 3, 4
+// and 5: a prompt of 8190 tokens with 32 heads of 128 527, 490, 454, 424, 399, 403 us; 24 drafts of 60 tokens over
+// contexts up to 8k 132, 127, 124, 120, 118, 118. Scores with a bias or a cap make tiles dearer, so that a unit
+// costs fewer of them: chunks of 600 tokens with spans and a bias 49, 47, 47, 51, 54, 57.
+constexpr int32_t kUnitCost = 4, kUnitCostMod = 2;
 
 // A unit in several runs, noted at the run that holds its second part: the runs
 // b0 to b1 hold it, the first as that block's part 0 or 1, the others as part 0.
@@ -79,6 +86,7 @@ struct Rows {
     int32_t* firsts;   // [n_seqs + 1]: each sequence's first tile
     PlanTile* plan;
     uint32_t most;     // entries of plan
+    int32_t cost;      // of a unit beside its key tiles, in key tiles: kUnitCost or kUnitCostMod
     Join* join;        // [blocks]
     float* part;       // [2 * blocks][kRowPart]
     uint32_t* fault;
@@ -131,7 +139,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* sums, int64_t*
 }
 
 // The plan, by a block: `firsts` [n_seqs + 1] and `plan` in global memory, or in
-// shared memory where they fit. Returns the row tiles; *total: key tiles of one head.
+// shared memory where they fit. Returns the row tiles; *total: the cost of one head's.
 template <int THREADS>
 __device__ __forceinline__ int32_t make_plan(const Rows& f, PlanTile* plan, int32_t* firsts, int64_t* sums, int64_t* total) {
     const KvAttend& a = f.a;
@@ -167,15 +175,15 @@ __device__ __forceinline__ int32_t make_plan(const Rows& f, PlanTile* plan, int3
         }
     }
     __syncthreads();
-    // 3. key tiles before each tile, and of its sequence
+    // 3. the cost before each tile, and of its sequence
     const int32_t tper = (tiles + THREADS - 1) / THREADS;
     const int32_t j0 = int32_t(tid) * tper, j1 = min(tiles, j0 + tper);
     mine = 0;
-    for (int32_t j = j0; j < j1; ++j) mine += plan[j].nt;
+    for (int32_t j = j0; j < j1; ++j) mine += plan[j].nt + f.cost;
     at = block_scan<THREADS>(mine, sums, &all);
     for (int32_t j = j0; j < j1; ++j) {
         plan[j].before = at;
-        at += plan[j].nt;
+        at += plan[j].nt + f.cost;
     }
     __syncthreads();
     for (int32_t j = j0; j < j1; ++j) {
@@ -215,14 +223,22 @@ struct Unit {
     int32_t draft[64];    // positions of the drafted tokens, if there is a tree
 };
 struct RowWalk {
-    int64_t at, end;
+    int64_t at, end;  // the segment's place among all tiles and units' costs, and the run's end
+    int64_t unit;     // the place of the unit's first tile
     int32_t j, h, tile, n;
     PlanTile t;
 };
+// The run's part of the unit that begins (with its cost) at place `start`.
+__device__ __forceinline__ void walk_segment(const Rows& f, RowWalk& w, int64_t start) {
+    w.unit = start + f.cost;
+    if (w.at < w.unit) w.at = w.unit;
+    w.tile = int32_t(w.at - w.unit);
+    w.n = int32_t(min(w.unit + w.t.nt, w.end) - w.at);
+}
 __device__ __forceinline__ bool walk_next(const Rows& f, const PlanTile* plan, RowWalk& w) {
-    w.at += w.n;
-    if (w.at >= w.end) return false;
-    w.tile = 0;
+    const int64_t start = w.unit + w.t.nt;
+    w.at = start;
+    if (start + f.cost >= w.end) return false;  // (nothing of the next unit but its cost)
     if (!w.t.last) {
         ++w.j;
     } else if (w.h + 1 < int32_t(f.a.pages.kv_heads)) {
@@ -233,7 +249,7 @@ __device__ __forceinline__ bool walk_next(const Rows& f, const PlanTile* plan, R
         w.h = 0;
     }
     w.t = plan[w.j];
-    w.n = int32_t(min(int64_t(w.t.nt), w.end - w.at));
+    walk_segment(f, w, start);
     return true;
 }
 __device__ __forceinline__ int32_t tile_slot(const KvSpan& s, int32_t i) { return (s.lo / kTileKeys + i) * kTileKeys; }
@@ -248,7 +264,7 @@ struct RowShared {
     uint64_t unit_full[kUnits], unit_empty[kUnits];
     Unit unit[kUnits];
     uint32_t tmem, dead;
-    int32_t start_j, start_h, start_tile;
+    int32_t start_j, start_h, start_at;
     int32_t firsts[kOwnPlan + 1];
     int64_t sums[kRowThreads / 32];
     PlanTile plan[kOwnPlan];
@@ -332,8 +348,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             const int64_t in = run0 - t.seq_before * K;
             if (in < 0 || in >= t.seq_total * K) continue;
             const int64_t r = in % t.seq_total - (t.before - t.seq_before);
-            if (r < 0 || r >= t.nt) continue;
-            sh.start_j = j, sh.start_h = int32_t(in / t.seq_total), sh.start_tile = int32_t(r);
+            if (r < 0 || r >= t.nt + f.cost) continue;
+            sh.start_j = j, sh.start_h = int32_t(in / t.seq_total), sh.start_at = int32_t(r);
         }
     }
     fence_before();
@@ -346,16 +362,18 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
         if (warp == 8) {
             // ---------------------------------------------------------- loads
             RowWalk w;
-            w.at = run0, w.end = run1, w.j = sh.start_j, w.h = sh.start_h, w.tile = sh.start_tile;
+            w.at = run0, w.end = run1, w.j = sh.start_j, w.h = sh.start_h;
             w.t = plan[w.j];
-            w.n = int32_t(min(int64_t(w.t.nt - w.tile), run1 - run0));
+            walk_segment(f, w, run0 - sh.start_at);
+            if (w.n < 0) w.n = 0;  // nothing but a unit's cost: a unit without tiles, and without another
+            const bool none = w.n == 0;
             uint32_t u = 0;  // units left in shared memory
             auto publish = [&]() -> bool {
                 if (!mbar_wait(bar(sh.unit_empty[u % kUnits]), (u / kUnits & 1) ^ 1, dead)) return false;
                 Unit& o = sh.unit[u % kUnits];
                 if (lane == 0) {
                     o.span = w.t.span, o.q = w.t.q, o.s = w.t.s, o.m = w.t.m, o.h = w.h, o.rows = w.t.rows;
-                    o.tile = w.tile, o.n = w.n, o.nt = w.t.nt, o.at = w.at, o.more = w.at + w.n < w.end;
+                    o.tile = w.tile, o.n = w.n, o.nt = w.t.nt, o.at = w.at, o.more = !none && w.unit + w.t.nt + f.cost < w.end;
                 }
                 if (a.tree) {
                     const int32_t ctx = w.t.q.len - w.t.q.n;
@@ -373,7 +391,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             const uint32_t mask = (1u << shift) - 1;
             const int halves = D > 64 ? 2 : 1;
             uint32_t n = 0;
-            bool more = true;
+            bool more = !none;
             while (more) {
                 const int32_t row_k = int32_t((a.pages.layer * 2 * a.pages.kv_heads + w.h) << shift);
                 const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
@@ -473,11 +491,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             auto tile = [&](uint32_t odd) {
                 const bool same = --left > 0;
                 kv ^= odd;
-                if (same) mbar_wait(bar(sh.full[2 - 2 * odd]), kv, dead);
                 pv(odd, 0, !same);
-                if (same) qk(odd ^ 1, 0);
+                if (!rare(!same)) {
+                    mbar_wait(bar(sh.full[2 - 2 * odd]), kv, dead);
+                    qk(odd ^ 1, 0);
+                }
                 if (two) pv(odd, 1, !same);
-                if (!same) {
+                if (rare(!same)) {
                     if (!follows || *dead) return false;
                     unit();
                     mbar_wait(bar(sh.full[2 - 2 * odd]), kv, dead);
@@ -489,12 +509,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 return ok;
             };
             unit();
-            mbar_wait(bar(sh.full[0]), 0, dead);
-            fence_after();
-            qk(0, 0);
-            if (two) qk(0, 1);
-            mbar_wait(bar(sh.full[1]), 0, dead);
-            for (uint32_t odd = 0; tile(odd); odd ^= 1) {
+            if (left) {
+                mbar_wait(bar(sh.full[0]), 0, dead);
+                fence_after();
+                qk(0, 0);
+                if (two) qk(0, 1);
+                mbar_wait(bar(sh.full[1]), 0, dead);
+                for (uint32_t odd = 0; tile(odd); odd ^= 1) {
+                }
             }
             if (*dead) {  // the products in flight end before the tensor memory is freed
                 const uint64_t t0 = now_ns();
@@ -516,7 +538,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
         const float kk = cap ? 1.0f : k2;  // what is left to scale after the cap
         bool gone = false;  // a wait ran out: what lies in shared memory is not to be gone by
         auto unit = [&](uint32_t u) -> const Unit& {
-            if (!mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead)) gone = true;
+            const bool got = mbar_wait(bar(sh.unit_full[u % kUnits]), u / kUnits & 1, dead);
+            if (!__all_sync(0xFFFFFFFFu, got)) gone = true;
             return sh.unit[u % kUnits];
         };
         auto done_with = [&](uint32_t u) {
@@ -551,13 +574,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 // this run's note of a unit that began in the run before it
                 const int64_t u0 = o.at - o.tile;
                 const int64_t b0 = ((u0 + 1) * blocks - 1) / total, b1 = ((u0 + o.nt) * blocks - 1) / total;
-                const bool here = o.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
+                const bool here = o.n > 0 && o.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
                 f.join[blockIdx.x] = {o.q.first, o.m, o.rows, o.h, int32_t(b0), int32_t(b1), b0 * total / blocks != u0, here};
             }
             load_q(o);
         }
         uint32_t n = 0, on = 0;  // tiles and units of this stage
-        bool more = true;
+        bool more = unit(0).n > 0;
+        if (!more) done_with(0);
         for (uint32_t u = 0; more; ++u) {
             const Unit& o = unit(u);
             more = o.more && !gone;
@@ -864,8 +888,9 @@ cudaError_t launch_rows(const KvAttend& a, const KvLaunch& l, cudaStream_t strea
     f.part = reinterpret_cast<float*>(p);
     f.fault = l.fault;
     // (MOD scales before it masks: a scale of 0 would turn a masked -infinity into NaN)
-    return a.softcap != 0.0f || a.slopes || a.scale == 0.0f ? launch_rows_as<T, true>(f, *l.map, l.sms, stream)
-                                                            : launch_rows_as<T, false>(f, *l.map, l.sms, stream);
+    const bool mod = a.softcap != 0.0f || a.slopes || a.scale == 0.0f;
+    f.cost = mod ? kUnitCostMod : kUnitCost;
+    return mod ? launch_rows_as<T, true>(f, *l.map, l.sms, stream) : launch_rows_as<T, false>(f, *l.map, l.sms, stream);
 }
 
 }  // namespace
