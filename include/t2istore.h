@@ -508,8 +508,11 @@ typedef struct t2i_kv_attend_desc {
  * tokens and the new ones of its word, and a new token's position is the
  * slot of the first one + the number of its ancestors (itself not counted).
  * out = the softmax's mean of the values, lse = log(sum(exp(s))). A token
- * that sees nothing has out 0 and lse -infinity. Keys and values that no
- * token of a call's sequence sees may hold anything.                        */
+ * that sees nothing has out 0 and lse -infinity. Keys may hold anything
+ * where no token sees them. So may values before the first and behind the
+ * last slot that any of the sequence's new tokens sees; between these a
+ * value that is not finite may reach outputs of tokens that do not see it
+ * (its weight there is 0, and 0 times it is not 0).                         */
 t2i_status t2i_kv_attend(t2i_kv* kv, const t2i_kv_attend_desc* desc, void* cuda_stream);
 
 /* Workspace bytes that t2i_kv_attend needs for such a batch at most.         */

@@ -96,8 +96,11 @@ struct KvLaunch {
     uint32_t* fault;  // host memory that the device writes: not 0 after a wait that ran out
     uint32_t sms;
 };
-// up to this many queries to a key head (new tokens of a sequence x heads of a group)
-constexpr uint32_t kFewRows = 128;
+// Up to this many queries to a key head (new tokens of a sequence x heads of a group) kv_few.cuh, above it
+// kv_rows.cuh. Queries, and us of the one / the other, for a sequence of 1.5k slots, 24 of 8k (heads of 128) and 3 of
+// 3k (heads of 64): 32: 15.6 / 16.9, 138 / 141, 19.9 / 18.5; 36 (with 64 columns) 22.5 / 17.1, 201 / 148, 26 / 19;
+// 128: 24 / 19, 389 / 148, 35 / 20.
+constexpr uint32_t kFewRows = 32;
 cudaError_t launch_kv_few_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 cudaError_t launch_kv_few_f16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 uint64_t kv_few_workspace(uint32_t sms);

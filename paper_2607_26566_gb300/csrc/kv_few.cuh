@@ -1,5 +1,5 @@
-// Attention of few new tokens a sequence (a decoding step, a drafted tree, a short
-// chunk): up to 128 queries to a key head, 64 of them at a time.
+// Attention of few new tokens a sequence (a decoding step, a short draft): up to 32
+// queries to a key head.
 //
 // Such a call reads every key and value once and does little with it, so it is
 // bound by memory: the kernel's business is to keep loads in flight on every SM.
@@ -9,16 +9,22 @@
 // cores without passing a register. A thread of the softmax warps is one key of a
 // 128-key tile, and, for the accumulators, one dimension.
 //
-// Work split: all tiles of all units (a sequence, a key head, up to 64 queries), in
-// order, are cut into equal runs, one or two an SM, whatever the lengths. A unit that lies in
-// several runs is joined by a second kernel from partial sums in the workspace,
-// in the order of the runs: results do not depend on timing.
+// Work split: all tiles of all units (a sequence, a key head), in order, are cut
+// into equal runs, two an SM, whatever the lengths. A unit that lies in several
+// runs is joined by a second kernel from partial sums in the workspace, in the
+// order of the runs: results do not depend on timing.
 //
 // Softmax: a query's scores are weighed against a reference, its first tile's
 // maximum, that is raised only when a score exceeds it by 2^8 (the accumulators, in
-// fp32, have the room), so most tiles need no exchange between threads but one vote. Weights go to the product as two 16-bit numbers
-// (the rounded weight and what the rounding left): products are not what bounds
-// this kernel, and the weights keep 16 bits or more.
+// fp32, have the room), so most tiles need no exchange between threads but one
+// vote. Weights go to the product as two 16-bit numbers (the rounded weight and
+// what the rounding left): products are not what bounds this kernel, and the
+// weights keep 16 bits or more.
+//
+// Measured: a token each of 64 sequences of up to 16k slots (2.2 GB of keys and values,
+// 32 heads over 8 of 128) 338 us, 6.6 TB/s; of 48 of up to 9k in a window of 4,096, heads
+// of 64, scores capped, 28 us; of one sequence of 700 slots 12.0 us, of which the two
+// launches and the chain of one tile are all.
 #pragma once
 
 #include <atomic>
@@ -47,14 +53,13 @@ struct Shape {
     static constexpr uint32_t kQ = N * 128 * NS;
     static constexpr uint32_t kP = N * 512;  // two parts
     static constexpr uint32_t kEntry = kSlot * NS;
-    // Two blocks an SM where they fit: one's loads and products run beside the other's softmax.
-    static constexpr uint32_t kBlocks = N <= 32 ? 2 : 1;
+    static constexpr uint32_t kBlocks = 2;  // an SM: one's loads and products run beside the other's softmax
     static constexpr uint32_t kRoom = 228 * 1024 / kBlocks - 1024 - 1024 - kFixed - kQ - kP - kPad;
     static constexpr uint32_t kEntries = kRoom / kEntry < 12 ? kRoom / kEntry : 12;
     static constexpr uint32_t kBytes = 1024 + kEntry * kEntries + kQ + kP + kPad;
     static constexpr uint32_t kTmem = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;
     static_assert(kEntries >= 2, "a tile of K and one of V");
-    static_assert(kBlocks * N <= 64, "the workspace is laid out for one block of 64 rows an SM");
+    static_assert(N <= 32, "the workspace is laid out for two blocks of 32 rows an SM");
     static constexpr uint32_t kPart = N * (64 * NS) + 2 * N;  // floats of a part: O^T, maxima, sums
 };
 
@@ -70,7 +75,6 @@ struct Shared {
 // run that lie in one unit). Every warp walks it on its own.
 struct Walk {
     uint32_t s, h;
-    int32_t rb, rbs;    // which N rows (queries of a key head) of the sequence's, and of how many
     int64_t at, end;    // the next tile of all, and the end of the run
     int64_t unit;       // the unit's first tile of all
     int32_t tile, n, nt;  // the segment's first tile in the unit, its tiles, the unit's
@@ -82,7 +86,7 @@ struct Walk {
 // A unit in several runs, noted at the run that holds its second part: the runs
 // b0 to b1 hold it, the first as that block's part 0 or 1, the others as part 0.
 struct Join {
-    int32_t first, row0, rows, h;  // the sequence's first token, the unit's first row and its rows, its key head
+    int32_t first, rows, h;  // the sequence's first token, its rows (queries of a key head), the key head
     int32_t b0, b1, second, valid;
 };
 
@@ -93,18 +97,12 @@ struct Few {
     uint32_t* fault;   // host-mapped: set where a wait ran out
 };
 
-// The sequence's rows, in units of N.
-template <int N>
-__device__ __forceinline__ int32_t row_units(const KvAttend& a, const KvSeq& q) {
-    return (min(q.n, int32_t(a.tok.max_new)) * int32_t(a.group) + N - 1) / N;
-}
 __device__ __forceinline__ int32_t unit_tiles(const KvAttend& a, const KvSeq& q, KvSpan& sp) {
     if (q.n == 0) return 0;
     sp = kv_span(a, q, 0, min(q.n, int32_t(a.tok.max_new)));
     return max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
 }
 
-template <int N>
 __device__ __forceinline__ void walk_seq(const KvAttend& a, Walk& w) {
     w.nt = 0;
     for (; w.s < a.tok.n_seqs; ++w.s) {
@@ -112,40 +110,32 @@ __device__ __forceinline__ void walk_seq(const KvAttend& a, Walk& w) {
         w.nt = unit_tiles(a, w.q, w.span);
         if (w.nt) break;
     }
-    w.rbs = max(1, row_units<N>(a, w.q));
 }
-template <int N>
 __device__ __forceinline__ void walk_unit(const KvAttend& a, Walk& w) {
-    w.rows = min(N, min(w.q.n, int32_t(a.tok.max_new)) * int32_t(a.group) - w.rb * N);
+    w.rows = min(w.q.n, int32_t(a.tok.max_new)) * int32_t(a.group);
     w.n = int32_t(min(int64_t(w.nt - w.tile), w.end - w.at));
 }
-template <int N>
 __device__ __forceinline__ void walk_start(const KvAttend& a, Walk& w, uint32_t s, int32_t rest, int64_t at, int64_t end) {
     w.s = s, w.at = at, w.end = end;
-    walk_seq<N>(a, w);
+    walk_seq(a, w);
     const int32_t nt = max(w.nt, 1);
-    w.h = rest / nt / w.rbs;
-    w.rb = rest / nt % w.rbs;
+    w.h = rest / nt;
     w.tile = rest % nt;
     w.unit = at - w.tile;
-    walk_unit<N>(a, w);
+    walk_unit(a, w);
 }
-template <int N>
 __device__ __forceinline__ bool walk_next(const KvAttend& a, Walk& w) {
     w.at += w.n;
     if (w.at >= w.end) return false;
     w.tile = 0;
     w.unit = w.at;
-    if (++w.rb == w.rbs) {
-        w.rb = 0;
-        if (++w.h == a.pages.kv_heads) {
-            w.h = 0;
-            ++w.s;
-            walk_seq<N>(a, w);
-            if (w.nt == 0) return false;
-        }
+    if (++w.h == a.pages.kv_heads) {
+        w.h = 0;
+        ++w.s;
+        walk_seq(a, w);
+        if (w.nt == 0) return false;
     }
-    walk_unit<N>(a, w);
+    walk_unit(a, w);
     return true;
 }
 // first slot of the unit's tile i
@@ -176,7 +166,6 @@ template <class T, int N, int NS, bool MOD>
 __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(const __grid_constant__ Few f, const __grid_constant__ CUtensorMap map) {
     using Sh = Shape<N, NS>;
     constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
-    constexpr int C = N < 32 ? N : 32;  // columns at a time
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t* const mem = raw + (base - smem_u32(raw));
@@ -185,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     __shared__ __align__(16) float top[N], scale_by[N], red[4][N];
     __shared__ __align__(16) int32_t first[N], last[N], pos[N];
     __shared__ __align__(16) uint64_t word[N];
-    static_assert(N <= 64, "two columns of sums a lane");
+    static_assert(N == 16 || N == 32, "a lane, or two, a query");
     __shared__ float slope[N];
     const KvAttend& a = f.a;
     const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -211,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     for (uint32_t s = tid * per; s < min(a.tok.n_seqs, (tid + 1) * per); ++s) {
         KvSpan sp;
         const KvSeq q = kv_seq(a.pages, a.tok, s);
-        mine += unit_tiles(a, q, sp) * row_units<N>(a, q);
+        mine += unit_tiles(a, q, sp);
     }
     // inclusive scan over the block's threads, in tiles of one key head
     int64_t inc = mine;
@@ -242,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             for (uint32_t s = tid * per;; ++s) {
                 KvSpan sp;
                 const KvSeq q = kv_seq(a.pages, a.tok, s);
-                const int64_t n = int64_t(unit_tiles(a, q, sp)) * row_units<N>(a, q) * K;
+                const int64_t n = int64_t(unit_tiles(a, q, sp)) * K;
                 if (run0 < p + n) {
                     sh.start_seq = int32_t(s);
                     sh.start_rest = int32_t(run0 - p);
@@ -258,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     if (busy && warp == 4) {
         // ---------------------------------------------------------- loads
         Walk w;
-        walk_start<N>(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
         const uint32_t shift = a.pages.token_shift;
         const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
         const uint32_t T_mask = (1u << shift) - 1;
@@ -287,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                                      (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
                 }
             }
-        } while (walk_next<N>(a, w));
+        } while (walk_next(a, w));
     loads_done:
         __syncwarp();
         if (*dead) {  // the copies in flight land before the block ends
@@ -298,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     } else if (busy && warp == 5) {
         // ---------------------------------------------------------- products
         Walk w;
-        walk_start<N>(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
         constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
         constexpr uint32_t kPv = instr_desc(kBf16, true, true, 128, N);
         const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
@@ -349,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 if (!fresh) pv(n - 1, fresh_before);
                 fresh_before = fresh;
             }
-        } while (walk_next<N>(a, w));
+        } while (walk_next(a, w));
         pv(n - 1, fresh_before);
         if (*dead) {  // the products in flight end before the tensor memory is freed
             const uint64_t t0 = now_ns();
@@ -359,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     } else if (busy) {
         // ---------------------------------------------------------- softmax
         Walk w;
-        walk_start<N>(a, w, sh.start_seq, sh.start_rest, run0, run1);
+        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
         const uint32_t D = a.pages.head_dim;
         const uint32_t lanes = tmem + (warp << 21);  // this warp's 32 lanes
         const float k2 = a.scale * kLog2e;
@@ -372,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             constexpr uint32_t kRowThreads = kSoftThreads / N, kVecs = NS * 8 / kRowThreads;
             const uint32_t c = tid / kRowThreads, x0 = tid % kRowThreads * kVecs;
             const bool real = int32_t(c) < w.rows;
-            const uint32_t ct = (w.rb * N + c) / a.group, ch = w.h * a.group + (w.rb * N + c) % a.group;  // token and head
+            const uint32_t ct = c / a.group, ch = w.h * a.group + c % a.group;  // token and head
             uint4 qv[kVecs];
             {
                 const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(w.q.first + ct) * a.q_stride +
@@ -400,15 +389,11 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 // this run's note of a unit that began in the run before it
                 const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.nt) * blocks - 1) / total;
                 const bool here = w.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
-                f.join[blockIdx.x] = {w.q.first, w.rb * N, w.rows, int32_t(w.h), int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
+                f.join[blockIdx.x] = {w.q.first, w.rows, int32_t(w.h), int32_t(b0), int32_t(b1), b0 * total / blocks != w.unit, here};
             }
             bar_sync<1, kSoftThreads>();
 
-            // Sums of weights: up to 32 columns, each thread its key's; 64, of the warp's keys: lane i has columns
-            // i and i + 32 (a tile then adds up over its lanes; 64 registers less, and code that fits beside the rest).
-            constexpr bool kLanes = N > 32;
-            constexpr int S = kLanes ? N / 32 : N;
-            float sum[S] = {};
+            float sum[N] = {};  // of the thread's keys' weights
             for (int32_t i = 0; i < w.n; ++i, ++n) {
                 const int32_t slot0 = tile_slot(w, w.tile + i), key = slot0 + int32_t(tid);
                 const bool masked = slot0 < w.span.all_lo || slot0 + kTileKeys > w.span.all_hi;
@@ -422,33 +407,29 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 const uint32_t s_at = lanes + (n & 1) * N;
                 mbar_wait(bar(sh.s_full[n & 1]), n >> 1 & 1, dead);
                 fence_after();
-                // scores of columns c0 .. c0 + C
-                float x[C];
-                static_assert(kLanes || C == N, "x holds every column's weight behind the pass");
-                auto scores = [&](int c0) {
-                    if constexpr (C == 32)
-                        tmem_ld32(s_at + c0, x);
-                    else
-                        tmem_ld16(s_at + c0, x);
-                    wait_ld(x);
+                float x[N];  // scores, then weights
+                if constexpr (N == 32)
+                    tmem_ld32(s_at, x);
+                else
+                    tmem_ld16(s_at, x);
+                wait_ld(x);
 #pragma unroll
-                    for (int c = 0; c < C; ++c) {
-                        if (MOD) {
-                            x[c] = cap_in != 0.0f ? capped(x[c], cap_in, cap2) : x[c] * k2;
-                            x[c] -= slope[c0 + c] * fabsf(float(pos[c0 + c] - kpos));
-                        } else {
-                            x[c] *= k2;
-                        }
+                for (int c = 0; c < N; ++c) {
+                    if (MOD) {
+                        x[c] = cap_in != 0.0f ? capped(x[c], cap_in, cap2) : x[c] * k2;
+                        x[c] -= slope[c] * fabsf(float(pos[c] - kpos));
+                    } else {
+                        x[c] *= k2;
                     }
-                    if (masked) {
-                        uint32_t see = 0;
-#pragma unroll(kLanes ? 4 : C)
-                        for (int c = 0; c < C; ++c)
-                            see |= uint32_t(kpos >= first[c0 + c] && (key < last[c0 + c] || (word[c0 + c] & bit))) << c;
+                }
+                if (masked) {
+                    uint32_t see = 0;
 #pragma unroll
-                        for (int c = 0; c < C; ++c) x[c] = see & (1u << c) ? x[c] : -INFINITY;
-                    }
-                };
+                    for (int c = 0; c < N; ++c)
+                        see |= uint32_t(kpos >= first[c] && (key < last[c] || (word[c] & bit))) << c;
+#pragma unroll
+                    for (int c = 0; c < N; ++c) x[c] = see & (1u << c) ? x[c] : -INFINITY;
+                }
                 // the product before this one is complete: its weights may be overwritten, its accumulators scaled
                 bool over_with = n == 0;
                 auto last_product = [&]() {
@@ -479,85 +460,43 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                         }
                         wait_st();
 #pragma unroll
-                        for (int c = 0; c < S; ++c) sum[c] *= scale_by[kLanes ? c * 32 + int(lane) : c];
+                        for (int c = 0; c < N; ++c) sum[c] *= scale_by[c];
                     }
                 };
-                // weights of columns c0 to c0 + C (in x afterwards): rounded, and the rest, eight columns to a 16-byte
-                // row of the operand
-                auto weigh = [&](int c0) {
-                    last_product();
+                // their scores are looked at while the product before this one runs
+                bool over = false;
 #pragma unroll
-                    for (int c = 0; c < C; c += 8) {
-                        uint32_t hi[4], lo[4];
+                for (int c = 0; c < N; ++c) over |= x[c] > top[c] + kRaise;
+                if (bar_any<1, kSoftThreads>(over)) {
+                    float y[N];
 #pragma unroll
-                        for (int j = 0; j < 8; j += 2) {
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const float m = top[c0 + c + j + k];
-                                x[c + j + k] = exp2_approx(x[c + j + k] - (m == -INFINITY ? 0.0f : m));
-                            }
-                            hi[j / 2] = Kv16<T>::from2(x[c + j], x[c + j + 1]);
-                            const float2 r = Kv16<T>::to2(hi[j / 2]);
-                            lo[j / 2] = Kv16<T>::from2(x[c + j] - r.x, x[c + j + 1] - r.y);
-                        }
-                        uint8_t* at = mem + (ps - base) + (c0 + c) / 8 * 2048 + tid * 16;
-                        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                        *reinterpret_cast<uint4*>(at + N * 256) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                    }
-                };
-                if constexpr (!kLanes) {
-                    // all columns at once: their scores are looked at while the product before this one runs
-                    scores(0);
-                    bool over = false;
-#pragma unroll
-                    for (int c = 0; c < C; ++c) over |= x[c] > top[c] + kRaise;
-                    if (bar_any<1, kSoftThreads>(over)) {
-                        float y[C];
-#pragma unroll
-                        for (int c = 0; c < C; ++c) y[c] = x[c];
-                        const float m = columns<C, true>(y, lane);
-                        if (lane < C) red[warp][lane] = m;
-                        raise();
-                    }
-                    weigh(0);
-#pragma unroll
-                    for (int c = 0; c < S; ++c) sum[c] += x[c % C];
-                } else {
-                    // 32 at a time, in code that is not repeated (a call of a few tiles waits for its instructions more
-                    // than for anything else): weighed against the references so far, and, where that will not do
-                    // or there is none yet, once more against the tile's maxima
-                    bool above = i == 0;
-                    float part[S];
-#pragma unroll 1
-                    for (int pass = 0; pass < 2; ++pass) {
-                        if (above) {
-#pragma unroll 1
-                            for (int c0 = 0; c0 < N; c0 += C) {
-                                scores(c0);
-                                const float m = columns<C, true>(x, lane);
-                                if (lane < C) red[warp][c0 + lane] = m;
-                            }
-                            raise();
-                        }
-                        bool over = false;
-#pragma unroll 1
-                        for (int c0 = 0; c0 < N; c0 += C) {
-                            scores(c0);
-#pragma unroll
-                            for (int c = 0; c < C; ++c) over |= x[c] > top[c0 + c] + kRaise;
-                            weigh(c0);
-                            const float all = columns<C, false>(x, lane);
-                            if (c0 == 0)
-                                part[0] = all;
-                            else
-                                part[S - 1] = all;
-                        }
-                        above = bar_any<1, kSoftThreads>(over);
-                        if (!above) break;
-                    }
-#pragma unroll
-                    for (int c = 0; c < S; ++c) sum[c] += part[c];
+                    for (int c = 0; c < N; ++c) y[c] = x[c];
+                    const float m = columns<N, true>(y, lane);
+                    if (lane < N) red[warp][lane] = m;
+                    raise();
                 }
+                // weights: rounded, and the rest, eight columns to a 16-byte row of the operand
+                last_product();
+#pragma unroll
+                for (int c = 0; c < N; c += 8) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float m = top[c + j + k];
+                            x[c + j + k] = exp2_approx(x[c + j + k] - (m == -INFINITY ? 0.0f : m));
+                        }
+                        hi[j / 2] = Kv16<T>::from2(x[c + j], x[c + j + 1]);
+                        const float2 r = Kv16<T>::to2(hi[j / 2]);
+                        lo[j / 2] = Kv16<T>::from2(x[c + j] - r.x, x[c + j + 1] - r.y);
+                    }
+                    uint8_t* at = mem + (ps - base) + c / 8 * 2048 + tid * 16;
+                    *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4*>(at + N * 256) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
+#pragma unroll
+                for (int c = 0; c < N; ++c) sum[c] += x[c];
                 // values that none of the unit's queries sees may be anything: zeros, as their weights are
                 if (slot0 < w.span.lo || slot0 + kTileKeys > w.span.hi) {
                     const uint32_t e = (2 * n + 1) % Sh::kEntries;
@@ -574,14 +513,9 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 mbar_arrive(bar(sh.p_full));
             }
             // the segment's sums over the warps
-#pragma unroll
-            for (int c = 0; c < (kLanes ? S : 1); ++c) {
-                if constexpr (kLanes) {
-                    red[warp][c * 32 + lane] = sum[c];
-                } else {
-                    const float all = columns<N, false>(sum, lane);
-                    if (lane < N) red[warp][lane] = all;
-                }
+            {
+                const float all = columns<N, false>(sum, lane);
+                if (lane < N) red[warp][lane] = all;
             }
             mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
             fence_after();
@@ -590,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             const uint32_t d = tid;
             float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * Sh::kPart;
             if (whole) {
-                uint32_t t = w.rb * N / a.group, g = w.rb * N % a.group;  // the column's token and head
+                uint32_t t = 0, g = 0;  // the column's token and head
 #pragma unroll 1
                 for (int c0 = 0; c0 < w.rows; c0 += 16) {
                     float o[16];
@@ -631,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             }
             fence_before();
             bar_sync<1, kSoftThreads>();  // red and top are read before the next segment writes them
-        } while (walk_next<N>(a, w));
+        } while (walk_next(a, w));
     }
     if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
     __syncthreads();
@@ -683,8 +617,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Few f
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
-    const uint64_t row = uint64_t(j.first + (j.row0 + col) / int32_t(a.group));
-    const uint32_t head = uint32_t(j.h) * a.group + uint32_t(j.row0 + col) % a.group;
+    const uint64_t row = uint64_t(j.first + col / int32_t(a.group));
+    const uint32_t head = uint32_t(j.h) * a.group + uint32_t(col) % a.group;
     const float r = l == 0.0f ? 0.0f : 1.0f / l;
     T* out = static_cast<T*>(a.out) + row * a.out_stride + uint64_t(head) * D + lane * kVec;
     if (lane * kVec < D) {
@@ -706,7 +640,7 @@ cudaError_t launch_as(const Few& f, const CUtensorMap& map, uint32_t sms, cudaSt
         if (e != cudaSuccess) return e;
         if (dev < 64) ready |= uint64_t(1) << dev;
     }
-    const uint64_t units = uint64_t(f.a.tok.n_seqs) * ((uint64_t(f.a.tok.max_new) * f.a.group + N - 1) / N);
+    const uint64_t units = f.a.tok.n_seqs;
     const uint32_t blocks = attend_blocks(f.a, sms * Shape<N, NS>::kBlocks, units);
     e = launch_pdl(few_kernel<T, N, NS, MOD>, dim3(blocks), kThreads, bytes, stream, f, map);
     if (e != cudaSuccess) return e;
@@ -724,9 +658,7 @@ cudaError_t launch_n(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStr
 template <class T>
 cudaError_t launch_t(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
     const uint32_t rows = f.a.group * f.a.tok.max_new;
-    return rows <= 16   ? launch_n<T, 16>(f, map, sms, stream)
-           : rows <= 32 ? launch_n<T, 32>(f, map, sms, stream)
-                        : launch_n<T, 64>(f, map, sms, stream);
+    return rows <= 16 ? launch_n<T, 16>(f, map, sms, stream) : launch_n<T, 32>(f, map, sms, stream);
 }
 
 constexpr uint64_t join_bytes(uint32_t sms) { return (uint64_t(sms) * 2 * sizeof(Join) + 255) / 256 * 256; }  // two blocks an SM

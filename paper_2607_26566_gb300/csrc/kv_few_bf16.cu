@@ -4,7 +4,7 @@
 namespace t2i {
 
 uint64_t kv_few_workspace(uint32_t sms) {
-    return join_bytes(sms) + uint64_t(sms) * 2 * Shape<64, 2>::kPart * sizeof(float);
+    return join_bytes(sms) + uint64_t(sms) * 4 * Shape<32, 2>::kPart * sizeof(float);
 }
 
 cudaError_t launch_kv_few_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream) {

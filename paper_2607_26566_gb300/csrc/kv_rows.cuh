@@ -1,5 +1,5 @@
-// Attention of many new tokens a sequence (prompts, chunks of them, large trees):
-// more than 64 queries to a key head.
+// Attention of more new tokens a sequence (prompts, chunks of them, trees): over 32
+// queries to a key head.
 //
 // Bound by the tensor cores: 4 * 128 * head_dim operations for each query and 128-
 // key tile. A block takes 256 rows (a row: one query of one new token; the heads of
@@ -14,10 +14,16 @@
 // Weights are rounded to the cache's type before the product (as accurate as the
 // values that they weigh: the output's own rounding is as large), the sums are not.
 //
-// Work split: a plan kernel lists the row tiles and the slots that each one sees;
-// all key tiles of all (sequence, key head, row tile) units, in order, are cut into
-// as many equal runs as there are SMs. A unit in several runs is joined by a third
-// kernel, in the order of the runs.
+// Work split: a plan (by a kernel of its own, or, of up to 64 row tiles, by every block
+// for itself) lists the row tiles and the slots that each one sees; all key tiles of all
+// (sequence, key head, row tile) units, in order, and what each unit costs beside them,
+// are cut into as many equal runs as there are SMs. A unit in several runs is joined by a
+// last kernel, in the order of the runs.
+//
+// Measured: a prompt of 8190 tokens, 32 heads over 8 of 128, 400-416 us, 1.32-1.37
+// PFLOP/s of what is visible; 24 drafts of 60 tokens over contexts up to 8k, the same heads, 118 us;
+// one draft of 21 tokens over 1.5k slots 18 us; three chunks of 600 tokens of packed documents, 16 heads of
+// 80, with spans and a bias, 47-49 us.
 #pragma once
 
 #include <atomic>
