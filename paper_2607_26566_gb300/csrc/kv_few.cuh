@@ -41,6 +41,7 @@ using namespace tc;
 constexpr int kSoftThreads = 128;
 constexpr int kThreads = kSoftThreads + 64;  // + the loading warp and the product warp
 constexpr uint32_t kSlot = 16384;            // 128 rows of 64 elements
+constexpr uint32_t kAhead = 4;
 constexpr float kRaise = 8.0f;  // in units of log2
 
 template <int N, int NS>
@@ -63,16 +64,9 @@ struct Shape {
     static constexpr uint32_t kPart = N * (64 * NS) + 2 * N;  // floats of a part: O^T, maxima, sums
 };
 
-struct Shared {
-    uint64_t full[12], empty[12];
-    uint64_t s_full[2], p_full, pv_done, q_full;
-    uint32_t tmem, dead;
-    int32_t start_seq, start_rest;
-    int64_t sums[kThreads / 32];
-};
-
 // The run of tiles of one block, segment by segment (a segment: the tiles of the
-// run that lie in one unit). Every warp walks it on its own.
+// run that lie in one unit). The loading warp walks it and leaves each segment, with
+// its queries, to the others.
 struct Walk {
     uint32_t s, h;
     int64_t at, end;    // the next tile of all, and the end of the run
@@ -81,6 +75,19 @@ struct Walk {
     KvSeq q;
     KvSpan span;
     int32_t rows;
+    bool more;  // segments behind this one
+};
+
+struct Shared {
+    uint64_t full[12], empty[12];
+    uint64_t s_full[2], p_full, pv_done, q_free;
+    // Segments that are handed out. Four, so that no barrier runs ahead of who waits for it: the one that follows a
+    // segment by three is written behind that segment's last scores' weights.
+    uint64_t q_full[kAhead];
+    Walk walk[kAhead];
+    uint32_t tmem, dead;
+    int32_t start_seq, start_rest;
+    int64_t sums[kThreads / 32];
 };
 
 // A unit in several runs, noted at the run that holds its second part: the runs
@@ -114,6 +121,7 @@ __device__ __forceinline__ void walk_seq(const KvAttend& a, Walk& w) {
 __device__ __forceinline__ void walk_unit(const KvAttend& a, Walk& w) {
     w.rows = min(w.q.n, int32_t(a.tok.max_new)) * int32_t(a.group);
     w.n = int32_t(min(int64_t(w.nt - w.tile), w.end - w.at));
+    w.more = w.at + w.n < w.end;
 }
 __device__ __forceinline__ void walk_start(const KvAttend& a, Walk& w, uint32_t s, int32_t rest, int64_t at, int64_t end) {
     w.s = s, w.at = at, w.end = end;
@@ -184,7 +192,8 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     if (tid == 0) {
         for (uint32_t i = 0; i < Sh::kEntries; ++i) mbar_init(bar(sh.full[i]), 1), mbar_init(bar(sh.empty[i]), 1);
         mbar_init(bar(sh.s_full[0]), 1), mbar_init(bar(sh.s_full[1]), 1);
-        mbar_init(bar(sh.p_full), kSoftThreads), mbar_init(bar(sh.pv_done), 1), mbar_init(bar(sh.q_full), kSoftThreads);
+        mbar_init(bar(sh.p_full), kSoftThreads), mbar_init(bar(sh.pv_done), 1), mbar_init(bar(sh.q_free), 1);
+        for (uint32_t i = 0; i < kAhead; ++i) mbar_init(bar(sh.q_full[i]), 32);
         sh.dead = 0;
         fence_mbar_init();
         tma_prefetch_map(&map);
@@ -251,8 +260,38 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
         const uint32_t shift = a.pages.token_shift;
         const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
         const uint32_t T_mask = (1u << shift) - 1;
-        uint32_t n = 0;
+        uint32_t n = 0, u = 0;
+        // A segment's queries, a 16-byte vector a lane in turn: on their way while the segment before is worked on, and
+        // to shared memory (64 dimensions at a time, 128-byte swizzle) when its last scores are there.
+        constexpr uint32_t kRowVecs = NS * 8, kVecs = N * kRowVecs / 32, kStep = 32 / kRowVecs;
+        uint4 qv[kVecs];
+        auto ask = [&]() {
+            const uint32_t D = a.pages.head_dim, G = a.group, x = lane % kRowVecs;
+            uint32_t c = lane / kRowVecs, t = c / G, g = c % G;
+            const T* const q0 = static_cast<const T*>(a.q) + uint64_t(w.q.first) * a.q_stride + uint64_t(w.h) * G * D + x * 8;
+#pragma unroll
+            for (uint32_t k = 0; k < kVecs; ++k, c += kStep) {
+                const bool real = int32_t(c) < w.rows && x * 8 < D;
+                qv[k] = real ? *reinterpret_cast<const uint4*>(q0 + t * a.q_stride + g * D) : make_uint4(0, 0, 0, 0);
+                g += kStep % G, t += kStep / G;
+                if (g >= G) g -= G, ++t;
+            }
+        };
+        auto publish = [&]() -> bool {
+            if (u && !mbar_wait(bar(sh.q_free), (u - 1) & 1, dead)) return false;
+            const uint32_t x = lane % kRowVecs;
+            uint32_t c = lane / kRowVecs;
+#pragma unroll
+            for (uint32_t k = 0; k < kVecs; ++k, c += kStep)
+                *reinterpret_cast<uint4*>(mem + (qs - base) + x / 8 * (N * 128) + c * 128 + ((x % 8) ^ (c % 8)) * 16) = qv[k];
+            if (lane == 0) sh.walk[u % kAhead] = w;
+            fence_async_smem();
+            mbar_arrive(bar(sh.q_full[u % kAhead]));
+            ++u;
+            return true;
+        };
         do {
+            ask();
             const int32_t row_k = int32_t(((a.pages.layer * 2) * a.pages.kv_heads + w.h) << shift);
             const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
             const int32_t* table = a.pages.table + w.s * a.pages.table_stride;
@@ -274,6 +313,10 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                         for (int x = 0; x < NS; ++x)
                             tma_load(ring + e * Sh::kEntry + x * kSlot + lane * box * 128, &map, x * 64,
                                      (kv ? row_v : row_k) + y, z, bar(sh.full[e]));
+                    if (i == 0 && kv == 0 && !__all_sync(0xFFFFFFFFu, publish())) {
+                        ++n;
+                        goto loads_done;
+                    }
                 }
             }
         } while (walk_next(a, w));
@@ -286,8 +329,6 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
         }
     } else if (busy && warp == 5) {
         // ---------------------------------------------------------- products
-        Walk w;
-        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
         constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
         constexpr uint32_t kPv = instr_desc(kBf16, true, true, 128, N);
         const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
@@ -295,8 +336,8 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
         // eight columns to 16 bytes, a key after the other
         const uint64_t kd = smem_desc(ring, 16, 1024, 2), qd = smem_desc(qs, 16, 1024, 2), vd = smem_desc(ring, kSlot, 1024, 2);
         const uint64_t pd = smem_desc(ps, 128, 2048, 0);
-        uint32_t n = 0, seg = 0;  // tile of the run
-        bool fresh_before = false;
+        uint32_t n = 0, u = 0;  // tiles and segments of the run
+        bool fresh_before = false, more;
         auto pv = [&](uint32_t i, bool fresh) {
             const uint32_t e = (2 * i + 1) % Sh::kEntries;
             mbar_wait(bar(sh.p_full), i & 1, dead);
@@ -316,10 +357,12 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             __syncwarp();
         };
         do {
-            for (int32_t i = 0; i < w.n; ++i, ++n) {
-                const bool fresh = i == 0;
-                if (fresh && n) pv(n - 1, fresh_before);
-                if (fresh) mbar_wait(bar(sh.q_full), seg++ & 1, dead);
+            const bool got = mbar_wait(bar(sh.q_full[u % kAhead]), u / kAhead & 1, dead);
+            if (!__all_sync(0xFFFFFFFFu, got)) break;
+            const int32_t tiles = sh.walk[u % kAhead].n;
+            more = sh.walk[u % kAhead].more;
+            ++u;
+            for (int32_t i = 0; i < tiles; ++i, ++n) {
                 const uint32_t e = (2 * n) % Sh::kEntries;
                 mbar_wait(bar(sh.full[e]), (2 * n) / Sh::kEntries & 1, dead);
                 fence_after();
@@ -333,13 +376,14 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                     }
                     mma_commit(bar(sh.empty[e]));
                     mma_commit(bar(sh.s_full[n & 1]));
+                    if (i + 1 == tiles) mma_commit(bar(sh.q_free));
                 }
                 __syncwarp();
-                if (!fresh) pv(n - 1, fresh_before);
-                fresh_before = fresh;
+                if (n) pv(n - 1, fresh_before);
+                fresh_before = i == 0;
             }
-        } while (walk_next(a, w));
-        pv(n - 1, fresh_before);
+        } while (more);
+        if (n) pv(n - 1, fresh_before);
         if (*dead) {  // the products in flight end before the tensor memory is freed
             const uint64_t t0 = now_ns();
             while (now_ns() - t0 < 50000) {
@@ -347,44 +391,29 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
         }
     } else if (busy) {
         // ---------------------------------------------------------- softmax
-        Walk w;
-        walk_start(a, w, sh.start_seq, sh.start_rest, run0, run1);
         const uint32_t D = a.pages.head_dim;
         const uint32_t lanes = tmem + (warp << 21);  // this warp's 32 lanes
         const float k2 = a.scale * kLog2e;
         const float cap_in = MOD && a.softcap != 0.0f ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
         uint32_t n = 0;
-        do {
+        bool more;
+        for (uint32_t u = 0;; ++u) {
+            const bool got = mbar_wait(bar(sh.q_full[u % kAhead]), u / kAhead & 1, dead);
+            if (bar_any<1, kSoftThreads>(!got)) break;  // (also: top and red were read before they are written again)
+            const Walk w = sh.walk[u % kAhead];
+            more = w.more;
             const int32_t ctx = w.q.len - w.q.n;
-            // the unit's queries: to shared memory, 64 dimensions at a time, 128-byte swizzle; kRowThreads threads
-            // a row, whose loads are all under way before the first is stored
-            constexpr uint32_t kRowThreads = kSoftThreads / N, kVecs = NS * 8 / kRowThreads;
-            const uint32_t c = tid / kRowThreads, x0 = tid % kRowThreads * kVecs;
-            const bool real = int32_t(c) < w.rows;
-            const uint32_t ct = c / a.group, ch = w.h * a.group + c % a.group;  // token and head
-            uint4 qv[kVecs];
-            {
-                const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + uint64_t(w.q.first + ct) * a.q_stride +
-                                                                  uint64_t(ch) * D) + x0;
-#pragma unroll
-                for (uint32_t x = 0; x < kVecs; ++x) qv[x] = real && (x0 + x) * 8 < D ? src[x] : make_uint4(0, 0, 0, 0);
-            }
-            if (tid % kRowThreads == 0) {
+            if (tid < N) {
                 KvQuery q{0, INT32_MAX, 0, 0};
                 float sl = 0.0f;
-                if (real) {
-                    q = kv_query(a, w.q, int32_t(ct));
-                    if (MOD && a.slopes) sl = a.slopes[ch] * kLog2e;
+                if (int32_t(tid) < w.rows) {
+                    q = kv_query(a, w.q, int32_t(tid / a.group));
+                    if (MOD && a.slopes) sl = a.slopes[w.h * a.group + tid % a.group] * kLog2e;
                 }
-                top[c] = -INFINITY;
-                first[c] = q.first, last[c] = q.last, pos[c] = q.pos, word[c] = q.word;
-                slope[c] = sl;
+                top[tid] = -INFINITY;
+                first[tid] = q.first, last[tid] = q.last, pos[tid] = q.pos, word[tid] = q.word;
+                slope[tid] = sl;
             }
-#pragma unroll
-            for (uint32_t x = 0; x < kVecs; ++x)
-                *reinterpret_cast<uint4*>(mem + (qs - base) + ((x0 + x) / 8) * (N * 128) + c * 128 + (((x0 + x) % 8) ^ (c % 8)) * 16) = qv[x];
-            fence_async_smem();
-            mbar_arrive(bar(sh.q_full));
             if (tid == 0 && w.at == run0) {
                 // this run's note of a unit that began in the run before it
                 const int64_t b0 = ((w.unit + 1) * blocks - 1) / total, b1 = ((w.unit + w.nt) * blocks - 1) / total;
@@ -564,8 +593,8 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 __stcg(part + N * 64 * NS + N + tid, red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]);
             }
             fence_before();
-            bar_sync<1, kSoftThreads>();  // red and top are read before the next segment writes them
-        } while (walk_next(a, w));
+            if (!more) break;
+        }
     }
     if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
     __syncthreads();
