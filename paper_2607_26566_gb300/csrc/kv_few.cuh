@@ -553,7 +553,15 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             const uint32_t d = tid;
             float* part = f.part + (uint64_t(blockIdx.x) * 2 + (w.at == run0 ? 0 : 1)) * Sh::kPart;
             if (whole) {
-                uint32_t t = 0, g = 0;  // the column's token and head
+                // lane c: the sum of column c's weights, and what divides by it
+                const uint32_t mc = lane % N;
+                const float l = red[0][mc] + red[1][mc] + red[2][mc] + red[3][mc], r = l == 0.0f ? 0.0f : 1.0f / l;
+                if (a.lse && warp == 0 && lane < N && int32_t(lane) < w.rows)
+                    a.lse[uint64_t(w.q.first + lane / a.group) * a.q_heads + w.h * a.group + lane % a.group] =
+                        l == 0.0f ? -INFINITY : (top[lane] + log2f(l)) * kLn2;
+                T* at = static_cast<T*>(a.out) + uint64_t(w.q.first) * a.out_stride + uint64_t(w.h) * a.group * D + d;
+                const uint64_t on = a.out_stride - uint64_t(a.group - 1) * D;  // from a token's last head to the next token
+                uint32_t g = 0;
 #pragma unroll 1
                 for (int c0 = 0; c0 < w.rows; c0 += 16) {
                     float o[16];
@@ -561,17 +569,12 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                     wait_ld(o);
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
-                        const int col = c0 + c;
-                        if (col < w.rows) {
-                            const float l = red[0][col] + red[1][col] + red[2][col] + red[3][col];
-                            const uint64_t row = uint64_t(w.q.first + t);
-                            const float r = l == 0.0f ? 0.0f : 1.0f / l;
-                            if (d < D)
-                                static_cast<T*>(a.out)[row * a.out_stride + uint64_t(w.h * a.group + g) * D + d] =
-                                    Kv16<T>::from1(o[c] * r);
-                            if (a.lse && d == 0)
-                                a.lse[row * a.q_heads + w.h * a.group + g] = l == 0.0f ? -INFINITY : (top[col] + log2f(l)) * kLn2;
-                            if (++g == a.group) g = 0, ++t;
+                        const float by = __shfl_sync(0xFFFFFFFFu, r, c0 + c);
+                        if (c0 + c < w.rows) {
+                            if (d < D) *at = Kv16<T>::from1(o[c] * by);
+                            const bool next = ++g == a.group;
+                            at += next ? on : D;
+                            if (next) g = 0;
                         }
                     }
                 }
