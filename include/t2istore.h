@@ -512,7 +512,8 @@ typedef struct t2i_kv_attend_desc {
  * where no token sees them. So may values before the first and behind the
  * last slot that any of the sequence's new tokens sees; between these a
  * value that is not finite may reach outputs of tokens that do not see it
- * (its weight there is 0, and 0 times it is not 0).                         */
+ * (its weight there is 0, and 0 times it is not 0). With a tree, all drafted
+ * tokens count as seen, and the slots in the window of the one before them. */
 t2i_status t2i_kv_attend(t2i_kv* kv, const t2i_kv_attend_desc* desc, void* cuda_stream);
 
 /* Workspace bytes that t2i_kv_attend needs for such a batch at most.         */

@@ -98,7 +98,7 @@ struct KvLaunch {
 };
 // Up to this many queries to a key head (new tokens of a sequence x heads of a group) kv_few.cuh, above it
 // kv_rows.cuh. Queries, and us of the one / the other, for a sequence of 1.5k slots, 24 of 8k (heads of 128) and 3 of
-// 3k (heads of 64): 32: 15.6 / 16.9, 138 / 141, 19.9 / 18.5; 36 (with 64 columns) 22.5 / 17.1, 201 / 148, 26 / 19;
+// 3k (heads of 64): 32: 15.3 / 16.9, 137 / 141, 19.2 / 18.5; 36 (with 64 columns) 22.5 / 17.1, 201 / 148, 26 / 19;
 // 128: 24 / 19, 389 / 148, 35 / 20.
 constexpr uint32_t kFewRows = 32;
 cudaError_t launch_kv_few_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);

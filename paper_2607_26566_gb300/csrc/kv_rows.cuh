@@ -20,10 +20,10 @@
 // are cut into as many equal runs as there are SMs. A unit in several runs is joined by a
 // last kernel, in the order of the runs.
 //
-// Measured: a prompt of 8190 tokens, 32 heads over 8 of 128, 400-416 us, 1.32-1.37
+// Measured: a prompt of 8190 tokens, 32 heads over 8 of 128, 400-420 us, 1.31-1.37
 // PFLOP/s of what is visible; 24 drafts of 60 tokens over contexts up to 8k, the same heads, 118 us;
 // one draft of 21 tokens over 1.5k slots 18 us; three chunks of 600 tokens of packed documents, 16 heads of
-// 80, with spans and a bias, 47-49 us.
+// 80, with spans and a bias, 47-50 us.
 #pragma once
 
 #include <atomic>
