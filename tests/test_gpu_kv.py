@@ -196,6 +196,19 @@ def test_chunks(dtype, heads, kv, dim, new, ctx):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("heads,kv,dim", [(2, 2, 64), (8, 2, 128)])
+@pytest.mark.parametrize("queries", [16, 20, 32, 36, 64, 68])
+def test_many_sequences_around_the_lines_between_kernels(dtype, heads, kv, dim, queries):
+    """Hundreds of units, several to a block: at and past 16 and 32 queries to a
+    key head, and past 64 row tiles; ragged, some sequences without a token."""
+    most = queries * kv // heads
+    new = [most if i % 3 == 0 else i % (most + 1) for i in range(330)]
+    ctx = [(i * 37) % 300 for i in range(330)]
+    c, lens, kvs, q = case(dtype, heads, kv, dim, new, ctx)
+    check(c, lens, new, kvs, q)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("how", ["cap", "bias", "window", "all", "window1"])
 @pytest.mark.parametrize("new,ctx", [([1, 1, 1], [0, 130, 700]), ([2, 9, 5], [3, 127, 400]), ([200, 40], [150, 0])])
 def test_score_options(dtype, how, new, ctx):
