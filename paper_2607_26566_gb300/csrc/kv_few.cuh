@@ -60,7 +60,7 @@ struct Shape {
     static constexpr uint32_t kRoom = 228 * 1024 / kBlocks - 1024 - 1024 - kFixed - kQ - kP - kPad;
     static constexpr uint32_t kEntries = kRoom / kEntry < 12 ? kRoom / kEntry : 12;
     static constexpr uint32_t kBytes = 1024 + kEntry * kEntries + kQ + kP + kPad;
-    static constexpr uint32_t kTmem = 3 * N <= 64 ? 64 : 3 * N <= 128 ? 128 : 3 * N <= 256 ? 256 : 512;
+    static constexpr uint32_t kTmem = 3 * N <= 64 ? 64 : 128;  // two tiles' scores and the accumulators
     static_assert(kEntries >= 2, "a tile of K and one of V");
     static_assert(N <= 32, "the workspace is laid out for two blocks of 32 rows an SM");
     static constexpr uint32_t kPart = N * (64 * NS) + 2 * N;  // floats of a part: O^T, maxima, sums
