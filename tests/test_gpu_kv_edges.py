@@ -1,0 +1,68 @@
+"""The key/value cache's scores and masks where they are hardest (marked gpu): short
+drafts and chunks with every mask, weights far below the largest, large caps, far
+positions, words with more bits than there are tokens."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from kv_plain import DEV, UNIT, attend64, make_cache, near_attend, words
+from test_gpu_kv import BF, HF, case, check, ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built(lib):
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    yield
+
+
+# (heads, kv_heads, dim, most new tokens): 5 to 16 and 17 to 32 queries to a key head
+FEW = [(2, 2, 64, 8), (4, 2, 80, 8), (8, 2, 128, 8), (5, 1, 64, 5), (4, 4, 128, 24), (2, 1, 96, 16)]
+
+
+def options(how, heads):
+    o = {}
+    if how in ("window", "all"):
+        o["window"] = 40
+    if how in ("bias", "all"):
+        o["slopes"] = torch.tensor([0.8 ** (h + 1) for h in range(heads)])
+    if how in ("cap", "all"):
+        o["softcap"] = 5.0
+    return o
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("heads,kv,dim,most", FEW)
+@pytest.mark.parametrize("how", ["plain", "window", "bias", "cap", "all"])
+def test_short_drafts(dtype, heads, kv, dim, most, how):
+    """Trees of few queries to a key head: contexts of none, in one tile, across the
+    edge of a tile, and over several runs of tiles."""
+    rng = np.random.default_rng(dim + most)
+    new = [1, min(5, most), most, 3, 2]
+    ctx = [0, 125, 700, 30, 2600]
+    c, lens, kvs, q = case(dtype, heads, kv, dim, new, ctx)
+    tree = torch.cat([words(m, rng) for m in new])
+    check(c, lens, new, kvs, q, tree=tree, **options(how, heads))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("heads,kv,dim,most", FEW)
+@pytest.mark.parametrize("how", ["plain", "bias", "cap"])
+def test_spans_of_few_tokens(dtype, heads, kv, dim, most, how):
+    """Spans that are any, empty, whole or look ahead, in one unit."""
+    g = np.random.default_rng(dim + most)
+    new = [1, min(5, most), most, 3, 2, 4]
+    ctx = [0, 125, 700, 30, 2600, 0]
+    c, lens, kvs, q = case(dtype, heads, kv, dim, new, ctx)
+    spans = []
+    for s, (m, L) in enumerate(zip(new, lens)):
+        for i in range(m):
+            a, b = sorted(int(x) for x in g.integers(0, L + 1, 2))
+            spans.append([(a, b), (b, a), (0, L), (max(0, L - m + i - 3), min(L, L - m + i + 2))][(i + s) % 4])
+    out, lse = check(c, lens, new, kvs, q, spans=torch.tensor(spans), **options(how, heads))
+    none = torch.tensor([b <= a for a, b in spans])
+    assert none.any() and not none.all()
+    assert (out.cpu()[none] == 0).all() and (lse.cpu()[none] == -math.inf).all()
