@@ -81,6 +81,19 @@ __device__ __forceinline__ float capped(float s, float cap_in, float cap) {
     return cap - 2.0f * cap * tc::rcp_approx(e + 1.0f);
 }
 
+// A sum of many positive numbers, with what its roundings lost (within a unit of the sum's last place or two,
+// whatever their number; the compiler keeps the order of fp32 operations).
+struct KvSum {
+    float sum = 0.0f, lost = 0.0f;
+    __device__ __forceinline__ void add(float x) {
+        const float s = sum + x, big = fmaxf(sum, x), small = fminf(sum, x);
+        lost += small - (s - big);
+        sum = s;
+    }
+    __device__ __forceinline__ void scale(float by) { sum *= by, lost *= by; }
+    __device__ __forceinline__ float value() const { return sum + lost; }
+};
+
 // Blocks of an attention launch: no more than there are key tiles, going by max_len
 // (a block without any still takes its place on an SM and has to be waited for).
 inline uint32_t attend_blocks(const KvAttend& a, uint32_t most, uint64_t units) {

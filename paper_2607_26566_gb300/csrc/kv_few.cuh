@@ -45,6 +45,9 @@ constexpr int kThreads = kSoftThreads + 64;  // + the loading warp and the produ
 constexpr uint32_t kSlot = 16384;            // 128 rows of 64 elements
 constexpr uint32_t kAhead = 4;
 constexpr float kRaise = 8.0f;  // in units of log2
+// A thread adds its keys' weights up over so many tiles, then they join the warp's sum: a thread's own sum over a long
+// run lost what is below half a unit of it (a key far above 131,072 others: 4e-5 of the sum).
+constexpr int32_t kSumTiles = 16;
 
 template <int N, int NS>
 struct Shape {
@@ -425,6 +428,12 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             bar_sync<1, kSoftThreads>();
 
             float sum[N] = {};  // of the thread's keys' weights
+            KvSum all;          // ... and of the warp's so far, column lane % N
+            auto add_up = [&]() {
+                all.add(columns<N, false>(sum, lane));
+#pragma unroll
+                for (int c = 0; c < N; ++c) sum[c] = 0.0f;
+            };
             for (int32_t i = 0; i < w.n; ++i, ++n) {
                 const int32_t slot0 = tile_slot(w, w.tile + i), key = slot0 + int32_t(tid);
                 const bool masked = slot0 < w.span.all_lo || slot0 + kTileKeys > w.span.all_hi;
@@ -492,6 +501,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                         wait_st();
 #pragma unroll
                         for (int c = 0; c < N; ++c) sum[c] *= scale_by[c];
+                        all.scale(scale_by[lane % N]);
                     }
                 };
                 // their scores are looked at while the product before this one runs
@@ -528,6 +538,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 }
 #pragma unroll
                 for (int c = 0; c < N; ++c) sum[c] += x[c];
+                if (i % kSumTiles == kSumTiles - 1) add_up();
                 // values that none of the unit's queries sees may be anything: zeros, as their weights are
                 if (slot0 < w.span.lo || slot0 + kTileKeys > w.span.hi) {
                     const uint32_t e = (2 * n + 1) % Sh::kEntries;
@@ -544,10 +555,8 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 mbar_arrive(bar(sh.p_full));
             }
             // the segment's sums over the warps
-            {
-                const float all = columns<N, false>(sum, lane);
-                if (lane < N) red[warp][lane] = all;
-            }
+            add_up();
+            if (lane < N) red[warp][lane] = all.value();
             mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
             fence_after();
             bar_sync<1, kSoftThreads>();

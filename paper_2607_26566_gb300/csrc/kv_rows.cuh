@@ -610,8 +610,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 for (int b = 0; b < 64; ++b)
                     if (o.draft[b] < qy.first) qy.word &= ~(uint64_t(1) << b);
             const float pos = float(qy.pos);
-            float ref = -INFINITY, sum = 0.0f, pend = 1.0f;  // pend: what O, once it is there, has to be scaled by
-            bool late = false;                               // ... of some row of the warp
+            float ref = -INFINITY, pend = 1.0f;  // pend: what O, once it is there, has to be scaled by
+            bool late = false;                   // ... of some row of the warp
+            KvSum sum;
             for (int32_t i = 0; i < tiles; ++i, ++n) {
                 const int32_t slot0 = tile_slot(span, o.tile + i);
                 const bool masked = slot0 < span.all_lo || slot0 + kTileKeys > span.all_hi;
@@ -679,7 +680,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                         const float m = fmaxf(t0, t1) * (MOD ? 1.0f : k2);
                         if (m > ref) {
                             const float by = i ? exp2_approx(ref - m) : 1.0f;  // at first there is nothing to scale
-                            ref = m, sum *= by, pend *= by;
+                            ref = m, sum.scale(by), pend *= by;
                         }
                         late = i != 0;
                     }
@@ -741,22 +742,23 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 wait_st();
                 fence_before();
                 mbar_arrive(bar(sh.p_full[st]));
-                sum += part;
+                sum.add(part);
                 // for the next tile: the reference, and what the accumulators follow it by
                 late = __any_sync(0xFFFFFFFFu, part > kRaise);
                 if (rare(late) && part > kRaise) {
                     ref += log2f(part);
                     pend = 1.0f / part;
-                    sum *= pend;
+                    sum.scale(pend);
                 }
             }
             if (more) load_q(unit(u + 1));  // the next unit's scores start while this one is written
             mbar_wait(bar(sh.pv_done[st]), on++ & 1, dead);
             fence_after();
+            const float all = sum.value();
             if (tiles == o.nt) {
                 const bool real = int32_t(st * 128 + r) < o.rows && !gone;
                 const uint32_t row = uint32_t(o.m) * kRows + st * 128 + r;
-                const float by = sum == 0.0f ? 0.0f : pend / sum;
+                const float by = all == 0.0f ? 0.0f : pend / all;
                 const uint64_t orow = uint64_t(o.q.first) + row / a.group;
                 const uint32_t head = o.h * a.group + row % a.group;
                 T* out = static_cast<T*>(a.out) + orow * a.out_stride + uint64_t(head) * D;
@@ -773,7 +775,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                         kv_store8(out + c0 + c, z);
                     }
                 }
-                if (real && a.lse) a.lse[orow * a.q_heads + head] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+                if (real && a.lse) a.lse[orow * a.q_heads + head] = all == 0.0f ? -INFINITY : (ref + log2f(all)) * kLn2;
             } else {
                 // a part of the unit: [head_dim / 4][256 rows] of four, maxima, sums
                 float* part = f.part + (uint64_t(blockIdx.x) * 2 + (o.at == run0 ? 0 : 1)) * kRowPart;
@@ -788,7 +790,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                                make_float4(y[c] * pend, y[c + 1] * pend, y[c + 2] * pend, y[c + 3] * pend));
                 }
                 __stcg(part + kRows * 128 + pr, ref);
-                __stcg(part + kRows * 128 + kRows + pr, sum);
+                __stcg(part + kRows * 128 + kRows + pr, all);
             }
             fence_before();
             done_with(u);

@@ -66,3 +66,36 @@ def test_spans_of_few_tokens(dtype, heads, kv, dim, most, how):
     none = torch.tensor([b <= a for a, b in spans])
     assert none.any() and not none.all()
     assert (out.cpu()[none] == 0).all() and (lse.cpu()[none] == -math.inf).all()
+
+
+def one_strong_key(dtype, new, seqs, above, where):
+    """`new` tokens of each of `seqs` sequences (on one sequence's pages) over 131,072
+    keys of score 0, value 1, and one of score `above`, value 0; out and lse, each with
+    what it should be and the bounds of near_attend."""
+    n, L = 1 << 17, (1 << 17) + new
+    c = make_cache(1, 64, dtype, [L], page=1 << 20)
+    key, val = torch.zeros(L, 1, 64, dtype=dtype), torch.ones(L, 1, 64, dtype=dtype)
+    key[where, 0, 0], val[where] = above, 0
+    q = torch.zeros(new, 1, 64, dtype=dtype)
+    q[:, 0, 0] = 1
+    c.append(key.to(DEV), val.to(DEV), ints([L]))
+    lse = torch.empty(new * seqs, 1, device=DEV)
+    table = c.table[:1].expand(seqs, -1).contiguous()
+    out = c.attend(q.to(DEV).repeat(seqs, 1, 1), ints([L] * seqs), lse=lse, scale=1.0, table=table)
+    want, want_lse, spread, big = attend64(q, key, val, 1.0)
+    slack = 1e-5 + 2.0 ** -20 * above
+    bound = UNIT[dtype] * want + (UNIT[dtype] + slack) * 1.01 * spread
+    return (out.double().cpu().view(seqs, new, 1, 64), want, bound,
+            lse.double().cpu().view(seqs, new, 1), want_lse, slack + 2.0 ** -22 * want_lse.abs())
+
+
+@pytest.mark.parametrize("new,seqs", [(1, 320), (24, 320), (40, 160)])
+@pytest.mark.parametrize("above", [16.0, 17.0])
+@pytest.mark.parametrize("where", [0, 131_071])
+def test_sums_of_long_runs(new, seqs, above, where):
+    """Over a run of a thousand tiles a sum keeps weights that are below half a unit of
+    it one by one, and are 4e-5 to 1e-4 of it together."""
+    out, want, bound, lse, want_lse, lse_bound = one_strong_key(BF, new, seqs, above, where)
+    assert ((out - want).abs() <= bound).all()
+    off = (lse - want_lse).abs()
+    assert (off <= lse_bound).all(), f"{float(off.max()):.3g}"
