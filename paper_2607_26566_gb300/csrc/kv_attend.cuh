@@ -12,6 +12,14 @@ namespace t2i {
 constexpr int kTileKeys = 128;       // keys of a tile
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+// A softmax's reference is so many powers of two below the maximum that it goes by. Weights go to the product in
+// 16 bits, and fp16 keeps nothing below 2^-25: without a lift, 131,072 keys at 2^-26 of the largest, 0.2% of the sum,
+// were no part of the output. With 2^7 a weight is off by 2^-32 of the largest at most (and by its own rounding),
+// and the largest stay below fp16's end (2^15 in kv_few.cuh, kFarOf in kv_rows.cuh). bf16 has fp32's exponents.
+template <class T>
+constexpr float kLift = 0.0f;
+template <>
+constexpr float kLift<__half> = 7.0f;
 
 // Slots [lo, hi) outside which none of tokens [t0, t1) of sequence q sees anything,
 // and slots [all_lo, all_hi) that all of them see.

@@ -19,7 +19,8 @@
 // fp32, have the room), so most tiles need no exchange between threads but one
 // vote. Weights go to the product as two 16-bit numbers (the rounded weight and
 // what the rounding left): products are not what bounds this kernel, and the
-// weights keep 16 bits or more.
+// weights keep 16 bits or more. In fp16, which ends at 2^-25, the reference lies
+// below the maximum (kLift).
 //
 // Measured: a token each of 64 sequences of up to 16k slots (2.2 GB of keys and values,
 // 32 heads over 8 of 128) 331 us, 6.8 TB/s; of 48 of up to 9k in a window of 4,096, heads
@@ -44,7 +45,7 @@ constexpr int kSoftThreads = 128;
 constexpr int kThreads = kSoftThreads + 64;  // + the loading warp and the product warp
 constexpr uint32_t kSlot = 16384;            // 128 rows of 64 elements
 constexpr uint32_t kAhead = 4;
-constexpr float kRaise = 8.0f;  // in units of log2
+constexpr float kRaise = 8.0f;  // in units of log2; weights are below 2^(kRaise + kLift)
 // A thread adds its keys' weights up over so many tiles, then they join the warp's sum: a thread's own sum over a long
 // run lost what is below half a unit of it (a key far above 131,072 others: 4e-5 of the sum).
 constexpr int32_t kSumTiles = 16;
@@ -476,12 +477,13 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                     if (!over_with) mbar_wait(bar(sh.pv_done), (n - 1) & 1, dead);
                     over_with = true;
                 };
-                // references become the tile's maxima (red: of each warp's keys)
+                // references become the tile's maxima (red: of each warp's keys), less kLift
                 auto raise = [&]() {
                     bar_sync<1, kSoftThreads>();
                     if (tid < N) {
                         const float was = top[tid];
-                        const float now = fmaxf(fmaxf(fmaxf(red[0][tid], red[1][tid]), fmaxf(red[2][tid], red[3][tid])), was);
+                        const float most = fmaxf(fmaxf(red[0][tid], red[1][tid]), fmaxf(red[2][tid], red[3][tid]));
+                        const float now = fmaxf(most - kLift<T>, was);
                         top[tid] = now;
                         scale_by[tid] = was == now ? 1.0f : exp2_approx(was - now);
                     }
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 // their scores are looked at while the product before this one runs
                 bool over = false;
 #pragma unroll
-                for (int c = 0; c < N; ++c) over |= x[c] > top[c] + kRaise;
+                for (int c = 0; c < N; ++c) over |= x[c] > top[c] + (kRaise + kLift<T>);
                 if (bar_any<1, kSoftThreads>(over)) {
                     float y[N];
 #pragma unroll

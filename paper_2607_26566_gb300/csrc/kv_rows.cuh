@@ -48,14 +48,20 @@ constexpr uint32_t kEntryBytes = 32768;  // a tile of K or V, 128 rows of 128 el
 constexpr uint32_t kRowEntries = 4;
 constexpr uint32_t kRowSmem = 1024 + 2 * kEntryBytes + kRowEntries * kEntryBytes;
 constexpr uint32_t kRowPart = kRows * 128 + 2 * kRows;  // floats of a part: O, maxima, sums
-// A row's scores are weighed against a reference: its first tile's maximum, raised
-// behind a tile whose weights add up to more than kRaise (the accumulators follow
-// in the next tile), and at once where a weight would exceed kFar.
-constexpr float kRaise = 256.0f;
+// A row's scores are weighed against a reference: its first tile's maximum (less
+// kLift), raised behind a tile whose weights add up to more than kRaise (the
+// accumulators follow in the next tile), and at once where they add up to more than
+// kFar, so that no weight exceeds it.
+template <class T>
+constexpr float kUnitOf = 1.0f;  // 2^kLift: the weight of the maximum
+template <>
+constexpr float kUnitOf<__half> = 0x1p7f;
+template <class T>
+constexpr float kRaiseOf = 256.0f * kUnitOf<T>;
 template <class T>
 constexpr float kFarOf = 0x1p64f;
 template <>
-constexpr float kFarOf<__half> = 0x1p12f;
+constexpr float kFarOf<__half> = 65504.0f;  // fp16's largest
 
 struct PlanTile {
     int32_t s, m;       // the sequence, and which 256 rows of it
@@ -304,7 +310,7 @@ __device__ __forceinline__ bool rare(bool c) { return __builtin_expect(c, 0); }
 template <class T, bool MOD>
 __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_constant__ Rows f, const __grid_constant__ CUtensorMap map) {
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-    constexpr float kFar = kFarOf<T>;
+    constexpr float kFar = kFarOf<T>, kRaise = kRaiseOf<T>, kUnit = kUnitOf<T>;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t* const mem = raw + (base - smem_u32(raw));
@@ -677,7 +683,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                         float t0 = max3(x[0], x[1], x[2]), t1 = x[3];
 #pragma unroll
                         for (int c = 4; c < 128; c += 4) t0 = max3(t0, x[c], x[c + 1]), t1 = max3(t1, x[c + 2], x[c + 3]);
-                        const float m = fmaxf(t0, t1) * (MOD ? 1.0f : k2);
+                        const float m = fmaxf(t0, t1) * (MOD ? 1.0f : k2) - kLift<T>;
                         if (m > ref) {
                             const float by = i ? exp2_approx(ref - m) : 1.0f;  // at first there is nothing to scale
                             ref = m, sum.scale(by), pend *= by;
@@ -746,8 +752,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 // for the next tile: the reference, and what the accumulators follow it by
                 late = __any_sync(0xFFFFFFFFu, part > kRaise);
                 if (rare(late) && part > kRaise) {
-                    ref += log2f(part);
-                    pend = 1.0f / part;
+                    ref += log2f(part) - kLift<T>;
+                    pend = kUnit / part;
                     sum.scale(pend);
                 }
             }

@@ -99,3 +99,15 @@ def test_sums_of_long_runs(new, seqs, above, where):
     assert ((out - want).abs() <= bound).all()
     off = (lse - want_lse).abs()
     assert (off <= lse_bound).all(), f"{float(off.max()):.3g}"
+
+
+@pytest.mark.parametrize("new,seqs", [(1, 320), (40, 160)])
+@pytest.mark.parametrize("above", [17.0625, 18.0, 20.0])
+@pytest.mark.parametrize("where", [0, 70_000, 131_071])
+def test_many_keys_far_below_the_largest(new, seqs, above, where):
+    """fp16: weights of 2^-24.6 to 2^-28.9 of the strong key's are all that the output
+    consists of. A weight is off by 2^-32 of the largest at most."""
+    out, want, bound, lse, want_lse, lse_bound = one_strong_key(HF, new, seqs, above, where)
+    err = (out - want).abs()
+    assert (err <= bound + 2.0 ** -32 * (1 << 17)).all(), f"{float((err / want).max()):.3f} of the output"
+    assert ((lse - want_lse).abs() <= lse_bound).all()
