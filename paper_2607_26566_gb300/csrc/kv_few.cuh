@@ -176,9 +176,10 @@ __device__ __forceinline__ float columns(float (&v)[n], uint32_t lane) {
     return v[0];
 }
 
-template <class T, int N, int NS, bool MOD>
+template <class T, int N, int NS, Mod MOD>
 __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(const __grid_constant__ Few f, const __grid_constant__ CUtensorMap map) {
     using Sh = Shape<N, NS>;
+    constexpr bool kMod = MOD != Mod::kNone;
     constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
         const uint32_t D = a.pages.head_dim;
         const uint32_t lanes = tmem + (warp << 21);  // this warp's 32 lanes
         const float k2 = a.scale * kLog2e;
-        const float cap_in = MOD && a.softcap != 0.0f ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
+        const float cap_in = kMod && a.softcap != 0.0f ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
         uint32_t n = 0;
         bool more;
         for (uint32_t u = 0;; ++u) {
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 float sl = 0.0f;
                 if (int32_t(tid) < w.rows) {
                     q = kv_query(a, w.q, int32_t(tid / a.group));
-                    if (MOD && a.slopes) sl = a.slopes[w.h * a.group + tid % a.group] * kLog2e;
+                    if (kMod && a.slopes) sl = a.slopes[w.h * a.group + tid % a.group] * kLog2e;
                 }
                 top[tid] = -INFINITY;
                 first[tid] = q.first, last[tid] = q.last, pos[tid] = q.pos, word[tid] = q.word;
@@ -456,8 +457,8 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 wait_ld(x);
 #pragma unroll
                 for (int c = 0; c < N; ++c) {
-                    if (MOD) {
-                        x[c] = cap_in != 0.0f ? capped(x[c], cap_in, cap2) : x[c] * k2;
+                    if (kMod) {
+                        x[c] = cap_in != 0.0f ? capped<MOD == Mod::kFine>(x[c], cap_in, cap2) : x[c] * k2;
                         x[c] -= slope[c] * fabsf(float(pos[c] - kpos));
                     } else {
                         x[c] *= k2;
@@ -673,7 +674,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Few f
     if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
 }
 
-template <class T, int N, int NS, bool MOD>
+template <class T, int N, int NS, Mod MOD>
 cudaError_t launch_as(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
     constexpr uint32_t bytes = Shape<N, NS>::kBytes;
     static std::atomic<uint64_t> ready{0};  // devices whose kernel may take this much shared memory
@@ -692,12 +693,18 @@ cudaError_t launch_as(const Few& f, const CUtensorMap& map, uint32_t sms, cudaSt
     return launch_pdl(join_kernel<T, N, NS>, dim3(blocks, (N + 7) / 8), 256, 0, stream, f);
 }
 
+template <class T, int N, int NS>
+cudaError_t launch_mod(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
+    switch (mod_of(f.a)) {
+        case Mod::kNone: return launch_as<T, N, NS, Mod::kNone>(f, map, sms, stream);
+        case Mod::kSome: return launch_as<T, N, NS, Mod::kSome>(f, map, sms, stream);
+        default: return launch_as<T, N, NS, Mod::kFine>(f, map, sms, stream);
+    }
+}
+
 template <class T, int N>
 cudaError_t launch_n(const Few& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
-    const bool mod = f.a.softcap != 0.0f || f.a.slopes;
-    if (f.a.pages.head_dim <= 64)
-        return mod ? launch_as<T, N, 1, true>(f, map, sms, stream) : launch_as<T, N, 1, false>(f, map, sms, stream);
-    return mod ? launch_as<T, N, 2, true>(f, map, sms, stream) : launch_as<T, N, 2, false>(f, map, sms, stream);
+    return f.a.pages.head_dim <= 64 ? launch_mod<T, N, 1>(f, map, sms, stream) : launch_mod<T, N, 2>(f, map, sms, stream);
 }
 
 template <class T>

@@ -307,9 +307,9 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 // a condition that seldom holds
 __device__ __forceinline__ bool rare(bool c) { return __builtin_expect(c, 0); }
 
-template <class T, bool MOD>
+template <class T, Mod MOD>
 __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_constant__ Rows f, const __grid_constant__ CUtensorMap map) {
-    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value, kMod = MOD != Mod::kNone;
     constexpr float kFar = kFarOf<T>, kRaise = kRaiseOf<T>, kUnit = kUnitOf<T>;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
         // a negative scale turns the queries' signs, so that the largest product is the largest score
         const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
         const float k2 = fabsf(a.scale) * kLog2e;
-        const bool cap = MOD && a.softcap != 0.0f;
+        const bool cap = kMod && a.softcap != 0.0f;
         const float cap_in = cap ? fabsf(a.scale) / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
         const float kk = cap ? 1.0f : k2;  // what is left to scale after the cap
         bool gone = false;  // a wait ran out: what lies in shared memory is not to be gone by
@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             if (real) {
                 const uint32_t row = uint32_t(o.m) * kRows + st * 128 + r;
                 qy = kv_query(a, o.q, int32_t(row / a.group));
-                if (MOD && a.slopes) slope = a.slopes[o.h * a.group + row % a.group] * kLog2e;
+                if (kMod && a.slopes) slope = a.slopes[o.h * a.group + row % a.group] * kLog2e;
             }
             if (a.tree && real)  // of the drafted tokens, those that are there and inside the window
                 for (int b = 0; b < 64; ++b)
@@ -646,7 +646,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                         tmem_ld32(s_at + c0, y);
                         wait_ld(y);
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) y[c] = capped(y[c], cap_in, cap2);
+                        for (int c = 0; c < 32; ++c) y[c] = capped<MOD == Mod::kFine>(y[c], cap_in, cap2);
                         tmem_st16(s_at + c0, reinterpret_cast<uint32_t*>(y));
                         tmem_st16(s_at + c0 + 16, reinterpret_cast<uint32_t*>(y) + 16);
                     }
@@ -655,8 +655,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 float x[128];
                 tmem_ld32(s_at, x), tmem_ld32(s_at + 32, x + 32), tmem_ld32(s_at + 64, x + 64), tmem_ld32(s_at + 96, x + 96);
                 wait_ld(x);
-                // bias (scores in units of log2 from here on, if MOD) and mask
-                if (MOD) {
+                // bias (scores in units of log2 from here on, if kMod) and mask
+                if (kMod) {
                     const float ahead = pos - float(slot0);
                     if (rare(drafts && a.slopes)) {
 #pragma unroll
@@ -683,7 +683,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                         float t0 = max3(x[0], x[1], x[2]), t1 = x[3];
 #pragma unroll
                         for (int c = 4; c < 128; c += 4) t0 = max3(t0, x[c], x[c + 1]), t1 = max3(t1, x[c + 2], x[c + 3]);
-                        const float m = fmaxf(t0, t1) * (MOD ? 1.0f : k2) - kLift<T>;
+                        const float m = fmaxf(t0, t1) * (kMod ? 1.0f : k2) - kLift<T>;
                         if (m > ref) {
                             const float by = i ? exp2_approx(ref - m) : 1.0f;  // at first there is nothing to scale
                             ref = m, sum.scale(by), pend *= by;
@@ -691,7 +691,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                         late = i != 0;
                     }
                     const float off = ref == -INFINITY ? 0.0f : -ref;
-                    const uint64_t off2 = pack2(off, off), by2 = pack2(MOD ? 1.0f : k2, MOD ? 1.0f : k2);
+                    const uint64_t off2 = pack2(off, off), by2 = pack2(kMod ? 1.0f : k2, kMod ? 1.0f : k2);
                     uint64_t sum2 = 0, sum3 = 0;
 #pragma unroll
                     for (int c0 = 0; c0 < 128; c0 += 32) {
@@ -868,7 +868,7 @@ constexpr uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
 // the parts of the workspace, in order: head, notes, firsts, plan, parts
 uint64_t plan_tiles(uint64_t n_seqs, uint64_t n_tokens, uint64_t group) { return n_tokens * group / kRows + n_seqs + 1; }
 
-template <class T, bool MOD>
+template <class T, Mod MOD>
 cudaError_t launch_rows_as(const Rows& f, const CUtensorMap& map, uint32_t sms, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};  // devices whose kernel may take this much shared memory
     int dev = 0;
@@ -901,10 +901,13 @@ cudaError_t launch_rows(const KvAttend& a, const KvLaunch& l, cudaStream_t strea
     p += up256(uint64_t(f.most) * sizeof(PlanTile));
     f.part = reinterpret_cast<float*>(p);
     f.fault = l.fault;
-    // (MOD scales before it masks: a scale of 0 would turn a masked -infinity into NaN)
-    const bool mod = a.softcap != 0.0f || a.slopes || a.scale == 0.0f;
-    f.cost = mod ? kUnitCostMod : kUnitCost;
-    return mod ? launch_rows_as<T, true>(f, *l.map, l.sms, stream) : launch_rows_as<T, false>(f, *l.map, l.sms, stream);
+    const Mod mod = mod_of(a);
+    // (Without Mod::kNone scores are scaled before they are masked: a scale of 0 would turn a masked -infinity into NaN.)
+    const bool none = mod == Mod::kNone && a.scale != 0.0f;
+    f.cost = none ? kUnitCost : kUnitCostMod;
+    if (none) return launch_rows_as<T, Mod::kNone>(f, *l.map, l.sms, stream);
+    return mod == Mod::kFine ? launch_rows_as<T, Mod::kFine>(f, *l.map, l.sms, stream)
+                             : launch_rows_as<T, Mod::kSome>(f, *l.map, l.sms, stream);
 }
 
 }  // namespace

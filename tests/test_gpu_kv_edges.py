@@ -111,3 +111,11 @@ def test_many_keys_far_below_the_largest(new, seqs, above, where):
     err = (out - want).abs()
     assert (err <= bound + 2.0 ** -32 * (1 << 17)).all(), f"{float((err / want).max()):.3f} of the output"
     assert ((lse - want_lse).abs() <= lse_bound).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("softcap", [1.0, 50.0, 1e3, 1e5, 1e7])
+@pytest.mark.parametrize("new,ctx", [([1, 1], [300, 20]), ([5], [200]), ([70], [150])])
+def test_caps_from_small_to_far_above_the_scores(dtype, softcap, new, ctx):
+    c, lens, kvs, q = case(dtype, 4, 2, 64, new, ctx)
+    check(c, lens, new, kvs, q, softcap=softcap)
