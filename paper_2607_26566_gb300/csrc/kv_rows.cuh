@@ -615,7 +615,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             if (a.tree && real)  // of the drafted tokens, those that are there and inside the window
                 for (int b = 0; b < 64; ++b)
                     if (o.draft[b] < qy.first) qy.word &= ~(uint64_t(1) << b);
-            const float pos = float(qy.pos);
             float ref = -INFINITY, pend = 1.0f;  // pend: what O, once it is there, has to be scaled by
             bool late = false;                   // ... of some row of the warp
             KvSum sum;
@@ -657,12 +656,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 wait_ld(x);
                 // bias (scores in units of log2 from here on, if kMod) and mask
                 if (kMod) {
-                    const float ahead = pos - float(slot0);
+                    // (differences first: fp32 does not count beyond 2^24)
+                    const float ahead = float(qy.pos - slot0);
                     if (rare(drafts && a.slopes)) {
 #pragma unroll
                         for (int c = 0; c < 128; ++c) {
                             const int32_t key = slot0 + c;
-                            const float far = key >= ctx ? pos - float(o.draft[min(key - ctx, 63)]) : ahead - float(c);
+                            const int32_t at = key >= ctx ? o.draft[min(key - ctx, 63)] : key;
+                            const float far = float(int32_t(uint32_t(qy.pos) - uint32_t(at)));
                             x[c] = x[c] * kk - slope * fabsf(far);
                         }
                     } else {

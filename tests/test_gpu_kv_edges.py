@@ -119,3 +119,22 @@ def test_many_keys_far_below_the_largest(new, seqs, above, where):
 def test_caps_from_small_to_far_above_the_scores(dtype, softcap, new, ctx):
     c, lens, kvs, q = case(dtype, 4, 2, 64, new, ctx)
     check(c, lens, new, kvs, q, softcap=softcap)
+
+
+@pytest.mark.parametrize("new", [3, 40])
+@pytest.mark.parametrize("tree", [False, True])
+def test_positions_that_fp32_cannot_count(new, tree):
+    """Distances count exactly where positions are above 2^24 (and odd)."""
+    ctx, window = (1 << 24) + 1001, 64
+    L = ctx + new
+    c = make_cache(1, 8, BF, [L], page=1 << 20)
+    g = torch.Generator().manual_seed(new)
+    key, val = (torch.randn(window + new, 1, 8, generator=g).to(BF) for _ in range(2))
+    q = torch.randn(new, 1, 8, generator=g).to(BF)
+    c.append(key.to(DEV), val.to(DEV), ints([L]))
+    lse = torch.empty(new, 1, device=DEV)
+    how = dict(lse=lse, slopes=torch.tensor([0.75], device=DEV), window=window)
+    t = words(new, np.random.default_rng(1)) if tree else None
+    out = c.attend_tree(q.to(DEV), ints([L]), t.to(DEV), **how) if tree else c.attend(q.to(DEV), ints([L]), **how)
+    # (only differences of positions count)
+    near_attend(out, lse, *attend64(q, key, val, 8 ** -0.5, slopes=torch.tensor([0.75]), window=window, tree=t), BF)
