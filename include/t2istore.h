@@ -486,7 +486,8 @@ typedef struct t2i_kv_attend_desc {
     const int32_t* spans;   /* device, [n_tokens][2], 8-byte aligned: slots
                                first, last + 1 that a token sees; NULL       */
     const uint64_t* tree;   /* device, [n_tokens]: ancestors of a drafted
-                               token (bit i: it sees new token i); NULL      */
+                               token (bit i: it sees new token i; bits with
+                               no token count nothing); NULL                 */
     uint32_t q_heads;       /* a multiple of kv_heads                        */
     uint32_t window;        /* 0: none                                       */
     uint32_t max_len;       /* the longest lens; it sets how work is split,

@@ -56,6 +56,13 @@ __device__ __forceinline__ KvSpan kv_span(const KvAttend& a, const KvSeq& q, int
     return r;
 }
 
+// The word of drafted token i of a sequence: bits behind its tokens (a caller's word
+// of ones) count nothing.
+__device__ __forceinline__ uint64_t kv_word(const KvAttend& a, const KvSeq& q, int32_t i) {
+    const uint64_t w = a.tree[q.first + i];
+    return q.n < 64 ? w & ((uint64_t(1) << q.n) - 1) : w;
+}
+
 // One query: it sees the keys of slots below `last`, and of the drafted tokens in
 // `word`, whose position is `first` or above. pos: its own position.
 struct KvQuery {
@@ -69,7 +76,7 @@ __device__ __forceinline__ KvQuery kv_query(const KvAttend& a, const KvSeq& q, i
     r.pos = ctx + i;
     r.last = r.pos + 1;
     if (a.tree) {
-        r.word = a.tree[t];
+        r.word = kv_word(a, q, i);
         r.pos = ctx + __popcll(r.word) - 1;
         r.last = ctx;
     }

@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 int32_t kpos = key;
                 if (a.tree && key >= ctx && key < w.q.len && key - ctx < 64) {
                     bit = uint64_t(1) << (key - ctx);
-                    kpos = ctx + __popcll(a.tree[w.q.first + key - ctx]) - 1;
+                    kpos = ctx + __popcll(kv_word(a, w.q, key - ctx)) - 1;
                 }
                 const uint32_t s_at = lanes + (n & 1) * N;
                 mbar_wait(bar(sh.s_full[n & 1]), n >> 1 & 1, dead);

@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 if (a.tree) {
                     const int32_t ctx = w.t.q.len - w.t.q.n;
                     for (int32_t b = int32_t(lane); b < 64; b += 32)
-                        o.draft[b] = b < w.t.q.n ? ctx + __popcll(a.tree[w.t.q.first + b]) - 1 : INT32_MIN;
+                        o.draft[b] = b < w.t.q.n ? ctx + __popcll(kv_word(a, w.t.q, b)) - 1 : INT32_MIN;
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sh.unit_full[u % kUnits]));

@@ -138,3 +138,17 @@ def test_positions_that_fp32_cannot_count(new, tree):
     out = c.attend_tree(q.to(DEV), ints([L]), t.to(DEV), **how) if tree else c.attend(q.to(DEV), ints([L]), **how)
     # (only differences of positions count)
     near_attend(out, lse, *attend64(q, key, val, 8 ** -0.5, slopes=torch.tensor([0.75]), window=window, tree=t), BF)
+
+
+@pytest.mark.parametrize("group", [1, 8])
+def test_bits_behind_a_drafts_tokens_count_nothing(group):
+    """A word of ones: the token sees the whole draft, whose tokens are fewer."""
+    new, ctx = [6, 2, 9], [200, 0, 90]
+    c, lens, kvs, q = case(BF, group, 1, 64, new, ctx)
+    tree = torch.full((sum(new),), -1, dtype=torch.int64)
+    own = torch.cat([torch.full((m,), (1 << m) - 1, dtype=torch.int64) for m in new])
+    opt = dict(slopes=torch.tensor([0.5] * group), window=30)
+    how = dict(starts=torch.tensor(np.cumsum([0] + new), dtype=torch.int32, device=DEV), max_new=9, window=30,
+               slopes=opt["slopes"].to(DEV))
+    want, _ = check(c, lens, new, kvs, q, tree=own, **opt)
+    assert torch.equal(c.attend_tree(q.to(DEV), ints(lens), tree.to(DEV), **how), want)
