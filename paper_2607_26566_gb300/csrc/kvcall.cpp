@@ -8,15 +8,16 @@
 #include <Python.h>
 
 #include <ATen/core/TensorBase.h>
+#include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <initializer_list>
 #include <string>
-#include <utility>
-#include <vector>
 
 #include "t2istore.h"
 
@@ -28,9 +29,7 @@ struct Cache {
     int device;
     at::ScalarType dtype;
     int64_t kv_heads, head_dim, max_seqs, max_pages;
-    PyObject* table;                              // the cache's own page table
-    PyObject* grow;                               // (stream, bytes) -> a workspace tensor
-    std::vector<std::pair<void*, PyObject*>> work;  // stream -> workspace
+    PyObject* table;  // the cache's own page table
 };
 
 constexpr const char* kCapsule = "t2i_kv";
@@ -154,6 +153,27 @@ t2i_kv_batch batch(const Cache& c, int64_t n, PyObject* lens, PyObject* starts, 
     return b;
 }
 
+// A call's workspace, from torch's allocator, for as long as the call takes: memory that is given back comes to
+// later calls on its stream alone, behind this call's kernels. While torch captures a graph on the stream it is the
+// graph's memory, and stays that. So nothing outlives a call, and threads, streams and graphs share none.
+class Workspace {
+  public:
+    Workspace(int device, uint64_t bytes, void* stream) {
+        if (!bytes) return;
+        const c10::cuda::CUDAGuard g{c10::DeviceIndex(device)};
+        p_ = c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(bytes, static_cast<cudaStream_t>(stream));
+    }
+    ~Workspace() {
+        if (p_) c10::cuda::CUDACachingAllocator::raw_delete(p_);
+    }
+    Workspace(const Workspace&) = delete;
+    Workspace& operator=(const Workspace&) = delete;
+    void* get() const { return p_; }
+
+  private:
+    void* p_ = nullptr;
+};
+
 // append(cache, k, v, lens, q, q_out, starts, max_new, layer, q_norm, k_norm, eps,
 //        cos, sin, interleaved, positions, table, stream) -> status
 PyObject* append(PyObject* const* a) {
@@ -196,7 +216,7 @@ PyObject* append(PyObject* const* a) {
 // attend(cache, q, lens, out, lse, starts, max_new, layer, scale, softcap, slopes,
 //        window, spans, tree, max_len, table, stream) -> status
 PyObject* attend(PyObject* const* a) {
-    Cache& c = cache(a[0]);
+    const Cache& c = cache(a[0]);
     const Rows q = rows(c, a[1], -1, "q", &c.dtype), o = rows(c, a[3], q.heads, "out", &c.dtype);
     if (o.n != q.n) value_error("q and out must have as many tokens");
     t2i_kv_attend_desc d{};
@@ -212,25 +232,10 @@ PyObject* attend(PyObject* const* a) {
     d.tree = static_cast<const uint64_t*>(plain(a[13], at::kLong, {q.n}, "tree"));
     d.max_len = u32(a[14], "max_len");
     void* s = stream_of(c, a[16]);
-    uint64_t need = 0;
-    if (t2i_kv_workspace_bytes(c.kv, d.batch.n_seqs, d.batch.n_tokens, d.q_heads, &need) == T2I_OK && need) {
-        std::pair<void*, PyObject*>* w = nullptr;
-        for (auto& e : c.work)
-            if (e.first == s) w = &e;
-        if (!w || uint64_t(THPVariable_Unpack(w->second).numel()) < need) {
-            PyObject* t = PyObject_CallFunction(c.grow, "KK", (unsigned long long)(uintptr_t)s, (unsigned long long)need);
-            if (!t) throw PyFail{};
-            if (!w) {
-                c.work.emplace_back(s, nullptr);
-                w = &c.work.back();
-            }
-            Py_XDECREF(w->second);
-            w->second = t;
-        }
-        const at::Tensor& t = THPVariable_Unpack(w->second);
-        d.workspace = t.data_ptr();
-        d.workspace_bytes = uint64_t(t.numel());
-    }
+    const t2i_status st = t2i_kv_workspace_bytes(c.kv, d.batch.n_seqs, d.batch.n_tokens, d.q_heads, &d.workspace_bytes);
+    if (st != T2I_OK || d.batch.n_tokens == 0) d.workspace_bytes = 0;
+    const Workspace w(c.device, d.workspace_bytes, s);
+    d.workspace = w.get();
     return PyLong_FromLong(t2i_kv_attend(c.kv, &d, s));
 }
 
@@ -250,15 +255,13 @@ PyObject* commit(PyObject* const* a) {
     return PyLong_FromLong(t2i_kv_commit(c.kv, &d, stream_of(c, a[5])));
 }
 
-// cache(kv, device, fp16, kv_heads, head_dim, table, grow) -> capsule
+// cache(kv, device, fp16, kv_heads, head_dim, table) -> capsule
 PyObject* make(PyObject* const* a) {
     const at::Tensor& t = tensor(a[5], "table");
     Cache* c = new Cache{};
     PyObject* cap = PyCapsule_New(c, kCapsule, [](PyObject* o) {
         Cache* d = static_cast<Cache*>(PyCapsule_GetPointer(o, kCapsule));
         Py_XDECREF(d->table);
-        Py_XDECREF(d->grow);
-        for (auto& w : d->work) Py_XDECREF(w.second);
         delete d;
     });
     if (!cap) {
@@ -280,8 +283,6 @@ PyObject* make(PyObject* const* a) {
     }
     Py_INCREF(a[5]);
     c->table = a[5];
-    Py_INCREF(a[6]);
-    c->grow = a[6];
     return cap;
 }
 
@@ -300,6 +301,13 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
         return F(args);
     } catch (const PyFail&) {
         return nullptr;
+    } catch (const c10::OutOfMemoryError& e) {
+        PyObject* torch = PyImport_ImportModule("torch");
+        PyObject* type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        if (type) PyErr_SetString(type, e.what_without_backtrace());
+        Py_XDECREF(type);
+        Py_XDECREF(torch);
+        return nullptr;
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
@@ -307,7 +315,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 #define ENTRY(name, f, n, doc) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f, n>)), METH_FASTCALL, doc}
-PyMethodDef methods[] = {ENTRY("cache", make, 7, "a cache's binding"),
+PyMethodDef methods[] = {ENTRY("cache", make, 6, "a cache's binding"),
                          ENTRY("close", shut, 1, "refuses later calls"),
                          ENTRY("append", append, 18, "t2i_kv_append"),
                          ENTRY("attend", attend, 17, "t2i_kv_attend"),

@@ -61,7 +61,11 @@ class KVCache:
     stride between tokens that is a multiple of 8. ``lens`` is the number of
     each sequence's tokens with the new ones (int32), ``starts`` the first new
     token of each and the end (int32), without it every sequence has as many;
-    ``max_new`` goes with it: the most new tokens of a sequence."""
+    ``max_new`` goes with it: the most new tokens of a sequence.
+
+    An attention's workspace comes from torch's allocator for the time of the
+    call. Calls that ``torch.cuda.graph`` captures have the graph's memory; a
+    capture by other means takes the C call, with a workspace that it keeps."""
 
     def __init__(self, store: Store, kv_heads: int, head_dim: int, dtype=torch.bfloat16, layers: int = 1,
                  max_seqs: int = 1, max_tokens: int = 4096, stream=None):
@@ -83,7 +87,7 @@ class KVCache:
         self._ids = [[] for _ in range(self.max_seqs)]     # the objects of each sequence, in token order
         self._pages = [0] * self.max_seqs                  # pages of each sequence
         self.table = torch.full((self.max_seqs, self.max_pages), -1, dtype=torch.int32, device=self.device)
-        self._c = _kv.cache(int(h.value), store.device, _dtype(dtype), self.kv_heads, self.head_dim, self.table, _workspace_on(self.device))
+        self._c = _kv.cache(int(h.value), store.device, _dtype(dtype), self.kv_heads, self.head_dim, self.table)
 
     def close(self):
         """Frees the pages of every sequence and the handle."""
@@ -236,12 +240,3 @@ class KVCache:
         st = _kv.commit(self._c, ctx, path, counts, table, stream)
         if st:
             self._done(st)
-
-
-def _workspace_on(device):
-    """Where the calls' workspaces come from: one a stream."""
-    def grow(stream, nbytes):
-        s = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
-        with torch.cuda.stream(s):
-            return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return grow
