@@ -52,8 +52,9 @@ class KVCache:
     device, -1 where a sequence has no page. :meth:`reserve` and
     :meth:`release` change it; after a compaction of the store call
     :meth:`refresh`. The pages belong to the stream they were last reserved,
-    refreshed or held for (:meth:`hold`): calls on other streams need a
-    ``hold`` first.
+    refreshed or held for (:meth:`hold`): calls on other streams,
+    :meth:`release` among them, need a ``hold`` first. ``stream``: a stream or
+    its address (0: the default one), None for the device's current one.
 
     The calls take the first rows of the table, one a sequence, unless
     ``table`` names others (``cache.table[slots]``). Token arrays are
@@ -86,7 +87,10 @@ class KVCache:
         self._host = np.full((self.max_seqs, self.max_pages), -1, np.int32)
         self._ids = [[] for _ in range(self.max_seqs)]     # the objects of each sequence, in token order
         self._pages = [0] * self.max_seqs                  # pages of each sequence
-        self.table = torch.full((self.max_seqs, self.max_pages), -1, dtype=torch.int32, device=self.device)
+        s = self._stream(stream)
+        with torch.cuda.stream(s):
+            self.table = torch.full((self.max_seqs, self.max_pages), -1, dtype=torch.int32, device=self.device)
+        s.synchronize()  # whichever stream writes or reads it next
         self._c = _kv.cache(int(h.value), store.device, _dtype(dtype), self.kv_heads, self.head_dim, self.table)
 
     def close(self):
@@ -106,6 +110,16 @@ class KVCache:
         except Exception:  # the interpreter is going down
             pass
 
+    def _stream(self, stream):
+        """The torch stream that a ``stream`` argument names, as the library's calls take it: None is the device's
+        current one, a number a stream's address (0: the default one)."""
+        if stream is None:
+            return torch.cuda.current_stream(self.device)
+        if isinstance(stream, torch.cuda.Stream):
+            return stream
+        at = int(stream) if isinstance(stream, int) else int(stream.cuda_stream)
+        return torch.cuda.ExternalStream(at, device=self.device) if at else torch.cuda.default_stream(self.device)
+
     # ---------------------------------------------------------------- pages
     def reserve(self, tokens, seqs=None, stream=None):
         """Pages for sequence ``seqs[i]`` (default: i) to hold ``tokens[i]``
@@ -124,6 +138,7 @@ class KVCache:
                 grow.append((s, need - self._pages[s]))
         if not grow:
             return
+        stream = self._stream(stream)
         nbytes = np.array([k for _, k in grow], np.uint64) * np.uint64(self.store.page_bytes)
         st, ids = self.store.put_batch(put_descs(np.zeros(len(grow), np.uint64), nbytes=nbytes), stream)
         self.store.check(st)
@@ -161,7 +176,7 @@ class KVCache:
     def hold(self, stream=None):
         """Gives the pages to ``stream``, after all that the stream that had
         them was given so far."""
-        self.store.check(self.store.hold(np.array([i for s in self._ids for i in s], np.uint64), stream))
+        self.store.check(self.store.hold(np.array([i for s in self._ids for i in s], np.uint64), self._stream(stream)))
 
     def pages(self, seq: int) -> list:
         """The page numbers of a sequence, in token order."""
@@ -169,8 +184,7 @@ class KVCache:
 
     def _upload(self, seqs, stream):
         lo, hi = min(seqs), max(seqs) + 1
-        s = torch.cuda.ExternalStream(stream, self.device) if isinstance(stream, int) and stream else stream or None
-        with torch.cuda.stream(s):
+        with torch.cuda.stream(self._stream(stream)):
             self.table[lo:hi].copy_(torch.from_numpy(self._host[lo:hi].copy()))
 
     # ---------------------------------------------------------------- calls

@@ -5,6 +5,7 @@ import threading
 import pytest
 import torch
 
+from paper_2607_26566_gb300 import KVCache, Store
 from kv_plain import DEV
 from test_gpu_kv import BF, case, ints, starts_of
 
@@ -113,3 +114,35 @@ def test_threads_with_streams_of_their_own():
     finally:
         sys.setswitchinterval(every)
     assert not bad, bad
+
+
+def test_a_cache_made_on_a_busy_stream_is_ready_for_any():
+    """The page table's first fill does not come after what another stream wrote to it."""
+    store = Store(torch.empty(64 << 16, dtype=torch.uint8, device=DEV), 1 << 16)
+    slow = torch.randn(4096, 4096, device=DEV)
+    s = torch.cuda.Stream()
+    for made in (None, s, s.cuda_stream, 0):
+        torch.cuda.synchronize()
+        for stream in (torch.cuda.current_stream(), s):
+            with torch.cuda.stream(stream):
+                for _ in range(10):
+                    slow = slow @ slow.clamp(-1e-3, 1e-3)
+        c = KVCache(store, 2, 64, max_seqs=2, max_tokens=400, stream=made)
+        other = torch.cuda.Stream()
+        c.reserve([300, 200], stream=other)
+        with torch.cuda.stream(other):
+            got = c.table.clone()
+        torch.cuda.synchronize()
+        for table in (got, c.table):  # as the reserving stream left it, and in the end
+            assert [[p for p in row if p >= 0] for row in table.tolist()] == [c.pages(0), c.pages(1)]
+        c.close()
+
+
+def test_a_stream_argument_names_the_same_stream_everywhere():
+    c, q, lens = split_case()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        assert c._stream(None) == s
+        assert c._stream(0) == torch.cuda.default_stream(DEV)
+        assert c._stream(s.cuda_stream).cuda_stream == s.cuda_stream
+    assert c._stream(s) is s
