@@ -54,7 +54,9 @@ class KVCache:
     :meth:`refresh`. The pages belong to the stream they were last reserved,
     refreshed or held for (:meth:`hold`): calls on other streams,
     :meth:`release` among them, need a ``hold`` first. ``stream``: a stream or
-    its address (0: the default one), None for the device's current one.
+    its address (0: the default one), None for the device's current one; an
+    output that a call makes belongs to the call's stream, like a tensor made
+    on it.
 
     The calls take the first rows of the table, one a sequence, unless
     ``table`` names others (``cache.table[slots]``). Token arrays are
@@ -188,6 +190,13 @@ class KVCache:
             self.table[lo:hi].copy_(torch.from_numpy(self._host[lo:hi].copy()))
 
     # ---------------------------------------------------------------- calls
+    def _output(self, q, stream):
+        # (of the stream that writes it: torch's allocator goes by the stream that a block was made on)
+        if stream is None:
+            return torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        with torch.cuda.stream(self._stream(stream)):
+            return torch.empty(q.shape, dtype=self.dtype, device=self.device)
+
     def _done(self, st):
         raise T2IError(st, self.store.last_error())
 
@@ -203,7 +212,7 @@ class KVCache:
         ``positions``: int32 [tokens], a token's slot by default. In fp32, rounded
         once. Returns ``q_out`` (made where only ``q`` is given)."""
         if q_out is None and q is not None:
-            q_out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            q_out = self._output(q, stream)
         st = _kv.append(self._c, k, v, lens, q, q_out, starts, max_new, layer, q_norm, k_norm, eps, cos, sin, interleaved,
                         positions, table, stream)
         if st:
@@ -223,7 +232,7 @@ class KVCache:
         ``max_len``: the longest of ``lens``, where the caller knows it (it only
         sets how the work is split)."""
         if out is None:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            out = self._output(q, stream)
         st = _kv.attend(self._c, q, lens, out, lse, starts, max_new, layer, self._scale if scale is None else scale, softcap,
                         slopes, window, spans, None, max_len, table, stream)
         if st:
@@ -240,7 +249,7 @@ class KVCache:
         if tree is None:
             raise TypeError("tree must be a tensor")
         if out is None:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            out = self._output(q, stream)
         st = _kv.attend(self._c, q, lens, out, lse, starts, max_new, layer, self._scale if scale is None else scale, softcap,
                         slopes, window, None, tree, max_len, table, stream)
         if st:

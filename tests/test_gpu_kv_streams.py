@@ -146,3 +146,26 @@ def test_a_stream_argument_names_the_same_stream_everywhere():
         assert c._stream(0) == torch.cuda.default_stream(DEV)
         assert c._stream(s.cuda_stream).cuda_stream == s.cuda_stream
     assert c._stream(s) is s
+
+
+def test_an_output_belongs_to_the_stream_that_writes_it():
+    """What a call with a stream makes comes from that stream's memory and goes back to it."""
+    c, q, lens = split_case()
+    kv = torch.zeros(3, 2, 128, dtype=BF, device=DEV)
+    one = torch.ones(3, dtype=torch.int64, device=DEV)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for call in (lambda: c.attend(q, lens, stream=s), lambda: c.attend(q, lens, stream=s.cuda_stream),
+                 lambda: c.attend_tree(q, lens, one, stream=s), lambda: c.append(kv, kv, lens, q=q, stream=s)):
+        with torch.cuda.stream(s):
+            mine = torch.empty_like(q)
+        at = mine.data_ptr()
+        del mine
+        out = call()
+        assert out.data_ptr() == at       # the block that the stream had free
+        torch.cuda.synchronize()
+        del out
+        keep = [torch.empty_like(q) for _ in range(8)]
+        assert all(x.data_ptr() != at for x in keep)
+        with torch.cuda.stream(s):
+            assert torch.empty_like(q).data_ptr() == at
