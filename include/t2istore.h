@@ -390,6 +390,9 @@ t2i_status t2i_gather_noalloc(const void* pool_dev, uint64_t pool_bytes, uint64_
  * enqueued). What lies in device memory cannot be: a page number outside the
  * pool, or a slot behind a table row's end, is never written and reads as
  * rows of zeros; a sequence whose bounds make no sense has no tokens.
+ * An attention whose own loads do not come within a second gives up and
+ * writes results that are not valid; the next call on the handle that has
+ * work to do returns CUDA, once, and enqueues nothing.
  * Order with other calls of the store comes from t2i_hold.
  * ========================================================================= */
 
@@ -516,6 +519,11 @@ typedef struct t2i_kv_attend_desc {
  * (its weight there is 0, and 0 times it is not 0). With a tree, all drafted
  * tokens count as seen, and the slots in the window of the one before them. */
 t2i_status t2i_kv_attend(t2i_kv* kv, const t2i_kv_attend_desc* desc, void* cuda_stream);
+
+/* Testing support: the countdown-th attention of this handle from now (0
+ * cancels) is launched without its loads, so that its kernels wait for them
+ * until they give up.                                                       */
+t2i_status t2i_kv_inject_timeout(t2i_kv* kv, uint32_t countdown);
 
 /* Workspace bytes that t2i_kv_attend needs for such a batch at most.         */
 t2i_status t2i_kv_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads,

@@ -107,6 +107,7 @@ PROTOTYPES = {
     "t2i_kv_attend": (_S, [_P, _P, _P]),
     "t2i_kv_workspace_bytes": (_S, [_P, _U32, _U32, _U32, _PU64]),
     "t2i_kv_commit": (_S, [_P, _P, _P]),
+    "t2i_kv_inject_timeout": (_S, [_P, _U32]),
     "t2i_e2e_latency": (_S, [_U32, _U32, C.c_double, C.c_double, C.POINTER(C.c_double)]),
     "t2i_prefix_layers": (_S, [_U32, C.c_double, C.c_double, _PU32]),
     "t2i_pipeline_latency": (_S, [C.POINTER(C.c_double), C.POINTER(C.c_double), _U32, _U32, C.POINTER(C.c_double)]),

@@ -23,6 +23,7 @@ struct t2i_kv {
     uint32_t* fault;       // pinned: a kernel's wait ran out
     uint32_t* fault_dev;
     CUtensorMap map;
+    uint32_t timeout_countdown;  // t2i_kv_inject_timeout
 };
 
 namespace t2i {
@@ -172,10 +173,11 @@ t2i_status launch(t2i_kv* kv, const char* call, Launch&& go) {
 }
 
 // Reported once, by the first call after it: what the kernel wrote is not valid.
-t2i_status past_fault(t2i_kv* kv) {
+t2i_status past_fault(t2i_kv* kv, const char* call) {
     if (*static_cast<volatile uint32_t*>(kv->fault) == 0) return T2I_OK;
     *kv->fault = 0;
-    store_set_error(kv->store, "an earlier attention kernel gave up waiting for its own loads: its results are not valid");
+    store_set_error(kv->store, std::string(call) + ": an earlier attention kernel gave up waiting for its own loads: "
+                                                   "its results are not valid, and this call did nothing");
     return T2I_ERR_CUDA;
 }
 
@@ -189,6 +191,8 @@ t2i_status append(t2i_kv* kv, const t2i_kv_append_desc& d, cudaStream_t stream) 
     c.require(!d.rotary_dim || (d.n_positions > 0 && d.n_positions <= 0x7FFFFFFFu), "a rotation needs n_positions rows of its tables");
     c.require(!(d.q_norm || d.k_norm) || (std::isfinite(d.eps) && d.eps >= 0.0f), "eps must be finite and not negative");
     if (!c.batch(d.batch)) return c.ok() ? T2I_OK : T2I_ERR_INVALID;
+    const t2i_status past = past_fault(kv, "kv_append");
+    if (past != T2I_OK) return past;
     const uint64_t n = d.batch.n_tokens;
     const uint32_t in = d.in_dtype == T2I_F32 ? 4 : 2;
     if (d.q) {
@@ -245,7 +249,7 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     c.require(d.batch.max_new || !d.batch.starts, "with starts, max_new must be given");
     if (!c.batch(d.batch)) return c.ok() ? T2I_OK : T2I_ERR_INVALID;
     KvAttend a{};
-    const t2i_status past = past_fault(kv);
+    const t2i_status past = past_fault(kv, "kv_attend");
     if (past != T2I_OK) return past;
     a.tok = tokens_of(d.batch);
     c.require(!d.tree || a.tok.max_new <= 64, "a tree has at most 64 tokens");
@@ -274,7 +278,8 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     a.max_len = d.max_len ? std::min(d.max_len, d.batch.table_pages << kv->token_shift) : d.batch.table_pages << kv->token_shift;
     a.scale = d.scale;
     a.softcap = d.softcap;
-    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms};
+    const uint32_t no_loads = kv->timeout_countdown && --kv->timeout_countdown == 0;
+    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms, no_loads};
     const bool bf16 = kv->layout.dtype == T2I_BF16;
     return launch(kv, "kv_attend", [&] {
         if (uint64_t(a.group) * a.tok.max_new <= kFewRows) return bf16 ? launch_kv_few_bf16(a, l, stream) : launch_kv_few_f16(a, l, stream);
@@ -288,6 +293,8 @@ t2i_status commit(t2i_kv* kv, const t2i_kv_commit_desc& d, cudaStream_t stream) 
     c.require(d.n_seqs <= 0x7FFFFFFFu && d.max_path <= 0x7FFFFFFFu, "too many sequences or path entries");
     if (!c.ok()) return T2I_ERR_INVALID;
     if (d.n_seqs == 0 || d.max_path == 0) return T2I_OK;
+    const t2i_status past = past_fault(kv, "kv_commit");
+    if (past != T2I_OK) return past;
     c.table(d.table, d.table_stride, d.table_pages, d.n_seqs);
     c.range("ctx", d.ctx, uint64_t(d.n_seqs) * 4, 4);
     c.range("path", d.path, uint64_t(d.n_seqs) * d.max_path * 4, 4);
@@ -437,6 +444,13 @@ t2i_status t2i_kv_commit(t2i_kv* kv, const t2i_kv_commit_desc* desc, void* cuda_
 t2i_status t2i_kv_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, uint64_t* out) {
     if (!kv || !out) return T2I_ERR_INVALID;
     *out = t2i::workspace_bytes(kv, n_seqs, n_tokens, q_heads);
+    return T2I_OK;
+}
+
+t2i_status t2i_kv_inject_timeout(t2i_kv* kv, uint32_t countdown) {
+    if (!kv) return T2I_ERR_INVALID;
+    std::lock_guard<std::mutex> lock(t2i::store_mutex(kv->store));
+    kv->timeout_countdown = countdown;
     return T2I_OK;
 }
 

@@ -95,6 +95,7 @@ struct KvLaunch {
     void* workspace;
     uint32_t* fault;  // host memory that the device writes: not 0 after a wait that ran out
     uint32_t sms;
+    uint32_t no_loads;  // testing: the loading warps do nothing
 };
 // Up to this many queries to a key head (new tokens of a sequence x heads of a group) kv_few.cuh, above it
 // kv_rows.cuh. Queries, and us of the one / the other, for a sequence of 1.5k slots, 24 of 8k (heads of 128) and 3 of

@@ -108,6 +108,7 @@ struct Few {
     Join* join;        // [blocks]
     float* part;       // [2 * blocks][kPart]
     uint32_t* fault;   // host-mapped: set where a wait ran out
+    uint32_t no_loads; // testing: nothing is loaded or handed out, so that waits run out
 };
 
 __device__ __forceinline__ int32_t unit_tiles(const KvAttend& a, const KvSeq& q, KvSpan& sp) {
@@ -208,6 +209,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
     if (warp == 5) tmem_alloc(smem_u32(&sh.tmem), Sh::kTmem);
     pdl_launch();
     pdl_wait();
+    if (tid == 0) f.join[blockIdx.x].valid = 0;  // (also where a wait runs out before the note is written)
 
     // the block's run of tiles
     const int64_t K = a.pages.kv_heads;
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             ++u;
             return true;
         };
-        do {
+        for (bool more = !f.no_loads; more; more = walk_next(a, w)) {
             ask();
             const int32_t row_k = int32_t(((a.pages.layer * 2) * a.pages.kv_heads + w.h) << shift);
             const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                     }
                 }
             }
-        } while (walk_next(a, w));
+        }
     loads_done:
         __syncwarp();
         if (*dead) {  // the copies in flight land before the block ends
@@ -613,7 +615,6 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             if (!more) break;
         }
     }
-    if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
     __syncthreads();
     if (tid == 0 && *dead) *f.fault = 1;
     if (warp == 5) {
@@ -722,6 +723,7 @@ cudaError_t launch_few(const KvAttend& a, const KvLaunch& l, cudaStream_t stream
     f.join = static_cast<Join*>(l.workspace);
     f.part = reinterpret_cast<float*>(static_cast<uint8_t*>(l.workspace) + join_bytes(l.sms));
     f.fault = l.fault;
+    f.no_loads = l.no_loads;
     return launch_t<T>(f, *l.map, l.sms, stream);
 }
 

@@ -102,6 +102,7 @@ struct Rows {
     Join* join;        // [blocks]
     float* part;       // [2 * blocks][kRowPart]
     uint32_t* fault;
+    uint32_t no_loads; // testing: nothing is loaded or handed out, so that waits run out
 };
 
 __device__ __forceinline__ int32_t row_tiles(const KvAttend& a, const KvSeq& q) {
@@ -338,6 +339,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
     if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
     pdl_launch();
     pdl_wait();
+    if (tid == 0) f.join[blockIdx.x].valid = 0;
 
     const bool own = f.most <= kOwnPlan;
     const PlanTile* const plan = own ? sh.plan : f.plan;
@@ -397,13 +399,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 ++u;
                 return true;
             };
-            publish();
+            if (!f.no_loads) publish();
             const uint32_t shift = a.pages.token_shift;
             const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
             const uint32_t mask = (1u << shift) - 1;
             const int halves = D > 64 ? 2 : 1;
             uint32_t n = 0;
-            bool more = !none;
+            bool more = !none && !f.no_loads;
             while (more) {
                 const int32_t row_k = int32_t((a.pages.layer * 2 * a.pages.kv_heads + w.h) << shift);
                 const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
@@ -586,7 +588,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 // this run's note of a unit that began in the run before it
                 const int64_t u0 = o.at - o.tile;
                 const int64_t b0 = ((u0 + 1) * blocks - 1) / total, b1 = ((u0 + o.nt) * blocks - 1) / total;
-                const bool here = o.n > 0 && o.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
+                const bool here = !gone && o.n > 0 && o.tile > 0 && b0 + 1 == int64_t(blockIdx.x);
                 f.join[blockIdx.x] = {o.q.first, o.m, o.rows, o.h, int32_t(b0), int32_t(b1), b0 * total / blocks != u0, here};
             }
             load_q(o);
@@ -803,7 +805,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
             done_with(u);
         }
     }
-    if (!busy && tid == 0) f.join[blockIdx.x].valid = 0;
     __syncthreads();
     if (tid == 0 && *dead) *f.fault = 1;
     if (warp == 9) {
@@ -902,6 +903,7 @@ cudaError_t launch_rows(const KvAttend& a, const KvLaunch& l, cudaStream_t strea
     p += up256(uint64_t(f.most) * sizeof(PlanTile));
     f.part = reinterpret_cast<float*>(p);
     f.fault = l.fault;
+    f.no_loads = l.no_loads;
     const Mod mod = mod_of(a);
     // (Without Mod::kNone scores are scaled before they are masked: a scale of 0 would turn a masked -infinity into NaN.)
     const bool none = mod == Mod::kNone && a.scale != 0.0f;

@@ -263,3 +263,7 @@ class KVCache:
         st = _kv.commit(self._c, ctx, path, counts, table, stream)
         if st:
             self._done(st)
+
+    def inject_timeout(self, countdown: int):
+        """t2i_kv_inject_timeout (testing)."""
+        self._lib.t2i_kv_inject_timeout(self._h, countdown)
