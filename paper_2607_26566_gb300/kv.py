@@ -94,9 +94,11 @@ class KVCache:
             self.table = torch.full((self.max_seqs, self.max_pages), -1, dtype=torch.int32, device=self.device)
         s.synchronize()  # whichever stream writes or reads it next
         self._c = _kv.cache(int(h.value), store.device, _dtype(dtype), self.kv_heads, self.head_dim, self.table)
+        store._users.add(self)
 
     def close(self):
-        """Frees the pages of every sequence and the handle."""
+        """Frees the pages of every sequence and the handle; later calls are
+        refused. Closing the store closes its caches."""
         if getattr(self, "_h", None):
             if self.store._h:
                 ids = [i for s in self._ids for i in s]
@@ -122,11 +124,16 @@ class KVCache:
         at = int(stream) if isinstance(stream, int) else int(stream.cuda_stream)
         return torch.cuda.ExternalStream(at, device=self.device) if at else torch.cuda.default_stream(self.device)
 
+    def _open(self):
+        if not getattr(self, "_h", None):
+            raise ValueError("the cache is closed")
+
     # ---------------------------------------------------------------- pages
     def reserve(self, tokens, seqs=None, stream=None):
         """Pages for sequence ``seqs[i]`` (default: i) to hold ``tokens[i]``
         tokens; sequences that hold as many already keep theirs. All or
         nothing: T2IError (NOSPACE) where the store has no room."""
+        self._open()
         seqs = range(len(tokens)) if seqs is None else [int(s) for s in seqs]
         if len(seqs) != len(tokens) or len(set(seqs)) != len(seqs):
             raise ValueError("one number of tokens for each sequence, each named once")
@@ -157,6 +164,7 @@ class KVCache:
 
     def release(self, seqs, stream=None):
         """Gives the pages of these sequences back to the store."""
+        self._open()
         seqs = [int(s) for s in seqs]
         ids = [i for s in dict.fromkeys(seqs) for i in self._ids[s]]
         if not ids:
@@ -178,6 +186,7 @@ class KVCache:
     def hold(self, stream=None):
         """Gives the pages to ``stream``, after all that the stream that had
         them was given so far."""
+        self._open()
         self.store.check(self.store.hold(np.array([i for s in self._ids for i in s], np.uint64), self._stream(stream)))
 
     def pages(self, seq: int) -> list:
@@ -266,4 +275,5 @@ class KVCache:
 
     def inject_timeout(self, countdown: int):
         """t2i_kv_inject_timeout (testing)."""
+        self._open()
         self._lib.t2i_kv_inject_timeout(self._h, countdown)

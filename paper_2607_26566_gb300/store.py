@@ -9,6 +9,7 @@ not a Python loop per object.
 from __future__ import annotations
 
 import ctypes as C
+import weakref
 
 import numpy as np
 
@@ -219,6 +220,7 @@ class Store:
     def __init__(self, pool, page_bytes: int, pool_bytes: int | None = None, device: int | None = None,
                  h2d_mode: int = 0, check_pointers: int = 1, alloc_policy: int = 0, d2h_mode: int = 0):
         self._lib = L.load()
+        self._users = weakref.WeakSet()  # what has a handle of the store (caches): closed before it
         self.pool = pool
         if pool_bytes is None:
             pool_bytes = _nbytes(pool)
@@ -239,6 +241,8 @@ class Store:
 
     def close(self):
         if getattr(self, "_h", None):
+            for user in list(self._users):
+                user.close()
             self._lib.t2i_store_destroy(self._h)
             self._h = None
             self._hi = 0

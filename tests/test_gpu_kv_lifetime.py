@@ -1,0 +1,49 @@
+"""The key/value cache's beginning and end (marked gpu): handles, pages and stores that
+are closed in any order."""
+import pytest
+import torch
+
+from paper_2607_26566_gb300 import KVCache, Store
+from kv_plain import DEV, make_cache
+from test_gpu_kv import BF, ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built(lib):
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    yield
+
+
+def every_call(c):
+    x = torch.zeros(1, 1, 64, dtype=BF, device=DEV)
+    one = ints([1])
+    return (lambda: c.append(x, x, one), lambda: c.attend(x, one), lambda: c.commit(one, one.view(1, 1), one),
+            lambda: c.attend_tree(x, one, torch.ones(1, dtype=torch.int64, device=DEV)), lambda: c.reserve([50]),
+            lambda: c.release([0]), c.refresh, c.hold, lambda: c.inject_timeout(1))
+
+
+def test_a_store_closed_before_its_caches_closes_them():
+    a = make_cache(1, 64, BF, [10])
+    b = KVCache(a.store, 1, 64, max_tokens=100)
+    gone = KVCache(a.store, 1, 64, max_tokens=100)
+    del gone
+    a.store.close()
+    for c in (a, b):
+        for call in every_call(c):
+            with pytest.raises(ValueError, match="closed"):
+                call()
+        c.close()
+    a.store.close()
+
+
+def test_a_closed_cache_takes_no_pages():
+    c = make_cache(1, 64, BF, [10])
+    c.close()
+    assert c.store.stats()["used_pages"] == 0
+    for call in every_call(c):
+        with pytest.raises(ValueError, match="closed"):
+            call()
+    assert c.store.stats()["used_pages"] == 0
+    c.close()
