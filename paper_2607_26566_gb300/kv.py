@@ -165,8 +165,11 @@ class KVCache:
     def release(self, seqs, stream=None):
         """Gives the pages of these sequences back to the store."""
         self._open()
-        seqs = [int(s) for s in seqs]
-        ids = [i for s in dict.fromkeys(seqs) for i in self._ids[s]]
+        seqs = list(dict.fromkeys(int(s) for s in seqs))
+        for s in seqs:
+            if not 0 <= s < self.max_seqs:
+                raise ValueError(f"sequence {s} is outside the cache ({self.max_seqs} sequences)")
+        ids = [i for s in seqs for i in self._ids[s]]
         if not ids:
             return
         self.store.check(self.store.free(np.array(ids, np.uint64)))

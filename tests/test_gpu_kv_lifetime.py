@@ -47,3 +47,15 @@ def test_a_closed_cache_takes_no_pages():
             call()
     assert c.store.stats()["used_pages"] == 0
     c.close()
+
+
+def test_a_sequence_that_is_none_is_not_released():
+    """(Python would count -1 from the end, and the page table keep what was freed.)"""
+    c = make_cache(1, 64, BF, [10, 20])
+    pages, table = [c.pages(0), c.pages(1)], c.table.clone()
+    for seqs in ([-1], [2], [0, -2], [0, 5]):
+        with pytest.raises(ValueError, match="outside the cache"):
+            c.release(seqs)
+    assert [c.pages(0), c.pages(1)] == pages and torch.equal(c.table, table)
+    c.release([1, 1])
+    assert c.pages(1) == [] and (c.table[1] == -1).all() and torch.equal(c.table[0], table[0])
