@@ -75,12 +75,6 @@ class KVCache:
         self._lib = L.load()
         self.store, self.dtype = store, dtype
         self.layers, self.kv_heads, self.head_dim = int(layers), int(kv_heads), int(head_dim)
-        lay = L.KvLayout(self.layers, self.kv_heads, self.head_dim, _dtype(dtype))
-        h = C.c_void_p()
-        st = self._lib.t2i_kv_create(store._h, C.byref(lay), C.byref(h))
-        if st != L.OK:
-            raise T2IError(st, self._lib.t2i_last_error(None).decode())
-        self._h = h
         self._scale = self.head_dim ** -0.5
         self.page_tokens = page_tokens(store.page_bytes, kv_heads, head_dim, dtype, layers)
         self.max_seqs = int(max_seqs)
@@ -93,7 +87,18 @@ class KVCache:
         with torch.cuda.stream(s):
             self.table = torch.full((self.max_seqs, self.max_pages), -1, dtype=torch.int32, device=self.device)
         s.synchronize()  # whichever stream writes or reads it next
-        self._c = _kv.cache(int(h.value), store.device, _dtype(dtype), self.kv_heads, self.head_dim, self.table)
+        # the handle last: a cache that could not be made leaves none behind
+        lay = L.KvLayout(self.layers, self.kv_heads, self.head_dim, _dtype(dtype))
+        h = C.c_void_p()
+        st = self._lib.t2i_kv_create(store._h, C.byref(lay), C.byref(h))
+        if st != L.OK:
+            raise T2IError(st, self._lib.t2i_last_error(None).decode())
+        try:
+            self._c = _kv.cache(int(h.value), store.device, _dtype(dtype), self.kv_heads, self.head_dim, self.table)
+        except BaseException:
+            self._lib.t2i_kv_destroy(h)
+            raise
+        self._h = h
         store._users.add(self)
 
     def close(self):

@@ -59,3 +59,38 @@ def test_a_sequence_that_is_none_is_not_released():
     assert [c.pages(0), c.pages(1)] == pages and torch.equal(c.table, table)
     c.release([1, 1])
     assert c.pages(1) == [] and (c.table[1] == -1).all() and torch.equal(c.table[0], table[0])
+
+
+@pytest.mark.parametrize("where", ["full", "cache"])
+def test_a_cache_that_cannot_be_made_leaves_nothing(monkeypatch, where):
+    from paper_2607_26566_gb300 import kv
+
+    class Counting:
+        def __init__(self, lib):
+            self.lib, self.handles = lib, 0
+
+        def __getattr__(self, name):
+            f = getattr(self.lib, name)
+            return {"t2i_kv_create": lambda *a: self.made(f(*a)), "t2i_kv_destroy": lambda h: self.gone(f(h))}.get(name, f)
+
+        def made(self, st):
+            self.handles += st == 0
+            return st
+
+        def gone(self, st):
+            self.handles -= 1
+            return st
+
+    def fails(*a, **k):
+        raise MemoryError("none left")
+
+    store = Store(torch.empty(64 << 16, dtype=torch.uint8, device=DEV), 1 << 16)
+    lib = Counting(kv.L.load())
+    with monkeypatch.context() as m:
+        m.setattr(kv.L, "load", lambda: lib)
+        KVCache(store, 2, 64).close()
+        assert lib.handles == 0
+        m.setattr(kv.torch if where == "full" else kv._kv, where, fails)
+        with pytest.raises(MemoryError):
+            KVCache(store, 2, 64)
+    assert lib.handles == 0 and not list(store._users)
