@@ -450,7 +450,8 @@ typedef struct t2i_kv_batch {
 } t2i_kv_batch;
 
 /* Token arrays are [n_tokens][heads][head_dim], heads contiguous, *_stride
- * elements from token to token: 16-byte aligned, strides multiples of 8.    */
+ * elements from token to token: 16-byte aligned, strides multiples of 8
+ * (of one token alone any).                                                 */
 typedef struct t2i_kv_append_desc {
     t2i_kv_batch batch;
     const void* q;          /* NULL with q_out NULL: keys and values only    */

@@ -61,7 +61,7 @@ class KVCache:
     The calls take the first rows of the table, one a sequence, unless
     ``table`` names others (``cache.table[slots]``). Token arrays are
     [tokens, heads, head_dim], the heads of a token next to one another, any
-    stride between tokens that is a multiple of 8. ``lens`` is the number of
+    stride between tokens that is a multiple of 8 (of one token any). ``lens`` is the number of
     each sequence's tokens with the new ones (int32), ``starts`` the first new
     token of each and the end (int32), without it every sequence has as many;
     ``max_new`` goes with it: the most new tokens of a sequence.

@@ -152,3 +152,18 @@ def test_bits_behind_a_drafts_tokens_count_nothing(group):
                slopes=opt["slopes"].to(DEV))
     want, _ = check(c, lens, new, kvs, q, tree=own, **opt)
     assert torch.equal(c.attend_tree(q.to(DEV), ints(lens), tree.to(DEV), **how), want)
+
+
+def test_one_token_has_no_stride():
+    """Whatever lies between tokens does not matter where there is one."""
+    from kv_plain import read_rows
+    c, lens, kvs, q = case(BF, 4, 2, 64, [1], [20])
+    want = c.attend(q.to(DEV), ints(lens))
+    odd = lambda x, s: torch.as_strided(x, x.shape, (s, x.shape[2], 1))  # noqa: E731
+    assert torch.equal(c.attend(odd(q.to(DEV), 259), ints(lens)), want)
+    out = odd(torch.zeros(1, 4, 64, dtype=BF, device=DEV), 1)
+    c.attend(q.to(DEV), ints(lens), out=out)
+    assert torch.equal(out, want)
+    k = torch.randn(1, 2, 64, device=DEV).to(BF)
+    c.append(odd(k, 3), odd(k, 5), ints(lens), q=odd(q.to(DEV), 7), q_out=out)
+    assert torch.equal(read_rows(c, 0, 0, lens[0])[:, -1], k.expand(2, 2, 64)) and torch.equal(out, q.to(DEV))
