@@ -458,7 +458,8 @@ typedef struct t2i_kv_append_desc {
     const void* k;
     const void* v;
     void* q_out;            /* of the layout's dtype; may be q itself, with
-                               the same dtype and stride                     */
+                               the same dtype and stride; its rows share no
+                               byte with k's and v's                         */
     uint64_t q_stride, k_stride, v_stride, q_out_stride;
     const float* q_norm;    /* device, [head_dim]; NULL: no norm             */
     const float* k_norm;

@@ -128,6 +128,23 @@ bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
     return x < y + nb && y < x + na;
 }
 
+// Whether rows of two token arrays (n rows each; bytes of a row, and from row to row) share a byte. Rows of one fused
+// projection lie between one another and share none.
+struct TokenRows {
+    const void* p;
+    uint64_t bytes, stride;
+};
+bool overlap(const TokenRows& a, const TokenRows& b, uint64_t n) {
+    if (n > 1 && (a.stride != b.stride || !a.stride))
+        return overlap(a.p, (n - 1) * a.stride + a.bytes, b.p, (n - 1) * b.stride + b.bytes);
+    // row i of b lies d + (i - j) * stride behind row j of a: the first i - j that reaches into it
+    const int64_t d = int64_t(reinterpret_cast<uint64_t>(b.p) - reinterpret_cast<uint64_t>(a.p));
+    const int64_t s = n > 1 ? int64_t(a.stride) : 1, most = int64_t(n) - 1, past = -int64_t(b.bytes) - d;
+    int64_t m = past / s - (past % s < 0 ? 1 : 0) + 1;  // (above past / s)
+    if (m < -most) m = -most;
+    return m <= most && d + m * s < int64_t(a.bytes);
+}
+
 KvPages pages_of(const t2i_kv* kv, const int32_t* table, uint64_t stride, uint32_t table_pages, uint32_t layer) {
     KvPages p{};
     p.pool = kv->info.pool;
@@ -212,11 +229,11 @@ t2i_status append(t2i_kv* kv, const t2i_kv_append_desc& d, cudaStream_t stream) 
     if (!c.ok()) return T2I_ERR_INVALID;
     if (d.q) {
         const bool in_place = d.q == d.q_out && d.in_dtype == kv->layout.dtype && (d.q_stride == d.q_out_stride || n == 1);
-        const uint64_t qb = c.token_bytes(n, d.q_heads, d.q_out_stride, 2);
-        c.require(in_place || (!overlap(d.q_out, qb, d.q, c.token_bytes(n, d.q_heads, d.q_stride, in)) &&
-                               !overlap(d.q_out, qb, d.k, c.token_bytes(n, K, d.k_stride, in)) &&
-                               !overlap(d.q_out, qb, d.v, c.token_bytes(n, K, d.v_stride, in))),
-                  "q_out overlaps q, k or v without being q itself");
+        const uint64_t row = uint64_t(D) * in;
+        const TokenRows to{d.q_out, uint64_t(d.q_heads) * D * 2, d.q_out_stride * 2};
+        c.require(in_place || !overlap(to, {d.q, d.q_heads * row, d.q_stride * in}, n), "q_out overlaps q without being q itself");
+        c.require(!overlap(to, {d.k, K * row, d.k_stride * in}, n) && !overlap(to, {d.v, K * row, d.v_stride * in}, n),
+                  "q_out overlaps k or v");
         if (!c.ok()) return T2I_ERR_INVALID;
     }
     KvAppend a{};

@@ -167,3 +167,28 @@ def test_one_token_has_no_stride():
     k = torch.randn(1, 2, 64, device=DEV).to(BF)
     c.append(odd(k, 3), odd(k, 5), ints(lens), q=odd(q.to(DEV), 7), q_out=out)
     assert torch.equal(read_rows(c, 0, 0, lens[0])[:, -1], k.expand(2, 2, 64)) and torch.equal(out, q.to(DEV))
+
+
+@pytest.mark.parametrize("n", [1, 5])
+def test_queries_in_place_beside_their_keys_and_values(n):
+    """In one fused projection's rows; keys and values that lie in the queries' own rows
+    would be read while they are written, and are refused."""
+    from kv_plain import read_rows
+    from paper_2607_26566_gb300 import T2IError
+    c, lens, _, _ = case(BF, 4, 2, 64, [n], [20])
+    x = torch.randn(n + 1, (4 + 2 * 2) * 64, device=DEV).to(BF)
+    q, k, v = (y.view(-1, h, 64) for y, h in zip(x.split([256, 128, 128], 1), (4, 2, 2)))
+    L, w = ints(lens), torch.rand(64, device=DEV) + 0.5
+    want = c.append(k[:n], v[:n], L, q=q[:n], q_norm=w)
+    before = c.store.pool.clone(), x.clone()
+    bad = [(q[:n, :2], v[:n]), (k[:n], q[:n, 2:]), (q[:n, 1:3], v[:n])]
+    if n > 1:
+        bad += [(q[1:n + 1, :2], v[:n]), (k[:n].contiguous(), x.view(-1)[64 * 8 * n - 256 - 64:][:n * 128].view(n, 2, 64))]
+    for kk, vv in bad:
+        with pytest.raises(T2IError, match="INVALID.*overlaps k or v"):
+            c.append(kk, vv, L, q=q[:n], q_out=q[:n], q_norm=w)
+    torch.cuda.synchronize()
+    assert torch.equal(c.store.pool, before[0]) and torch.equal(x, before[1])
+    assert c.append(k[:n], v[:n], L, q=q[:n], q_out=q[:n], q_norm=w) is not None
+    assert torch.equal(q[:n], want) and torch.equal(x[n], before[1][n]) and torch.equal(k, before[1][:, 256:384].view(-1, 2, 64))
+    assert torch.equal(read_rows(c, 0, 0, lens[0])[:, -n:], torch.stack([k[:n], v[:n]]))
