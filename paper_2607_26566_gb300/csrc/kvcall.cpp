@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/core/TensorBase.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -47,7 +48,10 @@ struct PyFail {};  // a Python error is set
 
 const at::Tensor& tensor(PyObject* o, const char* name) {
     if (!THPVariable_Check(o)) type_error(std::string(name) + " must be a tensor");
-    return THPVariable_Unpack(o);
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        value_error(std::string(name) + " requires a gradient, and the cache's calls have none: detach it, or call under torch.no_grad()");
+    return t;
 }
 
 int64_t integer(PyObject* o, const char* name, int64_t most) {

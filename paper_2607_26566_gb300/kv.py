@@ -66,6 +66,9 @@ class KVCache:
     token of each and the end (int32), without it every sequence has as many;
     ``max_new`` goes with it: the most new tokens of a sequence.
 
+    The calls have no gradients: a tensor that requires one is refused unless
+    gradients are off (``torch.no_grad()``).
+
     An attention's workspace comes from torch's allocator for the time of the
     call. Calls that ``torch.cuda.graph`` captures have the graph's memory; a
     capture by other means takes the C call, with a workspace that it keeps."""

@@ -192,3 +192,27 @@ def test_queries_in_place_beside_their_keys_and_values(n):
     assert c.append(k[:n], v[:n], L, q=q[:n], q_out=q[:n], q_norm=w) is not None
     assert torch.equal(q[:n], want) and torch.equal(x[n], before[1][n]) and torch.equal(k, before[1][:, 256:384].view(-1, 2, 64))
     assert torch.equal(read_rows(c, 0, 0, lens[0])[:, -n:], torch.stack([k[:n], v[:n]]))
+
+
+def test_a_gradient_is_not_lost_without_a_word():
+    c, lens, kvs, q = case(BF, 4, 2, 64, [2], [20])
+    q, L = q.to(DEV), ints(lens)
+    kv = torch.zeros(2, 2, 64, dtype=BF, device=DEV)
+    grad = lambda x: x.clone().requires_grad_()  # noqa: E731
+    w = torch.ones(64, device=DEV)
+    calls = (lambda: c.attend(grad(q), L), lambda: c.append(grad(kv), kv, L), lambda: c.append(kv, grad(kv), L),
+             lambda: c.append(kv, kv, L, q=grad(q)), lambda: c.append(kv, kv, L, k_norm=grad(w)),
+             lambda: c.attend(q, L, slopes=grad(w[:4])))
+    before = c.store.pool.clone()
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    torch.cuda.synchronize()
+    assert torch.equal(c.store.pool, before)
+    for off in (torch.no_grad, torch.inference_mode):
+        want = c.attend(q, L)  # (the appends below change the cache)
+        with off():
+            assert torch.equal(c.attend(grad(q), L), want)
+            for call in calls:
+                call()
+    assert torch.equal(c.attend(grad(q).detach(), L), c.attend(q, L))
