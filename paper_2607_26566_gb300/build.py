@@ -8,6 +8,7 @@ machine without a GPU driver (only the t2i_ctl_* calls work there).
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -66,8 +67,25 @@ def _have_python_h() -> bool:
     return os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h"))
 
 
+def _torch_dir() -> str | None:
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else None
+
+
+def _no_kvcall() -> str | None:
+    """Why the key/value cache's binding cannot be built here (None: it can)."""
+    if not _have_python_h():
+        return "Python.h not found"
+    torch_dir = _torch_dir()
+    if torch_dir is None:
+        return "torch not found"
+    if not os.path.exists(os.path.join(torch_dir, "lib", "libc10_cuda.so")):
+        return "torch has no CUDA"
+    return None
+
+
 def is_stale() -> bool:
-    outs = [LIB] + ([PYCALL, KVCALL] if _have_python_h() else [])
+    outs = [LIB] + ([PYCALL] if _have_python_h() else []) + ([] if _no_kvcall() else [KVCALL])
     if not all(os.path.exists(f) for f in outs):
         return True
     t = min(os.path.getmtime(f) for f in outs)
@@ -122,10 +140,15 @@ def build(verbose: bool = False, ptxas_info: bool = False, defines=(), out: str 
     if out is None:
         if _have_python_h():
             build_pycall(verbose)
-            build_kvcall(verbose)
         else:
             # the ctypes binding serves every call of the store; only its per-call cost is higher
-            sys.stderr.write("build: Python.h not found; the CPython bindings are not built (no KVCache)\n")
+            sys.stderr.write("build: Python.h not found; the CPython binding (_pycall) is not built\n")
+        why = _no_kvcall()
+        if why is None:
+            build_kvcall(verbose)
+        else:
+            # the store does without; importing KVCache says so
+            sys.stderr.write(f"build: {why}; the key/value cache's binding (_kvcall) is not built, there is no KVCache\n")
     return lib_path
 
 
@@ -150,12 +173,10 @@ def build_pycall(verbose: bool = False) -> str:
 def build_kvcall(verbose: bool = False) -> str:
     """Compiles the CPython module of csrc/kvcall.cpp next to LIB, against the
     installed torch's headers and libraries. Raises on failure."""
-    import importlib.util
-
-    spec = importlib.util.find_spec("torch")
-    if spec is None:
-        raise RuntimeError("torch not found: the key/value cache's binding cannot be built")
-    torch_dir = os.path.dirname(spec.origin)
+    why = _no_kvcall()
+    if why is not None:
+        raise RuntimeError(f"{why}: the key/value cache's binding cannot be built")
+    torch_dir = _torch_dir()
     lib = os.path.join(torch_dir, "lib")
     tmp = KVCALL + ".tmp"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", os.path.join(CSRC, KVCALL_SRC),
