@@ -439,7 +439,7 @@ typedef struct t2i_kv_batch {
     const int32_t* lens;    /* device, [n_seqs]: tokens with the new ones    */
     const int32_t* starts;  /* device, [n_seqs + 1], not decreasing; NULL:
                                n_tokens / n_seqs tokens of every sequence    */
-    uint32_t table_pages;   /* entries of a row                              */
+    uint32_t table_pages;   /* entries of a row, at most 2^31 - 256 tokens   */
     uint32_t n_seqs;
     uint32_t n_tokens;      /* rows of the token arrays                      */
     uint32_t max_new;       /* no sequence has more new tokens (those beyond

@@ -95,7 +95,8 @@ class Checks {
     }
     void table(const int32_t* t, uint64_t stride, uint32_t pages, uint32_t n_seqs) {
         require(pages > 0 && stride >= pages && stride <= kMaxStride, "table_stride must be at least table_pages, which is positive");
-        require(pages <= (0x7FFFFFFFu >> kv_->token_shift), "a table row must hold fewer than 2^31 tokens");
+        // (slots are counted in 32 bits with a sign, up to the end of a tile of 128)
+        require(pages <= (0x7FFFFF00u >> kv_->token_shift), "a table row must hold at most 2^31 - 256 tokens");
         if (ok_) range("table", t, ((n_seqs - 1) * stride + pages) * 4, 4);
     }
     // the batch; false (and ok()) where there is nothing to do

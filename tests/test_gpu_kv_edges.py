@@ -216,3 +216,18 @@ def test_a_gradient_is_not_lost_without_a_word():
             for call in calls:
                 call()
     assert torch.equal(c.attend(grad(q).detach(), L), c.attend(q, L))
+
+
+def test_a_table_row_ends_before_slots_cannot_be_counted():
+    """Tiles end at multiples of 128 slots, and 2^31 is none that 32 bits count."""
+    from paper_2607_26566_gb300 import T2IError
+    c, lens, kvs, q = case(BF, 1, 1, 8, [1], [20], page=256)
+    assert c.page_tokens == 8
+    want = c.attend(q.to(DEV), ints(lens))
+    most = (2 ** 31 - 256) // 8
+    table = torch.empty(1, most + 31, dtype=torch.int32, device=DEV)
+    table[:, :c.max_pages] = c.table
+    assert torch.equal(c.attend(q.to(DEV), ints(lens), table=table[:, :most]), want)
+    for pages in (most + 1, most + 31):
+        with pytest.raises(T2IError, match="INVALID.*2\\^31 - 256"):
+            c.attend(q.to(DEV), ints(lens), table=table[:, :pages])
