@@ -13,9 +13,9 @@ namespace {
 // before it works on the one it has. Bound by memory at many tokens (each byte is
 // read and written once), by the chain of look-ups at few. Measured: seven prompts of 8.7k
 // tokens in all, 32 + 2 x 8 heads of 128, norms and interleaved pairs, 45 us (4.8 TB/s); 192 tokens
-// from fp32 5.8 us, one token 2.9 us.
+// from fp32 5.2 us, one token 2.3 us (in a graph of 50 calls).
 constexpr uint32_t kLanes = 16;
-constexpr uint32_t kThreads = 64;  // (of 256, 128, 64, 32: prompts of 8.7k tokens 63, 50, 49, 52 us)
+constexpr uint32_t kThreads = 64;  // (of 256, 128, 64, 32: prompts of 8.7k tokens 58.8, 47.4, 46.2, 54.0 us)
 constexpr uint32_t kGroups = kThreads / kLanes;
 
 // How a pair's other element is reached: interleaved pairs lie in one lane; halves
@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 // One thread moves one 16-byte column of every accepted row, eight rows at a
 // time: a path ascends, so a row's new slot is at or before its old one, and no
 // row is overwritten before it was read. Bound by memory at many sequences: paths of six
-// rows of 96 sequences in 28 layers, 8 heads of 128, 27.7 us (4.8 TB/s); by the launch's
-// latency at few: one path in four layers 3.9 us.
+// rows of 96 sequences in 28 layers, 8 heads of 128, 25 us (3.9 TB/s); by the launch's
+// latency at few: one path in a layer 2.3 us (in a graph of 50 calls).
 constexpr uint32_t kCommitThreads = 256;
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_constant__ KvCommit c) {
     tc::pdl_launch();

@@ -23,7 +23,7 @@
 // Measured: a prompt of 8190 tokens, 32 heads over 8 of 128, 400-420 us, 1.31-1.37
 // PFLOP/s of what is visible; 24 drafts of 60 tokens over contexts up to 8k, the same heads, 118 us;
 // one draft of 21 tokens over 1.5k slots 18 us; three chunks of 600 tokens of packed documents, 16 heads of
-// 80, with spans and a bias, 47-50 us.
+// 80, with spans and a bias, 48 us.
 #pragma once
 
 #include <atomic>
@@ -82,7 +82,10 @@ struct PlanHead {
 // beside them, its output), in key tiles: it lies before its tiles when runs are cut. Measured with 0, 1, 2, 3, 4
 // and 5: a prompt of 8190 tokens with 32 heads of 128 527, 490, 454, 424, 399, 403 us; 24 drafts of 60 tokens over
 // contexts up to 8k 132, 127, 124, 120, 118, 118. Scores with a bias or a cap make tiles dearer, so that a unit
-// costs fewer of them: chunks of 600 tokens with spans and a bias 49, 47, 47, 51, 54, 57.
+// costs fewer of them. With 1, 2, 3 and 4: the prompt with a cap 957, 933, 946, 957, with a bias 770, 772, 782, 791;
+// the drafts with a cap 214, 209, 213, 219, with a bias 207, 204, 205, 201; chunks of 600 tokens with a bias 95, 95,
+// 97, 100, with spans and a bias 48, 47, 52, 54, with spans and a cap 55, 55, 60, 61. (With spans alone, which go
+// with the plain scores, 42, 42, 45, 47.)
 constexpr int32_t kUnitCost = 4, kUnitCostMod = 2;
 
 // A unit in several runs, noted at the run that holds its second part: the runs
