@@ -499,7 +499,8 @@ typedef struct t2i_kv_attend_desc {
                                never a result; 0: what the table holds       */
     float scale;
     float softcap;          /* 0: none                                       */
-    uint32_t reserved;      /* must be 0                                     */
+    uint32_t sinks;         /* beside a window: the first slots that stay
+                               visible; 0: none                              */
     void* workspace;        /* device, 256-byte aligned, holding anything; calls
                                on one stream share one, others need their own */
     uint64_t workspace_bytes;
@@ -509,14 +510,16 @@ typedef struct t2i_kv_attend_desc {
  * kv_heads queries to a key head. Scores s = scale q.k, capped to
  * softcap * tanh(s / softcap), less slope[head] * |position - position of
  * the key|. A token in slot p sees slots j <= p; with a window, j > p -
- * window; with spans, first <= j < last (window must be 0). With a tree
- * (max_new <= 64, no spans) it sees the slots before the sequence's new
- * tokens and the new ones of its word, and a new token's position is the
- * slot of the first one + the number of its ancestors (itself not counted).
+ * window or j < sinks; with spans, first <= j < last (window and sinks must
+ * be 0). With a tree (max_new <= 64, no spans) it sees the slots before the
+ * sequence's new tokens and the new ones of its word, and a new token's
+ * position, which a window and sinks go by, is the slot of the first one +
+ * the number of its ancestors (itself not counted).
  * out = the softmax's mean of the values, lse = log(sum(exp(s))). A token
  * that sees nothing has out 0 and lse -infinity. Keys may hold anything
  * where no token sees them. So may values before the first and behind the
- * last slot that any of the sequence's new tokens sees; between these a
+ * last slot that any of the sequence's new tokens sees, and those between its
+ * sinks and the first slot of its windows; between these a
  * value that is not finite may reach outputs of tokens that do not see it
  * (its weight there is 0, and 0 times it is not 0). With a tree, all drafted
  * tokens count as seen, and the slots in the window of the one before them. */

@@ -33,6 +33,7 @@ constexpr uint32_t kMaxDim = 128;
 constexpr uint32_t kMaxHeads = 1024;
 constexpr uint32_t kMaxLayers = 1024;
 constexpr uint32_t kMinPageTokens = 8;
+constexpr uint32_t kMaxSlots = 0x7FFFFF00u;  // of a sequence (slots are counted in 32 bits with a sign, up to the end of a tile of 128)
 constexpr uint64_t kMaxStride = uint64_t(1) << 40;
 
 struct DeviceScope {
@@ -95,8 +96,7 @@ class Checks {
     }
     void table(const int32_t* t, uint64_t stride, uint32_t pages, uint32_t n_seqs) {
         require(pages > 0 && stride >= pages && stride <= kMaxStride, "table_stride must be at least table_pages, which is positive");
-        // (slots are counted in 32 bits with a sign, up to the end of a tile of 128)
-        require(pages <= (0x7FFFFF00u >> kv_->token_shift), "a table row must hold at most 2^31 - 256 tokens");
+        require(pages <= (kMaxSlots >> kv_->token_shift), "a table row must hold at most 2^31 - 256 tokens");
         if (ok_) range("table", t, ((n_seqs - 1) * stride + pages) * 4, 4);
     }
     // the batch; false (and ok()) where there is nothing to do
@@ -260,10 +260,9 @@ uint64_t workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, u
 t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) {
     Checks c(kv, "kv_attend");
     const uint32_t K = kv->layout.kv_heads;
-    c.require(d.reserved == 0, "reserved must be 0");
     c.require(d.q_heads >= 1 && d.q_heads <= kMaxHeads && d.q_heads % K == 0, "q_heads must be a multiple of kv_heads, at most 1024");
     c.require(std::isfinite(d.scale) && std::isfinite(d.softcap) && d.softcap >= 0.0f, "scale and softcap must be finite, softcap not negative");
-    c.require(!d.spans || (!d.window && !d.tree), "spans go without a window and without a tree");
+    c.require(!d.spans || (!d.window && !d.sinks && !d.tree), "spans go without a window, sinks and a tree");
     c.require(d.batch.max_new || !d.batch.starts, "with starts, max_new must be given");
     if (!c.batch(d.batch)) return c.ok() ? T2I_OK : T2I_ERR_INVALID;
     KvAttend a{};
@@ -292,6 +291,7 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     a.q_heads = d.q_heads;
     a.group = d.q_heads / K;
     a.window = d.window;
+    a.sinks = d.window ? std::min(d.sinks, kMaxSlots) : 0;
     // (what a row of the table holds, where the caller does not say)
     a.max_len = d.max_len ? std::min(d.max_len, d.batch.table_pages << kv->token_shift) : d.batch.table_pages << kv->token_shift;
     a.scale = d.scale;

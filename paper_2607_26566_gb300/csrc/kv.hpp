@@ -69,6 +69,7 @@ struct KvAttend {
     uint32_t q_heads;
     uint32_t group;  // q_heads / kv_heads
     uint32_t window;
+    uint32_t sinks;  // 0 without a window; below 2^31 - 256
     uint32_t max_len;
     float scale;
     float softcap;

@@ -21,16 +21,38 @@ constexpr float kLift = 0.0f;
 template <>
 constexpr float kLift<__half> = 7.0f;
 
-// Slots [lo, hi) outside which none of tokens [t0, t1) of sequence q sees anything,
-// and slots [all_lo, all_hi) that all of them see.
+// Slots [0, head) and [lo, hi), head < lo, outside which none of tokens [t0, t1) of sequence q sees anything, and slots
+// [all_lo, all_hi) that all of them see (and [0, sinks), up to all_hi). Where the sinks reach the window there is one range.
 struct KvSpan {
-    int32_t lo, hi, all_lo, all_hi;
+    int32_t lo, hi, all_lo, all_hi, head;
 };
+// A span's key tiles: those of its head, then the others; a tile of both counts once.
+__device__ __forceinline__ int32_t head_tiles(const KvSpan& s) { return min((s.head + kTileKeys - 1) / kTileKeys, s.lo / kTileKeys); }
+__device__ __forceinline__ int32_t span_tiles(const KvSpan& s) {
+    return max(1, head_tiles(s) + (s.hi + kTileKeys - 1) / kTileKeys - s.lo / kTileKeys);
+}
+// the first slot of tile i
+__device__ __forceinline__ int32_t tile_slot(const KvSpan& s, int32_t i) {
+    const int32_t h = head_tiles(s);
+    return (i < h ? i : s.lo / kTileKeys + i - h) * kTileKeys;
+}
+// whether some token does not see some key of the tile
+__device__ __forceinline__ bool tile_masked(const KvAttend& a, const KvSpan& s, int32_t slot0) {
+    return (slot0 < s.all_lo && slot0 + kTileKeys > int32_t(a.sinks)) || slot0 + kTileKeys > s.all_hi;
+}
+// a slot that no token sees
+__device__ __forceinline__ bool unseen(const KvSpan& s, int32_t slot) { return (slot < s.lo && slot >= s.head) || slot >= s.hi; }
+__device__ __forceinline__ void add_sinks(const KvAttend& a, KvSpan& s) {
+    const int32_t n = int32_t(a.sinks);
+    if (n >= s.lo) s.lo = 0;
+    if (n >= s.all_lo) s.all_lo = 0;
+    s.head = s.lo ? n : 0;
+}
 __device__ __forceinline__ KvSpan kv_span(const KvAttend& a, const KvSeq& q, int32_t t0, int32_t t1) {
     const int32_t ctx = q.len - q.n;
     KvSpan r;
     if (a.spans) {
-        r = {INT32_MAX, 0, 0, INT32_MAX};
+        r = {INT32_MAX, 0, 0, INT32_MAX, 0};
         for (int32_t i = t0; i < t1; ++i) {
             const int2 s = reinterpret_cast<const int2*>(a.spans)[q.first + i];
             const int32_t f = max(s.x, 0), l = min(s.y, q.len);
@@ -47,12 +69,14 @@ __device__ __forceinline__ KvSpan kv_span(const KvAttend& a, const KvSeq& q, int
         r.hi = q.len;
         r.all_lo = a.window ? int32_t(max(int64_t(0), ctx + q.n - w)) : 0;
         r.all_hi = ctx;
+        add_sinks(a, r);
         return r;
     }
     r.lo = int32_t(max(int64_t(0), ctx + t0 + 1 - w));
     r.hi = ctx + t1;
     r.all_lo = int32_t(max(int64_t(0), ctx + t1 - w));
     r.all_hi = ctx + t0 + 1;
+    add_sinks(a, r);
     return r;
 }
 
@@ -64,7 +88,7 @@ __device__ __forceinline__ uint64_t kv_word(const KvAttend& a, const KvSeq& q, i
 }
 
 // One query: it sees the keys of slots below `last`, and of the drafted tokens in
-// `word`, whose position is `first` or above. pos: its own position.
+// `word`, whose position is `first` or above, or a sink's. pos: its own position.
 struct KvQuery {
     int32_t first, last, pos;
     uint64_t word;

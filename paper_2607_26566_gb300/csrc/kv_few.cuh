@@ -114,7 +114,7 @@ struct Few {
 __device__ __forceinline__ int32_t unit_tiles(const KvAttend& a, const KvSeq& q, KvSpan& sp) {
     if (q.n == 0) return 0;
     sp = kv_span(a, q, 0, min(q.n, int32_t(a.tok.max_new)));
-    return max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
+    return span_tiles(sp);
 }
 
 __device__ __forceinline__ void walk_seq(const KvAttend& a, Walk& w) {
@@ -153,9 +153,6 @@ __device__ __forceinline__ bool walk_next(const KvAttend& a, Walk& w) {
     walk_unit(a, w);
     return true;
 }
-// first slot of the unit's tile i
-__device__ __forceinline__ int32_t tile_slot(const Walk& w, int32_t i) { return (w.span.lo / kTileKeys + i) * kTileKeys; }
-
 // Sum or maximum over a warp's lanes of each of n = 16 or 32 columns: lane i gets
 // column i % n.
 template <int n, bool kMax>
@@ -305,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
             const int32_t* table = a.pages.table + w.s * a.pages.table_stride;
             for (int32_t i = 0; i < w.n; ++i) {
-                const uint32_t slot = uint32_t(tile_slot(w, w.tile + i)) + lane * box;
+                const uint32_t slot = uint32_t(tile_slot(w.span, w.tile + i)) + lane * box;
                 int32_t page = -1;
                 if (lane < boxes && slot < uint32_t(w.q.len)) page = table[slot >> shift];
                 // what the pool lacks, and what lies behind the sequence, is filled with zeros
@@ -439,8 +436,8 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 for (int c = 0; c < N; ++c) sum[c] = 0.0f;
             };
             for (int32_t i = 0; i < w.n; ++i, ++n) {
-                const int32_t slot0 = tile_slot(w, w.tile + i), key = slot0 + int32_t(tid);
-                const bool masked = slot0 < w.span.all_lo || slot0 + kTileKeys > w.span.all_hi;
+                const int32_t slot0 = tile_slot(w.span, w.tile + i), key = slot0 + int32_t(tid);
+                const bool masked = tile_masked(a, w.span, slot0);
                 // a drafted key's bit and position
                 uint64_t bit = 0;
                 int32_t kpos = key;
@@ -468,9 +465,10 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 }
                 if (masked) {
                     uint32_t see = 0;
+                    const bool sunk = kpos < int32_t(a.sinks);
 #pragma unroll
                     for (int c = 0; c < N; ++c)
-                        see |= uint32_t(kpos >= first[c] && (key < last[c] || (word[c] & bit))) << c;
+                        see |= uint32_t((kpos >= first[c] || sunk) && (key < last[c] || (word[c] & bit))) << c;
 #pragma unroll
                     for (int c = 0; c < N; ++c) x[c] = see & (1u << c) ? x[c] : -INFINITY;
                 }
@@ -548,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 if (slot0 < w.span.lo || slot0 + kTileKeys > w.span.hi) {
                     const uint32_t e = (2 * n + 1) % Sh::kEntries;
                     mbar_wait(bar(sh.full[e]), (2 * n + 1) / Sh::kEntries & 1, dead);
-                    if (key < w.span.lo || key >= w.span.hi) {
+                    if (unseen(w.span, key)) {
 #pragma unroll 1
                         for (int k = 0; k < NS * 8; ++k)
                             *reinterpret_cast<uint4*>(mem + e * Sh::kEntry + k / 8 * kSlot + tid * 128 + k % 8 * 16) =

@@ -115,7 +115,7 @@ __device__ __forceinline__ int32_t row_tiles(const KvAttend& a, const KvSeq& q) 
 // The span of a row tile, by a warp.
 __device__ __forceinline__ KvSpan tile_span(const KvAttend& a, const KvSeq& q, int32_t t0, int32_t t1, int32_t lane) {
     if (!a.spans) return kv_span(a, q, t0, t1);
-    KvSpan r{INT32_MAX, 0, 0, INT32_MAX};
+    KvSpan r{INT32_MAX, 0, 0, INT32_MAX, 0};
     for (int32_t i = t0 + lane; i < t1; i += 32) {
         const KvSpan x = kv_span(a, q, i, i + 1);
         if (x.hi > x.lo) r.lo = min(r.lo, x.lo), r.hi = max(r.hi, x.hi);
@@ -186,7 +186,7 @@ __device__ __forceinline__ int32_t make_plan(const Rows& f, PlanTile* plan, int3
         if (lane == 0) {
             PlanTile& t = plan[j];
             t.s = int32_t(s), t.m = m, t.span = sp, t.q = q, t.rows = end - m * kRows;
-            t.nt = max(1, (sp.hi + kTileKeys - 1) / kTileKeys - sp.lo / kTileKeys);
+            t.nt = span_tiles(sp);
             t.last = j + 1 == firsts[s + 1];
         }
     }
@@ -268,7 +268,6 @@ __device__ __forceinline__ bool walk_next(const Rows& f, const PlanTile* plan, R
     walk_segment(f, w, start);
     return true;
 }
-__device__ __forceinline__ int32_t tile_slot(const KvSpan& s, int32_t i) { return (s.lo / kTileKeys + i) * kTileKeys; }
 
 constexpr uint32_t kUnits = 8;      // in shared memory at a time
 constexpr uint32_t kUnitReaders = 9;  // eight softmax warps and the product warp
@@ -413,9 +412,10 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 const int32_t row_k = int32_t((a.pages.layer * 2 * a.pages.kv_heads + w.h) << shift);
                 const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
                 const int32_t* table = a.pages.table + uint32_t(w.t.s) * a.pages.table_stride;
-                const int32_t slot0 = tile_slot(w.t.span, w.tile), tiles = w.n, len = w.t.q.len;
+                const KvSpan span = w.t.span;
+                const int32_t tile0 = w.tile, tiles = w.n, len = w.t.q.len;
                 for (int32_t i = 0; i < tiles; ++i) {
-                    const uint32_t slot = uint32_t(slot0 + i * kTileKeys) + lane * box;
+                    const uint32_t slot = uint32_t(tile_slot(span, tile0 + i)) + lane * box;
                     int32_t page = -1;
                     if (lane < boxes && slot < uint32_t(len)) page = table[slot >> shift];
                     // what the pool lacks, and what lies behind the sequence, is filled with zeros
@@ -617,15 +617,15 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                 qy = kv_query(a, o.q, int32_t(row / a.group));
                 if (kMod && a.slopes) slope = a.slopes[o.h * a.group + row % a.group] * kLog2e;
             }
-            if (a.tree && real)  // of the drafted tokens, those that are there and inside the window
+            if (a.tree && real)  // of the drafted tokens, those that are there and inside the window, or sinks
                 for (int b = 0; b < 64; ++b)
-                    if (o.draft[b] < qy.first) qy.word &= ~(uint64_t(1) << b);
+                    if (o.draft[b] < qy.first && o.draft[b] >= int32_t(a.sinks)) qy.word &= ~(uint64_t(1) << b);
             float ref = -INFINITY, pend = 1.0f;  // pend: what O, once it is there, has to be scaled by
             bool late = false;                   // ... of some row of the warp
             KvSum sum;
             for (int32_t i = 0; i < tiles; ++i, ++n) {
                 const int32_t slot0 = tile_slot(span, o.tile + i);
-                const bool masked = slot0 < span.all_lo || slot0 + kTileKeys > span.all_hi;
+                const bool masked = tile_masked(a, span, slot0);
                 const bool drafts = a.tree && slot0 + kTileKeys > ctx;
                 // the row's visible keys of the tile, a bit each
                 uint64_t see0 = 0, see1 = 0;
@@ -637,8 +637,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                     }
                     auto below = [](int64_t n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
                     const int64_t f0 = int64_t(qy.first) - slot0, l0 = int64_t(qy.last) - slot0;
-                    see0 |= below(l0) & ~below(f0);
-                    see1 |= below(l0 - 64) & ~below(f0 - 64);
+                    const int64_t k0 = int64_t(a.sinks) - slot0;
+                    see0 |= below(l0) & (~below(f0) | below(k0));
+                    see1 |= below(l0 - 64) & (~below(f0 - 64) | below(k0 - 64));
                 }
                 mbar_wait(bar(sh.s_full[st]), n & 1, dead);
                 fence_after();
@@ -742,7 +743,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const __grid_const
                     const uint32_t e = (2 * n + 1) % kRowEntries;
                     mbar_wait(bar(sh.full[e]), (2 * n + 1) / kRowEntries & 1, dead);
                     const int32_t key = slot0 + int32_t(r);
-                    if (key < span.lo || key >= span.hi) {
+                    if (unseen(span, key)) {
 #pragma unroll 1
                         for (int k = 0; k < 16; ++k)
                             if (k < 8 || D > 64)

@@ -218,7 +218,7 @@ PyObject* append(PyObject* const* a) {
 }
 
 // attend(cache, q, lens, out, lse, starts, max_new, layer, scale, softcap, slopes,
-//        window, spans, tree, max_len, table, stream) -> status
+//        window, spans, tree, max_len, table, stream, sinks) -> status
 PyObject* attend(PyObject* const* a) {
     const Cache& c = cache(a[0]);
     const Rows q = rows(c, a[1], -1, "q", &c.dtype), o = rows(c, a[3], q.heads, "out", &c.dtype);
@@ -235,6 +235,7 @@ PyObject* attend(PyObject* const* a) {
     d.spans = static_cast<const int32_t*>(plain(a[12], at::kInt, {q.n, 2}, "spans"));
     d.tree = static_cast<const uint64_t*>(plain(a[13], at::kLong, {q.n}, "tree"));
     d.max_len = u32(a[14], "max_len");
+    d.sinks = u32(a[17], "sinks");
     void* s = stream_of(c, a[16]);
     const t2i_status st = t2i_kv_workspace_bytes(c.kv, d.batch.n_seqs, d.batch.n_tokens, d.q_heads, &d.workspace_bytes);
     if (st != T2I_OK || d.batch.n_tokens == 0) d.workspace_bytes = 0;
@@ -322,7 +323,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {ENTRY("cache", make, 6, "a cache's binding"),
                          ENTRY("close", shut, 1, "refuses later calls"),
                          ENTRY("append", append, 18, "t2i_kv_append"),
-                         ENTRY("attend", attend, 17, "t2i_kv_attend"),
+                         ENTRY("attend", attend, 18, "t2i_kv_attend"),
                          ENTRY("commit", commit, 6, "t2i_kv_commit"),
                          {nullptr, nullptr, 0, nullptr}};
 

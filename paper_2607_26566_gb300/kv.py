@@ -240,12 +240,13 @@ class KVCache:
         return q_out
 
     def attend(self, q, lens, out=None, lse=None, starts=None, max_new=0, layer=0, scale=None, softcap=0.0, slopes=None,
-               window=0, spans=None, max_len=0, table=None, stream=None):
+               window=0, spans=None, max_len=0, table=None, stream=None, sinks=0):
         """Attention of new tokens over the cache (t2i_kv_attend). Returns ``out``.
 
         ``scale``: 1 / sqrt(head_dim) by default. ``softcap``: scores become
         softcap * tanh(score / softcap). ``slopes``: fp32 [heads], less slope *
         distance. ``window``: a token sees the last ``window`` slots up to its own.
+        ``sinks``: beside a window, and the first ``sinks`` slots (up to its own).
         ``spans``: int32 [tokens, 2], the slots [first, last) that a token sees
         instead (documents, prefixes, padding: an empty one gives zeros).
         ``lse``: fp32 [tokens, heads], receives log(sum(exp(scores))).
@@ -254,24 +255,24 @@ class KVCache:
         if out is None:
             out = self._output(q, stream)
         st = _kv.attend(self._c, q, lens, out, lse, starts, max_new, layer, self._scale if scale is None else scale, softcap,
-                        slopes, window, spans, None, max_len, table, stream)
+                        slopes, window, spans, None, max_len, table, stream, sinks)
         if st:
             self._done(st)
         return out
 
     def attend_tree(self, q, lens, tree, out=None, lse=None, starts=None, max_new=0, layer=0, scale=None, softcap=0.0,
-                    slopes=None, window=0, max_len=0, table=None, stream=None):
+                    slopes=None, window=0, max_len=0, table=None, stream=None, sinks=0):
         """:meth:`attend` for drafted tokens, at most 64 a sequence, the last ones
         of its ``lens``. ``tree``: int64 [tokens], bit i of a token's word is set
         where it sees drafted token i of its sequence (its ancestors and itself);
         it sees all that came before the draft. A drafted token's position, for a
-        window or slopes, is the draft's first slot + the number of its ancestors."""
+        window, sinks or slopes, is the draft's first slot + the number of its ancestors."""
         if tree is None:
             raise TypeError("tree must be a tensor")
         if out is None:
             out = self._output(q, stream)
         st = _kv.attend(self._c, q, lens, out, lse, starts, max_new, layer, self._scale if scale is None else scale, softcap,
-                        slopes, window, None, tree, max_len, table, stream)
+                        slopes, window, None, tree, max_len, table, stream, sinks)
         if st:
             self._done(st)
         return out
