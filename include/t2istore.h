@@ -551,6 +551,97 @@ typedef struct t2i_kv_commit_desc {
  * to slot ctx + i, i < count, in every layer.                               */
 t2i_status t2i_kv_commit(t2i_kv* kv, const t2i_kv_commit_desc* desc, void* cuda_stream);
 
+/* ---- A cache that stays bounded: which slots got attention, which of them
+ * stay, and their rows moved together.                                      */
+
+typedef struct t2i_kv_weigh_desc {
+    t2i_kv_batch batch;
+    const void* q;          /* as in t2i_kv_attend_desc                      */
+    const float* lse;       /* device, [n_tokens][q_heads]: t2i_kv_attend's of
+                               the same queries, masks and score options     */
+    float* weights;         /* device, [n_seqs][kv_heads][n_slots]           */
+    uint64_t q_stride;
+    uint64_t seq_stride;    /* elements of weights from sequence to sequence, */
+    uint64_t head_stride;   /* and from head to head: rows do not overlap    */
+    const float* slopes;    /* these as in t2i_kv_attend_desc                */
+    const int32_t* spans;
+    uint32_t q_heads;
+    uint32_t n_slots;       /* of a row of weights; others are not counted   */
+    uint32_t window;
+    uint32_t sinks;
+    uint32_t max_len;
+    float scale;
+    float softcap;
+    float decay;            /* of the weights so far                         */
+    void* workspace;        /* as in t2i_kv_attend_desc                      */
+    uint64_t workspace_bytes;
+} t2i_kv_weigh_desc;
+
+/* The attention that slots get from new tokens: for each key head and slot j
+ * of a sequence, the sum of exp(s - lse) over its new tokens and the queries
+ * that share the head, for those that see j (scores s and who sees what as in
+ * t2i_kv_attend, without a tree). Slots before the new tokens: weights =
+ * decay * weights + sum (decay 0: the sum; weights so far may be anything).
+ * Slots of the new tokens: the sum. Others are left as they are. A query
+ * whose lse is -infinity counts nothing. Keys may hold anything where no
+ * token sees them. Sums are fp32, in an order that does not depend on timing. */
+t2i_status t2i_kv_weigh(t2i_kv* kv, const t2i_kv_weigh_desc* desc, void* cuda_stream);
+
+/* Workspace bytes that t2i_kv_weigh needs for such a batch at most.         */
+t2i_status t2i_kv_weigh_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads,
+                                        uint64_t* out);
+
+typedef struct t2i_kv_select_desc {
+    const float* weights;   /* device, [n_seqs][n_heads][n_slots]            */
+    float* weights_out;     /* device, likewise: receives the kept slots'
+                               weights, in order; may be weights itself, with
+                               the same strides; NULL                        */
+    const int32_t* lens;    /* device, [n_seqs]: slots of each sequence      */
+    const int32_t* keeps;   /* device, [n_seqs]: how many of them stay, at
+                               most keep; NULL: keep                         */
+    int32_t* kept;          /* device, [n_seqs][n_heads][min(keep, n_slots)] */
+    int32_t* counts;        /* device, [n_seqs]                              */
+    uint64_t seq_stride, head_stride;          /* elements, of weights       */
+    uint64_t out_seq_stride, out_head_stride;  /* of weights_out             */
+    uint64_t kept_seq_stride, kept_head_stride;
+    uint32_t n_seqs, n_heads, n_slots;
+    uint32_t keep;
+    uint32_t recent;        /* the last slots that stay whatever they weigh  */
+    uint32_t sinks;         /* and the first                                 */
+    uint32_t max_len;       /* the longest lens; it sets how work is split,
+                               never a result; 0: n_slots                    */
+    uint32_t reserved;      /* must be 0                                     */
+} t2i_kv_select_desc;
+
+/* Which slots of each sequence and head stay: counts[s] = n = min(lens, keeps,
+ * keep) of them: the first a = min(sinks, n), the last b = min(recent, n - a),
+ * and of the others the n - a - b of largest weight, of equals the first. (0
+ * and -0 are equal; NaN is below every number.) kept receives them, ascending;
+ * what lies behind n in kept and weights_out is left as it is. A sequence whose
+ * lens is negative or above n_slots has no slots.                           */
+t2i_status t2i_kv_select(t2i_kv* kv, const t2i_kv_select_desc* desc, void* cuda_stream);
+
+typedef struct t2i_kv_evict_desc {
+    const int32_t* table;   /* as in t2i_kv_batch                            */
+    uint64_t table_stride;
+    const int32_t* kept;    /* device, [n_seqs][kv_heads][max_kept]: slots,
+                               ascending, none twice                         */
+    const int32_t* counts;  /* device, [n_seqs]: entries of each row         */
+    uint64_t kept_seq_stride, kept_head_stride; /* elements; 0: shared       */
+    uint32_t table_pages;
+    uint32_t n_seqs;
+    uint32_t max_kept;
+    uint32_t layer;         /* the first of                                  */
+    uint32_t layers;        /* these layers                                  */
+    uint32_t reserved;      /* must be 0                                     */
+} t2i_kv_evict_desc;
+
+/* Moves the rows of keys and values of slot kept[i] to slot i, i < counts[s],
+ * for each key head of the layers. Rows behind are left as they are. An entry
+ * below its place i moves nothing; of a list that does not ascend the rows
+ * are not specified.                                                        */
+t2i_status t2i_kv_evict(t2i_kv* kv, const t2i_kv_evict_desc* desc, void* cuda_stream);
+
 /* =========================================================================
  * First-layer prefix caching (§5.1). A model of L layers keeps its first L_e
  * layers in the store and streams the rest from host memory while inference

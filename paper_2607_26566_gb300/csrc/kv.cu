@@ -326,6 +326,142 @@ t2i_status commit(t2i_kv* kv, const t2i_kv_commit_desc& d, cudaStream_t stream) 
     return launch(kv, "kv_commit", [&] { return launch_kv_commit(a, stream); });
 }
 
+// Rows [n_seqs][n_heads][width] of 4 bytes that a call writes lie apart.
+void rows_apart(Checks& c, const char* what, uint32_t n_seqs, uint32_t n_heads, uint64_t width, uint64_t seq_stride, uint64_t head_stride) {
+    c.require((n_heads == 1 || (head_stride >= width && head_stride <= kMaxStride)) &&
+                  (n_seqs == 1 || (seq_stride >= (n_heads - 1) * head_stride + width && seq_stride <= kMaxStride)), what);
+}
+// (2^62 for all that is more, which no allocation holds)
+uint64_t rows_bytes(uint32_t n_seqs, uint32_t n_heads, uint64_t width, uint64_t seq_stride, uint64_t head_stride) {
+    using Wide = unsigned __int128;
+    const Wide n = (Wide(n_seqs - 1) * seq_stride + Wide(n_heads - 1) * head_stride + width) * 4, most = Wide(1) << 62;
+    return uint64_t(n < most ? n : most);
+}
+
+t2i_status weigh(t2i_kv* kv, const t2i_kv_weigh_desc& d, cudaStream_t stream) {
+    Checks c(kv, "kv_weigh");
+    const uint32_t K = kv->layout.kv_heads;
+    c.require(d.q_heads >= 1 && d.q_heads <= kMaxHeads && d.q_heads % K == 0, "q_heads must be a multiple of kv_heads, at most 1024");
+    c.require(std::isfinite(d.scale) && std::isfinite(d.softcap) && d.softcap >= 0.0f, "scale and softcap must be finite, softcap not negative");
+    c.require(std::isfinite(d.decay), "decay must be finite");
+    c.require(!d.spans || (!d.window && !d.sinks), "spans go without a window and sinks");
+    c.require(d.batch.max_new || !d.batch.starts, "with starts, max_new must be given");
+    if (!c.batch(d.batch)) return c.ok() ? T2I_OK : T2I_ERR_INVALID;
+    const t2i_status past = past_fault(kv, "kv_weigh");
+    if (past != T2I_OK) return past;
+    KvWeigh w{};
+    KvAttend& a = w.a;
+    a.tok = tokens_of(d.batch);
+    const uint64_t n = d.batch.n_tokens;
+    const uint32_t seqs = d.batch.n_seqs;
+    c.require(uint64_t(seqs) * K <= 0x7FFFFFFFu, "too many sequences and heads");
+    c.require(d.n_slots > 0 && d.n_slots <= kMaxSlots, "n_slots must be 1 to 2^31 - 256");
+    c.tokens("q", d.q, n, d.q_heads, d.q_stride, 2, false);
+    c.range("lse", d.lse, n * d.q_heads * 4, 4);
+    rows_apart(c, "the rows of weights overlap (their strides are too small)", seqs, K, d.n_slots, d.seq_stride, d.head_stride);
+    const uint64_t bytes = rows_bytes(seqs, K, d.n_slots, d.seq_stride, d.head_stride);
+    c.range("weights", d.weights, bytes, 4);
+    if (d.slopes) c.range("slopes", d.slopes, d.q_heads * 4, 4);
+    if (d.spans) c.range("spans", d.spans, n * 8, 8);
+    const uint64_t need = kv_weigh_workspace(kv->sms, seqs, d.batch.n_tokens, d.q_heads / K);
+    c.require(d.workspace_bytes >= need, "the workspace is smaller than t2i_kv_weigh_workspace_bytes");
+    if (need) c.range("workspace", d.workspace, need, 256);
+    if (!c.ok()) return T2I_ERR_INVALID;
+    c.require(!overlap(d.weights, bytes, d.lse, n * d.q_heads * 4) &&
+                  !overlap(d.weights, bytes, d.q, c.token_bytes(n, d.q_heads, d.q_stride, 2)), "weights overlap q or lse");
+    if (!c.ok()) return T2I_ERR_INVALID;
+    a.pages = pages_of(kv, d.batch.table, d.batch.table_stride, d.batch.table_pages, d.batch.layer);
+    a.q = d.q;
+    a.q_stride = d.q_stride;
+    a.slopes = d.slopes, a.spans = d.spans;
+    a.q_heads = d.q_heads;
+    a.group = d.q_heads / K;
+    a.window = d.window;
+    a.sinks = d.window ? std::min(d.sinks, kMaxSlots) : 0;
+    a.max_len = d.max_len ? std::min(d.max_len, d.batch.table_pages << kv->token_shift) : d.batch.table_pages << kv->token_shift;
+    a.scale = d.scale;
+    a.softcap = d.softcap;
+    w.lse = d.lse, w.weights = d.weights;
+    w.seq_stride = d.seq_stride, w.head_stride = d.head_stride;
+    w.n_slots = d.n_slots;
+    w.decay = d.decay;
+    const uint32_t no_loads = kv->timeout_countdown && --kv->timeout_countdown == 0;
+    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms, no_loads};
+    return launch(kv, "kv_weigh", [&] {
+        return kv->layout.dtype == T2I_BF16 ? launch_kv_weigh_bf16(w, l, stream) : launch_kv_weigh_f16(w, l, stream);
+    });
+}
+
+t2i_status select(t2i_kv* kv, const t2i_kv_select_desc& d, cudaStream_t stream) {
+    Checks c(kv, "kv_select");
+    c.require(d.reserved == 0, "reserved must be 0");
+    c.require(d.n_seqs <= 0x7FFFFFFFu && d.n_heads >= 1 && d.n_heads <= kMaxHeads, "too many sequences, or n_heads is not 1 to 1024");
+    c.require(uint64_t(d.n_seqs) * d.n_heads <= 0x7FFFFFFFu / 8, "too many sequences and heads");
+    c.require(d.n_slots <= kMaxSlots, "n_slots must be at most 2^31 - 256");
+    if (!c.ok()) return T2I_ERR_INVALID;
+    if (d.n_seqs == 0) return T2I_OK;
+    const t2i_status past = past_fault(kv, "kv_select");
+    if (past != T2I_OK) return past;
+    const uint32_t width = std::min(d.keep, d.n_slots);
+    c.require(d.seq_stride <= kMaxStride && d.head_stride <= kMaxStride, "the strides of weights are too large");
+    if (!c.ok()) return T2I_ERR_INVALID;
+    const uint64_t in = rows_bytes(d.n_seqs, d.n_heads, d.n_slots, d.seq_stride, d.head_stride);
+    if (d.n_slots) c.range("weights", d.weights, in, 4);
+    c.range("lens", d.lens, uint64_t(d.n_seqs) * 4, 4);
+    if (d.keeps) c.range("keeps", d.keeps, uint64_t(d.n_seqs) * 4, 4);
+    c.range("counts", d.counts, uint64_t(d.n_seqs) * 4, 4);
+    if (width) {
+        rows_apart(c, "the rows of kept overlap (their strides are too small)", d.n_seqs, d.n_heads, width, d.kept_seq_stride, d.kept_head_stride);
+        const uint64_t kept = rows_bytes(d.n_seqs, d.n_heads, width, d.kept_seq_stride, d.kept_head_stride);
+        c.range("kept", d.kept, kept, 4);
+        c.require(!overlap(d.kept, kept, d.weights, in), "kept overlaps weights");
+        if (d.weights_out) {
+            const bool in_place = d.weights_out == d.weights && d.seq_stride == d.out_seq_stride && d.head_stride == d.out_head_stride;
+            rows_apart(c, "the rows of weights_out overlap (their strides are too small)", d.n_seqs, d.n_heads,
+                       in_place ? d.n_slots : width, d.out_seq_stride, d.out_head_stride);
+            const uint64_t out = rows_bytes(d.n_seqs, d.n_heads, width, d.out_seq_stride, d.out_head_stride);
+            c.range("weights_out", d.weights_out, out, 4);
+            c.require(in_place || !overlap(d.weights_out, out, d.weights, in), "weights_out overlaps weights without being them");
+            c.require(!overlap(d.weights_out, out, d.kept, kept), "weights_out overlaps kept");
+        }
+    }
+    if (!c.ok()) return T2I_ERR_INVALID;
+    KvSelect k{};
+    k.weights = d.weights, k.weights_out = width ? d.weights_out : nullptr;
+    k.lens = d.lens, k.keeps = d.keeps, k.kept = d.kept, k.counts = d.counts;
+    k.seq_stride = d.seq_stride, k.head_stride = d.head_stride;
+    k.out_seq_stride = d.out_seq_stride, k.out_head_stride = d.out_head_stride;
+    k.kept_seq_stride = d.kept_seq_stride, k.kept_head_stride = d.kept_head_stride;
+    k.n_seqs = d.n_seqs, k.n_heads = d.n_heads, k.n_slots = d.n_slots;
+    k.keep = width, k.recent = std::min(d.recent, kMaxSlots), k.sinks = std::min(d.sinks, kMaxSlots);
+    k.max_len = d.max_len ? std::min(d.max_len, d.n_slots) : d.n_slots;
+    return launch(kv, "kv_select", [&] { return launch_kv_select(k, kv->sms, stream); });
+}
+
+t2i_status evict(t2i_kv* kv, const t2i_kv_evict_desc& d, cudaStream_t stream) {
+    Checks c(kv, "kv_evict");
+    c.require(d.reserved == 0, "reserved must be 0");
+    c.require(d.n_seqs <= 0x7FFFFFFFu && d.max_kept <= kMaxSlots, "too many sequences or entries");
+    c.require(d.layers >= 1 && d.layers <= kv->layout.layers && d.layer <= kv->layout.layers - d.layers, "the layers are not the layout's");
+    c.require(uint64_t(d.n_seqs) * kv->layout.kv_heads <= 0x7FFFFFFFu, "too many sequences and heads");
+    c.require(d.kept_seq_stride <= kMaxStride && d.kept_head_stride <= kMaxStride, "the strides of kept are too large");
+    if (!c.ok()) return T2I_ERR_INVALID;
+    if (d.n_seqs == 0 || d.max_kept == 0) return T2I_OK;
+    const t2i_status past = past_fault(kv, "kv_evict");
+    if (past != T2I_OK) return past;
+    const uint32_t K = kv->layout.kv_heads;
+    c.table(d.table, d.table_stride, d.table_pages, d.n_seqs);
+    c.range("kept", d.kept, rows_bytes(d.n_seqs, K, d.max_kept, d.kept_seq_stride, d.kept_head_stride), 4);
+    c.range("counts", d.counts, uint64_t(d.n_seqs) * 4, 4);
+    if (!c.ok()) return T2I_ERR_INVALID;
+    KvEvict e{};
+    e.pages = pages_of(kv, d.table, d.table_stride, d.table_pages, d.layer);
+    e.kept = d.kept, e.counts = d.counts;
+    e.kept_seq_stride = d.kept_seq_stride, e.kept_head_stride = d.kept_head_stride;
+    e.n_seqs = d.n_seqs, e.max_kept = d.max_kept, e.layers = d.layers;
+    return launch(kv, "kv_evict", [&] { return launch_kv_evict(e, kv->sms, stream); });
+}
+
 using PFN_encodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -457,6 +593,24 @@ t2i_status t2i_kv_attend(t2i_kv* kv, const t2i_kv_attend_desc* desc, void* cuda_
 
 t2i_status t2i_kv_commit(t2i_kv* kv, const t2i_kv_commit_desc* desc, void* cuda_stream) {
     T2I_KV_CALL(kv, desc, t2i::commit(kv, *desc, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+t2i_status t2i_kv_weigh(t2i_kv* kv, const t2i_kv_weigh_desc* desc, void* cuda_stream) {
+    T2I_KV_CALL(kv, desc, t2i::weigh(kv, *desc, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+t2i_status t2i_kv_select(t2i_kv* kv, const t2i_kv_select_desc* desc, void* cuda_stream) {
+    T2I_KV_CALL(kv, desc, t2i::select(kv, *desc, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+t2i_status t2i_kv_evict(t2i_kv* kv, const t2i_kv_evict_desc* desc, void* cuda_stream) {
+    T2I_KV_CALL(kv, desc, t2i::evict(kv, *desc, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+t2i_status t2i_kv_weigh_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, uint64_t* out) {
+    if (!kv || !out) return T2I_ERR_INVALID;
+    *out = t2i::kv_weigh_workspace(kv->sms, n_seqs, n_tokens, q_heads / kv->layout.kv_heads);
+    return T2I_OK;
 }
 
 t2i_status t2i_kv_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, uint64_t* out) {

@@ -84,9 +84,43 @@ struct KvCommit {
     uint32_t max_path;
 };
 
+// Accumulated attention: what it goes by is an attention's arguments (out, lse and tree unused).
+struct KvWeigh {
+    KvAttend a;
+    const float* lse;
+    float* weights;
+    uint64_t seq_stride, head_stride;
+    uint32_t n_slots;
+    float decay;
+};
+
+struct KvSelect {
+    const float* weights;
+    float* weights_out;
+    const int32_t* lens;
+    const int32_t* keeps;
+    int32_t* kept;
+    int32_t* counts;
+    uint64_t seq_stride, head_stride, out_seq_stride, out_head_stride, kept_seq_stride, kept_head_stride;
+    uint32_t n_seqs, n_heads, n_slots;
+    uint32_t keep, recent, sinks;
+    uint32_t max_len;
+};
+
+struct KvEvict {
+    KvPages pages;  // its layer: the first of `layers`
+    const int32_t* kept;
+    const int32_t* counts;
+    uint64_t kept_seq_stride, kept_head_stride;
+    uint32_t n_seqs, max_kept, layers;
+};
+
 // dtype and in_dtype: T2I_BF16, T2I_F16, T2I_F32
 cudaError_t launch_kv_append(const KvAppend& a, uint32_t dtype, uint32_t in_dtype, cudaStream_t stream);
 cudaError_t launch_kv_commit(const KvCommit& c, cudaStream_t stream);
+
+cudaError_t launch_kv_select(const KvSelect& c, uint32_t sms, cudaStream_t stream);
+cudaError_t launch_kv_evict(const KvEvict& c, uint32_t sms, cudaStream_t stream);
 
 // What an attention launch needs beside its arguments.
 struct KvLaunch {
@@ -110,5 +144,8 @@ uint64_t kv_few_workspace(uint32_t sms);
 cudaError_t launch_kv_rows_bf16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 cudaError_t launch_kv_rows_f16(const KvAttend& a, const KvLaunch& l, cudaStream_t stream);
 uint64_t kv_rows_workspace(uint32_t sms, uint32_t n_seqs, uint32_t n_tokens, uint32_t group);
+cudaError_t launch_kv_weigh_bf16(const KvWeigh& w, const KvLaunch& l, cudaStream_t stream);
+cudaError_t launch_kv_weigh_f16(const KvWeigh& w, const KvLaunch& l, cudaStream_t stream);
+uint64_t kv_weigh_workspace(uint32_t sms, uint32_t n_seqs, uint32_t n_tokens, uint32_t group);
 
 }  // namespace t2i

@@ -260,6 +260,96 @@ PyObject* commit(PyObject* const* a) {
     return PyLong_FromLong(t2i_kv_commit(c.kv, &d, stream_of(c, a[5])));
 }
 
+// Rows [sequences, heads, any] of 4 bytes, a row's elements side by side.
+struct Rows4 {
+    void* p;
+    int64_t seqs, heads, width;
+    uint64_t seq_stride, head_stride;
+};
+Rows4 rows4(PyObject* o, at::ScalarType dtype, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    if (t.scalar_type() != dtype) type_error(std::string(name) + " has the wrong dtype");
+    if (t.dim() != 3 || !t.is_cuda() || (t.stride(2) != 1 && t.size(2) > 1) || t.size(0) > 0x7FFFFFFF || t.size(1) > 0x7FFFFFFF ||
+        t.size(2) > 0x7FFFFFFF)
+        value_error(std::string(name) + " must be a CUDA tensor [sequences, heads, slots], the slots of a head side by side");
+    return {t.data_ptr(), t.size(0), t.size(1), t.size(2), uint64_t(t.stride(0)), uint64_t(t.stride(1))};
+}
+
+// weigh(cache, q, lens, lse, weights, starts, max_new, layer, scale, softcap, slopes, window, sinks, spans, decay,
+//       max_len, table, stream) -> status
+PyObject* weigh(PyObject* const* a) {
+    const Cache& c = cache(a[0]);
+    const Rows q = rows(c, a[1], -1, "q", &c.dtype);
+    t2i_kv_weigh_desc d{};
+    d.batch = batch(c, q.n, a[2], a[5], a[6], a[7], a[16]);
+    d.q = q.p, d.q_stride = q.stride;
+    d.q_heads = uint32_t(q.heads);
+    if (a[3] == Py_None) type_error("lse must be a tensor");
+    d.lse = static_cast<const float*>(plain(a[3], at::kFloat, {q.n, q.heads}, "lse"));
+    const Rows4 w = rows4(a[4], at::kFloat, "weights");
+    if (w.seqs != int64_t(d.batch.n_seqs) || w.heads != c.kv_heads) value_error("weights must be [sequences, kv_heads, slots]");
+    d.weights = static_cast<float*>(w.p), d.seq_stride = w.seq_stride, d.head_stride = w.head_stride;
+    d.n_slots = uint32_t(w.width);
+    d.scale = real(a[8]);
+    d.softcap = real(a[9]);
+    d.slopes = static_cast<const float*>(plain(a[10], at::kFloat, {q.heads}, "slopes"));
+    d.window = u32(a[11], "window");
+    d.sinks = u32(a[12], "sinks");
+    d.spans = static_cast<const int32_t*>(plain(a[13], at::kInt, {q.n, 2}, "spans"));
+    d.decay = real(a[14]);
+    d.max_len = u32(a[15], "max_len");
+    void* s = stream_of(c, a[17]);
+    const t2i_status st = t2i_kv_weigh_workspace_bytes(c.kv, d.batch.n_seqs, d.batch.n_tokens, d.q_heads, &d.workspace_bytes);
+    if (st != T2I_OK || d.batch.n_tokens == 0) d.workspace_bytes = 0;
+    const Workspace m(c.device, d.workspace_bytes, s);
+    d.workspace = m.get();
+    return PyLong_FromLong(t2i_kv_weigh(c.kv, &d, s));
+}
+
+// select(cache, weights, lens, keep, keeps, kept, counts, weights_out, recent, sinks, max_len, stream) -> status
+PyObject* select(PyObject* const* a) {
+    const Cache& c = cache(a[0]);
+    const Rows4 w = rows4(a[1], at::kFloat, "weights"), k = rows4(a[5], at::kInt, "kept");
+    if (a[2] == Py_None || a[6] == Py_None) type_error("lens and counts must be tensors");
+    t2i_kv_select_desc d{};
+    d.weights = static_cast<const float*>(w.p), d.seq_stride = w.seq_stride, d.head_stride = w.head_stride;
+    d.n_seqs = uint32_t(w.seqs), d.n_heads = uint32_t(w.heads), d.n_slots = uint32_t(w.width);
+    d.lens = static_cast<const int32_t*>(plain(a[2], at::kInt, {w.seqs}, "lens"));
+    d.keep = u32(a[3], "keep");
+    d.keeps = static_cast<const int32_t*>(plain(a[4], at::kInt, {w.seqs}, "keeps"));
+    const int64_t width = std::min<int64_t>(d.keep, w.width);
+    if (k.seqs != w.seqs || k.heads != w.heads || k.width < width)
+        value_error("kept must be [sequences, heads, as many as stay] of the weights' sequences and heads");
+    d.kept = static_cast<int32_t*>(k.p), d.kept_seq_stride = k.seq_stride, d.kept_head_stride = k.head_stride;
+    d.counts = static_cast<int32_t*>(plain(a[6], at::kInt, {w.seqs}, "counts"));
+    if (a[7] != Py_None) {
+        const Rows4 o = rows4(a[7], at::kFloat, "weights_out");
+        if (o.seqs != w.seqs || o.heads != w.heads || o.width < width)
+            value_error("weights_out must be [sequences, heads, as many as stay] of the weights' sequences and heads");
+        d.weights_out = static_cast<float*>(o.p), d.out_seq_stride = o.seq_stride, d.out_head_stride = o.head_stride;
+    }
+    d.recent = u32(a[8], "recent");
+    d.sinks = u32(a[9], "sinks");
+    d.max_len = u32(a[10], "max_len");
+    return PyLong_FromLong(t2i_kv_select(c.kv, &d, stream_of(c, a[11])));
+}
+
+// evict(cache, kept, counts, layer, layers, table, stream) -> status
+PyObject* evict(PyObject* const* a) {
+    const Cache& c = cache(a[0]);
+    const Rows4 k = rows4(a[1], at::kInt, "kept");
+    if (a[2] == Py_None) type_error("counts must be a tensor");
+    if (k.heads != c.kv_heads) value_error("kept must be [sequences, kv_heads, slots]");
+    t2i_kv_evict_desc d{};
+    table(c, a[5], k.seqs, &d.table, &d.table_stride, &d.table_pages);
+    d.kept = static_cast<const int32_t*>(k.p), d.kept_seq_stride = k.seq_stride, d.kept_head_stride = k.head_stride;
+    d.counts = static_cast<const int32_t*>(plain(a[2], at::kInt, {k.seqs}, "counts"));
+    d.n_seqs = uint32_t(k.seqs), d.max_kept = uint32_t(k.width);
+    d.layer = u32(a[3], "layer");
+    d.layers = u32(a[4], "layers");
+    return PyLong_FromLong(t2i_kv_evict(c.kv, &d, stream_of(c, a[6])));
+}
+
 // cache(kv, device, fp16, kv_heads, head_dim, table) -> capsule
 PyObject* make(PyObject* const* a) {
     const at::Tensor& t = tensor(a[5], "table");
@@ -325,6 +415,9 @@ PyMethodDef methods[] = {ENTRY("cache", make, 6, "a cache's binding"),
                          ENTRY("append", append, 18, "t2i_kv_append"),
                          ENTRY("attend", attend, 18, "t2i_kv_attend"),
                          ENTRY("commit", commit, 6, "t2i_kv_commit"),
+                         ENTRY("weigh", weigh, 18, "t2i_kv_weigh"),
+                         ENTRY("select", select, 12, "t2i_kv_select"),
+                         ENTRY("evict", evict, 7, "t2i_kv_evict"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvcall", "CPython entry points for the calls of the key/value cache", -1,

@@ -2,8 +2,8 @@
 
 :class:`KVCache` reserves pages of a :class:`Store` for the sequences of a text
 model and keeps their page table on the device; its calls append keys and
-values to the pages and attend over them in place. As in the rest of the
-binding, arguments are only marshalled here: the kernels are the library's.
+values to the pages, attend over them in place and keep those that got most
+attention. As in the rest of the binding, arguments are only marshalled here: the kernels are the library's.
 """
 from __future__ import annotations
 
@@ -282,6 +282,58 @@ class KVCache:
         the rows of slot ctx[s] + path[s, i] move to slot ctx[s] + i, i <
         counts[s]. ``path``: int32 [sequences, any], ascending."""
         st = _kv.commit(self._c, ctx, path, counts, table, stream)
+        if st:
+            self._done(st)
+
+    # -------------------------------------------------------- a cache that stays bounded
+    def weigh(self, q, lens, lse, weights, starts=None, max_new=0, layer=0, scale=None, softcap=0.0, slopes=None, window=0,
+              sinks=0, spans=None, decay=1.0, max_len=0, table=None, stream=None):
+        """Adds the attention that slots got from new tokens to ``weights``
+        (t2i_kv_weigh), which it returns: fp32 [sequences, kv_heads, slots].
+
+        For a slot, the sum of exp(score - lse) over the new tokens that see it
+        and the heads that share its key head; ``q``, ``lse`` and the options
+        are those of the :meth:`attend` before it. A slot that was there before
+        has ``decay`` times what it had added (0: nothing, whatever that was);
+        the new tokens' slots start with their sum, slots behind them are left as
+        they are. The last tokens of a prompt alone, as new tokens, give what an
+        observation window sees."""
+        st = _kv.weigh(self._c, q, lens, lse, weights, starts, max_new, layer, self._scale if scale is None else scale, softcap,
+                       slopes, window, sinks, spans, decay, max_len, table, stream)
+        if st:
+            self._done(st)
+        return weights
+
+    def select(self, weights, lens, keep, kept=None, counts=None, weights_out=None, recent=0, sinks=0, keeps=None, max_len=0,
+               stream=None):
+        """Which slots stay (t2i_kv_select): of each sequence and head of
+        ``weights`` (fp32 [sequences, heads, slots]) at most ``keep``: the first
+        ``sinks``, the last ``recent`` and those of largest weight (of equals the
+        first). ``keeps``: int32 [sequences], fewer of some. ``weights_out``:
+        receives the weights of what stays, in order; may be ``weights`` itself.
+
+        Returns ``kept``, int32 [sequences, heads, ...], the slots in ascending
+        order (what lies behind their number is left as it is), and ``counts``,
+        int32 [sequences], their number: the new ``lens``."""
+        if kept is None or counts is None:
+            with torch.cuda.stream(self._stream(stream)):
+                if kept is None:
+                    kept = torch.empty((*weights.shape[:2], min(int(keep), weights.shape[2])), dtype=torch.int32, device=self.device)
+                if counts is None:
+                    counts = torch.empty(weights.shape[0], dtype=torch.int32, device=self.device)
+        st = _kv.select(self._c, weights, lens, keep, keeps, kept, counts, weights_out, recent, sinks, max_len, stream)
+        if st:
+            self._done(st)
+        return kept, counts
+
+    def evict(self, kept, counts, layer=None, table=None, stream=None):
+        """Moves the rows of the slots that stay together (t2i_kv_evict): for each
+        key head, of slot kept[s, head, i] to slot i, i < counts[s], in ``layer``,
+        or in all of them. ``kept``: int32 [sequences, kv_heads, any], ascending
+        (one list for all heads: ``kept.expand(-1, kv_heads, -1)``). The sequence
+        then has counts[s] tokens; a token's position is not its slot any more
+        (``append`` takes ``positions``)."""
+        st = _kv.evict(self._c, kept, counts, 0 if layer is None else layer, self.layers if layer is None else 1, table, stream)
         if st:
             self._done(st)
 

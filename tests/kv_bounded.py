@@ -49,3 +49,40 @@ def attend64(q, key, val, scale, softcap=0.0, slopes=None, window=0, sinks=0, tr
         v = val[:, h // (H // K)].double()
         out[:, h], spread[:, h] = p @ v, p @ v.abs()
     return out, lse, spread, big
+
+
+def weigh64(q, key, lse, scale, softcap=0.0, slopes=None, window=0, sinks=0, spans=None):
+    """What each slot gets [kv_heads, L], and how far a kernel may be from it: a score, in fp32 from exact products, is
+    within 2^-20 of its row's largest magnitude; a few units of exp2, of the scaled argument and of the distance's bias
+    are 1e-5 in all (arguments that matter are below 32); a weight below 2^-126 may be 0."""
+    m, H, _ = q.shape
+    L, K = key.shape[0], key.shape[1]
+    see, pos, kpos = visible(m, L, window, sinks, spans)
+    got, off = torch.zeros(K, L, dtype=torch.float64), torch.zeros(K, L, dtype=torch.float64)
+    for h in range(H):
+        x, big = scores64(q, key, h, see, pos, kpos, scale, softcap, slopes)
+        some = lse[:, h] > -math.inf
+        p = torch.exp(x[some] - lse[some, h].double()[:, None])
+        got[h // (H // K)] += p.sum(0)
+        off[h // (H // K)] += ((1e-5 + 2.0 ** -20 * big[some])[:, None] * p).sum(0) + m * 2.0 ** -126
+    return got, 1.01 * off
+
+
+def near_weights(got, held, want, off, ctx, decay, what=""):
+    """A row's weights [kv_heads, L] after the call: decay * held + want before the new tokens, want from there on; a few
+    roundings of the whole sum (each below 2^-24 of it, in pieces that are added up apart) are 2^-20 of it."""
+    old = torch.where(torch.arange(want.shape[1]) < ctx, held.double() * decay if decay else 0.0, 0.0)
+    err = (got.double() - (old + want)).abs()
+    bound = off + 2.0 ** -20 * (old.abs() + want)
+    assert torch.isfinite(got).all(), f"{what}: not finite"
+    assert (err <= bound).all(), f"{what}: {float((err / bound).nan_to_num().max()):.3f} of the bound"
+
+
+def select_plain(w, n, sinks, recent):
+    """Slots of a row w [L] that stay, ascending, n of them: an order by numbers, of equals by slot."""
+    L = len(w)
+    a = min(sinks, n)
+    b = min(recent, n - a)
+    middle = [j for j in range(a, L - b)]
+    middle.sort(key=lambda j: (1, 0.0) if math.isnan(w[j]) else (0, -w[j]))  # (sort keeps the order of equals)
+    return sorted([*range(a), *middle[:n - a - b], *range(L - b, L)])
