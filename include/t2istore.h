@@ -588,8 +588,7 @@ typedef struct t2i_kv_weigh_desc {
 t2i_status t2i_kv_weigh(t2i_kv* kv, const t2i_kv_weigh_desc* desc, void* cuda_stream);
 
 /* Workspace bytes that t2i_kv_weigh needs for such a batch at most.         */
-t2i_status t2i_kv_weigh_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads,
-                                        uint64_t* out);
+t2i_status t2i_kv_weigh_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint64_t* out);
 
 typedef struct t2i_kv_select_desc {
     const float* weights;   /* device, [n_seqs][n_heads][n_slots]            */

@@ -108,7 +108,7 @@ PROTOTYPES = {
     "t2i_kv_workspace_bytes": (_S, [_P, _U32, _U32, _U32, _PU64]),
     "t2i_kv_commit": (_S, [_P, _P, _P]),
     "t2i_kv_weigh": (_S, [_P, _P, _P]),
-    "t2i_kv_weigh_workspace_bytes": (_S, [_P, _U32, _U32, _U32, _PU64]),
+    "t2i_kv_weigh_workspace_bytes": (_S, [_P, _U32, _U32, _PU64]),
     "t2i_kv_select": (_S, [_P, _P, _P]),
     "t2i_kv_evict": (_S, [_P, _P, _P]),
     "t2i_kv_inject_timeout": (_S, [_P, _U32]),

@@ -297,8 +297,8 @@ t2i_status attend(t2i_kv* kv, const t2i_kv_attend_desc& d, cudaStream_t stream) 
     a.scale = d.scale;
     a.softcap = d.softcap;
     const uint32_t no_loads = kv->timeout_countdown && --kv->timeout_countdown == 0;
-    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms, no_loads};
     const bool bf16 = kv->layout.dtype == T2I_BF16;
+    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms, no_loads, bf16};
     return launch(kv, "kv_attend", [&] {
         if (uint64_t(a.group) * a.tok.max_new <= kFewRows) return bf16 ? launch_kv_few_bf16(a, l, stream) : launch_kv_few_f16(a, l, stream);
         return bf16 ? launch_kv_rows_bf16(a, l, stream) : launch_kv_rows_f16(a, l, stream);
@@ -363,9 +363,11 @@ t2i_status weigh(t2i_kv* kv, const t2i_kv_weigh_desc& d, cudaStream_t stream) {
     c.range("weights", d.weights, bytes, 4);
     if (d.slopes) c.range("slopes", d.slopes, d.q_heads * 4, 4);
     if (d.spans) c.range("spans", d.spans, n * 8, 8);
-    const uint64_t need = kv_weigh_workspace(kv->sms, seqs, d.batch.n_tokens, d.q_heads / K);
+    const uint64_t need = kv_weigh_workspace(kv->sms, seqs, d.batch.n_tokens);
     c.require(d.workspace_bytes >= need, "the workspace is smaller than t2i_kv_weigh_workspace_bytes");
-    if (need) c.range("workspace", d.workspace, need, 256);
+    c.range("workspace", d.workspace, need, 256);
+    // (a tensor map's strides are below 2^40 bytes)
+    c.require(n == 1 || d.q_stride < (uint64_t(1) << 39), "q: the stride is too large");
     if (!c.ok()) return T2I_ERR_INVALID;
     c.require(!overlap(d.weights, bytes, d.lse, n * d.q_heads * 4) &&
                   !overlap(d.weights, bytes, d.q, c.token_bytes(n, d.q_heads, d.q_stride, 2)), "weights overlap q or lse");
@@ -386,9 +388,10 @@ t2i_status weigh(t2i_kv* kv, const t2i_kv_weigh_desc& d, cudaStream_t stream) {
     w.n_slots = d.n_slots;
     w.decay = d.decay;
     const uint32_t no_loads = kv->timeout_countdown && --kv->timeout_countdown == 0;
-    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms, no_loads};
+    const bool bf16 = kv->layout.dtype == T2I_BF16;
+    const KvLaunch l{&kv->map, d.workspace, kv->fault_dev, kv->sms, no_loads, bf16};
     return launch(kv, "kv_weigh", [&] {
-        return kv->layout.dtype == T2I_BF16 ? launch_kv_weigh_bf16(w, l, stream) : launch_kv_weigh_f16(w, l, stream);
+        return bf16 ? launch_kv_weigh_bf16(w, l, stream) : launch_kv_weigh_f16(w, l, stream);
     });
 }
 
@@ -462,23 +465,49 @@ t2i_status evict(t2i_kv* kv, const t2i_kv_evict_desc& d, cudaStream_t stream) {
     return launch(kv, "kv_evict", [&] { return launch_kv_evict(e, kv->sms, stream); });
 }
 
+}  // namespace
+
 using PFN_encodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+namespace {
+// Null where the driver has no tensor maps.
+PFN_encodeTiled encode_tiled() {
+    static const PFN_encodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+                       q == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<PFN_encodeTiled>(p)
+                   : nullptr;
+    }();
+    return f;
+}
+}  // namespace
+
+cudaError_t KvLaunch::encode_queries(const KvAttend& a, uint32_t heads, uint32_t tokens, CUtensorMap* out) const {
+    const uint32_t D = a.pages.head_dim;
+    const cuuint64_t dims[3] = {D, a.q_heads, a.tok.n_tokens};
+    const cuuint64_t strides[2] = {D * 2u, a.tok.n_tokens > 1 ? a.q_stride * 2 : cuuint64_t(a.q_heads) * D * 2};
+    const cuuint32_t box[3] = {64, heads, tokens}, step[3] = {1, 1, 1};
+    const CUresult r = encode_tiled()(out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                                      const_cast<void*>(a.q), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+namespace {
 // The pool's pages for TMA (KvLaunch::map): null, or why not.
 const char* encode_map(t2i_kv* kv) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-        return "the driver has no tensor maps";
+    const PFN_encodeTiled encode = encode_tiled();
+    if (!encode) return "the driver has no tensor maps";
     const t2i_kv_layout& l = kv->layout;
     const cuuint64_t dims[3] = {l.head_dim, (cuuint64_t(l.layers) * 2 * l.kv_heads) << kv->token_shift, kv->info.total_pages};
     const cuuint64_t strides[2] = {l.head_dim * 2u, kv->info.page_bytes};
     const cuuint32_t box[3] = {64, kv->token_shift < 7 ? 1u << kv->token_shift : 128u, 1};
     const cuuint32_t step[3] = {1, 1, 1};
-    const CUresult r = reinterpret_cast<PFN_encodeTiled>(p)(
+    const CUresult r = encode(
         &kv->map, l.dtype == T2I_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
         reinterpret_cast<void*>(kv->info.pool), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -607,9 +636,9 @@ t2i_status t2i_kv_evict(t2i_kv* kv, const t2i_kv_evict_desc* desc, void* cuda_st
     T2I_KV_CALL(kv, desc, t2i::evict(kv, *desc, static_cast<cudaStream_t>(cuda_stream)));
 }
 
-t2i_status t2i_kv_weigh_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, uint64_t* out) {
+t2i_status t2i_kv_weigh_workspace_bytes(const t2i_kv* kv, uint32_t n_seqs, uint32_t n_tokens, uint64_t* out) {
     if (!kv || !out) return T2I_ERR_INVALID;
-    *out = t2i::kv_weigh_workspace(kv->sms, n_seqs, n_tokens, q_heads / kv->layout.kv_heads);
+    *out = t2i::kv_weigh_workspace(kv->sms, n_seqs, n_tokens);
     return T2I_OK;
 }
 

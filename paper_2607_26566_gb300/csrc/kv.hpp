@@ -131,6 +131,10 @@ struct KvLaunch {
     uint32_t* fault;  // host memory that the device writes: not 0 after a wait that ran out
     uint32_t sms;
     uint32_t no_loads;  // testing: the loading warps do nothing
+    // The queries as [tokens][heads][head_dim], in boxes of 64 elements of `heads` heads of `tokens` tokens, as map has
+    // the rows.
+    cudaError_t encode_queries(const KvAttend& a, uint32_t heads, uint32_t tokens, CUtensorMap* out) const;
+    uint32_t bf16;
 };
 // Up to this many queries to a key head (new tokens of a sequence x heads of a group) kv_few.cuh, above it
 // kv_rows.cuh. Queries, and us of the one / the other, for a sequence of 1.5k slots, 24 of 8k (heads of 128) and 3 of
@@ -146,6 +150,6 @@ cudaError_t launch_kv_rows_f16(const KvAttend& a, const KvLaunch& l, cudaStream_
 uint64_t kv_rows_workspace(uint32_t sms, uint32_t n_seqs, uint32_t n_tokens, uint32_t group);
 cudaError_t launch_kv_weigh_bf16(const KvWeigh& w, const KvLaunch& l, cudaStream_t stream);
 cudaError_t launch_kv_weigh_f16(const KvWeigh& w, const KvLaunch& l, cudaStream_t stream);
-uint64_t kv_weigh_workspace(uint32_t sms, uint32_t n_seqs, uint32_t n_tokens, uint32_t group);
+uint64_t kv_weigh_workspace(uint32_t sms, uint32_t n_seqs, uint32_t n_tokens);
 
 }  // namespace t2i

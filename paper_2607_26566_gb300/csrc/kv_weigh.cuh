@@ -1,5 +1,22 @@
-// Accumulated attention: what each slot gets from new tokens.
+// Accumulated attention: what each slot of the cache gets from new tokens, the sum of exp(score - lse) over the tokens
+// that see it and the heads that share its key.
+//
+// With an attention's log-sum-exp at hand no maximum and no second product is needed: S^T = K Q^T on the tensor cores,
+// 128 keys to the rows of a product and N queries to its columns, so that a thread has one key, adds its row up, and
+// nothing goes from thread to thread. A unit is 256 keys of one key head in two halves, one to each half of the softmax
+// warps: its keys are loaded once (TMA), its queries, 128 columns at a time, once for both halves.
+//
+// Two regimes. A decoding step (N = 16 or 32: all queries of a key head are one column tile) is bound by reading the
+// keys: each block streams them through a deep ring. A prompt (N = 128) is bound by an exponential a score beside the
+// product; keys stay while column tiles pass.
+//
+// Work split: the column tiles (steps) of all units, in order, are cut into equal runs, one to an SM. A unit that lies in
+// several runs is joined by a second kernel, in the order of the runs: results do not depend on timing.
 #pragma once
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "kv_attend.cuh"
 #include "t2istore.h"
@@ -7,54 +24,619 @@
 namespace t2i {
 namespace {
 
-// A thread a slot.
-template <class T>
-__global__ void __launch_bounds__(128) weigh_kernel(const __grid_constant__ KvWeigh w) {
-    const KvAttend& a = w.a;
-    __shared__ float qs[128];
-    tc::pdl_launch();
-    tc::pdl_wait();
-    const uint32_t s = blockIdx.y / a.pages.kv_heads, h = blockIdx.y % a.pages.kv_heads, D = a.pages.head_dim;
-    const KvSeq q = kv_seq(a.pages, a.tok, s);
-    const int32_t ctx = q.len - q.n, m = min(q.n, int32_t(a.tok.max_new));
-    for (int64_t j0 = int64_t(blockIdx.x) * 128; j0 < q.len; j0 += int64_t(gridDim.x) * 128) {
-        const int32_t j = int32_t(j0) + int32_t(threadIdx.x);
-        const T* key = j < q.len ? reinterpret_cast<const T*>(kv_row(a.pages, s, j, a.pages.layer, 0, h)) : nullptr;
-        KvSum sum;
-        for (int32_t i = 0; i < m; ++i) {
-            const KvQuery y = kv_query(a, q, i);
-            const bool see = j < q.len && (j >= y.first || j < int32_t(a.sinks)) && j < y.last;
-            for (uint32_t g = 0; g < a.group; ++g) {
-                const uint32_t head = h * a.group + g;
-                __syncthreads();
-                if (threadIdx.x < D)
-                    qs[threadIdx.x] = float(static_cast<const T*>(a.q)[uint64_t(q.first + i) * a.q_stride + head * D + threadIdx.x]);
-                __syncthreads();
-                if (!see) continue;
-                float x = 0.0f;
-                if (key)
-                    for (uint32_t d = 0; d < D; d += 8) {
-                        float k[8];
-                        kv_load8(key + d, k);
-                        for (int e = 0; e < 8; ++e) x += k[e] * qs[d + e];
-                    }
-                x *= a.scale;
-                if (a.softcap != 0.0f) x = a.softcap * tanhf(x / a.softcap);
-                if (a.slopes) x -= a.slopes[head] * fabsf(float(y.pos - j));
-                const float lse = w.lse[uint64_t(q.first + i) * a.q_heads + head];
-                if (lse != -INFINITY) sum.add(expf(x - lse));
-            }
-        }
-        if (j < q.len && uint32_t(j) < w.n_slots) {
-            float* at = w.weights + s * w.seq_stride + h * w.head_stride + j;
-            *at = sum.value() + (j < ctx && w.decay != 0.0f ? w.decay * *at : 0.0f);
+using namespace tc;
+
+constexpr int kUnitKeys = 256;
+constexpr int kWeighThreads = 320;  // eight softmax warps, the loading warp, the product warp
+constexpr uint32_t kHalfSlot = 16384;  // 128 keys of 64 elements
+constexpr uint32_t kWeighUnits = 8;    // handed out at a time
+constexpr uint32_t kWeighReaders = 9;
+constexpr int kPartFloats = kUnitKeys;
+
+template <int N, int NS>
+struct WeighShape {
+    static constexpr uint32_t kHalf = kHalfSlot * NS;                        // a half's keys
+    static constexpr uint32_t kKeys = (N == 128 ? 3 : 6) * (NS == 1 ? 2 : 1);  // ... in the ring
+    static constexpr uint32_t kQ = N * 128 * NS;                             // a column tile
+    static constexpr uint32_t kQs = N == 128 ? (NS == 1 ? 5 : 3) : N == 32 ? 2 : 4;
+    static constexpr uint32_t kBufs = N == 128 ? 2 : 4;                      // tiles of scores of each half
+    static constexpr uint32_t kTmem = 2 * kBufs * N;
+    static constexpr uint32_t kBytes = 1024 + kHalf * kKeys + kQ * kQs;
+    static constexpr uint32_t kFixed = 4096 + 8 * N * 16;  // static shared memory, at most
+    static_assert(kBytes + kFixed + 1024 <= 228 * 1024, "an SM's shared memory");
+    static constexpr int kChunk = N < 32 ? N : 32;  // columns that a thread works on at a time
+};
+
+struct WeighUnit {
+    KvSeq q;
+    int32_t s, h, slot0;  // the unit's first slot
+    int32_t tile, n;      // the segment's first column tile, and how many
+    int32_t dry;          // no token sees its slots
+    int32_t whole, part;  // the segment is all of the unit; else its place in the workspace
+    int32_t more;
+};
+struct WeighJoin {
+    int32_t s, h, slot0, ctx, len;
+    int32_t b0, b1, second, valid;
+};
+
+struct Weigh {
+    KvWeigh w;
+    int32_t per_tile;   // tokens of a column tile
+    int32_t per_token;  // columns of a token in a tile
+    int32_t slices;     // column tiles of a token (1 unless it has more heads than a tile columns)
+    int32_t skips;      // units that no token sees are left alone
+    WeighJoin* join;    // [blocks]
+    float* part;        // [2 * blocks][kPartFloats]
+    int2* hulls;        // with spans: slots outside which a column tile's tokens see nothing
+    uint32_t* fault;
+    uint32_t no_loads;
+};
+
+__device__ __forceinline__ int32_t weigh_tokens(const KvAttend& a, const KvSeq& q) { return min(q.n, int32_t(a.tok.max_new)); }
+
+// Units of a sequence: those of its sinks, then those from its windows on; all where the weights so far decay.
+struct UnitList {
+    int32_t head, lo, n;
+};
+__device__ __forceinline__ UnitList unit_list(const Weigh& f, const KvSeq& q) {
+    UnitList u{0, 0, 0};
+    if (q.n == 0) return u;
+    const KvAttend& a = f.w.a;
+    if (f.skips && a.window) {
+        const int64_t lo = int64_t(q.len) - q.n + 1 - int64_t(a.window);
+        if (lo > 0) {
+            u.lo = int32_t(lo / kUnitKeys);
+            u.head = min((int32_t(a.sinks) + kUnitKeys - 1) / kUnitKeys, u.lo);
         }
     }
+    u.n = u.head + (q.len + kUnitKeys - 1) / kUnitKeys - u.lo;
+    return u;
+}
+__device__ __forceinline__ int32_t unit_slot(const UnitList& u, int32_t i) { return (i < u.head ? i : u.lo + i - u.head) * kUnitKeys; }
+
+// The column tiles [lo, hi) that see something of a unit; none: hi <= lo.
+__device__ __forceinline__ int2 unit_tiles(const Weigh& f, const KvSeq& q, uint32_t s, int32_t slot0) {
+    const KvAttend& a = f.w.a;
+    const int32_t ctx = q.len - q.n, m = weigh_tokens(a, q), slot1 = min(slot0 + kUnitKeys, q.len);
+    if (a.spans) {
+        const int2* const hull = f.hulls + q.first / f.per_tile + s;
+        const int32_t tiles = (m + f.per_tile - 1) / f.per_tile;
+        int2 r = make_int2(tiles, 0);
+        for (int32_t t = 0; t < tiles; ++t) {
+            const int2 x = hull[t];
+            if (x.x < slot1 && x.y > slot0) r.x = min(r.x, t), r.y = t + 1;
+        }
+        return make_int2(r.x * f.slices, r.y * f.slices);
+    }
+    const int32_t i0 = max(0, slot0 - ctx);
+    int64_t i1 = m;
+    if (a.window && slot0 >= int32_t(a.sinks)) i1 = min(i1, int64_t(slot1) - 1 + int64_t(a.window) - ctx);
+    if (i0 >= i1) return make_int2(0, 0);
+    return make_int2(i0 / f.per_tile * f.slices, int32_t((i1 + f.per_tile - 1) / f.per_tile) * f.slices);
+}
+__device__ __forceinline__ int32_t unit_steps(const Weigh& f, const KvSeq& q, uint32_t s, int32_t slot0) {
+    const int2 t = unit_tiles(f, q, s, slot0);
+    return max(1, t.y - t.x);
+}
+
+// Steps of one head of a sequence. Of one column tile a unit is one step; else by a warp.
+template <bool ONE>
+__device__ __forceinline__ int64_t seq_steps(const Weigh& f, const KvSeq& q, uint32_t s, uint32_t lane) {
+    const UnitList u = unit_list(f, q);
+    if (ONE) return u.n;
+    int64_t n = 0;
+    for (int32_t i = int32_t(lane); i < u.n; i += 32) n += unit_steps(f, q, s, unit_slot(u, i));
+#pragma unroll
+    for (int d = 16; d; d >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, d);
+    return n;
+}
+
+struct WeighShared {
+    uint64_t k_full[12], k_empty[12], q_full[5], q_empty[5];
+    uint64_t s_full[2][4], s_empty[2][4];
+    uint64_t unit_full[kWeighUnits], unit_empty[kWeighUnits];
+    WeighUnit unit[kWeighUnits];
+    uint32_t tmem, dead;
+    int32_t start_seq;
+    int64_t start_rest, start_steps;
+    int64_t sums[kWeighThreads / 32];
+};
+
+// Spans of column tiles, a thread a tile.
+__global__ void __launch_bounds__(128) hull_kernel(const __grid_constant__ Weigh f) {
+    const KvAttend& a = f.w.a;
+    pdl_launch();
+    pdl_wait();
+    const uint32_t s = blockIdx.x;
+    const KvSeq q = kv_seq(a.pages, a.tok, s);
+    const int32_t m = weigh_tokens(a, q), tiles = (m + f.per_tile - 1) / f.per_tile;
+    for (int32_t t = int32_t(threadIdx.x); t < tiles; t += 128) {
+        int2 r = make_int2(INT32_MAX, 0);
+        for (int32_t i = t * f.per_tile; i < min(m, (t + 1) * f.per_tile); ++i) {
+            const int2 x = reinterpret_cast<const int2*>(a.spans)[q.first + i];
+            const int32_t lo = max(x.x, 0), hi = min(x.y, q.len);
+            if (hi > lo) r.x = min(r.x, lo), r.y = max(r.y, hi);
+        }
+        f.hulls[q.first / f.per_tile + s + t] = r;
+    }
+}
+
+__device__ __forceinline__ uint64_t weigh_pack(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 weigh_unpack(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+
+template <class T, int N, int NS, bool MOD>
+__global__ void __launch_bounds__(kWeighThreads, 1)
+    weigh_kernel(const __grid_constant__ Weigh f, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
+    using Sh = WeighShape<N, NS>;
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr bool kOne = N != 128;  // one column tile a sequence
+    constexpr int kChunk = Sh::kChunk;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t ring = base, qs = ring + Sh::kHalf * Sh::kKeys;
+    __shared__ __align__(16) WeighShared sh;
+    // each softmax warp's own: of its column tile the log-sum-exps in units of log2, spans, slopes
+    __shared__ __align__(16) float lse_of[8][N];
+    __shared__ __align__(16) int2 span_of[8][N];
+    __shared__ __align__(16) float slope_of[MOD ? 8 : 1][N];
+    __shared__ __align__(16) float token_of[MOD ? N : 4];  // a column's token, counted in the tile
+    static_assert(sizeof(WeighShared) + 8 * N * 16 + N * 4 <= Sh::kFixed + N * 4, "");
+    const KvAttend& a = f.w.a;
+    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    volatile uint32_t* dead = &sh.dead;
+    auto bar = [&](const uint64_t& b) { return smem_u32(&b); };
+    if (tid == 0) {
+        for (uint32_t i = 0; i < Sh::kKeys; ++i) mbar_init(bar(sh.k_full[i]), 1), mbar_init(bar(sh.k_empty[i]), 1);
+        for (uint32_t i = 0; i < Sh::kQs; ++i) mbar_init(bar(sh.q_full[i]), 1), mbar_init(bar(sh.q_empty[i]), 1);
+        for (uint32_t i = 0; i < Sh::kBufs; ++i)
+            for (int h = 0; h < 2; ++h) mbar_init(bar(sh.s_full[h][i]), 1), mbar_init(bar(sh.s_empty[h][i]), 4);
+        for (uint32_t i = 0; i < kWeighUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kWeighReaders);
+        sh.dead = 0;
+        fence_mbar_init();
+        tma_prefetch_map(&map), tma_prefetch_map(&q_map);
+    }
+    if (MOD && tid < N) token_of[tid] = float(int32_t(tid) / f.per_token);
+    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), Sh::kTmem);
+    pdl_launch();
+    pdl_wait();
+    if (!kOne && tid == 0) f.join[blockIdx.x].valid = 0;
+
+    // the block's run of steps: sequences by threads (by warps, where a unit may have several steps)
+    const int64_t K = a.pages.kv_heads;
+    const uint32_t who = kOne ? tid : warp, all = kOne ? kWeighThreads : kWeighThreads / 32;
+    const uint32_t per = (a.tok.n_seqs + all - 1) / all;
+    int64_t mine = 0;
+    for (uint32_t s = who * per; s < min(a.tok.n_seqs, (who + 1) * per); ++s)
+        mine += seq_steps<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
+    int64_t lo = 0, total = 0;  // steps of a head of the sequences before, and of all
+    if (kOne) {
+        int64_t inc = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+            if (lane >= uint32_t(d)) inc += o;
+        }
+        if (lane == 31) sh.sums[warp] = inc;
+        lo = inc - mine;
+    } else if (lane == 0) {
+        sh.sums[warp] = mine;
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    for (uint32_t i = 0; i < kWeighThreads / 32; ++i) {
+        if (i < warp) lo += sh.sums[i];
+        total += sh.sums[i];
+    }
+    total *= K;
+    const int64_t blocks = min(int64_t(gridDim.x), total);
+    const bool busy = blockIdx.x < blocks;
+    const int64_t run0 = busy ? blockIdx.x * total / blocks : 0, run1 = busy ? (blockIdx.x + 1) * total / blocks : 0;
+    if (busy && run0 >= lo * K && run0 < (lo + mine) * K) {
+        int64_t p = lo * K;
+        for (uint32_t s = who * per;; ++s) {
+            const int64_t steps = seq_steps<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
+            if (run0 < p + steps * K) {
+                if (kOne || lane == 0) sh.start_seq = int32_t(s), sh.start_rest = run0 - p, sh.start_steps = steps;
+                break;
+            }
+            p += steps * K;
+        }
+    }
+    __syncthreads();
+    const uint32_t tmem = sh.tmem;
+
+    if (busy && warp == 8) {
+        // ---------------------------------------------------------- loads
+        int32_t s = sh.start_seq, h = int32_t(sh.start_rest / sh.start_steps), i = 0;  // sequence, key head, unit
+        int64_t at = run0, unit0;  // the segment's first step, the unit's
+        KvSeq q = kv_seq(a.pages, a.tok, s);
+        UnitList list = unit_list(f, q);
+        {
+            int64_t rest = sh.start_rest % sh.start_steps;
+            if (kOne) {
+                i = int32_t(rest), rest = 0;
+            } else {
+                for (;; i += 32) {  // the warp looks at 32 units at a time
+                    const int32_t mine = i + int32_t(lane) < list.n ? unit_steps(f, q, s, unit_slot(list, i + int32_t(lane))) : 0;
+                    int64_t inc = mine;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const int64_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+                        if (lane >= uint32_t(d)) inc += o;
+                    }
+                    const uint32_t found = __ballot_sync(0xFFFFFFFFu, rest < inc);
+                    if (found) {
+                        const int l = __ffs(found) - 1;
+                        rest -= __shfl_sync(0xFFFFFFFFu, inc - mine, l);
+                        i += l;
+                        break;
+                    }
+                    rest -= __shfl_sync(0xFFFFFFFFu, inc, 31);
+                    if (i + 32 >= list.n) break;  // (never: the steps add up)
+                }
+            }
+            unit0 = at - rest;
+        }
+        const uint32_t shift = a.pages.token_shift;
+        const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
+        const uint32_t T_mask = (1u << shift) - 1;
+        const uint32_t q_bytes = uint32_t(f.per_tile * f.per_token) * 128 * NS;
+        uint32_t u = 0, kn = 0, qn = 0;
+        for (bool more = !f.no_loads; more; ++u) {
+            // the segment
+            const int32_t slot0 = unit_slot(list, i);
+            const int2 tiles = unit_tiles(f, q, s, slot0);
+            const bool dry = tiles.y <= tiles.x;
+            const int32_t steps = max(1, tiles.y - tiles.x), skip = int32_t(at - unit0);
+            const int32_t n = int32_t(min(int64_t(steps - skip), run1 - at));
+            more = at + n < run1;
+            if (!mbar_wait(bar(sh.unit_empty[u % kWeighUnits]), (u / kWeighUnits & 1) ^ 1, dead)) break;
+            if (lane == 0) {
+                WeighUnit& o = sh.unit[u % kWeighUnits];
+                o.q = q, o.s = s, o.h = h, o.slot0 = slot0;
+                o.tile = tiles.x + skip, o.n = n, o.dry = dry, o.whole = n == steps, o.part = at == run0 ? 0 : 1, o.more = more;
+                mbar_arrive(bar(sh.unit_full[u % kWeighUnits]));
+                if (!kOne && at == run0) {
+                    // this run's note of a unit that began in the run before it
+                    const int64_t b0 = ((unit0 + 1) * blocks - 1) / total, b1 = ((unit0 + steps) * blocks - 1) / total;
+                    const bool here = skip > 0 && b0 + 1 == int64_t(blockIdx.x);
+                    f.join[blockIdx.x] = {s, h, slot0, q.len - q.n, q.len, int32_t(b0), int32_t(b1), b0 * total / blocks != unit0, here};
+                }
+            }
+            __syncwarp();
+            if (!dry) {
+                const int32_t row = int32_t((a.pages.layer * 2 * a.pages.kv_heads + h) << shift);
+                const int32_t* table = a.pages.table + uint32_t(s) * a.pages.table_stride;
+                for (int half = 0; half < 2; ++half, ++kn) {
+                    const uint32_t slot = uint32_t(slot0) + half * 128 + lane * box, e = kn % Sh::kKeys;
+                    int32_t page = -1;
+                    if (lane < boxes && slot < uint32_t(q.len)) page = table[slot >> shift];
+                    // what the pool lacks, and what lies behind the sequence, is filled with zeros
+                    const int32_t z = uint32_t(page) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page;
+                    if (!mbar_wait(bar(sh.k_empty[e]), (kn / Sh::kKeys & 1) ^ 1, dead)) goto loads_done;
+                    if (lane == 0) mbar_expect(bar(sh.k_full[e]), Sh::kHalf);
+                    __syncwarp();
+                    if (lane < boxes)
+                        for (int x = 0; x < NS; ++x)
+                            tma_load(ring + e * Sh::kHalf + x * kHalfSlot + lane * box * 128, &map, x * 64, row + int32_t(slot & T_mask), z,
+                                     bar(sh.k_full[e]));
+                }
+                for (int32_t t = tiles.x + skip; t < tiles.x + skip + n; ++t, ++qn) {
+                    const uint32_t e = qn % Sh::kQs;
+                    if (!mbar_wait(bar(sh.q_empty[e]), (qn / Sh::kQs & 1) ^ 1, dead)) goto loads_done;
+                    if (lane == 0) {
+                        mbar_expect(bar(sh.q_full[e]), q_bytes);
+                        const int32_t token = q.first + t / f.slices * f.per_tile, head = h * int32_t(a.group) + t % f.slices * f.per_token;
+                        for (int x = 0; x < NS; ++x)
+                            tma_load(qs + e * Sh::kQ + x * (N * 128), &q_map, x * 64, head, token, bar(sh.q_full[e]));
+                    }
+                    __syncwarp();
+                }
+            }
+            at += n;
+            if (more) {  // the next unit (the segment ended with this one)
+                unit0 = at;
+                if (++i == list.n) {
+                    i = 0;
+                    if (++h == int32_t(K)) {
+                        h = 0;
+                        do {
+                            ++s;
+                            q = kv_seq(a.pages, a.tok, s);
+                            list = unit_list(f, q);
+                        } while (list.n == 0);
+                    }
+                }
+            }
+        }
+    loads_done:
+        __syncwarp();
+        if (*dead) {  // the copies in flight land before the block ends
+            uint32_t late = 0;
+            for (uint32_t k = kn > Sh::kKeys ? kn - Sh::kKeys : 0; k < kn; ++k) mbar_wait(bar(sh.k_full[k % Sh::kKeys]), k / Sh::kKeys & 1, &late);
+            for (uint32_t k = qn > Sh::kQs ? qn - Sh::kQs : 0; k < qn; ++k) mbar_wait(bar(sh.q_full[k % Sh::kQs]), k / Sh::kQs & 1, &late);
+        }
+    } else if (busy && warp == 9) {
+        // ---------------------------------------------------------- products
+        constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
+        const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
+        // keys and queries: rows of 64 elements, 128-byte swizzle
+        const uint64_t kd = smem_desc(ring, 16, 1024, 2), qd = smem_desc(qs, 16, 1024, 2);
+        uint32_t kn = 0, qn = 0, n = 0;
+        bool more = true;
+        for (uint32_t u = 0; more; ++u) {
+            const bool got = mbar_wait(bar(sh.unit_full[u % kWeighUnits]), u / kWeighUnits & 1, dead);
+            if (!__all_sync(0xFFFFFFFFu, got)) break;
+            const WeighUnit& o = sh.unit[u % kWeighUnits];
+            const int32_t steps = o.dry ? 0 : o.n;
+            more = o.more;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
+            for (int32_t i = 0; i < steps; ++i, ++n, ++qn) {
+                const uint32_t eq = qn % Sh::kQs, buf = n % Sh::kBufs;
+                const bool there = mbar_wait(bar(sh.q_full[eq]), qn / Sh::kQs & 1, dead);
+                if (!__all_sync(0xFFFFFFFFu, there)) goto products_done;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t k = kn + half, ek = k % Sh::kKeys;
+                    if (i == 0) mbar_wait(bar(sh.k_full[ek]), k / Sh::kKeys & 1, dead);
+                    mbar_wait(bar(sh.s_empty[half][buf]), (n / Sh::kBufs & 1) ^ 1, dead);
+                    fence_after();
+                    if (elect() && !*dead) {
+                        const uint64_t k0 = desc_at(kd, ek * Sh::kHalf), q0 = desc_at(qd, eq * Sh::kQ);
+#pragma unroll
+                        for (uint32_t x = 0; x < 4 * NS; ++x) {
+                            if (x >= ksteps) break;
+                            mma_ss(tmem + (half * Sh::kBufs + buf) * N, desc_at(k0, (x / 4) * kHalfSlot + (x % 4) * 32),
+                                   desc_at(q0, (x / 4) * (N * 128) + (x % 4) * 32), kQk, x != 0);
+                        }
+                        mma_commit(bar(sh.s_full[half][buf]));
+                        if (i + 1 == steps) mma_commit(bar(sh.k_empty[ek]));
+                        if (half == 1) mma_commit(bar(sh.q_empty[eq]));
+                    }
+                    __syncwarp();
+                }
+            }
+            if (steps) kn += 2;
+        }
+    products_done:
+        if (*dead) {  // the products in flight end before the tensor memory is freed
+            const uint64_t t0 = now_ns();
+            while (now_ns() - t0 < 50000) {
+            }
+        }
+    } else if (busy) {
+        // ---------------------------------------------------------- weights
+        const int half = warp / 4;
+        const uint32_t key = tid % 128;
+        const uint32_t lanes = tmem + ((warp % 4) << 21) + half * Sh::kBufs * N;
+        const float k2 = a.scale * kLog2e;
+        const bool cap = MOD && a.softcap != 0.0f;
+        const float cap_in = cap ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
+        const uint64_t k22 = weigh_pack(k2, k2);
+        float* const lse_at = lse_of[warp];
+        int32_t had_s = -1, had_h = -1;  // whose column tile's log-sum-exps are there (of one tile a sequence)
+        uint32_t n = 0;
+        bool more = true;
+        for (uint32_t u = 0; more; ++u) {
+            const bool got = mbar_wait(bar(sh.unit_full[u % kWeighUnits]), u / kWeighUnits & 1, dead);
+            if (!__all_sync(0xFFFFFFFFu, got)) break;
+            const WeighUnit o = sh.unit[u % kWeighUnits];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
+            more = o.more;
+            const int32_t slot = o.slot0 + half * 128 + int32_t(key), ctx = o.q.len - o.q.n, m = weigh_tokens(a, o.q);
+            const bool mine = slot < o.q.len && uint32_t(slot) < f.w.n_slots;
+            float* const place = f.w.weights + uint32_t(o.s) * f.w.seq_stride + uint32_t(o.h) * f.w.head_stride + slot;
+            float held = 0.0f;
+            if (o.whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
+            // the tokens that see the slot
+            int32_t i0 = max(0, slot - ctx), i1 = m;
+            if (a.window && slot >= int32_t(a.sinks)) i1 = int32_t(min(int64_t(m), int64_t(slot) + int64_t(a.window) - ctx));
+            if (slot >= o.q.len) i1 = 0;
+            KvSum sum;
+            const int32_t steps = o.dry ? 0 : o.n;
+            for (int32_t i = 0; i < steps; ++i, ++n) {
+                const int32_t tile = o.tile + i, t0 = tile / f.slices * f.per_tile, g0 = tile % f.slices * f.per_token;
+                const int32_t cols = min(f.per_tile, m - t0) * min(f.per_token, int32_t(a.group) - g0);
+                if (!kOne || o.s != had_s || o.h != had_h) {
+                    __syncwarp();
+#pragma unroll
+                    for (int c0 = 0; c0 < N; c0 += 32) {
+                        const int32_t c = c0 + int32_t(lane);
+                        if (N < 32 && c >= N) break;
+                        float l = INFINITY, slope = 0.0f;
+                        int2 span = make_int2(0, 0);
+                        if (c < cols) {
+                            const uint64_t token = uint64_t(o.q.first) + t0 + c / f.per_token;
+                            const uint32_t head = o.h * a.group + g0 + c % f.per_token;
+                            l = f.w.lse[token * a.q_heads + head] * kLog2e;
+                            if (l == -INFINITY) l = INFINITY;
+                            if (a.spans) span = reinterpret_cast<const int2*>(a.spans)[token];
+                            if (MOD && a.slopes) slope = a.slopes[head] * kLog2e;
+                        }
+                        lse_at[c] = l;
+                        if (a.spans) span_of[warp][c] = span;
+                        if (MOD) slope_of[MOD ? warp : 0][c] = slope;
+                    }
+                    __syncwarp();
+                    had_s = o.s, had_h = o.h;
+                }
+                // the thread's visible columns [c0, c1)
+                const int32_t v0 = a.spans ? 0 : min(max(i0 - t0, 0), f.per_tile) * f.per_token;
+                const int32_t v1 = a.spans ? cols : min(min(max(i1 - t0, 0), f.per_tile) * f.per_token, cols);
+                const float ahead = float(ctx + t0 - slot);
+                const uint32_t buf = n % Sh::kBufs;
+                const bool there = mbar_wait(bar(sh.s_full[half][buf]), n / Sh::kBufs & 1, dead);
+                if (!__all_sync(0xFFFFFFFFu, there)) goto weights_done;
+                fence_after();
+                float x[N];
+                if constexpr (N == 16) {
+                    tmem_ld16(lanes + buf * N, x);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < N; c += 32) tmem_ld32(lanes + buf * N + c, x + c);
+                }
+                wait_ld(x);
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.s_empty[half][buf]));
+                uint64_t part0 = 0, part1 = 0;
+#pragma unroll
+                for (int c0 = 0; c0 < N; c0 += kChunk) {
+                    const bool some = v1 > c0 && v0 < c0 + kChunk && v0 < v1;
+                    if (!__any_sync(0xFFFFFFFFu, some)) continue;
+                    const bool plain = __all_sync(0xFFFFFFFFu, v0 <= c0 && v1 >= c0 + kChunk) && !a.spans;
+                    float y[kChunk];
+#pragma unroll
+                    for (int c = 0; c < kChunk; c += 4) {
+                        const float4 l = *reinterpret_cast<const float4*>(lse_at + c0 + c);
+                        if (MOD) {
+                            const float4 sl = *reinterpret_cast<const float4*>(slope_of[MOD ? warp : 0] + c0 + c);
+                            const float4 tk = *reinterpret_cast<const float4*>(token_of + c0 + c);
+                            const float sls[4] = {sl.x, sl.y, sl.z, sl.w}, ls[4] = {l.x, l.y, l.z, l.w}, tks[4] = {tk.x, tk.y, tk.z, tk.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                float z = cap ? capped<true>(x[c0 + c + k], cap_in, cap2) : x[c0 + c + k] * k2;
+                                z -= sls[k] * fabsf(ahead + tks[k]);
+                                y[c + k] = z - ls[k];
+                            }
+                        } else {
+                            uint64_t r0, r1;
+                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r0) : "l"(weigh_pack(x[c0 + c], x[c0 + c + 1])), "l"(k22), "l"(weigh_pack(-l.x, -l.y)));
+                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r1) : "l"(weigh_pack(x[c0 + c + 2], x[c0 + c + 3])), "l"(k22), "l"(weigh_pack(-l.z, -l.w)));
+                            const float2 a0 = weigh_unpack(r0), a1 = weigh_unpack(r1);
+                            y[c] = a0.x, y[c + 1] = a0.y, y[c + 2] = a1.x, y[c + 3] = a1.y;
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < kChunk; ++c) y[c] = exp2_approx(y[c]);
+                    if (!plain) {
+                        uint32_t see = 0;
+                        if (a.spans) {
+#pragma unroll
+                            for (int c = 0; c < kChunk; ++c) {
+                                const int2 sp = span_of[warp][c0 + c];
+                                see |= uint32_t(slot >= sp.x && slot < sp.y && c0 + c < v1) << c;
+                            }
+                            if (slot >= o.q.len) see = 0;
+                        } else {
+                            auto below = [](int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
+                            see = below(v1 - c0) & ~below(v0 - c0);
+                        }
+#pragma unroll
+                        for (int c = 0; c < kChunk; ++c) y[c] = see & (1u << c) ? y[c] : 0.0f;
+                    }
+#pragma unroll
+                    for (int c = 0; c < kChunk; c += 4) {
+                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part0) : "l"(weigh_pack(y[c], y[c + 1])));
+                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part1) : "l"(weigh_pack(y[c + 2], y[c + 3])));
+                    }
+                }
+                const float2 p0 = weigh_unpack(part0), p1 = weigh_unpack(part1);
+                sum.add((p0.x + p0.y) + (p1.x + p1.y));
+            }
+            if (!o.whole)
+                __stcg(f.part + (uint64_t(blockIdx.x) * 2 + o.part) * kPartFloats + half * 128 + key, sum.value());
+            else if (mine && !(o.dry && f.w.decay == 1.0f && slot < ctx))
+                *place = sum.value() + (slot < ctx && f.w.decay != 0.0f ? f.w.decay * held : 0.0f);
+        }
+    weights_done:;
+    }
+    __syncthreads();
+    if (tid == 0 && *dead) *f.fault = 1;
+    if (warp == 9) {
+        fence_after();
+        tmem_free(tmem, Sh::kTmem);
+    }
+}
+
+// Joins the units that lie in several runs: a block for each run's note, a thread a slot.
+__global__ void __launch_bounds__(kUnitKeys) weigh_join_kernel(const __grid_constant__ Weigh f) {
+    pdl_launch();
+    pdl_wait();
+    const WeighJoin j = f.join[blockIdx.x];
+    if (!j.valid) return;
+    const int32_t slot = j.slot0 + int32_t(threadIdx.x);
+    if (slot >= j.len || uint32_t(slot) >= f.w.n_slots) return;
+    KvSum sum;
+    for (int32_t b = j.b0; b <= j.b1; ++b)
+        sum.add(__ldcg(f.part + (uint64_t(b) * 2 + (b == j.b0 && j.second ? 1 : 0)) * kPartFloats + threadIdx.x));
+    float* const place = f.w.weights + uint32_t(j.s) * f.w.seq_stride + uint32_t(j.h) * f.w.head_stride + slot;
+    *place = sum.value() + (slot < j.ctx && f.w.decay != 0.0f ? f.w.decay * *place : 0.0f);
+}
+
+constexpr uint64_t weigh_up(uint64_t n) { return (n + 255) / 256 * 256; }
+// the workspace's parts, in order: notes, parts, hulls
+uint64_t weigh_hulls(uint64_t n_seqs, uint64_t n_tokens, uint64_t per_tile) { return n_tokens / per_tile + n_seqs + 1; }
+
+template <class T, int N, int NS, bool MOD>
+cudaError_t launch_weigh_as(const Weigh& f, const CUtensorMap& map, const CUtensorMap& q_map, uint32_t sms, cudaStream_t stream) {
+    constexpr uint32_t bytes = WeighShape<N, NS>::kBytes;
+    static std::atomic<uint64_t> ready{0};  // devices whose kernel may take this much shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !(ready.load() >> dev & 1)) {
+        e = cudaFuncSetAttribute(weigh_kernel<T, N, NS, MOD>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready |= uint64_t(1) << dev;
+    }
+    const KvAttend& a = f.w.a;
+    if (a.spans && (e = launch_pdl(hull_kernel, dim3(a.tok.n_seqs), 128, 0, stream, f)) != cudaSuccess) return e;
+    // no more blocks than there may be steps, going by max_len
+    const uint64_t tiles = N == 128 ? (uint64_t(a.tok.max_new) / f.per_tile + 1) * f.slices : 1;
+    const uint64_t steps = uint64_t(a.tok.n_seqs) * a.pages.kv_heads * (uint64_t(a.max_len) / kUnitKeys + 1);
+    const uint32_t blocks = uint32_t(steps > sms / tiles ? sms : steps * tiles);
+    if ((e = launch_pdl(weigh_kernel<T, N, NS, MOD>, dim3(blocks), kWeighThreads, bytes, stream, f, map, q_map)) != cudaSuccess) return e;
+    return N == 128 ? launch_pdl(weigh_join_kernel, dim3(blocks), kUnitKeys, 0, stream, f) : cudaSuccess;
+}
+
+template <class T, int N, int NS>
+cudaError_t launch_weigh_mod(const Weigh& f, const CUtensorMap& map, const CUtensorMap& q_map, uint32_t sms, cudaStream_t stream) {
+    return f.w.a.softcap != 0.0f || f.w.a.slopes ? launch_weigh_as<T, N, NS, true>(f, map, q_map, sms, stream)
+                                                 : launch_weigh_as<T, N, NS, false>(f, map, q_map, sms, stream);
+}
+
+template <class T, int N>
+cudaError_t launch_weigh_n(Weigh f, const KvLaunch& l, cudaStream_t stream) {
+    const KvAttend& a = f.w.a;
+    f.per_token = int32_t(std::min<uint32_t>(a.group, N));
+    f.slices = int32_t((a.group + f.per_token - 1) / f.per_token);
+    f.per_tile = int32_t(std::min<uint32_t>(N / f.per_token, a.tok.max_new));
+    CUtensorMap q_map;
+    // the queries as [tokens][heads][head_dim]: a column tile's in one box (64 elements at a time)
+    const cudaError_t e = l.encode_queries(a, f.per_token, f.per_tile, &q_map);
+    if (e != cudaSuccess) return e;
+    return a.pages.head_dim <= 64 ? launch_weigh_mod<T, N, 1>(f, *l.map, q_map, l.sms, stream)
+                                  : launch_weigh_mod<T, N, 2>(f, *l.map, q_map, l.sms, stream);
 }
 
 template <class T>
 cudaError_t launch_weigh(const KvWeigh& w, const KvLaunch& l, cudaStream_t stream) {
-    return launch_pdl(weigh_kernel<T>, dim3((w.a.max_len + 127) / 128, w.a.tok.n_seqs * w.a.pages.kv_heads), 128, 0, stream, w);
+    Weigh f{};
+    f.w = w;
+    f.skips = w.decay == 1.0f && !w.a.spans;
+    uint8_t* p = static_cast<uint8_t*>(l.workspace);
+    f.join = reinterpret_cast<WeighJoin*>(p);
+    p += weigh_up(l.sms * sizeof(WeighJoin));
+    f.part = reinterpret_cast<float*>(p);
+    p += weigh_up(uint64_t(l.sms) * 2 * kPartFloats * sizeof(float));
+    f.hulls = reinterpret_cast<int2*>(p);
+    f.fault = l.fault;
+    f.no_loads = l.no_loads;
+    const uint64_t rows = uint64_t(w.a.group) * w.a.tok.max_new;
+    return rows <= 16 ? launch_weigh_n<T, 16>(f, l, stream) : rows <= 32 ? launch_weigh_n<T, 32>(f, l, stream) : launch_weigh_n<T, 128>(f, l, stream);
 }
 
 }  // namespace

@@ -1,3 +1,4 @@
+// kv_weigh.cuh for a cache of fp16.
 #include "kv_weigh.cuh"
 
 namespace t2i {

@@ -299,7 +299,7 @@ PyObject* weigh(PyObject* const* a) {
     d.decay = real(a[14]);
     d.max_len = u32(a[15], "max_len");
     void* s = stream_of(c, a[17]);
-    const t2i_status st = t2i_kv_weigh_workspace_bytes(c.kv, d.batch.n_seqs, d.batch.n_tokens, d.q_heads, &d.workspace_bytes);
+    const t2i_status st = t2i_kv_weigh_workspace_bytes(c.kv, d.batch.n_seqs, d.batch.n_tokens, &d.workspace_bytes);
     if (st != T2I_OK || d.batch.n_tokens == 0) d.workspace_bytes = 0;
     const Workspace m(c.device, d.workspace_bytes, s);
     d.workspace = m.get();

@@ -161,8 +161,9 @@ def test_what_no_token_sees_may_be_anything(new):
 @pytest.mark.parametrize("max_len", [1, 700, 1 << 30])
 def test_a_wrong_max_len_changes_no_result(new, max_len):
     c, lens, kvs, q = case(BF, 8, 2, 64, new, [800, 100])
-    a = check(c, lens, new, kvs, q)
-    assert torch.equal(a, check(c, lens, new, kvs, q, max_len=max_len))
+    # (within the bound of the sum: a split elsewhere adds the same terms up in other groups, and fp32 addition is not
+    # associative, so the last bits may differ)
+    check(c, lens, new, kvs, q, max_len=max_len)
 
 
 def test_a_negative_scale_and_none():
@@ -258,3 +259,27 @@ def test_of_a_gradient_and_other_refusals():
     no2 = pytest.raises(ValueError, match="closed")
     with no2:
         c.weigh(q, L, lse, w)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 1, 300]])
+def test_a_wait_that_runs_out_is_reported_and_harms_nothing(new):
+    """The loads are left out on request, so that the bounded waits for them run their second."""
+    c, lens, kvs, q = case(BF, 8, 2, 128, new, [3000, 50, 1500])
+    lse = sums(new, kvs, q, 128).to(DEV)
+    q, L = q.to(DEV), ints(lens)
+    how = dict(starts=starts_of(new), max_new=max(new))
+    room = torch.full((3, 4, max(lens) + 64), 7.0, device=DEV)
+    used = torch.full((64 << 20,), 1, dtype=torch.uint8, device=DEV)  # what the workspace finds: notes that look valid
+    torch.cuda.synchronize()
+    del used
+    c.inject_timeout(1)
+    c.weigh(q, L, lse, room[:, 1:3, 32:-32], decay=0.0, **how)
+    torch.cuda.synchronize()
+    assert (room[:, 0] == 7).all() and (room[:, 3] == 7).all() and (room[..., :32] == 7).all()
+    assert all((room[s, 1:3, 32 + n:] == 7).all() for s, n in enumerate(lens))
+    w = torch.zeros(3, 2, max(lens), device=DEV)
+    with pytest.raises(T2IError, match="CUDA.*weigh.*gave up"):
+        c.weigh(q, L, lse, w, **how)
+    c.weigh(q, L, lse, w, **how)                                      # reported once
+    total = w.double().sum()
+    assert abs(float(total) - sum(new) * 8) < 1e-3 * sum(new) * 8      # every query's weights add up to 1
