@@ -27,10 +27,8 @@ namespace {
 using namespace tc;
 
 constexpr int kUnitKeys = 256;
-constexpr int kWeighThreads = 320;  // eight softmax warps, the loading warp, the product warp
 constexpr uint32_t kHalfSlot = 16384;  // 128 keys of 64 elements
 constexpr uint32_t kWeighUnits = 8;    // handed out at a time
-constexpr uint32_t kWeighReaders = 9;
 constexpr int kPartFloats = kUnitKeys;
 
 template <int N, int NS>
@@ -42,9 +40,14 @@ struct WeighShape {
     static constexpr uint32_t kBufs = N == 128 ? 2 : 4;                      // tiles of scores of each half
     static constexpr uint32_t kTmem = 2 * kBufs * N;
     static constexpr uint32_t kBytes = 1024 + kHalf * kKeys + kQ * kQs;
-    static constexpr uint32_t kFixed = 4096 + 8 * N * 16;  // static shared memory, at most
+    // The warps that add up come in groups of four: one a half, or two, each with half of the columns. Then the loading
+    // warp and the product warp.
+    static constexpr int kGroups = N == 128 ? 4 : 2;
+    static constexpr int kCols = 2 * N / kGroups;  // of a group
+    static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + 64;
+    static constexpr uint32_t kFixed = 8192 + kSumWarps * kCols * 16;  // static shared memory, at most
     static_assert(kBytes + kFixed + 1024 <= 228 * 1024, "an SM's shared memory");
-    static constexpr int kChunk = N < 32 ? N : 32;  // columns that a thread works on at a time
+    static constexpr int kChunk = kCols < 32 ? kCols : 32;  // columns that a thread works on at a time
 };
 
 struct WeighUnit {
@@ -135,12 +138,14 @@ __device__ __forceinline__ int64_t seq_steps(const Weigh& f, const KvSeq& q, uin
 struct WeighShared {
     uint64_t k_full[12], k_empty[12], q_full[5], q_empty[5];
     uint64_t s_full[2][4], s_empty[2][4];
+    uint64_t sum_full[2][2], sum_empty[2][2];  // [half][parity of the unit]
+    float sum[2][2][128];  // of the groups with the second half of the columns
     uint64_t unit_full[kWeighUnits], unit_empty[kWeighUnits];
     WeighUnit unit[kWeighUnits];
     uint32_t tmem, dead;
     int32_t start_seq;
     int64_t start_rest, start_steps;
-    int64_t sums[kWeighThreads / 32];
+    int64_t sums[18];
 };
 
 // Spans of column tiles, a thread a tile.
@@ -174,7 +179,7 @@ __device__ __forceinline__ float2 weigh_unpack(uint64_t v) {
 }
 
 template <class T, int N, int NS, bool MOD>
-__global__ void __launch_bounds__(kWeighThreads, 1)
+__global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     weigh_kernel(const __grid_constant__ Weigh f, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
     using Sh = WeighShape<N, NS>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
@@ -184,12 +189,13 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t ring = base, qs = ring + Sh::kHalf * Sh::kKeys;
     __shared__ __align__(16) WeighShared sh;
-    // each softmax warp's own: of its column tile the log-sum-exps in units of log2, spans, slopes
-    __shared__ __align__(16) float lse_of[8][N];
-    __shared__ __align__(16) int2 span_of[8][N];
-    __shared__ __align__(16) float slope_of[MOD ? 8 : 1][N];
+    constexpr int kThreads = Sh::kThreads, kSumWarps = Sh::kSumWarps, kCols = Sh::kCols;
+    // each adding warp's own: of its columns the log-sum-exps in units of log2, negative; spans, slopes
+    __shared__ __align__(16) float lse_of[kSumWarps][kCols];
+    __shared__ __align__(16) int2 span_of[kSumWarps][kCols];
+    __shared__ __align__(16) float slope_of[MOD ? kSumWarps : 1][kCols];
     __shared__ __align__(16) float token_of[MOD ? N : 4];  // a column's token, counted in the tile
-    static_assert(sizeof(WeighShared) + 8 * N * 16 + N * 4 <= Sh::kFixed + N * 4, "");
+    static_assert(sizeof(WeighShared) + N * 4 <= 8192, "kFixed");
     const KvAttend& a = f.w.a;
     const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     volatile uint32_t* dead = &sh.dead;
@@ -198,21 +204,31 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
         for (uint32_t i = 0; i < Sh::kKeys; ++i) mbar_init(bar(sh.k_full[i]), 1), mbar_init(bar(sh.k_empty[i]), 1);
         for (uint32_t i = 0; i < Sh::kQs; ++i) mbar_init(bar(sh.q_full[i]), 1), mbar_init(bar(sh.q_empty[i]), 1);
         for (uint32_t i = 0; i < Sh::kBufs; ++i)
-            for (int h = 0; h < 2; ++h) mbar_init(bar(sh.s_full[h][i]), 1), mbar_init(bar(sh.s_empty[h][i]), 4);
-        for (uint32_t i = 0; i < kWeighUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kWeighReaders);
+            for (int h = 0; h < 2; ++h) mbar_init(bar(sh.s_full[h][i]), 1), mbar_init(bar(sh.s_empty[h][i]), 2 * Sh::kGroups);
+        for (uint32_t i = 0; i < kWeighUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kSumWarps + 1);
+        for (int h = 0; h < 2; ++h)
+            for (int i = 0; i < 2; ++i) mbar_init(bar(sh.sum_full[h][i]), 4), mbar_init(bar(sh.sum_empty[h][i]), 4);
         sh.dead = 0;
         fence_mbar_init();
         tma_prefetch_map(&map), tma_prefetch_map(&q_map);
     }
+    {  // rows of the queries' ring that no box fills: their columns, whose log-sum-exp is infinite, add 0
+        const uint32_t real = uint32_t(f.per_tile * f.per_token), idle = N - real;
+        for (uint32_t i = tid; i < idle * Sh::kQs * NS * 8; i += kThreads) {
+            const uint32_t row = i / 8 % idle, piece = i / 8 / idle;
+            *reinterpret_cast<uint4*>(raw + (qs - smem_u32(raw)) + piece * (N * 128) + (real + row) * 128 + i % 8 * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_async_smem();
+    }
     if (MOD && tid < N) token_of[tid] = float(int32_t(tid) / f.per_token);
-    if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), Sh::kTmem);
+    if (warp == kSumWarps + 1) tmem_alloc(smem_u32(&sh.tmem), Sh::kTmem);
     pdl_launch();
     pdl_wait();
     if (!kOne && tid == 0) f.join[blockIdx.x].valid = 0;
 
     // the block's run of steps: sequences by threads (by warps, where a unit may have several steps)
     const int64_t K = a.pages.kv_heads;
-    const uint32_t who = kOne ? tid : warp, all = kOne ? kWeighThreads : kWeighThreads / 32;
+    const uint32_t who = kOne ? tid : warp, all = kOne ? kThreads : kThreads / 32;
     const uint32_t per = (a.tok.n_seqs + all - 1) / all;
     int64_t mine = 0;
     for (uint32_t s = who * per; s < min(a.tok.n_seqs, (who + 1) * per); ++s)
@@ -233,7 +249,7 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
     fence_before();
     __syncthreads();
     fence_after();
-    for (uint32_t i = 0; i < kWeighThreads / 32; ++i) {
+    for (uint32_t i = 0; i < kThreads / 32; ++i) {
         if (i < warp) lo += sh.sums[i];
         total += sh.sums[i];
     }
@@ -255,7 +271,7 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
     __syncthreads();
     const uint32_t tmem = sh.tmem;
 
-    if (busy && warp == 8) {
+    if (busy && warp == kSumWarps) {
         // ---------------------------------------------------------- loads
         int32_t s = sh.start_seq, h = int32_t(sh.start_rest / sh.start_steps), i = 0;  // sequence, key head, unit
         int64_t at = run0, unit0;  // the segment's first step, the unit's
@@ -292,6 +308,16 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
         const uint32_t T_mask = (1u << shift) - 1;
         const uint32_t q_bytes = uint32_t(f.per_tile * f.per_token) * 128 * NS;
         uint32_t u = 0, kn = 0, qn = 0;
+        // A segment's pages, a lane a box of each half: looked up while the segment before is loaded.
+        auto pages_at = [&](int2& to) {
+            const int32_t* table = a.pages.table + uint32_t(s) * a.pages.table_stride;
+            const uint32_t slot = uint32_t(unit_slot(list, i)) + lane * box;
+            to = make_int2(-1, -1);
+            if (lane < boxes && slot < uint32_t(q.len)) to.x = table[slot >> shift];
+            if (lane < boxes && slot + 128 < uint32_t(q.len)) to.y = table[(slot + 128) >> shift];
+        };
+        int2 pages, ahead;
+        pages_at(ahead);
         for (bool more = !f.no_loads; more; ++u) {
             // the segment
             const int32_t slot0 = unit_slot(list, i);
@@ -299,7 +325,10 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
             const bool dry = tiles.y <= tiles.x;
             const int32_t steps = max(1, tiles.y - tiles.x), skip = int32_t(at - unit0);
             const int32_t n = int32_t(min(int64_t(steps - skip), run1 - at));
+            const int32_t first = q.first, head0 = h * int32_t(a.group);
+            const int32_t row = int32_t((a.pages.layer * 2 * a.pages.kv_heads + h) << shift);
             more = at + n < run1;
+            pages = ahead;
             if (!mbar_wait(bar(sh.unit_empty[u % kWeighUnits]), (u / kWeighUnits & 1) ^ 1, dead)) break;
             if (lane == 0) {
                 WeighUnit& o = sh.unit[u % kWeighUnits];
@@ -314,13 +343,26 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
                 }
             }
             __syncwarp();
+            at += n;
+            if (more) {  // the next unit (the segment ended with this one)
+                unit0 = at;
+                if (++i == list.n) {
+                    i = 0;
+                    if (++h == int32_t(K)) {
+                        h = 0;
+                        do {
+                            ++s;
+                            q = kv_seq(a.pages, a.tok, s);
+                            list = unit_list(f, q);
+                        } while (list.n == 0);
+                    }
+                }
+                pages_at(ahead);
+            }
             if (!dry) {
-                const int32_t row = int32_t((a.pages.layer * 2 * a.pages.kv_heads + h) << shift);
-                const int32_t* table = a.pages.table + uint32_t(s) * a.pages.table_stride;
                 for (int half = 0; half < 2; ++half, ++kn) {
                     const uint32_t slot = uint32_t(slot0) + half * 128 + lane * box, e = kn % Sh::kKeys;
-                    int32_t page = -1;
-                    if (lane < boxes && slot < uint32_t(q.len)) page = table[slot >> shift];
+                    const int32_t page = half ? pages.y : pages.x;
                     // what the pool lacks, and what lies behind the sequence, is filled with zeros
                     const int32_t z = uint32_t(page) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page;
                     if (!mbar_wait(bar(sh.k_empty[e]), (kn / Sh::kKeys & 1) ^ 1, dead)) goto loads_done;
@@ -336,26 +378,11 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
                     if (!mbar_wait(bar(sh.q_empty[e]), (qn / Sh::kQs & 1) ^ 1, dead)) goto loads_done;
                     if (lane == 0) {
                         mbar_expect(bar(sh.q_full[e]), q_bytes);
-                        const int32_t token = q.first + t / f.slices * f.per_tile, head = h * int32_t(a.group) + t % f.slices * f.per_token;
+                        const int32_t token = first + t / f.slices * f.per_tile, head = head0 + t % f.slices * f.per_token;
                         for (int x = 0; x < NS; ++x)
                             tma_load(qs + e * Sh::kQ + x * (N * 128), &q_map, x * 64, head, token, bar(sh.q_full[e]));
                     }
                     __syncwarp();
-                }
-            }
-            at += n;
-            if (more) {  // the next unit (the segment ended with this one)
-                unit0 = at;
-                if (++i == list.n) {
-                    i = 0;
-                    if (++h == int32_t(K)) {
-                        h = 0;
-                        do {
-                            ++s;
-                            q = kv_seq(a.pages, a.tok, s);
-                            list = unit_list(f, q);
-                        } while (list.n == 0);
-                    }
                 }
             }
         }
@@ -366,7 +393,7 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
             for (uint32_t k = kn > Sh::kKeys ? kn - Sh::kKeys : 0; k < kn; ++k) mbar_wait(bar(sh.k_full[k % Sh::kKeys]), k / Sh::kKeys & 1, &late);
             for (uint32_t k = qn > Sh::kQs ? qn - Sh::kQs : 0; k < qn; ++k) mbar_wait(bar(sh.q_full[k % Sh::kQs]), k / Sh::kQs & 1, &late);
         }
-    } else if (busy && warp == 9) {
+    } else if (busy && warp == kSumWarps + 1) {
         // ---------------------------------------------------------- products
         constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
         const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
@@ -417,145 +444,206 @@ __global__ void __launch_bounds__(kWeighThreads, 1)
         }
     } else if (busy) {
         // ---------------------------------------------------------- weights
-        const int half = warp / 4;
+        const int half = warp / 4 % 2, side = warp / 8;  // which 128 keys, and which columns
         const uint32_t key = tid % 128;
-        const uint32_t lanes = tmem + ((warp % 4) << 21) + half * Sh::kBufs * N;
+        const uint32_t lanes = tmem + ((warp % 4) << 21) + half * Sh::kBufs * N + side * kCols;
         const float k2 = a.scale * kLog2e;
         const bool cap = MOD && a.softcap != 0.0f;
         const float cap_in = cap ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
         const uint64_t k22 = weigh_pack(k2, k2);
         float* const lse_at = lse_of[warp];
+        // the lane's columns of a tile: token and head, counted in the tile
+        constexpr int kMine = kCols < 32 ? 1 : kCols / 32;
+        int32_t token_at[kMine], head_at[kMine];
+        float next[kMine];  // their log-sum-exps of the next tile
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            const int32_t c = side * kCols + k * 32 + int32_t(lane);
+            token_at[k] = c / f.per_token, head_at[k] = c % f.per_token;
+            if (k * 32 + int32_t(lane) >= kCols) token_at[k] = INT32_MAX;  // none
+        }
+        // of the tile that begins with token t0 and the head's query g0 (first: the sequence's first token)
+        auto look_up = [&](int32_t first, int32_t h, int32_t m, int32_t t0, int32_t g0) {
+            const float* const at = f.w.lse + uint64_t(uint32_t(first + t0)) * a.q_heads + h * a.group + g0;
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                next[k] = -INFINITY;
+                if (token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0)
+                    next[k] = at[uint32_t(token_at[k]) * a.q_heads + uint32_t(head_at[k])];
+            }
+        };
         int32_t had_s = -1, had_h = -1;  // whose column tile's log-sum-exps are there (of one tile a sequence)
+        bool known = false;              // `next` is the next tile's
         uint32_t n = 0;
         bool more = true;
         for (uint32_t u = 0; more; ++u) {
             const bool got = mbar_wait(bar(sh.unit_full[u % kWeighUnits]), u / kWeighUnits & 1, dead);
             if (!__all_sync(0xFFFFFFFFu, got)) break;
-            const WeighUnit o = sh.unit[u % kWeighUnits];
+            const WeighUnit& rec = sh.unit[u % kWeighUnits];
+            const int32_t s = rec.s, h = rec.h, len = rec.q.len, ctx = len - rec.q.n, first = rec.q.first, m = weigh_tokens(a, rec.q);
+            const int32_t slot = rec.slot0 + half * 128 + int32_t(key), steps = rec.dry ? 0 : rec.n;
+            const bool dry = rec.dry, whole = rec.whole;
+            const int32_t in_part = rec.part, tile0 = rec.tile;
+            more = rec.more;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
-            more = o.more;
-            const int32_t slot = o.slot0 + half * 128 + int32_t(key), ctx = o.q.len - o.q.n, m = weigh_tokens(a, o.q);
-            const bool mine = slot < o.q.len && uint32_t(slot) < f.w.n_slots;
-            float* const place = f.w.weights + uint32_t(o.s) * f.w.seq_stride + uint32_t(o.h) * f.w.head_stride + slot;
+            const bool mine = side == 0 && slot < len && uint32_t(slot) < f.w.n_slots;
+            float* const place = f.w.weights + uint32_t(s) * f.w.seq_stride + uint32_t(h) * f.w.head_stride + slot;
             float held = 0.0f;
-            if (o.whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
-            // the tokens that see the slot
+            if (whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
+            // the tokens [i0, i1) that see the slot, and those that see all of the warp's slots
             int32_t i0 = max(0, slot - ctx), i1 = m;
             if (a.window && slot >= int32_t(a.sinks)) i1 = int32_t(min(int64_t(m), int64_t(slot) + int64_t(a.window) - ctx));
-            if (slot >= o.q.len) i1 = 0;
+            const int32_t all0 = __reduce_max_sync(0xFFFFFFFFu, i0), all1 = a.spans ? 0 : __reduce_min_sync(0xFFFFFFFFu, i1);
+            if (slot >= len) i1 = 0;  // (what lies behind the sequence is not written, so it may be added up)
             KvSum sum;
-            const int32_t steps = o.dry ? 0 : o.n;
+            uint64_t part0 = 0, part1 = 0;
+            int32_t t0 = tile0, g0 = 0;
+            if (f.slices > 1) t0 = tile0 / f.slices, g0 = (tile0 - t0 * f.slices) * f.per_token;
+            t0 *= f.per_tile;
             for (int32_t i = 0; i < steps; ++i, ++n) {
-                const int32_t tile = o.tile + i, t0 = tile / f.slices * f.per_tile, g0 = tile % f.slices * f.per_token;
-                const int32_t cols = min(f.per_tile, m - t0) * min(f.per_token, int32_t(a.group) - g0);
-                if (!kOne || o.s != had_s || o.h != had_h) {
+                if (!kOne || s != had_s || h != had_h) {
+                    if (!known) look_up(first, h, m, t0, g0);
+                    known = false;
                     __syncwarp();
 #pragma unroll
-                    for (int c0 = 0; c0 < N; c0 += 32) {
-                        const int32_t c = c0 + int32_t(lane);
-                        if (N < 32 && c >= N) break;
-                        float l = INFINITY, slope = 0.0f;
-                        int2 span = make_int2(0, 0);
-                        if (c < cols) {
-                            const uint64_t token = uint64_t(o.q.first) + t0 + c / f.per_token;
-                            const uint32_t head = o.h * a.group + g0 + c % f.per_token;
-                            l = f.w.lse[token * a.q_heads + head] * kLog2e;
-                            if (l == -INFINITY) l = INFINITY;
-                            if (a.spans) span = reinterpret_cast<const int2*>(a.spans)[token];
-                            if (MOD && a.slopes) slope = a.slopes[head] * kLog2e;
+                    for (int k = 0; k < kMine; ++k) {
+                        const int32_t c = k * 32 + int32_t(lane);
+                        if (kCols < 32 && c >= kCols) break;
+                        lse_at[c] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
+                        if (MOD || a.spans) {
+                            const bool real = token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0;
+                            int2 span = make_int2(0, 0);
+                            if (a.spans && real) span = reinterpret_cast<const int2*>(a.spans)[first + t0 + token_at[k]];
+                            if (a.spans) span_of[warp][c] = span;
+                            if (MOD) slope_of[MOD ? warp : 0][c] = a.slopes && real ? a.slopes[h * a.group + g0 + head_at[k]] * kLog2e : 0.0f;
                         }
-                        lse_at[c] = l;
-                        if (a.spans) span_of[warp][c] = span;
-                        if (MOD) slope_of[MOD ? warp : 0][c] = slope;
                     }
                     __syncwarp();
-                    had_s = o.s, had_h = o.h;
+                    had_s = s, had_h = h;
                 }
-                // the thread's visible columns [c0, c1)
-                const int32_t v0 = a.spans ? 0 : min(max(i0 - t0, 0), f.per_tile) * f.per_token;
-                const int32_t v1 = a.spans ? cols : min(min(max(i1 - t0, 0), f.per_tile) * f.per_token, cols);
                 const float ahead = float(ctx + t0 - slot);
+                const bool plain = t0 >= all0 && t0 + f.per_tile <= all1 && g0 + f.per_token <= int32_t(a.group);
+                // the thread's visible columns [v0, v1), where not all are
+                int32_t v0 = 0, v1 = kCols;
+                if (!plain) {
+                    const int32_t cols = min(f.per_tile, m - t0) * min(f.per_token, int32_t(a.group) - g0);
+                    v0 = a.spans ? 0 : min(max(i0 - t0, 0), f.per_tile) * f.per_token - side * kCols;
+                    v1 = (slot >= len ? 0 : a.spans ? cols : min(min(max(i1 - t0, 0), f.per_tile) * f.per_token, cols)) - side * kCols;
+                }
+                if (f.slices > 1) {
+                    g0 += f.per_token;
+                    if (g0 >= int32_t(a.group)) g0 = 0, t0 += f.per_tile;
+                } else {
+                    t0 += f.per_tile;
+                }
+                if (!kOne) {  // the next tile's, on their way while this one is worked on
+                    if (i + 1 < steps) {
+                        look_up(first, h, m, t0, g0), known = true;
+                    } else if (more) {
+                        const uint32_t v = u + 1;
+                        const WeighUnit& o = sh.unit[v % kWeighUnits];
+                        const bool out = mbar_test(bar(sh.unit_full[v % kWeighUnits]), v / kWeighUnits & 1);
+                        if (__all_sync(0xFFFFFFFFu, out) && !o.dry && f.slices == 1)
+                            look_up(o.q.first, o.h, weigh_tokens(a, o.q), o.tile * f.per_tile, 0), known = true;
+                    }
+                }
                 const uint32_t buf = n % Sh::kBufs;
                 const bool there = mbar_wait(bar(sh.s_full[half][buf]), n / Sh::kBufs & 1, dead);
                 if (!__all_sync(0xFFFFFFFFu, there)) goto weights_done;
                 fence_after();
-                float x[N];
-                if constexpr (N == 16) {
-                    tmem_ld16(lanes + buf * N, x);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < N; c += 32) tmem_ld32(lanes + buf * N + c, x + c);
-                }
-                wait_ld(x);
-                fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sh.s_empty[half][buf]));
-                uint64_t part0 = 0, part1 = 0;
-#pragma unroll
-                for (int c0 = 0; c0 < N; c0 += kChunk) {
-                    const bool some = v1 > c0 && v0 < c0 + kChunk && v0 < v1;
-                    if (!__any_sync(0xFFFFFFFFu, some)) continue;
-                    const bool plain = __all_sync(0xFFFFFFFFu, v0 <= c0 && v1 >= c0 + kChunk) && !a.spans;
-                    float y[kChunk];
+#pragma unroll 1
+                for (int c0 = 0; c0 < kCols; c0 += kChunk) {
+                    float x[kChunk];
+                    if constexpr (kChunk == 16)
+                        tmem_ld16(lanes + buf * N + c0, x);
+                    else
+                        tmem_ld32(lanes + buf * N + c0, x);
+                    wait_ld(x);
+                    if (c0 + kChunk == kCols) {  // the scores are read: their columns may be written again
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(sh.s_empty[half][buf]));
+                    }
+                    // scores, less the log-sum-exp, in units of log2
 #pragma unroll
                     for (int c = 0; c < kChunk; c += 4) {
                         const float4 l = *reinterpret_cast<const float4*>(lse_at + c0 + c);
                         if (MOD) {
                             const float4 sl = *reinterpret_cast<const float4*>(slope_of[MOD ? warp : 0] + c0 + c);
-                            const float4 tk = *reinterpret_cast<const float4*>(token_of + c0 + c);
+                            const float4 tk = *reinterpret_cast<const float4*>(token_of + (MOD ? side * kCols + c0 + c : 0));
                             const float sls[4] = {sl.x, sl.y, sl.z, sl.w}, ls[4] = {l.x, l.y, l.z, l.w}, tks[4] = {tk.x, tk.y, tk.z, tk.w};
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                float z = cap ? capped<true>(x[c0 + c + k], cap_in, cap2) : x[c0 + c + k] * k2;
+                                float z = cap ? capped<true>(x[c + k], cap_in, cap2) : x[c + k] * k2;
                                 z -= sls[k] * fabsf(ahead + tks[k]);
-                                y[c + k] = z - ls[k];
+                                x[c + k] = z + ls[k];
                             }
                         } else {
                             uint64_t r0, r1;
-                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r0) : "l"(weigh_pack(x[c0 + c], x[c0 + c + 1])), "l"(k22), "l"(weigh_pack(-l.x, -l.y)));
-                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r1) : "l"(weigh_pack(x[c0 + c + 2], x[c0 + c + 3])), "l"(k22), "l"(weigh_pack(-l.z, -l.w)));
+                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r0) : "l"(weigh_pack(x[c], x[c + 1])), "l"(k22), "l"(weigh_pack(l.x, l.y)));
+                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r1) : "l"(weigh_pack(x[c + 2], x[c + 3])), "l"(k22), "l"(weigh_pack(l.z, l.w)));
                             const float2 a0 = weigh_unpack(r0), a1 = weigh_unpack(r1);
-                            y[c] = a0.x, y[c + 1] = a0.y, y[c + 2] = a1.x, y[c + 3] = a1.y;
+                            x[c] = a0.x, x[c + 1] = a0.y, x[c + 2] = a1.x, x[c + 3] = a1.y;
                         }
                     }
-#pragma unroll
-                    for (int c = 0; c < kChunk; ++c) y[c] = exp2_approx(y[c]);
                     if (!plain) {
                         uint32_t see = 0;
                         if (a.spans) {
-#pragma unroll
+#pragma unroll 4
                             for (int c = 0; c < kChunk; ++c) {
                                 const int2 sp = span_of[warp][c0 + c];
                                 see |= uint32_t(slot >= sp.x && slot < sp.y && c0 + c < v1) << c;
                             }
-                            if (slot >= o.q.len) see = 0;
                         } else {
                             auto below = [](int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
                             see = below(v1 - c0) & ~below(v0 - c0);
                         }
 #pragma unroll
-                        for (int c = 0; c < kChunk; ++c) y[c] = see & (1u << c) ? y[c] : 0.0f;
+                        for (int c = 0; c < kChunk; ++c) x[c] = see & (1u << c) ? x[c] : -INFINITY;
                     }
 #pragma unroll
                     for (int c = 0; c < kChunk; c += 4) {
-                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part0) : "l"(weigh_pack(y[c], y[c + 1])));
-                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part1) : "l"(weigh_pack(y[c + 2], y[c + 3])));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[c + k] = exp2_approx(x[c + k]);
+                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part0) : "l"(weigh_pack(x[c], x[c + 1])));
+                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part1) : "l"(weigh_pack(x[c + 2], x[c + 3])));
                     }
                 }
-                const float2 p0 = weigh_unpack(part0), p1 = weigh_unpack(part1);
-                sum.add((p0.x + p0.y) + (p1.x + p1.y));
+                if (i % 4 == 3 || i + 1 == steps) {
+                    const float2 p0 = weigh_unpack(part0), p1 = weigh_unpack(part1);
+                    sum.add((p0.x + p0.y) + (p1.x + p1.y));
+                    part0 = part1 = 0;
+                }
             }
-            if (!o.whole)
-                __stcg(f.part + (uint64_t(blockIdx.x) * 2 + o.part) * kPartFloats + half * 128 + key, sum.value());
-            else if (mine && !(o.dry && f.w.decay == 1.0f && slot < ctx))
-                *place = sum.value() + (slot < ctx && f.w.decay != 0.0f ? f.w.decay * held : 0.0f);
+            float got_all = sum.value();
+            if (Sh::kGroups == 4) {  // the sums of both halves of the columns meet
+                const uint32_t b = u & 1;
+                float* const other = sh.sum[half][b];
+                if (side) {
+                    const bool there = mbar_wait(bar(sh.sum_empty[half][b]), (u >> 1 & 1) ^ 1, dead);
+                    if (!__all_sync(0xFFFFFFFFu, there)) goto weights_done;
+                    other[key] = got_all;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(sh.sum_full[half][b]));
+                    continue;
+                }
+                const bool there = mbar_wait(bar(sh.sum_full[half][b]), u >> 1 & 1, dead);
+                if (!__all_sync(0xFFFFFFFFu, there)) goto weights_done;
+                got_all += other[key];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.sum_empty[half][b]));
+            }
+            if (!whole)
+                __stcg(f.part + (uint64_t(blockIdx.x) * 2 + in_part) * kPartFloats + half * 128 + key, got_all);
+            else if (mine && !(dry && f.w.decay == 1.0f && slot < ctx))
+                *place = got_all + (slot < ctx && f.w.decay != 0.0f ? f.w.decay * held : 0.0f);
         }
     weights_done:;
     }
     __syncthreads();
     if (tid == 0 && *dead) *f.fault = 1;
-    if (warp == 9) {
+    if (warp == kSumWarps + 1) {
         fence_after();
         tmem_free(tmem, Sh::kTmem);
     }
@@ -598,7 +686,7 @@ cudaError_t launch_weigh_as(const Weigh& f, const CUtensorMap& map, const CUtens
     const uint64_t tiles = N == 128 ? (uint64_t(a.tok.max_new) / f.per_tile + 1) * f.slices : 1;
     const uint64_t steps = uint64_t(a.tok.n_seqs) * a.pages.kv_heads * (uint64_t(a.max_len) / kUnitKeys + 1);
     const uint32_t blocks = uint32_t(steps > sms / tiles ? sms : steps * tiles);
-    if ((e = launch_pdl(weigh_kernel<T, N, NS, MOD>, dim3(blocks), kWeighThreads, bytes, stream, f, map, q_map)) != cudaSuccess) return e;
+    if ((e = launch_pdl(weigh_kernel<T, N, NS, MOD>, dim3(blocks), WeighShape<N, NS>::kThreads, bytes, stream, f, map, q_map)) != cudaSuccess) return e;
     return N == 128 ? launch_pdl(weigh_join_kernel, dim3(blocks), kUnitKeys, 0, stream, f) : cudaSuccess;
 }
 
