@@ -44,7 +44,10 @@ struct WeighShape {
     // warp and the product warp.
     static constexpr int kGroups = N == 128 ? 4 : 2;
     static constexpr int kCols = 2 * N / kGroups;  // of a group
-    static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + 64;
+    // (with two that idle where registers are shared out, by groups of four warps)
+    static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + (kGroups == 4 ? 128 : 64);
+    static constexpr int kRegs = 96, kSumRegs = 104, kOtherRegs = 64;
+    static_assert(kGroups != 4 || kSumRegs * kSumWarps * 32 + kOtherRegs * 128 <= kRegs * kThreads, "what a block was launched with");
     static constexpr uint32_t kFixed = 8192 + kSumWarps * kCols * 16;  // static shared memory, at most
     static_assert(kBytes + kFixed + 1024 <= 228 * 1024, "an SM's shared memory");
     static constexpr int kChunk = kCols < 32 ? kCols : 32;  // columns that a thread works on at a time
@@ -145,7 +148,7 @@ struct WeighShared {
     uint32_t tmem, dead;
     int32_t start_seq;
     int64_t start_rest, start_steps;
-    int64_t sums[18];
+    int64_t sums[20];
 };
 
 // Spans of column tiles, a thread a tile.
@@ -165,17 +168,6 @@ __global__ void __launch_bounds__(128) hull_kernel(const __grid_constant__ Weigh
         }
         f.hulls[q.first / f.per_tile + s + t] = r;
     }
-}
-
-__device__ __forceinline__ uint64_t weigh_pack(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 weigh_unpack(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
 }
 
 template <class T, int N, int NS, bool MOD>
@@ -271,7 +263,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     __syncthreads();
     const uint32_t tmem = sh.tmem;
 
-    if (busy && warp == kSumWarps) {
+    if (busy && warp >= kSumWarps) {
+        if (Sh::kGroups == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
+        if (warp == kSumWarps) {
         // ---------------------------------------------------------- loads
         int32_t s = sh.start_seq, h = int32_t(sh.start_rest / sh.start_steps), i = 0;  // sequence, key head, unit
         int64_t at = run0, unit0;  // the segment's first step, the unit's
@@ -393,7 +387,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             for (uint32_t k = kn > Sh::kKeys ? kn - Sh::kKeys : 0; k < kn; ++k) mbar_wait(bar(sh.k_full[k % Sh::kKeys]), k / Sh::kKeys & 1, &late);
             for (uint32_t k = qn > Sh::kQs ? qn - Sh::kQs : 0; k < qn; ++k) mbar_wait(bar(sh.q_full[k % Sh::kQs]), k / Sh::kQs & 1, &late);
         }
-    } else if (busy && warp == kSumWarps + 1) {
+    } else if (warp == kSumWarps + 1) {
         // ---------------------------------------------------------- products
         constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
         const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
@@ -442,34 +436,41 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             while (now_ns() - t0 < 50000) {
             }
         }
+    }
     } else if (busy) {
         // ---------------------------------------------------------- weights
+        if (Sh::kGroups == 4) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kSumRegs));
         const int half = warp / 4 % 2, side = warp / 8;  // which 128 keys, and which columns
         const uint32_t key = tid % 128;
         const uint32_t lanes = tmem + ((warp % 4) << 21) + half * Sh::kBufs * N + side * kCols;
         const float k2 = a.scale * kLog2e;
         const bool cap = MOD && a.softcap != 0.0f;
         const float cap_in = cap ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
-        const uint64_t k22 = weigh_pack(k2, k2);
         float* const lse_at = lse_of[warp];
         // the lane's columns of a tile: token and head, counted in the tile
         constexpr int kMine = kCols < 32 ? 1 : kCols / 32;
         int32_t token_at[kMine], head_at[kMine];
         float next[kMine];  // their log-sum-exps of the next tile
+        bool pad[kMine];        // no column of a complete tile
+        uint32_t offset[kMine];
 #pragma unroll
         for (int k = 0; k < kMine; ++k) {
             const int32_t c = side * kCols + k * 32 + int32_t(lane);
             token_at[k] = c / f.per_token, head_at[k] = c % f.per_token;
             if (k * 32 + int32_t(lane) >= kCols) token_at[k] = INT32_MAX;  // none
+            pad[k] = token_at[k] >= f.per_tile;
+            offset[k] = pad[k] ? 0 : uint32_t(token_at[k]) * a.q_heads + uint32_t(head_at[k]);
         }
+        constexpr bool kLean = !kOne && !MOD;
+        const bool lean = f.slices == 1 && !a.spans;
         // of the tile that begins with token t0 and the head's query g0 (first: the sequence's first token)
         auto look_up = [&](int32_t first, int32_t h, int32_t m, int32_t t0, int32_t g0) {
             const float* const at = f.w.lse + uint64_t(uint32_t(first + t0)) * a.q_heads + h * a.group + g0;
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
-                next[k] = -INFINITY;
-                if (token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0)
-                    next[k] = at[uint32_t(token_at[k]) * a.q_heads + uint32_t(head_at[k])];
+                const bool real = token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0;
+                next[k] = at[real ? uint32_t(token_at[k]) * a.q_heads + uint32_t(head_at[k]) : 0];  // (a tile has a first column)
+                if (!real) next[k] = -INFINITY;
             }
         };
         int32_t had_s = -1, had_h = -1;  // whose column tile's log-sum-exps are there (of one tile a sequence)
@@ -497,11 +498,46 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             const int32_t all0 = __reduce_max_sync(0xFFFFFFFFu, i0), all1 = a.spans ? 0 : __reduce_min_sync(0xFFFFFFFFu, i1);
             if (slot >= len) i1 = 0;  // (what lies behind the sequence is not written, so it may be added up)
             KvSum sum;
-            uint64_t part0 = 0, part1 = 0;
+            float part[4] = {};
             int32_t t0 = tile0, g0 = 0;
             if (f.slices > 1) t0 = tile0 / f.slices, g0 = (tile0 - t0 * f.slices) * f.per_token;
             t0 *= f.per_tile;
             for (int32_t i = 0; i < steps; ++i, ++n) {
+                if (kLean && known && lean && t0 >= all0) {
+                    // Tiles that all of the warp's slots see, and the next of which is complete: nothing to decide.
+                    const int32_t last = min(steps - 1, i + (all1 - t0) / f.per_tile - 1);
+                    const uint64_t stride = uint64_t(uint32_t(f.per_tile)) * a.q_heads;
+                    const float* at = f.w.lse + uint64_t(uint32_t(first + t0)) * a.q_heads + h * a.group;
+#pragma unroll 1
+                    for (; i < last; ++i, ++n, t0 += f.per_tile) {
+                        __syncwarp();
+#pragma unroll
+                        for (int k = 0; k < kMine; ++k) lse_at[k * 32 + lane] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
+                        __syncwarp();
+                        at += stride;
+#pragma unroll
+                        for (int k = 0; k < kMine; ++k) next[k] = pad[k] ? -INFINITY : at[offset[k]];
+                        const uint32_t buf = n % Sh::kBufs;
+                        const bool there = mbar_wait(bar(sh.s_full[half][buf]), n / Sh::kBufs & 1, dead);
+                        if (!__all_sync(0xFFFFFFFFu, there)) goto weights_done;
+                        fence_after();
+                        float x[kCols];
+#pragma unroll
+                        for (int c = 0; c < kCols; c += 32) tmem_ld32(lanes + buf * N + c, x + c);
+                        wait_ld(x);
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(sh.s_empty[half][buf]));
+                        float add[4] = {};
+#pragma unroll
+                        for (int c = 0; c < kCols; c += 4) {
+                            const float4 l = *reinterpret_cast<const float4*>(lse_at + c);
+                            add[0] += exp2_approx(fmaf(x[c], k2, l.x)), add[1] += exp2_approx(fmaf(x[c + 1], k2, l.y));
+                            add[2] += exp2_approx(fmaf(x[c + 2], k2, l.z)), add[3] += exp2_approx(fmaf(x[c + 3], k2, l.w));
+                        }
+                        sum.add((add[0] + add[1]) + (add[2] + add[3]));
+                    }
+                }
                 if (!kOne || s != had_s || h != had_h) {
                     if (!known) look_up(first, h, m, t0, g0);
                     known = false;
@@ -556,10 +592,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                 for (int c0 = 0; c0 < kCols; c0 += kChunk) {
                     float x[kChunk];
                     if constexpr (kChunk == 16)
-                        tmem_ld16(lanes + buf * N + c0, x);
+                        tmem_get16(lanes + buf * N + c0, x);
                     else
-                        tmem_ld32(lanes + buf * N + c0, x);
-                    wait_ld(x);
+                        tmem_get32(lanes + buf * N + c0, x);
                     if (c0 + kChunk == kCols) {  // the scores are read: their columns may be written again
                         fence_before();
                         __syncwarp();
@@ -580,11 +615,8 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                                 x[c + k] = z + ls[k];
                             }
                         } else {
-                            uint64_t r0, r1;
-                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r0) : "l"(weigh_pack(x[c], x[c + 1])), "l"(k22), "l"(weigh_pack(l.x, l.y)));
-                            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r1) : "l"(weigh_pack(x[c + 2], x[c + 3])), "l"(k22), "l"(weigh_pack(l.z, l.w)));
-                            const float2 a0 = weigh_unpack(r0), a1 = weigh_unpack(r1);
-                            x[c] = a0.x, x[c + 1] = a0.y, x[c + 2] = a1.x, x[c + 3] = a1.y;
+                            x[c] = fmaf(x[c], k2, l.x), x[c + 1] = fmaf(x[c + 1], k2, l.y);
+                            x[c + 2] = fmaf(x[c + 2], k2, l.z), x[c + 3] = fmaf(x[c + 3], k2, l.w);
                         }
                     }
                     if (!plain) {
@@ -605,15 +637,12 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
 #pragma unroll
                     for (int c = 0; c < kChunk; c += 4) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[c + k] = exp2_approx(x[c + k]);
-                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part0) : "l"(weigh_pack(x[c], x[c + 1])));
-                        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(part1) : "l"(weigh_pack(x[c + 2], x[c + 3])));
+                        for (int k = 0; k < 4; ++k) part[k] += exp2_approx(x[c + k]);
                     }
                 }
                 if (i % 4 == 3 || i + 1 == steps) {
-                    const float2 p0 = weigh_unpack(part0), p1 = weigh_unpack(part1);
-                    sum.add((p0.x + p0.y) + (p1.x + p1.y));
-                    part0 = part1 = 0;
+                    sum.add((part[0] + part[1]) + (part[2] + part[3]));
+                    part[0] = part[1] = part[2] = part[3] = 0.0f;
                 }
             }
             float got_all = sum.value();
