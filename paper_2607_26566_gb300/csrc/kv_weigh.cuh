@@ -446,6 +446,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
         const float k2 = a.scale * kLog2e;
         const bool cap = MOD && a.softcap != 0.0f;
         const float cap_in = cap ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
+        const uint64_t k22 = pack2(k2, k2);
         float* const lse_at = lse_of[warp];
         // the lane's columns of a tile: token and head, counted in the tile
         constexpr int kMine = kCols < 32 ? 1 : kCols / 32;
@@ -528,14 +529,19 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                         fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bar(sh.s_empty[half][buf]));
-                        float add[4] = {};
+                        uint64_t add0 = 0, add1 = 0;
 #pragma unroll
                         for (int c = 0; c < kCols; c += 4) {
-                            const float4 l = *reinterpret_cast<const float4*>(lse_at + c);
-                            add[0] += exp2_approx(fmaf(x[c], k2, l.x)), add[1] += exp2_approx(fmaf(x[c + 1], k2, l.y));
-                            add[2] += exp2_approx(fmaf(x[c + 2], k2, l.z)), add[3] += exp2_approx(fmaf(x[c + 3], k2, l.w));
+                            const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(lse_at + c);
+                            float y0, y1, y2, y3;
+                            unpack2(fma2(pack2(x[c], x[c + 1]), k22, l.x), y0, y1);
+                            unpack2(fma2(pack2(x[c + 2], x[c + 3]), k22, l.y), y2, y3);
+                            add0 = add2(add0, pack2(exp2_approx(y0), exp2_approx(y1)));
+                            add1 = add2(add1, pack2(exp2_approx(y2), exp2_approx(y3)));
                         }
-                        sum.add((add[0] + add[1]) + (add[2] + add[3]));
+                        float y0, y1;
+                        unpack2(add2(add0, add1), y0, y1);
+                        sum.add(y0 + y1);
                     }
                 }
                 if (!kOne || s != had_s || h != had_h) {
