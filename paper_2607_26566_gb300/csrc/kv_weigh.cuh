@@ -41,11 +41,11 @@ struct WeighShape {
     static constexpr uint32_t kTmem = 2 * kBufs * N;
     static constexpr uint32_t kBytes = 1024 + kHalf * kKeys + kQ * kQs;
     // The warps that add up come in groups of four: one a half, or two, each with half of the columns. Then the loading
-    // warp and the product warp.
+    // warp, a product warp for each half (one's products run while the other waits), and one that idles, so that registers
+    // can be shared out by groups of four.
     static constexpr int kGroups = N == 128 ? 4 : 2;
     static constexpr int kCols = 2 * N / kGroups;  // of a group
-    // (with two that idle where registers are shared out, by groups of four warps)
-    static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + (kGroups == 4 ? 128 : 64);
+    static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + 128;
     static constexpr int kRegs = 96, kSumRegs = 104, kOtherRegs = 64;
     static_assert(kGroups != 4 || kSumRegs * kSumWarps * 32 + kOtherRegs * 128 <= kRegs * kThreads, "what a block was launched with");
     static constexpr uint32_t kFixed = 8192 + kSumWarps * kCols * 16;  // static shared memory, at most
@@ -121,18 +121,19 @@ __device__ __forceinline__ int2 unit_tiles(const Weigh& f, const KvSeq& q, uint3
     if (i0 >= i1) return make_int2(0, 0);
     return make_int2(i0 / f.per_tile * f.slices, int32_t((i1 + f.per_tile - 1) / f.per_tile) * f.slices);
 }
-__device__ __forceinline__ int32_t unit_steps(const Weigh& f, const KvSeq& q, uint32_t s, int32_t slot0) {
-    const int2 t = unit_tiles(f, q, s, slot0);
-    return max(1, t.y - t.x);
-}
+// What a unit costs where runs are cut: its steps, and so many before them (its keys' way, tiles with a mask, its sums'
+// way out). Measured with 0, 2, 4, 8 and 14: prompts of 4,096 tokens 89, 84, 79, 82, 86 us, of 8,190 284, 273, 265, 262,
+// 266.
+constexpr int32_t kUnitCost = 6;
+__device__ __forceinline__ int32_t unit_cost(int2 tiles) { return tiles.y > tiles.x ? kUnitCost + tiles.y - tiles.x : 1; }
 
-// Steps of one head of a sequence. Of one column tile a unit is one step; else by a warp.
+// The cost of one head of a sequence. Of one column tile a unit costs one step; else by a warp.
 template <bool ONE>
-__device__ __forceinline__ int64_t seq_steps(const Weigh& f, const KvSeq& q, uint32_t s, uint32_t lane) {
+__device__ __forceinline__ int64_t seq_cost(const Weigh& f, const KvSeq& q, uint32_t s, uint32_t lane) {
     const UnitList u = unit_list(f, q);
     if (ONE) return u.n;
     int64_t n = 0;
-    for (int32_t i = int32_t(lane); i < u.n; i += 32) n += unit_steps(f, q, s, unit_slot(u, i));
+    for (int32_t i = int32_t(lane); i < u.n; i += 32) n += unit_cost(unit_tiles(f, q, s, unit_slot(u, i)));
 #pragma unroll
     for (int d = 16; d; d >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, d);
     return n;
@@ -194,10 +195,10 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     auto bar = [&](const uint64_t& b) { return smem_u32(&b); };
     if (tid == 0) {
         for (uint32_t i = 0; i < Sh::kKeys; ++i) mbar_init(bar(sh.k_full[i]), 1), mbar_init(bar(sh.k_empty[i]), 1);
-        for (uint32_t i = 0; i < Sh::kQs; ++i) mbar_init(bar(sh.q_full[i]), 1), mbar_init(bar(sh.q_empty[i]), 1);
+        for (uint32_t i = 0; i < Sh::kQs; ++i) mbar_init(bar(sh.q_full[i]), 1), mbar_init(bar(sh.q_empty[i]), 2);
         for (uint32_t i = 0; i < Sh::kBufs; ++i)
             for (int h = 0; h < 2; ++h) mbar_init(bar(sh.s_full[h][i]), 1), mbar_init(bar(sh.s_empty[h][i]), 2 * Sh::kGroups);
-        for (uint32_t i = 0; i < kWeighUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kSumWarps + 1);
+        for (uint32_t i = 0; i < kWeighUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kSumWarps + 2);
         for (int h = 0; h < 2; ++h)
             for (int i = 0; i < 2; ++i) mbar_init(bar(sh.sum_full[h][i]), 4), mbar_init(bar(sh.sum_empty[h][i]), 4);
         sh.dead = 0;
@@ -224,8 +225,8 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     const uint32_t per = (a.tok.n_seqs + all - 1) / all;
     int64_t mine = 0;
     for (uint32_t s = who * per; s < min(a.tok.n_seqs, (who + 1) * per); ++s)
-        mine += seq_steps<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
-    int64_t lo = 0, total = 0;  // steps of a head of the sequences before, and of all
+        mine += seq_cost<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
+    int64_t lo = 0, total = 0;  // the cost of a head of the sequences before, and of all
     if (kOne) {
         int64_t inc = mine;
 #pragma unroll
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     if (busy && run0 >= lo * K && run0 < (lo + mine) * K) {
         int64_t p = lo * K;
         for (uint32_t s = who * per;; ++s) {
-            const int64_t steps = seq_steps<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
+            const int64_t steps = seq_cost<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
             if (run0 < p + steps * K) {
                 if (kOne || lane == 0) sh.start_seq = int32_t(s), sh.start_rest = run0 - p, sh.start_steps = steps;
                 break;
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
         if (warp == kSumWarps) {
         // ---------------------------------------------------------- loads
         int32_t s = sh.start_seq, h = int32_t(sh.start_rest / sh.start_steps), i = 0;  // sequence, key head, unit
-        int64_t at = run0, unit0;  // the segment's first step, the unit's
+        int64_t at = run0, unit;  // the segment's first place, the unit's
         KvSeq q = kv_seq(a.pages, a.tok, s);
         UnitList list = unit_list(f, q);
         {
@@ -277,7 +278,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                 i = int32_t(rest), rest = 0;
             } else {
                 for (;; i += 32) {  // the warp looks at 32 units at a time
-                    const int32_t mine = i + int32_t(lane) < list.n ? unit_steps(f, q, s, unit_slot(list, i + int32_t(lane))) : 0;
+                    const int32_t mine = i + int32_t(lane) < list.n ? unit_cost(unit_tiles(f, q, s, unit_slot(list, i + int32_t(lane)))) : 0;
                     int64_t inc = mine;
 #pragma unroll
                     for (int d = 1; d < 32; d <<= 1) {
@@ -292,10 +293,10 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                         break;
                     }
                     rest -= __shfl_sync(0xFFFFFFFFu, inc, 31);
-                    if (i + 32 >= list.n) break;  // (never: the steps add up)
+                    if (i + 32 >= list.n) break;  // (never: the costs add up)
                 }
             }
-            unit0 = at - rest;
+            unit = at - rest;
         }
         const uint32_t shift = a.pages.token_shift;
         const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
@@ -317,29 +318,32 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             const int32_t slot0 = unit_slot(list, i);
             const int2 tiles = unit_tiles(f, q, s, slot0);
             const bool dry = tiles.y <= tiles.x;
-            const int32_t steps = max(1, tiles.y - tiles.x), skip = int32_t(at - unit0);
-            const int32_t n = int32_t(min(int64_t(steps - skip), run1 - at));
+            const int32_t steps = max(1, tiles.y - tiles.x);
+            const int64_t unit0 = unit + (kOne || dry ? 0 : kUnitCost);  // its first step
+            if (at < unit0) at = unit0;
+            const int32_t skip = int32_t(at - unit0);
+            const int32_t n = int32_t(max(int64_t(0), min(int64_t(steps - skip), run1 - at)));  // (0: a run of nothing but a unit's cost)
             const int32_t first = q.first, head0 = h * int32_t(a.group);
             const int32_t row = int32_t((a.pages.layer * 2 * a.pages.kv_heads + h) << shift);
-            more = at + n < run1;
+            at = unit0 + steps;  // the next unit's place
+            more = at < run1;
             pages = ahead;
             if (!mbar_wait(bar(sh.unit_empty[u % kWeighUnits]), (u / kWeighUnits & 1) ^ 1, dead)) break;
             if (lane == 0) {
                 WeighUnit& o = sh.unit[u % kWeighUnits];
                 o.q = q, o.s = s, o.h = h, o.slot0 = slot0;
-                o.tile = tiles.x + skip, o.n = n, o.dry = dry, o.whole = n == steps, o.part = at == run0 ? 0 : 1, o.more = more;
+                o.tile = tiles.x + skip, o.n = n, o.dry = dry, o.whole = n == steps, o.part = u ? 1 : 0, o.more = more;
                 mbar_arrive(bar(sh.unit_full[u % kWeighUnits]));
-                if (!kOne && at == run0) {
+                if (!kOne && u == 0) {
                     // this run's note of a unit that began in the run before it
                     const int64_t b0 = ((unit0 + 1) * blocks - 1) / total, b1 = ((unit0 + steps) * blocks - 1) / total;
                     const bool here = skip > 0 && b0 + 1 == int64_t(blockIdx.x);
-                    f.join[blockIdx.x] = {s, h, slot0, q.len - q.n, q.len, int32_t(b0), int32_t(b1), b0 * total / blocks != unit0, here};
+                    f.join[blockIdx.x] = {s, h, slot0, q.len - q.n, q.len, int32_t(b0), int32_t(b1), b0 * total / blocks < unit, here};
                 }
             }
             __syncwarp();
-            at += n;
             if (more) {  // the next unit (the segment ended with this one)
-                unit0 = at;
+                unit = at;
                 if (++i == list.n) {
                     i = 0;
                     if (++h == int32_t(K)) {
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                 }
                 pages_at(ahead);
             }
-            if (!dry) {
+            if (!dry && n) {
                 for (int half = 0; half < 2; ++half, ++kn) {
                     const uint32_t slot = uint32_t(slot0) + half * 128 + lane * box, e = kn % Sh::kKeys;
                     const int32_t page = half ? pages.y : pages.x;
@@ -387,50 +391,52 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             for (uint32_t k = kn > Sh::kKeys ? kn - Sh::kKeys : 0; k < kn; ++k) mbar_wait(bar(sh.k_full[k % Sh::kKeys]), k / Sh::kKeys & 1, &late);
             for (uint32_t k = qn > Sh::kQs ? qn - Sh::kQs : 0; k < qn; ++k) mbar_wait(bar(sh.q_full[k % Sh::kQs]), k / Sh::kQs & 1, &late);
         }
-    } else if (warp == kSumWarps + 1) {
+    } else if (warp <= kSumWarps + 2) {
         // ---------------------------------------------------------- products
+        const uint32_t half = warp - (kSumWarps + 1);
         constexpr uint32_t kQk = instr_desc(kBf16, false, false, 128, N);
         const uint32_t ksteps = (a.pages.head_dim + 15) / 16;
         // keys and queries: rows of 64 elements, 128-byte swizzle
         const uint64_t kd = smem_desc(ring, 16, 1024, 2), qd = smem_desc(qs, 16, 1024, 2);
-        uint32_t kn = 0, qn = 0, n = 0;
-        bool more = true;
-        for (uint32_t u = 0; more; ++u) {
-            const bool got = mbar_wait(bar(sh.unit_full[u % kWeighUnits]), u / kWeighUnits & 1, dead);
-            if (!__all_sync(0xFFFFFFFFu, got)) break;
+        // (One lane issues them all: what stands between two products is short.)
+        bool more = lane == 0, ok = true;
+        uint32_t kn = half, qn = 0, n = 0;
+        auto products = [&](uint64_t k0, uint64_t q0, uint32_t to, auto all) {
+#pragma unroll
+            for (uint32_t x = 0; x < 4 * NS; ++x) {
+                if (!decltype(all)::value && x >= ksteps) break;
+                mma_ss(to, desc_at(k0, (x / 4) * kHalfSlot + (x % 4) * 32), desc_at(q0, (x / 4) * (N * 128) + (x % 4) * 32), kQk, x != 0);
+            }
+        };
+        for (uint32_t u = 0; more && ok; ++u) {
+            if (!mbar_wait(bar(sh.unit_full[u % kWeighUnits]), u / kWeighUnits & 1, dead)) break;
             const WeighUnit& o = sh.unit[u % kWeighUnits];
             const int32_t steps = o.dry ? 0 : o.n;
             more = o.more;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
-            for (int32_t i = 0; i < steps; ++i, ++n, ++qn) {
+            mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
+            if (!steps) continue;
+            const uint32_t ek = kn % Sh::kKeys;
+            ok = mbar_wait(bar(sh.k_full[ek]), kn / Sh::kKeys & 1, dead);
+            const uint64_t k0 = desc_at(kd, ek * Sh::kHalf);
+            for (int32_t i = 0; i < steps && ok; ++i, ++n, ++qn) {
                 const uint32_t eq = qn % Sh::kQs, buf = n % Sh::kBufs;
-                const bool there = mbar_wait(bar(sh.q_full[eq]), qn / Sh::kQs & 1, dead);
-                if (!__all_sync(0xFFFFFFFFu, there)) goto products_done;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t k = kn + half, ek = k % Sh::kKeys;
-                    if (i == 0) mbar_wait(bar(sh.k_full[ek]), k / Sh::kKeys & 1, dead);
-                    mbar_wait(bar(sh.s_empty[half][buf]), (n / Sh::kBufs & 1) ^ 1, dead);
-                    fence_after();
-                    if (elect() && !*dead) {
-                        const uint64_t k0 = desc_at(kd, ek * Sh::kHalf), q0 = desc_at(qd, eq * Sh::kQ);
-#pragma unroll
-                        for (uint32_t x = 0; x < 4 * NS; ++x) {
-                            if (x >= ksteps) break;
-                            mma_ss(tmem + (half * Sh::kBufs + buf) * N, desc_at(k0, (x / 4) * kHalfSlot + (x % 4) * 32),
-                                   desc_at(q0, (x / 4) * (N * 128) + (x % 4) * 32), kQk, x != 0);
-                        }
-                        mma_commit(bar(sh.s_full[half][buf]));
-                        if (i + 1 == steps) mma_commit(bar(sh.k_empty[ek]));
-                        if (half == 1) mma_commit(bar(sh.q_empty[eq]));
-                    }
-                    __syncwarp();
-                }
+                ok = mbar_wait(bar(sh.s_empty[half][buf]), (n / Sh::kBufs & 1) ^ 1, dead) &&
+                     mbar_wait(bar(sh.q_full[eq]), qn / Sh::kQs & 1, dead);
+                if (!ok) break;
+                fence_after();
+                const uint64_t q0 = desc_at(qd, eq * Sh::kQ);
+                const uint32_t to = tmem + (half * Sh::kBufs + buf) * N;
+                if (ksteps == 4 * NS)
+                    products(k0, q0, to, std::true_type());
+                else
+                    products(k0, q0, to, std::false_type());
+                mma_commit(bar(sh.s_full[half][buf]));
+                mma_commit(bar(sh.q_empty[eq]));
             }
-            if (steps) kn += 2;
+            if (ok) mma_commit(bar(sh.k_empty[ek]));
+            kn += 2;
         }
-    products_done:
+        __syncwarp();
         if (*dead) {  // the products in flight end before the tensor memory is freed
             const uint64_t t0 = now_ns();
             while (now_ns() - t0 < 50000) {
@@ -484,11 +490,12 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             const WeighUnit& rec = sh.unit[u % kWeighUnits];
             const int32_t s = rec.s, h = rec.h, len = rec.q.len, ctx = len - rec.q.n, first = rec.q.first, m = weigh_tokens(a, rec.q);
             const int32_t slot = rec.slot0 + half * 128 + int32_t(key), steps = rec.dry ? 0 : rec.n;
-            const bool dry = rec.dry, whole = rec.whole;
+            const bool dry = rec.dry, whole = rec.whole, none = rec.n == 0;
             const int32_t in_part = rec.part, tile0 = rec.tile;
             more = rec.more;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
+            if (none) break;
             const bool mine = side == 0 && slot < len && uint32_t(slot) < f.w.n_slots;
             float* const place = f.w.weights + uint32_t(s) * f.w.seq_stride + uint32_t(h) * f.w.head_stride + slot;
             float held = 0.0f;
@@ -532,12 +539,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                         uint64_t add0 = 0, add1 = 0;
 #pragma unroll
                         for (int c = 0; c < kCols; c += 4) {
-                            const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(lse_at + c);
-                            float y0, y1, y2, y3;
-                            unpack2(fma2(pack2(x[c], x[c + 1]), k22, l.x), y0, y1);
-                            unpack2(fma2(pack2(x[c + 2], x[c + 3]), k22, l.y), y2, y3);
-                            add0 = add2(add0, pack2(exp2_approx(y0), exp2_approx(y1)));
-                            add1 = add2(add1, pack2(exp2_approx(y2), exp2_approx(y3)));
+                            const float4 l = *reinterpret_cast<const float4*>(lse_at + c);
+                            add0 = add2(add0, pack2(exp2_approx(fmaf(x[c], k2, l.x)), exp2_approx(fmaf(x[c + 1], k2, l.y))));
+                            add1 = add2(add1, pack2(exp2_approx(fmaf(x[c + 2], k2, l.z)), exp2_approx(fmaf(x[c + 3], k2, l.w))));
                         }
                         float y0, y1;
                         unpack2(add2(add0, add1), y0, y1);
