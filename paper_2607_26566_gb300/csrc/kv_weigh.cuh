@@ -35,14 +35,15 @@ template <int N, int NS>
 struct WeighShape {
     static constexpr uint32_t kHalf = kHalfSlot * NS;                        // a half's keys
     static constexpr uint32_t kKeys = (N == 128 ? 3 : 6) * (NS == 1 ? 2 : 1);  // ... in the ring
+    static_assert(N == 128 || kKeys % 2 == 0, "every other entry is a loading warp's");
     static constexpr uint32_t kQ = N * 128 * NS;                             // a column tile
     static constexpr uint32_t kQs = N == 128 ? (NS == 1 ? 5 : 3) : N == 32 ? 2 : 4;
     static constexpr uint32_t kBufs = N == 128 ? 2 : 4;                      // tiles of scores of each half
     static constexpr uint32_t kTmem = 2 * kBufs * N;
     static constexpr uint32_t kBytes = 1024 + kHalf * kKeys + kQ * kQs;
-    // The warps that add up come in groups of four: one a half, or two, each with half of the columns. Then the loading
-    // warp, a product warp for each half (one's products run while the other waits), and one that idles, so that registers
-    // can be shared out by groups of four.
+    // The warps that add up come in groups of four: one a half, or two, each with half of the columns. Then a
+    // loading warp and a product warp for each half (one's products run while the other waits; N = 128 has one loading warp, and
+    // one that idles).
     static constexpr int kGroups = N == 128 ? 4 : 2;
     static constexpr int kCols = 2 * N / kGroups;  // of a group
     static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + 128;
@@ -266,8 +267,14 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
 
     if (busy && warp >= kSumWarps) {
         if (Sh::kGroups == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
-        if (warp == kSumWarps) {
+        if (warp == kSumWarps || (kOne && warp == kSumWarps + 3)) {
         // ---------------------------------------------------------- loads
+        // A warp a half, each with every other entry of the ring: both walk the run, the first hands units out and loads
+        // queries. (One warp for both halves issued a load of 2 KiB, as pages of 16 tokens have them, every 66 ns: a token
+        // each of 64 sequences of up to 16k slots 243 us, with two 179.) Where keys stay for many column tiles one warp
+        // loads both: the ring is an odd number of halves, so its entries cannot be shared out.
+        const uint32_t half0 = warp == kSumWarps ? 0 : 1;
+        constexpr uint32_t kLoads = kOne ? 1 : 2;
         int32_t s = sh.start_seq, h = int32_t(sh.start_rest / sh.start_steps), i = 0;  // sequence, key head, unit
         int64_t at = run0, unit;  // the segment's first place, the unit's
         KvSeq q = kv_seq(a.pages, a.tok, s);
@@ -302,17 +309,18 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
         const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
         const uint32_t T_mask = (1u << shift) - 1;
         const uint32_t q_bytes = uint32_t(f.per_tile * f.per_token) * 128 * NS;
-        uint32_t u = 0, kn = 0, qn = 0;
-        // A segment's pages, a lane a box of each half: looked up while the segment before is loaded.
-        auto pages_at = [&](int2& to) {
+        uint32_t u = 0, kn = half0, qn = 0;
+        // A segment's pages, a lane a box: looked up while the segment before is loaded.
+        int32_t page[kLoads], ahead[kLoads];
+        auto pages_at = [&]() {
             const int32_t* table = a.pages.table + uint32_t(s) * a.pages.table_stride;
-            const uint32_t slot = uint32_t(unit_slot(list, i)) + lane * box;
-            to = make_int2(-1, -1);
-            if (lane < boxes && slot < uint32_t(q.len)) to.x = table[slot >> shift];
-            if (lane < boxes && slot + 128 < uint32_t(q.len)) to.y = table[(slot + 128) >> shift];
+#pragma unroll
+            for (uint32_t k = 0; k < kLoads; ++k) {
+                const uint32_t slot = uint32_t(unit_slot(list, i)) + (half0 + k) * 128 + lane * box;
+                ahead[k] = lane < boxes && slot < uint32_t(q.len) ? table[slot >> shift] : -1;
+            }
         };
-        int2 pages, ahead;
-        pages_at(ahead);
+        pages_at();
         for (bool more = !f.no_loads; more; ++u) {
             // the segment
             const int32_t slot0 = unit_slot(list, i);
@@ -327,9 +335,10 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             const int32_t row = int32_t((a.pages.layer * 2 * a.pages.kv_heads + h) << shift);
             at = unit0 + steps;  // the next unit's place
             more = at < run1;
-            pages = ahead;
-            if (!mbar_wait(bar(sh.unit_empty[u % kWeighUnits]), (u / kWeighUnits & 1) ^ 1, dead)) break;
-            if (lane == 0) {
+#pragma unroll
+            for (uint32_t k = 0; k < kLoads; ++k) page[k] = ahead[k];
+            if (half0 == 0 && !mbar_wait(bar(sh.unit_empty[u % kWeighUnits]), (u / kWeighUnits & 1) ^ 1, dead)) break;
+            if (half0 == 0 && lane == 0) {
                 WeighUnit& o = sh.unit[u % kWeighUnits];
                 o.q = q, o.s = s, o.h = h, o.slot0 = slot0;
                 o.tile = tiles.x + skip, o.n = n, o.dry = dry, o.whole = n == steps, o.part = u ? 1 : 0, o.more = more;
@@ -355,14 +364,14 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                         } while (list.n == 0);
                     }
                 }
-                pages_at(ahead);
+                pages_at();
             }
             if (!dry && n) {
-                for (int half = 0; half < 2; ++half, ++kn) {
-                    const uint32_t slot = uint32_t(slot0) + half * 128 + lane * box, e = kn % Sh::kKeys;
-                    const int32_t page = half ? pages.y : pages.x;
+#pragma unroll
+                for (uint32_t k = 0; k < kLoads; ++k, kn += 2 / kLoads) {
+                    const uint32_t slot = uint32_t(slot0) + (half0 + k) * 128 + lane * box, e = kn % Sh::kKeys;
                     // what the pool lacks, and what lies behind the sequence, is filled with zeros
-                    const int32_t z = uint32_t(page) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page;
+                    const int32_t z = uint32_t(page[k]) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page[k];
                     if (!mbar_wait(bar(sh.k_empty[e]), (kn / Sh::kKeys & 1) ^ 1, dead)) goto loads_done;
                     if (lane == 0) mbar_expect(bar(sh.k_full[e]), Sh::kHalf);
                     __syncwarp();
@@ -371,6 +380,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                             tma_load(ring + e * Sh::kHalf + x * kHalfSlot + lane * box * 128, &map, x * 64, row + int32_t(slot & T_mask), z,
                                      bar(sh.k_full[e]));
                 }
+                if (half0) continue;
                 for (int32_t t = tiles.x + skip; t < tiles.x + skip + n; ++t, ++qn) {
                     const uint32_t e = qn % Sh::kQs;
                     if (!mbar_wait(bar(sh.q_empty[e]), (qn / Sh::kQs & 1) ^ 1, dead)) goto loads_done;
@@ -388,7 +398,8 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
         __syncwarp();
         if (*dead) {  // the copies in flight land before the block ends
             uint32_t late = 0;
-            for (uint32_t k = kn > Sh::kKeys ? kn - Sh::kKeys : 0; k < kn; ++k) mbar_wait(bar(sh.k_full[k % Sh::kKeys]), k / Sh::kKeys & 1, &late);
+            for (uint32_t k = kn > Sh::kKeys ? kn - Sh::kKeys : half0; k < kn; k += 2 / kLoads)
+                mbar_wait(bar(sh.k_full[k % Sh::kKeys]), k / Sh::kKeys & 1, &late);
             for (uint32_t k = qn > Sh::kQs ? qn - Sh::kQs : 0; k < qn; ++k) mbar_wait(bar(sh.q_full[k % Sh::kQs]), k / Sh::kQs & 1, &late);
         }
     } else if (warp <= kSumWarps + 2) {
@@ -480,6 +491,14 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                 if (!real) next[k] = -INFINITY;
             }
         };
+        // the weight so far of the thread's slot of a unit
+        auto weight_so_far = [&](const WeighUnit& o) {
+            const int32_t slot = o.slot0 + half * 128 + int32_t(key);
+            const bool old = slot < o.q.len - o.q.n && uint32_t(slot) < f.w.n_slots && f.w.decay != 0.0f;
+            return old ? f.w.weights[uint32_t(o.s) * f.w.seq_stride + uint32_t(o.h) * f.w.head_stride + slot] : 0.0f;
+        };
+        float then = 0.0f;  // ... of the next unit
+        bool then_known = false;
         int32_t had_s = -1, had_h = -1;  // whose column tile's log-sum-exps are there (of one tile a sequence)
         bool known = false;              // `next` is the next tile's
         uint32_t n = 0;
@@ -493,13 +512,22 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             const bool dry = rec.dry, whole = rec.whole, none = rec.n == 0;
             const int32_t in_part = rec.part, tile0 = rec.tile;
             more = rec.more;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
             if (none) break;
             const bool mine = side == 0 && slot < len && uint32_t(slot) < f.w.n_slots;
             float* const place = f.w.weights + uint32_t(s) * f.w.seq_stride + uint32_t(h) * f.w.head_stride + slot;
-            float held = 0.0f;
-            if (whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
+            float held = then;
+            if (!kOne && whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
+            if (kOne) {  // the next unit's, on their way while this one is worked on
+                if (!then_known) held = weight_so_far(rec);
+                then_known = false;
+                if (more) {
+                    const uint32_t v = u + 1;
+                    const bool out = mbar_test(bar(sh.unit_full[v % kWeighUnits]), v / kWeighUnits & 1);
+                    if (__all_sync(0xFFFFFFFFu, out)) then = weight_so_far(sh.unit[v % kWeighUnits]), then_known = true;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
             // the tokens [i0, i1) that see the slot, and those that see all of the warp's slots
             int32_t i0 = max(0, slot - ctx), i1 = m;
             if (a.window && slot >= int32_t(a.sinks)) i1 = int32_t(min(int64_t(m), int64_t(slot) + int64_t(a.window) - ctx));
