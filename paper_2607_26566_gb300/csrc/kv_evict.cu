@@ -3,7 +3,6 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "kv_attend.cuh"
 #include "t2istore.h"
@@ -17,60 +16,75 @@ namespace cg = cooperative_groups;
 // The r largest of a row's weights, of equals the first: the r-th largest is found by its bits (weights as numbers whose
 // order is that of the integers, NaN as the lowest), eleven, eleven and ten at a time, from counts of each value of
 // these bits; then one pass in the order of slots writes those above it and the first ones equal to it. Counts are
-// integers, so their order does not matter. A cluster of blocks shares a row; each has its part of the row in shared
-// memory, so that weights are read once, and adds up the counts of all. A part that does not fit is read from memory
-// in each pass.
-constexpr uint32_t kSelThreads = 512;
+// integers, so their order does not matter. A cluster of blocks shares a row and adds up the counts of all of them. A
+// warp has a stretch of its block's slots, I to a lane, in registers, so that weights are read once; a row that is longer
+// than its caller said, or than a cluster holds, is read from memory in each pass.
+constexpr uint32_t kSelThreads = 1024;
 constexpr uint32_t kSelWarps = kSelThreads / 32;
 constexpr uint32_t kBins = 2048;
 constexpr uint32_t kMostBlocks = 8;  // of a cluster
-constexpr uint32_t kPartMost = 40960;  // weights of a part in shared memory: 160 KiB
 
 // A weight's place in the order: 0 for NaN, 0 and -0 alike.
 __device__ __forceinline__ uint32_t order_of(float w) {
-    if (w != w) return 0;
     const uint32_t b = __float_as_uint(w + 0.0f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    const uint32_t k = b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
+    return w != w ? 0 : k;
 }
+constexpr uint32_t kLowest = 0x007FFFFFu, kHighest = 0xFF800000u;  // of -infinity and infinity
+__device__ __forceinline__ float weight_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
 struct SelShared {
     uint32_t hist[3][kBins];
     uint32_t warp_sums[2][kSelWarps];
-    uint32_t base[2][kSelWarps];  // such slots of the warps before, in the block
     uint32_t mine[2];     // this block's slots above the threshold (or staying whatever they weigh), and equal to it
     uint32_t bin, above, in;
 };
 
-__global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_constant__ KvSelect c, const uint32_t part_room) {
-    extern __shared__ float part[];
-    __shared__ SelShared sh;
+// One row, by a cluster. HELD: a lane's I weights are in registers.
+template <int I, bool HELD>
+__device__ __forceinline__ void select_row(const KvSelect& c, SelShared& sh, uint32_t s, uint32_t head, uint32_t len, uint32_t n) {
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t blocks = cluster.num_blocks(), rank = cluster.block_rank();
     const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    const uint32_t row = blockIdx.x / blocks, s = row / c.n_heads, head = row % c.n_heads;
-    for (uint32_t i = tid; i < 3 * kBins; i += kSelThreads) (&sh.hist[0][0])[i] = 0;
-    tc::pdl_launch();
-    tc::pdl_wait();
-    const int32_t given = c.lens[s];
-    const uint32_t len = given > 0 && uint32_t(given) <= c.n_slots ? uint32_t(given) : 0;
-    uint32_t n = min(len, c.keep);
-    if (c.keeps) n = min(n, uint32_t(max(c.keeps[s], 0)));
     const uint32_t a = min(c.sinks, n), b = min(c.recent, n - a);
-    if (tid == 0 && rank == 0 && head == 0) c.counts[s] = int32_t(n);
     const float* const w = c.weights + s * c.seq_stride + head * c.head_stride;
     float* const out = c.weights_out ? c.weights_out + s * c.out_seq_stride + head * c.out_head_stride : nullptr;
     int32_t* const kept = c.kept + s * c.kept_seq_stride + head * c.kept_head_stride;
-    if (n == 0) return;  // (of all of the cluster's blocks)
+    auto sync = [&]() {
+        if (blocks > 1)
+            cluster.sync();
+        else
+            __syncthreads();
+    };
+    // the warp's slots, and in it those that are chosen by weight
+    const uint32_t stretch = (len + blocks * kSelThreads - 1) / (blocks * kSelThreads) * 32;
+    const uint32_t w0 = min(uint64_t(len), uint64_t(rank * kSelWarps + warp) * stretch), w1 = min(len, w0 + stretch);
+    const int mine = int((w1 - w0 + 31) / 32);  // of each lane, the last one maybe not
+    float held[HELD ? I : 1];
+    if (HELD) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) held[i] = w0 + i * 32 + lane < w1 ? w[w0 + i * 32 + lane] : 0.0f;
+    }
+    // f(slot, weight) for the lane's slots in turn, also (with any weight) for those from w1 on
+    auto each = [&](auto&& f) {
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                if (i >= mine) break;
+                f(w0 + i * 32 + lane, held[i]);
+            }
+        } else {
+            for (uint32_t j = w0; j < w1; j += 32) f(j + lane, j + lane < w1 ? w[j + lane] : 0.0f);
+        }
+    };
 
-    // this block's slots, and in it those that are chosen by weight
-    const uint32_t per = (len + blocks - 1) / blocks;
-    const uint32_t j0 = min(len, rank * per), j1 = min(len, j0 + per);
-    const uint32_t f0 = max(j0, a), f1 = min(j1, len - b);
-    const bool here = per <= part_room;
-    if (here)
-        for (uint32_t j = j0 + tid; j < j1; j += kSelThreads) part[j - j0] = w[j];
-    __syncthreads();
-    auto at = [&](uint32_t j) { return here ? part[j - j0] : w[j]; };
+    // the lane's slots that are there, and those that are chosen by weight, a bit each (HELD)
+    uint32_t live = 0, choice = 0;
+    if (HELD) {
+        auto below = [](uint32_t n) { return n >= 32 ? ~0u : (1u << n) - 1; };  // of slots at 32 i + lane
+        auto bits = [&](uint32_t j) { return below(j > w0 + lane ? (j - w0 - lane + 31) / 32 : 0); };
+        live = bits(w1), choice = bits(min(w1, len - b)) & ~bits(a);
+    }
 
     // the threshold: weights above `edge` stay, and the first `ties` of those equal to it
     uint32_t need = n - a - b, edge = 0xFFFFFFFFu, ties = 0;
@@ -82,19 +96,44 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         for (int pass = 0; pass < 3; ++pass) {
             const uint32_t bits = pass < 2 ? 11 : 10, shift = 32 - known - bits;
             uint32_t* const h = sh.hist[pass];
-            for (uint32_t j = f0 + tid; j < f1; j += kSelThreads) {
-                const uint32_t k = order_of(at(j));
-                if (known == 0 || k >> (32 - known) == prefix) atomicAdd(&h[k >> shift & ((1u << bits) - 1)], 1u);
+            if (pass)
+                for (uint32_t i = tid; i < kBins / 4; i += kSelThreads) reinterpret_cast<uint4*>(h)[i] = make_uint4(0, 0, 0, 0);
+            if (pass) __syncthreads();  // (the first one's are zeros from the start)
+            // numbers between these have the leading bits (NaN, and what no number has, are not looked for by them)
+            const uint32_t lo = known ? prefix << (32 - known) : 0, hi = known ? lo + (0xFFFFFFFFu >> known) : 0xFFFFFFFFu;
+            if (HELD && pass && lo >= kLowest) {
+                const float from = weight_of(lo), upto = weight_of(hi == 0x7FFFFFFFu ? hi - 1 : min(hi, kHighest));
+#pragma unroll
+                for (int i = 0; i < I; ++i) {
+                    if (i >= mine) break;
+                    if (held[HELD ? i : 0] >= from && held[HELD ? i : 0] <= upto && (choice >> i & 1))
+                        atomicAdd(&h[order_of(held[HELD ? i : 0]) >> shift & ((1u << bits) - 1)], 1u);
+                }
+            } else {
+                uint32_t i = 0;
+                each([&](uint32_t j, float x) {
+                    const uint32_t k = order_of(x);
+                    const bool counts = HELD ? choice >> i++ & 1 : j >= a && j < min(w1, len - b);
+                    if (counts && k >= lo && k <= hi) atomicAdd(&h[k >> shift & ((1u << bits) - 1)], 1u);
+                });
             }
-            cluster.sync();
-            // each thread: four bins, highest first, of all blocks
-            uint32_t v[4] = {0, 0, 0, 0};
-            const uint32_t b0 = kBins - 4 - tid * 4;
-            for (uint32_t r = 0; r < blocks; ++r) {
-                const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(h, r) + b0);
-                v[0] += x.w, v[1] += x.z, v[2] += x.y, v[3] += x.x;
+            sync();
+            // each thread: two bins, the higher first, of all blocks
+            static_assert(kBins == 2 * kSelThreads, "");
+            uint2 v = make_uint2(0, 0);
+            const uint32_t b0 = kBins - 2 - tid * 2;
+            auto add = [&](const uint2& x) { v.x += x.y, v.y += x.x; };
+            if (blocks == 1) {
+                add(*reinterpret_cast<const uint2*>(h + b0));
+            } else {
+                uint2 x[kMostBlocks];
+#pragma unroll
+                for (uint32_t r = 0; r < kMostBlocks; ++r)
+                    x[r] = r < blocks ? *reinterpret_cast<const uint2*>(cluster.map_shared_rank(h, r) + b0) : make_uint2(0, 0);
+#pragma unroll
+                for (uint32_t r = 0; r < kMostBlocks; ++r) add(x[r]);
             }
-            const uint32_t sum = v[0] + v[1] + v[2] + v[3];
+            const uint32_t sum = v.x + v.y;
             uint32_t inc = sum;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -103,12 +142,10 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
             }
             if (lane == 31) sh.warp_sums[0][warp] = inc;
             __syncthreads();
-            uint32_t before = inc - sum;
-            for (uint32_t i = 0; i < warp; ++i) before += sh.warp_sums[0][i];
+            uint32_t before = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sh.warp_sums[0][lane] : 0) + inc - sum;
             if (before < need && before + sum >= need) {
-                int i = 0;
-                while (before + v[i] < need) before += v[i++];
-                sh.bin = b0 + 3 - i, sh.above = before, sh.in = v[i];
+                const bool second = before + v.x < need;
+                sh.bin = second ? b0 : b0 + 1, sh.above = second ? before + v.x : before, sh.in = second ? v.y : v.x;
             }
             __syncthreads();
             prefix = prefix << bits | sh.bin;
@@ -117,62 +154,98 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
             const bool all = sh.in == need;  // the whole bin stays
             edge = known == 32 ? prefix : prefix << (32 - known);
             ties = need;
-            __syncthreads();
             if (all) {
                 if (known < 32) --edge, ties = 0;  // (edge > 0: a bin 0 with all of the rest would be every slot)
                 break;
             }
         }
     }
-    // in the order of slots: a warp has a stretch of the block's, counts it, and writes
-    const uint32_t stretch = ((j1 - j0 + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
-    const uint32_t w0 = min(j1, j0 + warp * stretch), w1 = min(j1, w0 + stretch);
-    auto look = [&](uint32_t j, bool& over, bool& equal) {
-        over = equal = false;
-        if (j >= w1) return 0.0f;
-        const float x = at(j);
-        const bool held = j < a || j >= len - b;
-        const uint32_t k = order_of(x);
-        over = held || k > edge;
-        equal = !held && k == edge;
-        return x;
+    // in the order of slots: a warp counts its stretch, then writes it
+    const float at = weight_of(edge == 0x7FFFFFFFu ? edge - 1 : edge);  // (-0 has 0's place: what is above an edge just below that is above -0x1p-149)
+    const bool low = edge < kLowest;  // (no number is below: all of them are above)
+    auto look = [&](uint32_t j, float x, bool& over, bool& equal) {
+        const bool stays = j < a || j >= len - b;
+        over = j < w1 && (stays || (low ? x == x : x > at));
+        equal = j < w1 && !stays && (edge == 0 ? x != x : x == at);
     };
-    uint32_t overs = 0, equals = 0;
-    for (uint32_t j = w0; j < w1; j += 32) {
-        bool over, equal;
-        look(j + lane, over, equal);
-        overs += __popc(__ballot_sync(0xFFFFFFFFu, over));
-        equals += __popc(__ballot_sync(0xFFFFFFFFu, equal));
+    uint32_t overs = 0, equals = 0, over_bits = 0, equal_bits = 0;  // (HELD: a bit a slot of the lane)
+    if (HELD) {
+        if (edge == 0) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) over_bits |= uint32_t(held[HELD ? i : 0] == held[HELD ? i : 0]) << i;
+            equal_bits = choice & ~over_bits;
+        } else {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                if (i >= mine) break;
+                over_bits |= uint32_t(low ? held[HELD ? i : 0] == held[HELD ? i : 0] : held[HELD ? i : 0] > at) << i;
+                equal_bits |= uint32_t(held[HELD ? i : 0] == at) << i;
+            }
+            equal_bits &= choice;
+        }
+        over_bits = (over_bits & choice) | (live & ~choice);
+        overs = __reduce_add_sync(0xFFFFFFFFu, __popc(over_bits)), equals = __reduce_add_sync(0xFFFFFFFFu, __popc(equal_bits));
+    } else {
+        each([&](uint32_t j, float x) {
+            bool over, equal;
+            look(j, x, over, equal);
+            overs += __popc(__ballot_sync(0xFFFFFFFFu, over));
+            equals += __popc(__ballot_sync(0xFFFFFFFFu, equal));
+        });
     }
+    const bool none_equal = equals == 0;
+    __syncthreads();  // (warp_sums are read)
     if (lane == 0) sh.warp_sums[0][warp] = overs, sh.warp_sums[1][warp] = equals;
     __syncthreads();
-    overs = equals = 0;
-    for (uint32_t i = 0; i < kSelWarps; ++i) {
-        if (i == warp && lane == 0) sh.base[0][warp] = overs, sh.base[1][warp] = equals;
-        overs += sh.warp_sums[0][i], equals += sh.warp_sums[1][i];
+    {  // of the warps before; and the block's
+        const uint32_t o = lane < kSelWarps ? sh.warp_sums[0][lane] : 0, e = lane < kSelWarps ? sh.warp_sums[1][lane] : 0;
+        overs = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? o : 0), equals = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? e : 0);
+        const uint32_t all_o = __reduce_add_sync(0xFFFFFFFFu, o), all_e = __reduce_add_sync(0xFFFFFFFFu, e);
+        if (tid == 0) sh.mine[0] = all_o, sh.mine[1] = all_e;
     }
-    if (tid == 0) sh.mine[0] = overs, sh.mine[1] = equals;
-    cluster.sync();
-    overs = sh.base[0][warp], equals = sh.base[1][warp];
-    for (uint32_t r = 0; r < rank; ++r) {
-        const uint32_t* m = cluster.map_shared_rank(sh.mine, r);
-        overs += m[0], equals += m[1];
-    }
-    const bool copy = out && (here || out != w);
-    for (uint32_t j = w0; j < w1; j += 32) {
-        bool over, equal;
-        const float x = look(j + lane, over, equal);
-        const uint32_t mo = __ballot_sync(0xFFFFFFFFu, over), me = __ballot_sync(0xFFFFFFFFu, equal), lower = (1u << lane) - 1;
-        const uint32_t e = equals + __popc(me & lower);
-        const uint32_t to = overs + __popc(mo & lower) + min(e, ties);
-        if (over || (equal && e < ties)) {
-            kept[to] = int32_t(j + lane);
-            if (copy) out[to] = x;
+    if (blocks > 1) {
+        cluster.sync();
+        for (uint32_t r = 0; r < rank; ++r) {
+            const uint32_t* m = cluster.map_shared_rank(sh.mine, r);
+            overs += m[0], equals += m[1];
         }
-        overs += __popc(mo), equals += __popc(me);
     }
-    cluster.sync();  // (shared memory lives until the others have read it; and kept is complete)
-    if (out && !copy && rank == 0) {
+    const bool copy = out && (HELD || out != w);
+    const uint32_t lower = (1u << lane) - 1;
+    if (HELD && none_equal) {
+        uint32_t base = overs + min(equals, ties);
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if (i >= mine) break;
+            const bool over = over_bits >> i & 1;
+            const uint32_t mo = __ballot_sync(0xFFFFFFFFu, over);
+            const uint32_t to = base + __popc(mo & lower);
+            if (over) {
+                kept[to] = int32_t(w0 + i * 32 + lane);
+                if (copy) out[to] = held[HELD ? i : 0];
+            }
+            base += __popc(mo);
+        }
+    } else {
+        uint32_t i = 0;
+        each([&](uint32_t j, float x) {
+            bool over, equal;
+            if (HELD)
+                over = over_bits >> i & 1, equal = equal_bits >> i & 1, ++i;
+            else
+                look(j, x, over, equal);
+            const uint32_t mo = __ballot_sync(0xFFFFFFFFu, over), me = __ballot_sync(0xFFFFFFFFu, equal);
+            const uint32_t e = equals + __popc(me & lower);
+            const uint32_t to = overs + __popc(mo & lower) + min(e, ties);
+            if (over || (equal && e < ties)) {
+                kept[to] = int32_t(j);
+                if (copy) out[to] = x;
+            }
+            overs += __popc(mo), equals += __popc(me);
+        });
+    }
+    if (blocks > 1 || !HELD) sync();  // (shared memory lives until the others have read it; and kept is complete)
+    if (!HELD && out && !copy && rank == 0) {
         // in place, from memory: a slot's weight moves down, so a stretch is read before it is written over
         for (uint32_t i0 = 0; i0 < n; i0 += kSelThreads) {
             const uint32_t i = i0 + tid;
@@ -183,6 +256,27 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
             __syncthreads();
         }
     }
+}
+
+template <int I>
+__global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_constant__ KvSelect c) {
+    __shared__ SelShared sh;
+    const uint32_t blocks = cg::this_cluster().num_blocks(), rank = cg::this_cluster().block_rank();
+    const uint32_t row = blockIdx.x / blocks, s = row / c.n_heads, head = row % c.n_heads;
+    for (uint32_t i = threadIdx.x; i < kBins / 4; i += kSelThreads) reinterpret_cast<uint4*>(sh.hist[0])[i] = make_uint4(0, 0, 0, 0);
+    tc::pdl_launch();
+    tc::pdl_wait();
+    const int32_t given = c.lens[s];
+    const uint32_t len = given > 0 && uint32_t(given) <= c.n_slots ? uint32_t(given) : 0;
+    uint32_t n = min(len, c.keep);
+    if (c.keeps) n = min(n, uint32_t(max(c.keeps[s], 0)));
+    if (threadIdx.x == 0 && rank == 0 && head == 0) c.counts[s] = int32_t(n);
+    if (n == 0) return;  // (of all of the cluster's blocks)
+    __syncthreads();
+    if (len <= blocks * (I * kSelThreads))
+        select_row<I, true>(c, sh, s, head, len, n);
+    else
+        select_row<I, false>(c, sh, s, head, len, n);
 }
 
 // ------------------------------------------------------------------ evict
@@ -226,25 +320,11 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_const
 
 }  // namespace
 
-cudaError_t launch_kv_select(const KvSelect& c, uint32_t sms, cudaStream_t stream) {
-    const uint32_t rows = c.n_seqs * c.n_heads;
-    const uint32_t most = c.max_len;
-    uint32_t blocks = 1;
-    while (blocks < kMostBlocks && (most / blocks > kPartMost || (most / blocks > 2048 && rows * blocks * 2 <= sms * 2))) blocks *= 2;
-    const uint32_t room = std::min((most + blocks - 1) / blocks, kPartMost);
-    static std::atomic<uint64_t> ready{0};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev >= 64 || !(ready.load() >> dev & 1)) {
-        e = cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kPartMost * 4));
-        if (e != cudaSuccess) return e;
-        if (dev < 64) ready |= uint64_t(1) << dev;
-    }
+template <int I>
+cudaError_t launch_select(const KvSelect& c, uint32_t blocks, cudaStream_t stream) {
     cudaLaunchConfig_t l{};
-    l.gridDim = dim3(rows * blocks);
+    l.gridDim = dim3(c.n_seqs * c.n_heads * blocks);
     l.blockDim = dim3(kSelThreads);
-    l.dynamicSmemBytes = room * 4;
     l.stream = stream;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -253,7 +333,16 @@ cudaError_t launch_kv_select(const KvSelect& c, uint32_t sms, cudaStream_t strea
     at[1].val.clusterDim.x = blocks, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     l.attrs = at;
     l.numAttrs = 2;
-    return cudaLaunchKernelEx(&l, select_kernel, c, room);
+    return cudaLaunchKernelEx(&l, select_kernel<I>, c);
+}
+
+cudaError_t launch_kv_select(const KvSelect& c, uint32_t sms, cudaStream_t stream) {
+    const uint64_t rows = uint64_t(c.n_seqs) * c.n_heads;
+    // blocks to a row: what holds it, and more while SMs are idle and a block has two weights a thread and more
+    uint32_t blocks = 1;
+    while (blocks < kMostBlocks && (c.max_len / blocks > 16 * kSelThreads || (c.max_len / blocks > 2 * kSelThreads && rows * blocks * 2 <= sms))) blocks *= 2;
+    const uint32_t each = (c.max_len + blocks * kSelThreads - 1) / (blocks * kSelThreads);
+    return each <= 2 ? launch_select<2>(c, blocks, stream) : each <= 8 ? launch_select<8>(c, blocks, stream) : launch_select<16>(c, blocks, stream);
 }
 
 cudaError_t launch_kv_evict(const KvEvict& c, uint32_t sms, cudaStream_t stream) {

@@ -236,3 +236,20 @@ def test_refusals(any_cache):
     no(T2IError, "layers", c.evict, kept[:1], counts[:1], layer=1)
     c.evict(kept[:0], counts[:0])
     c.evict(kept[:1, :, :0], counts[:1])
+
+
+def test_thresholds_at_zero(any_cache):
+    """Exactly the numbers from 0 (and -0) on stay, or from infinity on, or all but NaN, or some of the zeros."""
+    g = np.random.default_rng(1)
+    neg = -np.exp(g.standard_normal(300)).astype(np.float32)
+    tiny = np.array([-1.4e-45, 1.4e-45, -1e-38, 1e-38], np.float32)
+    rows = [np.concatenate([neg, np.zeros(40), -np.zeros(40), np.exp(g.standard_normal(100)), tiny, [math.inf] * 5,
+                            [-math.inf] * 5, [math.nan] * 6]).astype(np.float32) for _ in range(4)]
+    for r in rows:
+        g.shuffle(r)
+    w = torch.from_numpy(np.stack(rows))[None]
+    L = w.shape[2]
+    positive, zeros = 100 + 2 + 5, 80
+    for keep in (5, positive, positive + 1, positive + 37, positive + zeros, positive + zeros + 1, L - 11, L - 6, L - 5, L - 1):
+        check(any_cache, w, [L], keep)
+        check(any_cache, w, [L], keep, in_place=True)
