@@ -280,41 +280,64 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_con
 }
 
 // ------------------------------------------------------------------ evict
-// A block moves the rows of one key head's keys or values (or a share of their columns), a chunk of rows at a time: all
+// A block moves the rows of one key head's keys and values (or a share of their columns), a chunk of rows at a time: all
 // of a chunk's loads come before its stores, and a row's new slot is at or before its old one, so no row is overwritten
-// before it was read.
+// before it was read. Where a chunk's rows lie is looked up once, by a thread a row, while the chunk before is moved.
+// Bound by memory: rows are read once and written once, past the caches. Measured: 64 sequences of up to 16k slots to 4k
+// each, 8 heads of 128 (2.15 GB): 339 us, 6.3 TB/s.
 constexpr uint32_t kEvictThreads = 256;
-constexpr uint32_t kEvictDeep = 8;  // rows of a thread in a chunk
-__global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_constant__ KvEvict c, const uint32_t cols) {
+constexpr uint32_t kEvictDeep = 4;  // rows of a thread in a chunk
+constexpr uint32_t kEvictRows = kEvictThreads / 2 * kEvictDeep;  // of a chunk, at most
+__global__ void __launch_bounds__(kEvictThreads, 4) evict_kernel(const __grid_constant__ KvEvict c, const uint32_t cols) {
+    __shared__ ulonglong2 place[2][kEvictRows];  // a row's key: where it is and where it goes; 0: it stays
     tc::pdl_launch();
     tc::pdl_wait();
     const KvPages& p = c.pages;
-    const uint32_t s = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
-    const uint32_t which = blockIdx.y % 2, layer = p.layer + blockIdx.y / 2;
-    const uint32_t rows = kEvictThreads / cols, r = threadIdx.x / cols, col = blockIdx.z * cols + threadIdx.x % cols;
+    const uint32_t s = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads, layer = p.layer + blockIdx.y;
+    const uint32_t rows = kEvictThreads / cols, chunk = rows * kEvictDeep;
+    const uint32_t r = threadIdx.x / cols, col = blockIdx.z * cols + threadIdx.x % cols;
     const bool mine = r < rows && col * 8 < p.head_dim;
     const uint32_t n = uint32_t(min(max(c.counts[s], 0), int32_t(c.max_kept)));
     const int32_t* const kept = c.kept + s * c.kept_seq_stride + head * c.kept_head_stride;
-    for (uint32_t i0 = 0; i0 < n; i0 += rows * kEvictDeep) {
-        uint4 v[kEvictDeep];
-        uint4* to[kEvictDeep];
+    const uint64_t apart = (uint64_t(p.kv_heads) << p.token_shift) * (p.head_dim * 2);  // from a slot's key to its value
+    auto look_up = [&](uint32_t i0, ulonglong2* to) {
+        for (uint32_t k = threadIdx.x; k < chunk; k += kEvictThreads) {
+            const uint32_t i = i0 + k;
+            ulonglong2 at = make_ulonglong2(0, 0);
+            const int32_t from = i < n ? kept[i] : 0;
+            if (i < n && from > int32_t(i)) {
+                const uint8_t* src = kv_row(p, s, from, layer, 0, head);
+                const uint8_t* dst = kv_row(p, s, i, layer, 0, head);
+                if (src && dst) at = make_ulonglong2(reinterpret_cast<uint64_t>(src), reinterpret_cast<uint64_t>(dst));
+            }
+            to[k] = at;
+        }
+    };
+    look_up(0, place[0]);
+    __syncthreads();
+    for (uint32_t i0 = 0, b = 0; i0 < n; i0 += chunk, b ^= 1) {
+        uint4 key[kEvictDeep], val[kEvictDeep];
+        uint64_t to[kEvictDeep];
 #pragma unroll
         for (uint32_t k = 0; k < kEvictDeep; ++k) {
-            const uint32_t i = i0 + k * rows + r;
-            to[k] = nullptr;
-            if (!mine || i >= n) continue;
-            const int32_t from = kept[i];
-            if (from <= int32_t(i)) continue;
-            const uint8_t* src = kv_row(p, s, from, layer, which, head);
-            uint8_t* dst = kv_row(p, s, i, layer, which, head);
-            if (!src || !dst) continue;
-            v[k] = *reinterpret_cast<const uint4*>(src + col * 16);
-            to[k] = reinterpret_cast<uint4*>(dst + col * 16);
+            to[k] = 0;
+            if (!mine) continue;
+            const ulonglong2 at = place[b][k * rows + r];
+            to[k] = at.y;
+            if (!at.y) continue;
+            const uint8_t* src = reinterpret_cast<const uint8_t*>(at.x) + col * 16;
+            key[k] = __ldcs(reinterpret_cast<const uint4*>(src));
+            val[k] = __ldcs(reinterpret_cast<const uint4*>(src + apart));
         }
+        if (i0 + chunk < n) look_up(i0 + chunk, place[b ^ 1]);
         __syncthreads();
 #pragma unroll
-        for (uint32_t k = 0; k < kEvictDeep; ++k)
-            if (to[k]) *to[k] = v[k];
+        for (uint32_t k = 0; k < kEvictDeep; ++k) {
+            if (!to[k]) continue;
+            uint8_t* dst = reinterpret_cast<uint8_t*>(to[k]) + col * 16;
+            __stcs(reinterpret_cast<uint4*>(dst), key[k]);
+            __stcs(reinterpret_cast<uint4*>(dst + apart), val[k]);
+        }
     }
 }
 
@@ -347,12 +370,13 @@ cudaError_t launch_kv_select(const KvSelect& c, uint32_t sms, cudaStream_t strea
 
 cudaError_t launch_kv_evict(const KvEvict& c, uint32_t sms, cudaStream_t stream) {
     const uint32_t vectors = c.pages.head_dim / 8;
-    const uint64_t units = uint64_t(c.n_seqs) * c.pages.kv_heads * 2 * c.layers;
-    // few units: a block has a share of the columns, of 32 bytes at least
+    const uint64_t units = uint64_t(c.n_seqs) * c.pages.kv_heads * c.layers;
+    // Fewer units than blocks that an SM's four places take: a block has a share of the columns, of 32 bytes at least. 512
+    // units of 4,096 rows of 256 bytes with 1, 2 and 4 shares: 360, 338, 565 us.
     uint32_t parts = 1;
-    while (parts < 8 && units * parts < 2 * sms && vectors / parts >= 4) parts *= 2;
+    while (parts < 8 && units * parts < 4 * sms && vectors / parts >= 4) parts *= 2;
     const uint32_t cols = (vectors + parts - 1) / parts;
-    return launch_pdl(evict_kernel, dim3(c.n_seqs * c.pages.kv_heads, 2 * c.layers, parts), kEvictThreads, 0, stream, c, cols);
+    return launch_pdl(evict_kernel, dim3(c.n_seqs * c.pages.kv_heads, c.layers, parts), kEvictThreads, 0, stream, c, cols);
 }
 
 }  // namespace t2i
