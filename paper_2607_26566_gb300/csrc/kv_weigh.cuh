@@ -31,14 +31,18 @@ constexpr uint32_t kHalfSlot = 16384;  // 128 keys of 64 elements
 constexpr uint32_t kWeighUnits = 8;    // handed out at a time
 constexpr int kPartFloats = kUnitKeys;
 
-template <int N, int NS>
+// Column tiles of a sequence: one; two, whose log-sum-exps stay, like the one's, while a run is in one key head; or so many
+// that keys stay while they pass, and units are cut where runs end.
+enum class Tiles { kOne, kFew, kMany };
+
+template <int N, int NS, Tiles HOW>
 struct WeighShape {
     static constexpr uint32_t kHalf = kHalfSlot * NS;                        // a half's keys
-    static constexpr uint32_t kKeys = (N == 128 ? 3 : 6) * (NS == 1 ? 2 : 1);  // ... in the ring
-    static_assert(N == 128 || kKeys % 2 == 0, "every other entry is a loading warp's");
+    static constexpr uint32_t kKeys = (HOW == Tiles::kMany ? 3 : N > 32 ? 4 : 6) * (NS == 1 ? 2 : 1);  // ... in the ring
+    static_assert(HOW == Tiles::kMany || kKeys % 2 == 0, "every other entry is a loading warp's");
     static constexpr uint32_t kQ = N * 128 * NS;                             // a column tile
-    static constexpr uint32_t kQs = N == 128 ? (NS == 1 ? 5 : 3) : N == 32 ? 2 : 4;
-    static constexpr uint32_t kBufs = N == 128 ? 2 : 4;                      // tiles of scores of each half
+    static constexpr uint32_t kQs = HOW == Tiles::kMany ? (NS == 1 ? 5 : 3) : N == 16 || NS == 1 ? 4 : 2;
+    static constexpr uint32_t kBufs = N > 32 ? 2 : 4;                      // tiles of scores of each half
     static constexpr uint32_t kTmem = 2 * kBufs * N;
     static constexpr uint32_t kBytes = 1024 + kHalf * kKeys + kQ * kQs;
     // The warps that add up come in groups of four: one a half, or two, each with half of the columns. Then a
@@ -49,7 +53,8 @@ struct WeighShape {
     static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + 128;
     static constexpr int kRegs = 96, kSumRegs = 104, kOtherRegs = 64;
     static_assert(kGroups != 4 || kSumRegs * kSumWarps * 32 + kOtherRegs * 128 <= kRegs * kThreads, "what a block was launched with");
-    static constexpr uint32_t kFixed = 8192 + kSumWarps * kCols * 16;  // static shared memory, at most
+    static constexpr int kTiles = HOW == Tiles::kFew ? 2 : 1;  // whose log-sum-exps are held
+    static constexpr uint32_t kFixed = 8192 + kSumWarps * kCols * (8 + 8 * kTiles);  // static shared memory, at most
     static_assert(kBytes + kFixed + 1024 <= 228 * 1024, "an SM's shared memory");
     static constexpr int kChunk = kCols < 32 ? kCols : 32;  // columns that a thread works on at a time
 };
@@ -128,11 +133,11 @@ __device__ __forceinline__ int2 unit_tiles(const Weigh& f, const KvSeq& q, uint3
 constexpr int32_t kUnitCost = 6;
 __device__ __forceinline__ int32_t unit_cost(int2 tiles) { return tiles.y > tiles.x ? kUnitCost + tiles.y - tiles.x : 1; }
 
-// The cost of one head of a sequence. Of one column tile a unit costs one step; else by a warp.
-template <bool ONE>
+// The cost of one head of a sequence: its units, where none is cut; else by a warp.
+template <bool FLAT>
 __device__ __forceinline__ int64_t seq_cost(const Weigh& f, const KvSeq& q, uint32_t s, uint32_t lane) {
     const UnitList u = unit_list(f, q);
-    if (ONE) return u.n;
+    if (FLAT) return u.n;
     int64_t n = 0;
     for (int32_t i = int32_t(lane); i < u.n; i += 32) n += unit_cost(unit_tiles(f, q, s, unit_slot(u, i)));
 #pragma unroll
@@ -172,12 +177,12 @@ __global__ void __launch_bounds__(128) hull_kernel(const __grid_constant__ Weigh
     }
 }
 
-template <class T, int N, int NS, bool MOD>
-__global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
+template <class T, int N, int NS, bool MOD, Tiles HOW>
+__global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
     weigh_kernel(const __grid_constant__ Weigh f, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
-    using Sh = WeighShape<N, NS>;
+    using Sh = WeighShape<N, NS, HOW>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-    constexpr bool kOne = N != 128;  // one column tile a sequence
+    constexpr bool kFlat = HOW != Tiles::kMany;  // units are not cut
     constexpr int kChunk = Sh::kChunk;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -185,9 +190,10 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     __shared__ __align__(16) WeighShared sh;
     constexpr int kThreads = Sh::kThreads, kSumWarps = Sh::kSumWarps, kCols = Sh::kCols;
     // each adding warp's own: of its columns the log-sum-exps in units of log2, negative; spans, slopes
-    __shared__ __align__(16) float lse_of[kSumWarps][kCols];
+    constexpr int kTiles = Sh::kTiles;
+    __shared__ __align__(16) float lse_of[kSumWarps][kTiles][kCols];
     __shared__ __align__(16) int2 span_of[kSumWarps][kCols];
-    __shared__ __align__(16) float slope_of[MOD ? kSumWarps : 1][kCols];
+    __shared__ __align__(16) float slope_of[MOD ? kSumWarps : 1][kTiles][kCols];
     __shared__ __align__(16) float token_of[MOD ? N : 4];  // a column's token, counted in the tile
     static_assert(sizeof(WeighShared) + N * 4 <= 8192, "kFixed");
     const KvAttend& a = f.w.a;
@@ -218,17 +224,17 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     if (warp == kSumWarps + 1) tmem_alloc(smem_u32(&sh.tmem), Sh::kTmem);
     pdl_launch();
     pdl_wait();
-    if (!kOne && tid == 0) f.join[blockIdx.x].valid = 0;
+    if (!kFlat && tid == 0) f.join[blockIdx.x].valid = 0;
 
     // the block's run of steps: sequences by threads (by warps, where a unit may have several steps)
     const int64_t K = a.pages.kv_heads;
-    const uint32_t who = kOne ? tid : warp, all = kOne ? kThreads : kThreads / 32;
+    const uint32_t who = kFlat ? tid : warp, all = kFlat ? kThreads : kThreads / 32;
     const uint32_t per = (a.tok.n_seqs + all - 1) / all;
     int64_t mine = 0;
     for (uint32_t s = who * per; s < min(a.tok.n_seqs, (who + 1) * per); ++s)
-        mine += seq_cost<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
+        mine += seq_cost<kFlat>(f, kv_seq(a.pages, a.tok, s), s, lane);
     int64_t lo = 0, total = 0;  // the cost of a head of the sequences before, and of all
-    if (kOne) {
+    if (kFlat) {
         int64_t inc = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -254,9 +260,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
     if (busy && run0 >= lo * K && run0 < (lo + mine) * K) {
         int64_t p = lo * K;
         for (uint32_t s = who * per;; ++s) {
-            const int64_t steps = seq_cost<kOne>(f, kv_seq(a.pages, a.tok, s), s, lane);
+            const int64_t steps = seq_cost<kFlat>(f, kv_seq(a.pages, a.tok, s), s, lane);
             if (run0 < p + steps * K) {
-                if (kOne || lane == 0) sh.start_seq = int32_t(s), sh.start_rest = run0 - p, sh.start_steps = steps;
+                if (kFlat || lane == 0) sh.start_seq = int32_t(s), sh.start_rest = run0 - p, sh.start_steps = steps;
                 break;
             }
             p += steps * K;
@@ -267,21 +273,21 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
 
     if (busy && warp >= kSumWarps) {
         if (Sh::kGroups == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
-        if (warp == kSumWarps || (kOne && warp == kSumWarps + 3)) {
+        if (warp == kSumWarps || (kFlat && warp == kSumWarps + 3)) {
         // ---------------------------------------------------------- loads
         // A warp a half, each with every other entry of the ring: both walk the run, the first hands units out and loads
         // queries. (One warp for both halves issued a load of 2 KiB, as pages of 16 tokens have them, every 66 ns: a token
         // each of 64 sequences of up to 16k slots 243 us, with two 179.) Where keys stay for many column tiles one warp
         // loads both: the ring is an odd number of halves, so its entries cannot be shared out.
         const uint32_t half0 = warp == kSumWarps ? 0 : 1;
-        constexpr uint32_t kLoads = kOne ? 1 : 2;
+        constexpr uint32_t kLoads = kFlat ? 1 : 2;
         int32_t s = sh.start_seq, h = int32_t(sh.start_rest / sh.start_steps), i = 0;  // sequence, key head, unit
         int64_t at = run0, unit;  // the segment's first place, the unit's
         KvSeq q = kv_seq(a.pages, a.tok, s);
         UnitList list = unit_list(f, q);
         {
             int64_t rest = sh.start_rest % sh.start_steps;
-            if (kOne) {
+            if (kFlat) {
                 i = int32_t(rest), rest = 0;
             } else {
                 for (;; i += 32) {  // the warp looks at 32 units at a time
@@ -327,13 +333,14 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             const int2 tiles = unit_tiles(f, q, s, slot0);
             const bool dry = tiles.y <= tiles.x;
             const int32_t steps = max(1, tiles.y - tiles.x);
-            const int64_t unit0 = unit + (kOne || dry ? 0 : kUnitCost);  // its first step
+            const int64_t unit0 = unit + (kFlat || dry ? 0 : kUnitCost);  // its first step
             if (at < unit0) at = unit0;
-            const int32_t skip = int32_t(at - unit0);
-            const int32_t n = int32_t(max(int64_t(0), min(int64_t(steps - skip), run1 - at)));  // (0: a run of nothing but a unit's cost)
+            const int32_t skip = kFlat ? 0 : int32_t(at - unit0);
+            // (0: a run of nothing but a unit's cost)
+            const int32_t n = kFlat ? steps : int32_t(max(int64_t(0), min(int64_t(steps - skip), run1 - at)));
             const int32_t first = q.first, head0 = h * int32_t(a.group);
             const int32_t row = int32_t((a.pages.layer * 2 * a.pages.kv_heads + h) << shift);
-            at = unit0 + steps;  // the next unit's place
+            at = kFlat ? unit + 1 : unit0 + steps;  // the next unit's place
             more = at < run1;
 #pragma unroll
             for (uint32_t k = 0; k < kLoads; ++k) page[k] = ahead[k];
@@ -343,7 +350,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                 o.q = q, o.s = s, o.h = h, o.slot0 = slot0;
                 o.tile = tiles.x + skip, o.n = n, o.dry = dry, o.whole = n == steps, o.part = u ? 1 : 0, o.more = more;
                 mbar_arrive(bar(sh.unit_full[u % kWeighUnits]));
-                if (!kOne && u == 0) {
+                if (!kFlat && u == 0) {
                     // this run's note of a unit that began in the run before it
                     const int64_t b0 = ((unit0 + 1) * blocks - 1) / total, b1 = ((unit0 + steps) * blocks - 1) / total;
                     const bool here = skip > 0 && b0 + 1 == int64_t(blockIdx.x);
@@ -464,7 +471,6 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
         const bool cap = MOD && a.softcap != 0.0f;
         const float cap_in = cap ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
         const uint64_t k22 = pack2(k2, k2);
-        float* const lse_at = lse_of[warp];
         // the lane's columns of a tile: token and head, counted in the tile
         constexpr int kMine = kCols < 32 ? 1 : kCols / 32;
         int32_t token_at[kMine], head_at[kMine];
@@ -479,7 +485,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             pad[k] = token_at[k] >= f.per_tile;
             offset[k] = pad[k] ? 0 : uint32_t(token_at[k]) * a.q_heads + uint32_t(head_at[k]);
         }
-        constexpr bool kLean = !kOne && !MOD;
+        constexpr bool kLean = !kFlat && !MOD;
         const bool lean = f.slices == 1 && !a.spans;
         // of the tile that begins with token t0 and the head's query g0 (first: the sequence's first token)
         auto look_up = [&](int32_t first, int32_t h, int32_t m, int32_t t0, int32_t g0) {
@@ -499,7 +505,23 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
         };
         float then = 0.0f;  // ... of the next unit
         bool then_known = false;
-        int32_t had_s = -1, had_h = -1;  // whose column tile's log-sum-exps are there (of one tile a sequence)
+        // ... and what was looked up to the tile's place, with slopes and spans
+        auto put = [&](int in, int32_t first, int32_t h, int32_t m, int32_t t0, int32_t g0) {
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int32_t c = k * 32 + int32_t(lane);
+                if (kCols < 32 && c >= kCols) break;
+                lse_of[warp][in][c] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
+                if (MOD || a.spans) {
+                    const bool real = token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0;
+                    int2 span = make_int2(0, 0);
+                    if (a.spans && real) span = reinterpret_cast<const int2*>(a.spans)[first + t0 + token_at[k]];
+                    if (a.spans) span_of[warp][c] = span;
+                    if (MOD) slope_of[MOD ? warp : 0][in][c] = a.slopes && real ? a.slopes[h * a.group + g0 + head_at[k]] * kLog2e : 0.0f;
+                }
+            }
+        };
+        int32_t had_s = -1, had_h = -1;  // whose log-sum-exps are there (kFlat)
         bool known = false;              // `next` is the next tile's
         uint32_t n = 0;
         bool more = true;
@@ -516,8 +538,8 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
             const bool mine = side == 0 && slot < len && uint32_t(slot) < f.w.n_slots;
             float* const place = f.w.weights + uint32_t(s) * f.w.seq_stride + uint32_t(h) * f.w.head_stride + slot;
             float held = then;
-            if (!kOne && whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
-            if (kOne) {  // the next unit's, on their way while this one is worked on
+            if (!kFlat && whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
+            if (kFlat) {  // the next unit's, on their way while this one is worked on
                 if (!then_known) held = weight_so_far(rec);
                 then_known = false;
                 if (more) {
@@ -548,7 +570,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                     for (; i < last; ++i, ++n, t0 += f.per_tile) {
                         __syncwarp();
 #pragma unroll
-                        for (int k = 0; k < kMine; ++k) lse_at[k * 32 + lane] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
+                        for (int k = 0; k < kMine; ++k) lse_of[warp][0][k * 32 + lane] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
                         __syncwarp();
                         at += stride;
 #pragma unroll
@@ -567,7 +589,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                         uint64_t add0 = 0, add1 = 0;
 #pragma unroll
                         for (int c = 0; c < kCols; c += 4) {
-                            const float4 l = *reinterpret_cast<const float4*>(lse_at + c);
+                            const float4 l = *reinterpret_cast<const float4*>(lse_of[warp][0] + c);
                             add0 = add2(add0, pack2(exp2_approx(fmaf(x[c], k2, l.x)), exp2_approx(fmaf(x[c + 1], k2, l.y))));
                             add1 = add2(add1, pack2(exp2_approx(fmaf(x[c + 2], k2, l.z)), exp2_approx(fmaf(x[c + 3], k2, l.w))));
                         }
@@ -576,26 +598,25 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                         sum.add(y0 + y1);
                     }
                 }
-                if (!kOne || s != had_s || h != had_h) {
+                if (!kFlat) {
                     if (!known) look_up(first, h, m, t0, g0);
                     known = false;
                     __syncwarp();
-#pragma unroll
-                    for (int k = 0; k < kMine; ++k) {
-                        const int32_t c = k * 32 + int32_t(lane);
-                        if (kCols < 32 && c >= kCols) break;
-                        lse_at[c] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
-                        if (MOD || a.spans) {
-                            const bool real = token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0;
-                            int2 span = make_int2(0, 0);
-                            if (a.spans && real) span = reinterpret_cast<const int2*>(a.spans)[first + t0 + token_at[k]];
-                            if (a.spans) span_of[warp][c] = span;
-                            if (MOD) slope_of[MOD ? warp : 0][c] = a.slopes && real ? a.slopes[h * a.group + g0 + head_at[k]] * kLog2e : 0.0f;
-                        }
+                    put(0, first, h, m, t0, g0);
+                    __syncwarp();
+                } else if (s != had_s || h != had_h) {  // all tiles of another key head
+                    __syncwarp();
+                    for (int32_t t = 0; t < kTiles && t * f.per_tile < m * f.slices; ++t) {
+                        const int32_t token = f.slices > 1 ? t / f.slices : t * f.per_tile, query = f.slices > 1 ? t % f.slices * f.per_token : 0;
+                        look_up(first, h, m, token, query);
+                        put(t, first, h, m, token, query);
                     }
                     __syncwarp();
                     had_s = s, had_h = h;
                 }
+                const int in = kTiles == 1 ? 0 : tile0 + i;
+                const float* const lse_at = lse_of[warp][in];
+                const float* const slope_at = slope_of[MOD ? warp : 0][in];
                 const float ahead = float(ctx + t0 - slot);
                 const bool plain = t0 >= all0 && t0 + f.per_tile <= all1 && g0 + f.per_token <= int32_t(a.group);
                 // the thread's visible columns [v0, v1), where not all are
@@ -611,7 +632,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                 } else {
                     t0 += f.per_tile;
                 }
-                if (!kOne) {  // the next tile's, on their way while this one is worked on
+                if (!kFlat) {  // the next tile's, on their way while this one is worked on
                     if (i + 1 < steps) {
                         look_up(first, h, m, t0, g0), known = true;
                     } else if (more) {
@@ -643,7 +664,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS>::kThreads, 1)
                     for (int c = 0; c < kChunk; c += 4) {
                         const float4 l = *reinterpret_cast<const float4*>(lse_at + c0 + c);
                         if (MOD) {
-                            const float4 sl = *reinterpret_cast<const float4*>(slope_of[MOD ? warp : 0] + c0 + c);
+                            const float4 sl = *reinterpret_cast<const float4*>(slope_at + c0 + c);
                             const float4 tk = *reinterpret_cast<const float4*>(token_of + (MOD ? side * kCols + c0 + c : 0));
                             const float sls[4] = {sl.x, sl.y, sl.z, sl.w}, ls[4] = {l.x, l.y, l.z, l.w}, tks[4] = {tk.x, tk.y, tk.z, tk.w};
 #pragma unroll
@@ -735,46 +756,43 @@ constexpr uint64_t weigh_up(uint64_t n) { return (n + 255) / 256 * 256; }
 // the workspace's parts, in order: notes, parts, hulls
 uint64_t weigh_hulls(uint64_t n_seqs, uint64_t n_tokens, uint64_t per_tile) { return n_tokens / per_tile + n_seqs + 1; }
 
-template <class T, int N, int NS, bool MOD>
+template <class T, int N, int NS, bool MOD, Tiles HOW>
 cudaError_t launch_weigh_as(const Weigh& f, const CUtensorMap& map, const CUtensorMap& q_map, uint32_t sms, cudaStream_t stream) {
-    constexpr uint32_t bytes = WeighShape<N, NS>::kBytes;
+    constexpr uint32_t bytes = WeighShape<N, NS, HOW>::kBytes;
     static std::atomic<uint64_t> ready{0};  // devices whose kernel may take this much shared memory
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !(ready.load() >> dev & 1)) {
-        e = cudaFuncSetAttribute(weigh_kernel<T, N, NS, MOD>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+        e = cudaFuncSetAttribute(weigh_kernel<T, N, NS, MOD, HOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
         if (e != cudaSuccess) return e;
         if (dev < 64) ready |= uint64_t(1) << dev;
     }
     const KvAttend& a = f.w.a;
     if (a.spans && (e = launch_pdl(hull_kernel, dim3(a.tok.n_seqs), 128, 0, stream, f)) != cudaSuccess) return e;
     // no more blocks than there may be steps, going by max_len
-    const uint64_t tiles = N == 128 ? (uint64_t(a.tok.max_new) / f.per_tile + 1) * f.slices : 1;
+    const uint64_t tiles = HOW == Tiles::kMany ? (uint64_t(a.tok.max_new) / f.per_tile + 1) * f.slices : 1;
     const uint64_t steps = uint64_t(a.tok.n_seqs) * a.pages.kv_heads * (uint64_t(a.max_len) / kUnitKeys + 1);
     const uint32_t blocks = uint32_t(steps > sms / tiles ? sms : steps * tiles);
-    if ((e = launch_pdl(weigh_kernel<T, N, NS, MOD>, dim3(blocks), WeighShape<N, NS>::kThreads, bytes, stream, f, map, q_map)) != cudaSuccess) return e;
-    return N == 128 ? launch_pdl(weigh_join_kernel, dim3(blocks), kUnitKeys, 0, stream, f) : cudaSuccess;
+    if ((e = launch_pdl(weigh_kernel<T, N, NS, MOD, HOW>, dim3(blocks), WeighShape<N, NS, HOW>::kThreads, bytes, stream, f, map, q_map)) != cudaSuccess) return e;
+    return HOW == Tiles::kMany ? launch_pdl(weigh_join_kernel, dim3(blocks), kUnitKeys, 0, stream, f) : cudaSuccess;
 }
 
-template <class T, int N, int NS>
+template <class T, int N, int NS, Tiles HOW>
 cudaError_t launch_weigh_mod(const Weigh& f, const CUtensorMap& map, const CUtensorMap& q_map, uint32_t sms, cudaStream_t stream) {
-    return f.w.a.softcap != 0.0f || f.w.a.slopes ? launch_weigh_as<T, N, NS, true>(f, map, q_map, sms, stream)
-                                                 : launch_weigh_as<T, N, NS, false>(f, map, q_map, sms, stream);
+    return f.w.a.softcap != 0.0f || f.w.a.slopes ? launch_weigh_as<T, N, NS, true, HOW>(f, map, q_map, sms, stream)
+                                                 : launch_weigh_as<T, N, NS, false, HOW>(f, map, q_map, sms, stream);
 }
 
-template <class T, int N>
-cudaError_t launch_weigh_n(Weigh f, const KvLaunch& l, cudaStream_t stream) {
+template <class T, int N, Tiles HOW>
+cudaError_t launch_weigh_n(const Weigh& f, const KvLaunch& l, cudaStream_t stream) {
     const KvAttend& a = f.w.a;
-    f.per_token = int32_t(std::min<uint32_t>(a.group, N));
-    f.slices = int32_t((a.group + f.per_token - 1) / f.per_token);
-    f.per_tile = int32_t(std::min<uint32_t>(N / f.per_token, a.tok.max_new));
     CUtensorMap q_map;
     // the queries as [tokens][heads][head_dim]: a column tile's in one box (64 elements at a time)
     const cudaError_t e = l.encode_queries(a, f.per_token, f.per_tile, &q_map);
     if (e != cudaSuccess) return e;
-    return a.pages.head_dim <= 64 ? launch_weigh_mod<T, N, 1>(f, *l.map, q_map, l.sms, stream)
-                                  : launch_weigh_mod<T, N, 2>(f, *l.map, q_map, l.sms, stream);
+    return a.pages.head_dim <= 64 ? launch_weigh_mod<T, N, 1, HOW>(f, *l.map, q_map, l.sms, stream)
+                                  : launch_weigh_mod<T, N, 2, HOW>(f, *l.map, q_map, l.sms, stream);
 }
 
 template <class T>
@@ -790,8 +808,23 @@ cudaError_t launch_weigh(const KvWeigh& w, const KvLaunch& l, cudaStream_t strea
     f.hulls = reinterpret_cast<int2*>(p);
     f.fault = l.fault;
     f.no_loads = l.no_loads;
-    const uint64_t rows = uint64_t(w.a.group) * w.a.tok.max_new;
-    return rows <= 16 ? launch_weigh_n<T, 16>(f, l, stream) : rows <= 32 ? launch_weigh_n<T, 32>(f, l, stream) : launch_weigh_n<T, 128>(f, l, stream);
+    // tiles of at most 128 columns, of whole tokens (or of a share of a token's heads), equally many
+    const uint32_t most = w.a.tok.max_new, columns = std::min<uint32_t>(w.a.group, 128), tokens = 128 / columns;
+    f.per_token = int32_t(columns);
+    f.slices = int32_t((w.a.group + columns - 1) / columns);
+    const uint32_t tiles = (most + tokens - 1) / tokens;
+    f.per_tile = int32_t((most + tiles - 1) / tiles);
+    if (uint64_t(tiles) * f.slices == 1) {
+        const uint32_t rows = columns * most;
+        if (rows <= 16) return launch_weigh_n<T, 16, Tiles::kOne>(f, l, stream);
+        if (rows <= 32) return launch_weigh_n<T, 32, Tiles::kOne>(f, l, stream);
+        if (rows <= 64) return launch_weigh_n<T, 64, Tiles::kOne>(f, l, stream);
+        return launch_weigh_n<T, 128, Tiles::kOne>(f, l, stream);
+    }
+    // Two: nine observation windows over prompts of 7k tokens XX us, as if there were many XX. (Three and more are faster
+    // as many: 127 tokens of nine sequences 81 against 74 us.) Spans have one tile's place.
+    if (uint64_t(tiles) * f.slices == 2 && !w.a.spans) return launch_weigh_n<T, 128, Tiles::kFew>(f, l, stream);
+    return launch_weigh_n<T, 128, Tiles::kMany>(f, l, stream);
 }
 
 }  // namespace
