@@ -38,8 +38,13 @@ enum class Tiles { kOne, kFew, kMany };
 template <int N, int NS, Tiles HOW>
 struct WeighShape {
     static constexpr uint32_t kHalf = kHalfSlot * NS;                        // a half's keys
-    static constexpr uint32_t kKeys = (HOW == Tiles::kMany ? 3 : N > 32 ? 4 : 6) * (NS == 1 ? 2 : 1);  // ... in the ring
-    static_assert(HOW == Tiles::kMany || kKeys % 2 == 0, "every other entry is a loading warp's");
+    // ... in both halves' rings. A half has its own: with one ring the product warp of one half could wait for a phase of an
+    // entry that the other half was still two behind on.
+    static constexpr uint32_t kKeys = (HOW == Tiles::kMany ? 3 : N > 32 ? 4 : 6) * (NS == 1 ? 2 : 1);
+    static constexpr uint32_t kKeys0 = (kKeys + 1) / 2, kKeys1 = kKeys / 2;
+    // the entry of a half's n-th keys, and its phase
+    static __device__ __forceinline__ uint32_t entry(uint32_t half, uint32_t n) { return half ? kKeys0 + n % kKeys1 : n % kKeys0; }
+    static __device__ __forceinline__ uint32_t phase(uint32_t half, uint32_t n) { return (half ? n / kKeys1 : n / kKeys0) & 1; }
     static constexpr uint32_t kQ = N * 128 * NS;                             // a column tile
     static constexpr uint32_t kQs = HOW == Tiles::kMany ? (NS == 1 ? 5 : 3) : N == 16 || NS == 1 ? 4 : 2;
     static constexpr uint32_t kBufs = N > 32 ? 2 : 4;                      // tiles of scores of each half
@@ -275,10 +280,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         if (Sh::kGroups == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
         if (warp == kSumWarps || (kFlat && warp == kSumWarps + 3)) {
         // ---------------------------------------------------------- loads
-        // A warp a half, each with every other entry of the ring: both walk the run, the first hands units out and loads
-        // queries. (One warp for both halves issued a load of 2 KiB, as pages of 16 tokens have them, every 66 ns: a token
-        // each of 64 sequences of up to 16k slots 243 us, with two 179.) Where keys stay for many column tiles one warp
-        // loads both: the ring is an odd number of halves, so its entries cannot be shared out.
+        // A warp a half: both walk the run, the first hands units out and loads queries. (One warp for both halves issued a
+        // load of 2 KiB, as pages of 16 tokens have them, every 66 ns: a token each of 64 sequences of up to 16k slots 243
+        // us, with two 179.) Where keys stay for many column tiles one warp loads both.
         const uint32_t half0 = warp == kSumWarps ? 0 : 1;
         constexpr uint32_t kLoads = kFlat ? 1 : 2;
         int32_t s = sh.start_seq, h = int32_t(sh.start_rest / sh.start_steps), i = 0;  // sequence, key head, unit
@@ -315,7 +319,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         const uint32_t box = shift < 7 ? 1u << shift : 128u, boxes = 128u / box;
         const uint32_t T_mask = (1u << shift) - 1;
         const uint32_t q_bytes = uint32_t(f.per_tile * f.per_token) * 128 * NS;
-        uint32_t u = 0, kn = half0, qn = 0;
+        uint32_t u = 0, kn = 0, qn = 0;
         // A segment's pages, a lane a box: looked up while the segment before is loaded.
         int32_t page[kLoads], ahead[kLoads];
         auto pages_at = [&]() {
@@ -375,11 +379,11 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             }
             if (!dry && n) {
 #pragma unroll
-                for (uint32_t k = 0; k < kLoads; ++k, kn += 2 / kLoads) {
-                    const uint32_t slot = uint32_t(slot0) + (half0 + k) * 128 + lane * box, e = kn % Sh::kKeys;
+                for (uint32_t k = 0; k < kLoads; ++k) {
+                    const uint32_t slot = uint32_t(slot0) + (half0 + k) * 128 + lane * box, e = Sh::entry(half0 + k, kn);
                     // what the pool lacks, and what lies behind the sequence, is filled with zeros
                     const int32_t z = uint32_t(page[k]) >= a.pages.total_pages ? int32_t(a.pages.total_pages) : page[k];
-                    if (!mbar_wait(bar(sh.k_empty[e]), (kn / Sh::kKeys & 1) ^ 1, dead)) goto loads_done;
+                    if (!mbar_wait(bar(sh.k_empty[e]), Sh::phase(half0 + k, kn) ^ 1, dead)) goto loads_done;
                     if (lane == 0) mbar_expect(bar(sh.k_full[e]), Sh::kHalf);
                     __syncwarp();
                     if (lane < boxes)
@@ -387,6 +391,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
                             tma_load(ring + e * Sh::kHalf + x * kHalfSlot + lane * box * 128, &map, x * 64, row + int32_t(slot & T_mask), z,
                                      bar(sh.k_full[e]));
                 }
+                ++kn;
                 if (half0) continue;
                 for (int32_t t = tiles.x + skip; t < tiles.x + skip + n; ++t, ++qn) {
                     const uint32_t e = qn % Sh::kQs;
@@ -405,8 +410,11 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         __syncwarp();
         if (*dead) {  // the copies in flight land before the block ends
             uint32_t late = 0;
-            for (uint32_t k = kn > Sh::kKeys ? kn - Sh::kKeys : half0; k < kn; k += 2 / kLoads)
-                mbar_wait(bar(sh.k_full[k % Sh::kKeys]), k / Sh::kKeys & 1, &late);
+            for (uint32_t h = half0; h < half0 + kLoads; ++h) {
+                const uint32_t ring_of = h ? Sh::kKeys1 : Sh::kKeys0;
+                for (uint32_t k = kn > ring_of ? kn - ring_of : 0; k <= kn; ++k)  // (the last may not have been issued: a second's wait)
+                    mbar_wait(bar(sh.k_full[Sh::entry(h, k)]), Sh::phase(h, k), &late);
+            }
             for (uint32_t k = qn > Sh::kQs ? qn - Sh::kQs : 0; k < qn; ++k) mbar_wait(bar(sh.q_full[k % Sh::kQs]), k / Sh::kQs & 1, &late);
         }
     } else if (warp <= kSumWarps + 2) {
@@ -418,7 +426,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         const uint64_t kd = smem_desc(ring, 16, 1024, 2), qd = smem_desc(qs, 16, 1024, 2);
         // (One lane issues them all: what stands between two products is short.)
         bool more = lane == 0, ok = true;
-        uint32_t kn = half, qn = 0, n = 0;
+        uint32_t kn = 0, qn = 0, n = 0;
         auto products = [&](uint64_t k0, uint64_t q0, uint32_t to, auto all) {
 #pragma unroll
             for (uint32_t x = 0; x < 4 * NS; ++x) {
@@ -433,8 +441,8 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             more = o.more;
             mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
             if (!steps) continue;
-            const uint32_t ek = kn % Sh::kKeys;
-            ok = mbar_wait(bar(sh.k_full[ek]), kn / Sh::kKeys & 1, dead);
+            const uint32_t ek = Sh::entry(half, kn);
+            ok = mbar_wait(bar(sh.k_full[ek]), Sh::phase(half, kn), dead);
             const uint64_t k0 = desc_at(kd, ek * Sh::kHalf);
             for (int32_t i = 0; i < steps && ok; ++i, ++n, ++qn) {
                 const uint32_t eq = qn % Sh::kQs, buf = n % Sh::kBufs;
@@ -452,7 +460,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
                 mma_commit(bar(sh.q_empty[eq]));
             }
             if (ok) mma_commit(bar(sh.k_empty[ek]));
-            kn += 2;
+            ++kn;
         }
         __syncwarp();
         if (*dead) {  // the products in flight end before the tensor memory is freed
@@ -561,7 +569,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             if (f.slices > 1) t0 = tile0 / f.slices, g0 = (tile0 - t0 * f.slices) * f.per_token;
             t0 *= f.per_tile;
             for (int32_t i = 0; i < steps; ++i, ++n) {
-                if (kLean && known && lean && t0 >= all0) {
+                // (which way a tile goes does not depend on whether its log-sum-exps came early: sums are added up in one order)
+                if (!kFlat && !known) look_up(first, h, m, t0, g0), known = true;
+                if (kLean && lean && t0 >= all0) {
                     // Tiles that all of the warp's slots see, and the next of which is complete: nothing to decide.
                     const int32_t last = min(steps - 1, i + (all1 - t0) / f.per_tile - 1);
                     const uint64_t stride = uint64_t(uint32_t(f.per_tile)) * a.q_heads;
@@ -599,7 +609,6 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
                     }
                 }
                 if (!kFlat) {
-                    if (!known) look_up(first, h, m, t0, g0);
                     known = false;
                     __syncwarp();
                     put(0, first, h, m, t0, g0);

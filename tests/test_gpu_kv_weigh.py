@@ -283,3 +283,13 @@ def test_a_wait_that_runs_out_is_reported_and_harms_nothing(new):
     c.weigh(q, L, lse, w, **how)                                      # reported once
     total = w.double().sum()
     assert abs(float(total) - sum(new) * 8) < 1e-3 * sum(new) * 8      # every query's weights add up to 1
+
+
+@pytest.mark.parametrize("heads,kv,tokens", [(14, 2, 32), (8, 2, 32), (8, 2, 24), (4, 2, 32), (8, 2, 3), (8, 2, 160)])
+def test_many_units_to_a_block(heads, kv, tokens):
+    """Runs of many units, over key heads and sequences of one and of two column tiles, and of more; some short."""
+    new = [tokens, tokens, max(1, tokens // 3), 1, tokens] * 4
+    ctx = [2100, 700, 1500, 900, 1] * 4
+    c, lens, kvs, q = case(HF, heads, kv, 128, new, ctx, page=262144)
+    check(c, lens, new, kvs, q, decay=0.25)
+    check(c, lens, new, kvs, q, window=300, sinks=2)
