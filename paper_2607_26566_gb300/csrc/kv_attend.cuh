@@ -27,21 +27,29 @@ struct KvSpan {
     int32_t lo, hi, all_lo, all_hi, head;
 };
 // A span's key tiles: those of its head, then the others; a tile of both counts once.
-__device__ __forceinline__ int32_t head_tiles(const KvSpan& s) { return min((s.head + kTileKeys - 1) / kTileKeys, s.lo / kTileKeys); }
+__device__ __forceinline__ int32_t head_tiles(const KvSpan& s) {
+    return int32_t(min(uint32_t(s.head + kTileKeys - 1) / kTileKeys, uint32_t(s.lo) / kTileKeys));
+}
 __device__ __forceinline__ int32_t span_tiles(const KvSpan& s) {
     return max(1, head_tiles(s) + (s.hi + kTileKeys - 1) / kTileKeys - s.lo / kTileKeys);
 }
-// the first slot of tile i
+// the first slot of tile i (SINKS: there may be a head)
+template <bool SINKS>
 __device__ __forceinline__ int32_t tile_slot(const KvSpan& s, int32_t i) {
+    if (!SINKS || s.head == 0) return (int32_t(uint32_t(s.lo) / kTileKeys) + i) * kTileKeys;
     const int32_t h = head_tiles(s);
-    return (i < h ? i : s.lo / kTileKeys + i - h) * kTileKeys;
+    return (i < h ? i : int32_t(uint32_t(s.lo) / kTileKeys) + i - h) * kTileKeys;
 }
 // whether some token does not see some key of the tile
+template <bool SINKS>
 __device__ __forceinline__ bool tile_masked(const KvAttend& a, const KvSpan& s, int32_t slot0) {
-    return (slot0 < s.all_lo && slot0 + kTileKeys > int32_t(a.sinks)) || slot0 + kTileKeys > s.all_hi;
+    return (slot0 < s.all_lo && (!SINKS || slot0 + kTileKeys > int32_t(a.sinks))) || slot0 + kTileKeys > s.all_hi;
 }
 // a slot that no token sees
-__device__ __forceinline__ bool unseen(const KvSpan& s, int32_t slot) { return (slot < s.lo && slot >= s.head) || slot >= s.hi; }
+template <bool SINKS>
+__device__ __forceinline__ bool unseen(const KvSpan& s, int32_t slot) {
+    return (slot < s.lo && (!SINKS || slot >= s.head)) || slot >= s.hi;
+}
 __device__ __forceinline__ void add_sinks(const KvAttend& a, KvSpan& s) {
     const int32_t n = int32_t(a.sinks);
     if (n >= s.lo) s.lo = 0;

@@ -302,10 +302,12 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
             const int32_t row_v = row_k + int32_t(a.pages.kv_heads << shift);
             const int32_t* table = a.pages.table + w.s * a.pages.table_stride;
             for (int32_t i = 0; i < w.n; ++i) {
-                const uint32_t slot = uint32_t(tile_slot(w.span, w.tile + i)) + lane * box;
+                const uint32_t slot = uint32_t(tile_slot<true>(w.span, w.tile + i)) + lane * box;
                 int32_t page = -1;
-                if (lane < boxes && slot < uint32_t(w.q.len)) page = table[slot >> shift];
-                // what the pool lacks, and what lies behind the sequence, is filled with zeros
+                // (pages of a tile that no token sees are not read: most of the sinks' tile, and what lies before a window)
+                const bool seen = int32_t(slot) < w.span.hi && (int32_t(slot + box) > w.span.lo || int32_t(slot) < w.span.head);
+                if (lane < boxes && seen) page = table[slot >> shift];
+                // what the pool lacks, and what no token sees, is filled with zeros
                 const bool none = uint32_t(page) >= a.pages.total_pages;
                 const int32_t z = none ? int32_t(a.pages.total_pages) : page;
                 const int32_t y = int32_t(slot & T_mask);
@@ -436,8 +438,8 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 for (int c = 0; c < N; ++c) sum[c] = 0.0f;
             };
             for (int32_t i = 0; i < w.n; ++i, ++n) {
-                const int32_t slot0 = tile_slot(w.span, w.tile + i), key = slot0 + int32_t(tid);
-                const bool masked = tile_masked(a, w.span, slot0);
+                const int32_t slot0 = tile_slot<true>(w.span, w.tile + i), key = slot0 + int32_t(tid);
+                const bool masked = tile_masked<true>(a, w.span, slot0);
                 // a drafted key's bit and position
                 uint64_t bit = 0;
                 int32_t kpos = key;
@@ -546,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, Shape<N, NS>::kBlocks) few_kernel(co
                 if (slot0 < w.span.lo || slot0 + kTileKeys > w.span.hi) {
                     const uint32_t e = (2 * n + 1) % Sh::kEntries;
                     mbar_wait(bar(sh.full[e]), (2 * n + 1) / Sh::kEntries & 1, dead);
-                    if (unseen(w.span, key)) {
+                    if (unseen<true>(w.span, key)) {
 #pragma unroll 1
                         for (int k = 0; k < NS * 8; ++k)
                             *reinterpret_cast<uint4*>(mem + e * Sh::kEntry + k / 8 * kSlot + tid * 128 + k % 8 * 16) =
