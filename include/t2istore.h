@@ -560,7 +560,7 @@ typedef struct t2i_kv_weigh_desc {
     const float* lse;       /* device, [n_tokens][q_heads]: t2i_kv_attend's of
                                the same queries, masks and score options     */
     float* weights;         /* device, [n_seqs][kv_heads][n_slots]           */
-    uint64_t q_stride;
+    uint64_t q_stride;      /* of several tokens q_heads * head_dim or more  */
     uint64_t seq_stride;    /* elements of weights from sequence to sequence, */
     uint64_t head_stride;   /* and from head to head: rows do not overlap    */
     const float* slopes;    /* these as in t2i_kv_attend_desc                */
@@ -583,7 +583,7 @@ typedef struct t2i_kv_weigh_desc {
  * t2i_kv_attend, without a tree). Slots before the new tokens: weights =
  * decay * weights + sum (decay 0: the sum; weights so far may be anything).
  * Slots of the new tokens: the sum. Others are left as they are. A query
- * whose lse is -infinity counts nothing. Keys may hold anything where no
+ * whose lse is -infinity (and whose q is finite) counts nothing. Keys may hold anything where no
  * token sees them. Sums are fp32, in an order that does not depend on timing. */
 t2i_status t2i_kv_weigh(t2i_kv* kv, const t2i_kv_weigh_desc* desc, void* cuda_stream);
 
@@ -617,7 +617,8 @@ typedef struct t2i_kv_select_desc {
  * and of the others the n - a - b of largest weight, of equals the first. (0
  * and -0 are equal; NaN is below every number.) kept receives them, ascending;
  * what lies behind n in kept and weights_out is left as it is. A sequence whose
- * lens is negative or above n_slots has no slots.                           */
+ * lens is negative or above n_slots has no slots. No output shares a byte
+ * with another array, but weights_out with weights.                         */
 t2i_status t2i_kv_select(t2i_kv* kv, const t2i_kv_select_desc* desc, void* cuda_stream);
 
 typedef struct t2i_kv_evict_desc {
@@ -638,7 +639,7 @@ typedef struct t2i_kv_evict_desc {
 /* Moves the rows of keys and values of slot kept[i] to slot i, i < counts[s],
  * for each key head of the layers. Rows behind are left as they are. An entry
  * below its place i moves nothing; of a list that does not ascend the rows
- * are not specified.                                                        */
+ * are not specified, nor those of pages that two sequences of a call share.  */
 t2i_status t2i_kv_evict(t2i_kv* kv, const t2i_kv_evict_desc* desc, void* cuda_stream);
 
 /* =========================================================================

@@ -366,8 +366,9 @@ t2i_status weigh(t2i_kv* kv, const t2i_kv_weigh_desc& d, cudaStream_t stream) {
     const uint64_t need = kv_weigh_workspace(kv->sms, seqs, d.batch.n_tokens);
     c.require(d.workspace_bytes >= need, "the workspace is smaller than t2i_kv_weigh_workspace_bytes");
     c.range("workspace", d.workspace, need, 256);
-    // (a tensor map's strides are below 2^40 bytes)
-    c.require(n == 1 || d.q_stride < (uint64_t(1) << 39), "q: the stride is too large");
+    // (queries come by a tensor map: its strides are below 2^40 bytes, and rows lie apart)
+    c.require(n == 1 || (d.q_stride < (uint64_t(1) << 39) && d.q_stride >= uint64_t(d.q_heads) * kv->layout.head_dim),
+              "q: the stride must be at least a token's heads, and below 2^39");
     if (!c.ok()) return T2I_ERR_INVALID;
     c.require(!overlap(d.weights, bytes, d.lse, n * d.q_heads * 4) &&
                   !overlap(d.weights, bytes, d.q, c.token_bytes(n, d.q_heads, d.q_stride, 2)), "weights overlap q or lse");
@@ -413,6 +414,10 @@ t2i_status select(t2i_kv* kv, const t2i_kv_select_desc& d, cudaStream_t stream) 
     c.range("lens", d.lens, uint64_t(d.n_seqs) * 4, 4);
     if (d.keeps) c.range("keeps", d.keeps, uint64_t(d.n_seqs) * 4, 4);
     c.range("counts", d.counts, uint64_t(d.n_seqs) * 4, 4);
+    const uint64_t per_seq = uint64_t(d.n_seqs) * 4;
+    auto apart = [&](const char* name, const void* p, uint64_t bytes) {
+        if (c.ok() && (overlap(p, bytes, d.lens, per_seq) || (d.keeps && overlap(p, bytes, d.keeps, per_seq)))) c.fail(name, "overlaps lens or keeps");
+    };
     if (width) {
         rows_apart(c, "the rows of kept overlap (their strides are too small)", d.n_seqs, d.n_heads, width, d.kept_seq_stride, d.kept_head_stride);
         const uint64_t kept = rows_bytes(d.n_seqs, d.n_heads, width, d.kept_seq_stride, d.kept_head_stride);
@@ -426,8 +431,14 @@ t2i_status select(t2i_kv* kv, const t2i_kv_select_desc& d, cudaStream_t stream) 
             c.range("weights_out", d.weights_out, out, 4);
             c.require(in_place || !overlap(d.weights_out, out, d.weights, in), "weights_out overlaps weights without being them");
             c.require(!overlap(d.weights_out, out, d.kept, kept), "weights_out overlaps kept");
+            apart("weights_out", d.weights_out, out);
         }
+        apart("kept", d.kept, kept);
+        c.require(!overlap(d.kept, kept, d.counts, per_seq), "kept overlaps counts");
     }
+    // (a block of one head may write a sequence's count before another's reads its length)
+    apart("counts", d.counts, per_seq);
+    if (d.n_slots) c.require(!overlap(d.counts, per_seq, d.weights, in), "counts overlap weights");
     if (!c.ok()) return T2I_ERR_INVALID;
     KvSelect k{};
     k.weights = d.weights, k.weights_out = width ? d.weights_out : nullptr;

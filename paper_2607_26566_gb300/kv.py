@@ -293,7 +293,7 @@ class KVCache:
 
         For a slot, the sum of exp(score - lse) over the new tokens that see it
         and the heads that share its key head; ``q``, ``lse`` and the options
-        are those of the :meth:`attend` before it. A slot that was there before
+        are those of the :meth:`attend` before it (``q``'s tokens lie apart). A slot that was there before
         has ``decay`` times what it had added (0: nothing, whatever that was);
         the new tokens' slots start with their sum, slots behind them are left as
         they are. The last tokens of a prompt alone, as new tokens, give what an
@@ -315,10 +315,11 @@ class KVCache:
         Returns ``kept``, int32 [sequences, heads, ...], the slots in ascending
         order (what lies behind their number is left as it is), and ``counts``,
         int32 [sequences], their number: the new ``lens``."""
-        if kept is None or counts is None:
+        if (kept is None or counts is None) and torch.is_tensor(weights) and weights.dim() == 3:  # (others are refused below)
             with torch.cuda.stream(self._stream(stream)):
                 if kept is None:
-                    kept = torch.empty((*weights.shape[:2], min(int(keep), weights.shape[2])), dtype=torch.int32, device=self.device)
+                    kept = torch.empty((*weights.shape[:2], max(0, min(int(keep), weights.shape[2]))), dtype=torch.int32,
+                                       device=self.device)
                 if counts is None:
                     counts = torch.empty(weights.shape[0], dtype=torch.int32, device=self.device)
         st = _kv.select(self._c, weights, lens, keep, keeps, kept, counts, weights_out, recent, sinks, max_len, stream)

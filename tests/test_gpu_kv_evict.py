@@ -215,6 +215,9 @@ def test_refusals(any_cache):
     no(TypeError, "dtype", c.select, w.half(), L, 5)
     no(TypeError, "dtype", c.select, w, L, 5, kept=kept.long())
     no(ValueError, "weights", c.select, w[0], L, 5, kept=kept, counts=counts)
+    no(ValueError, "weights", c.select, w[0], L, 5)
+    no(TypeError, "weights", c.select, None, L, 5)
+    no(ValueError, "keep", c.select, w, L, -1)
     no(ValueError, "lens", c.select, w, L[:1], 5)
     no(ValueError, "kept", c.select, w, L, 6, kept=kept)
     no(ValueError, "kept", c.select, w, L, 5, kept=kept[:, :1])
@@ -226,6 +229,12 @@ def test_refusals(any_cache):
     no(T2IError, "overlap", c.select, w, L, 5, kept=kept[:1].expand(2, -1, -1))
     no(T2IError, "overlap", c.select, w[:1].expand(2, -1, -1), L, 5, weights_out=w[:1].expand(2, -1, -1))
     no(T2IError, "overlap", c.select, w, L, 5, kept=w.view(torch.int32)[..., :5])
+    no(T2IError, "counts.*overlaps lens", c.select, w, L, 5, counts=L)          # (lens would change while it is read)
+    no(T2IError, "counts.*overlaps lens", c.select, w, L, 5, keeps=counts, counts=counts)
+    no(T2IError, "overlap", c.select, w, L, 5, counts=kept[0, 0, :2], kept=kept)
+    no(T2IError, "overlap", c.select, w, L, 5, counts=w.view(torch.int32)[0, 0, :2])
+    both = torch.zeros(22, dtype=torch.int32, device=DEV)
+    no(T2IError, "kept.*overlaps lens", c.select, w, both[:2], 5, kept=both[:20].view(2, 2, 5))
     assert c.select(w[:0], L[:0], 5)[0].shape == (0, 2, 5)
     no(TypeError, "counts", c.evict, kept[:1], None)
     no(TypeError, "dtype", c.evict, kept[:1].long(), counts[:1])

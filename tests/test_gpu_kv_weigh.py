@@ -254,6 +254,8 @@ def test_of_a_gradient_and_other_refusals():
     no(T2IError, "spans", q, L, lse, w, spans=torch.zeros(2, 2, dtype=torch.int32, device=DEV), sinks=3)
     no(T2IError, "max_new", q, L, lse, w, starts=ints([0, 1, 2]))
     no(ValueError, "sinks", q, L, lse, w, sinks=-1)
+    no(T2IError, "q: the stride", q[:1].expand(2, -1, -1), L, lse, w)
+    no(T2IError, "q: the stride", torch.as_strided(q, (2, 4, 64), (128, 64, 1)), L, lse, w)
     assert c.weigh(q[:0], L[:0], lse[:0], w[:0]).shape == (0, 2, 20)      # nothing to do
     c.close()
     no2 = pytest.raises(ValueError, match="closed")
@@ -293,3 +295,36 @@ def test_many_units_to_a_block(heads, kv, tokens):
     c, lens, kvs, q = case(HF, heads, kv, 128, new, ctx, page=262144)
     check(c, lens, new, kvs, q, decay=0.25)
     check(c, lens, new, kvs, q, window=300, sinks=2)
+
+
+@pytest.mark.parametrize("stride", [4 * 64 + 8, 4 * 64 + 24, 5 * 64, 4 * 64])
+@pytest.mark.parametrize("new", [[1, 1], [20, 3], [150, 40]])
+def test_strides_between_tokens(stride, new):
+    c, lens, kvs, q = case(BF, 4, 2, 64, new, [300, 70])
+    n = sum(new)
+    wide = torch.full((n * stride,), math.nan, dtype=BF, device=DEV)
+    view = torch.as_strided(wide, (n, 4, 64), (stride, 64, 1))
+    view.copy_(q)
+    lse = sums(new, kvs, q, 64)
+    w = torch.zeros(2, 2, max(lens), device=DEV)
+    c.weigh(view, ints(lens), lse.to(DEV), w, starts=starts_of(new), max_new=max(new))
+    want = torch.zeros_like(w)
+    c.weigh(q.to(DEV), ints(lens), lse.to(DEV), want, starts=starts_of(new), max_new=max(new))
+    assert torch.equal(w, want) and float(w.sum()) > n * 3.9
+
+
+@pytest.mark.parametrize("new,most", [([7, 3], 4), ([200, 90], 60)])
+def test_tokens_beyond_max_new_are_not_counted(new, most):
+    """As they are not attended; their slots are new ones all the same."""
+    c, lens, kvs, q = case(BF, 8, 2, 64, new, [100, 40])
+    lse = sums(new, kvs, q, 64)
+    held = torch.rand(2, 2, max(lens) + PAD, generator=gen(2))
+    w = held.clone().to(DEV)
+    c.weigh(q.to(DEV), ints(lens), lse.to(DEV), w, starts=starts_of(new), max_new=most)
+    at = 0
+    for s, (m, L) in enumerate(zip(new, lens)):
+        some = lse[at:at + m].clone()
+        some[most:] = -math.inf
+        want, off = weigh64(q[at:at + m], kvs[s][0], some, 0.125)
+        near_weights(w[s, :, :L].cpu(), held[s, :, :L], want, off, L - m, 1.0)
+        at += m
