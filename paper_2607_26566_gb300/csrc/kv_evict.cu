@@ -18,7 +18,10 @@ namespace cg = cooperative_groups;
 // these bits; then one pass in the order of slots writes those above it and the first ones equal to it. Counts are
 // integers, so their order does not matter. A cluster of blocks shares a row and adds up the counts of all of them. A
 // warp has a stretch of its block's slots, I to a lane, in registers, so that weights are read once; a row that is longer
-// than its caller said, or than a cluster holds, is read from memory in each pass.
+// than its caller said, or than a cluster holds (131,072), is read from memory in each pass.
+// Bound by instructions: some 75 for each 32 weights (order, counts, votes, places) and 500 a warp beside them. Measured: 64
+// x 8 rows of up to 16k slots to 4k 32-33 us, 8 rows of 131k to 8k 21 us, 8 of 1,100 6.4 us. In shared memory in place of
+// registers the first took 57 us, in blocks of 512 threads 35.
 constexpr uint32_t kSelThreads = 1024;
 constexpr uint32_t kSelWarps = kSelThreads / 32;
 constexpr uint32_t kBins = 2048;
@@ -361,7 +364,7 @@ cudaError_t launch_select(const KvSelect& c, uint32_t blocks, cudaStream_t strea
 
 cudaError_t launch_kv_select(const KvSelect& c, uint32_t sms, cudaStream_t stream) {
     const uint64_t rows = uint64_t(c.n_seqs) * c.n_heads;
-    // blocks to a row: what holds it, and more while SMs are idle and a block has two weights a thread and more
+    // blocks to a row: what holds it, and more while SMs are idle and a thread has more than two weights
     uint32_t blocks = 1;
     while (blocks < kMostBlocks && (c.max_len / blocks > 16 * kSelThreads || (c.max_len / blocks > 2 * kSelThreads && rows * blocks * 2 <= sms))) blocks *= 2;
     const uint32_t each = (c.max_len + blocks * kSelThreads - 1) / (blocks * kSelThreads);

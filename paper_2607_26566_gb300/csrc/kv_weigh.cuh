@@ -6,12 +6,21 @@
 // nothing goes from thread to thread. A unit is 256 keys of one key head in two halves, one to each half of the softmax
 // warps: its keys are loaded once (TMA), its queries, 128 columns at a time, once for both halves.
 //
-// Two regimes. A decoding step (N = 16 or 32: all queries of a key head are one column tile) is bound by reading the
-// keys: each block streams them through a deep ring. A prompt (N = 128) is bound by an exponential a score beside the
-// product; keys stay while column tiles pass.
+// Two regimes. Where all queries of a key head are one column tile or two (a decoding step, an observation window) the
+// call is bound by reading the keys: each block streams them through a ring. Of more (a prompt) it is bound by the sums
+// beside the products, an exponential a score; keys stay while column tiles pass.
 //
 // Work split: the column tiles (steps) of all units, in order, are cut into equal runs, one to an SM. A unit that lies in
-// several runs is joined by a second kernel, in the order of the runs: results do not depend on timing.
+// several runs is joined by a second kernel, in the order of the runs; with one or two tiles units are not cut. Results do
+// not depend on timing.
+//
+// Accuracy: products are exact, sums fp32 (what a thread adds up over tiles keeps what its additions lose). The argument of
+// the exponential, score - lse in units of log2, is rounded once in fp32 from a scale that is rounded too: 2e-6 of a
+// weight whose score and lse are 30, 3e-7 of a prompt's sums.
+//
+// Measured, 32 heads over 8 of 128: one token over 700 slots 5.7 us; a token each of 64 sequences of up to 16k slots (1.16
+// GB) 178 us, 6.5 TB/s; a prompt of 8190 tokens 257-268 us, 1.03-1.07 PFLOP/s of what is visible, where the products alone
+// (no sums) took 192; 32 tokens of nine prompts of up to 7k, 28 heads over 4, 24-25 us.
 #pragma once
 
 #include <algorithm>
@@ -830,8 +839,8 @@ cudaError_t launch_weigh(const KvWeigh& w, const KvLaunch& l, cudaStream_t strea
         if (rows <= 64) return launch_weigh_n<T, 64, Tiles::kOne>(f, l, stream);
         return launch_weigh_n<T, 128, Tiles::kOne>(f, l, stream);
     }
-    // Two: nine observation windows over prompts of 7k tokens XX us, as if there were many XX. (Three and more are faster
-    // as many: 127 tokens of nine sequences 81 against 74 us.) Spans have one tile's place.
+    // Two: 32 tokens of nine prompts of up to 7k slots 24 us, as if there were many 33; of one of 3k 10 against 15. (Three
+    // are slower so, 81 against 74 us, but over short contexts.) There is room for one tile's spans.
     if (uint64_t(tiles) * f.slices == 2 && !w.a.spans) return launch_weigh_n<T, 128, Tiles::kFew>(f, l, stream);
     return launch_weigh_n<T, 128, Tiles::kMany>(f, l, stream);
 }
