@@ -68,6 +68,10 @@ int page_token_shift(uint64_t page_bytes, const t2i_kv_layout& l) {
     return s >= 0 && (1u << s) >= kMinPageTokens ? s : -1;
 }
 
+// Bytes that strides of up to 2^40 span, counted in full: 2^62 for all that is more, which no allocation holds.
+using Wide = unsigned __int128;
+uint64_t at_most(Wide bytes) { return bytes >> 62 ? uint64_t(1) << 62 : uint64_t(bytes); }
+
 // One call's checks. A check that fails sets the store's error; the ones after
 // it do nothing.
 class Checks {
@@ -85,7 +89,7 @@ class Checks {
     }
     // [n][heads][head_dim] elements with a stride between tokens
     uint64_t token_bytes(uint64_t n, uint32_t heads, uint64_t stride, uint32_t elem) const {
-        return ((n - 1) * stride + uint64_t(heads) * kv_->layout.head_dim) * elem;
+        return at_most((Wide(n - 1) * stride + uint64_t(heads) * kv_->layout.head_dim) * elem);
     }
     void tokens(const char* name, const void* p, uint64_t n, uint32_t heads, uint64_t stride, uint32_t elem, bool written) {
         if (!ok_) return;
@@ -97,7 +101,7 @@ class Checks {
     void table(const int32_t* t, uint64_t stride, uint32_t pages, uint32_t n_seqs) {
         require(pages > 0 && stride >= pages && stride <= kMaxStride, "table_stride must be at least table_pages, which is positive");
         require(pages <= (kMaxSlots >> kv_->token_shift), "a table row must hold at most 2^31 - 256 tokens");
-        if (ok_) range("table", t, ((n_seqs - 1) * stride + pages) * 4, 4);
+        if (ok_) range("table", t, at_most((Wide(n_seqs - 1) * stride + pages) * 4), 4);
     }
     // the batch; false (and ok()) where there is nothing to do
     bool batch(const t2i_kv_batch& b) {
@@ -331,11 +335,8 @@ void rows_apart(Checks& c, const char* what, uint32_t n_seqs, uint32_t n_heads, 
     c.require((n_heads == 1 || (head_stride >= width && head_stride <= kMaxStride)) &&
                   (n_seqs == 1 || (seq_stride >= (n_heads - 1) * head_stride + width && seq_stride <= kMaxStride)), what);
 }
-// (2^62 for all that is more, which no allocation holds)
 uint64_t rows_bytes(uint32_t n_seqs, uint32_t n_heads, uint64_t width, uint64_t seq_stride, uint64_t head_stride) {
-    using Wide = unsigned __int128;
-    const Wide n = (Wide(n_seqs - 1) * seq_stride + Wide(n_heads - 1) * head_stride + width) * 4, most = Wide(1) << 62;
-    return uint64_t(n < most ? n : most);
+    return at_most((Wide(n_seqs - 1) * seq_stride + Wide(n_heads - 1) * head_stride + width) * 4);
 }
 
 t2i_status weigh(t2i_kv* kv, const t2i_kv_weigh_desc& d, cudaStream_t stream) {

@@ -1,5 +1,6 @@
 """Accumulated attention over the cache (marked gpu), against a plain form in 64 bits, at the sizes, masks and places
 where it can go wrong. Every byte of a pool that holds no row of the case is NaN."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -328,3 +329,36 @@ def test_tokens_beyond_max_new_are_not_counted(new, most):
         want, off = weigh64(q[at:at + m], kvs[s][0], some, 0.125)
         near_weights(w[s, :, :L].cpu(), held[s, :, :L], want, off, L - m, 1.0)
         at += m
+
+
+class WeighDesc(C.Structure):
+    """t2i_kv_weigh_desc, its batch first."""
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_uint64), ("lens", C.c_void_p), ("starts", C.c_void_p),
+                *[(n, C.c_uint32) for n in ("table_pages", "n_seqs", "n_tokens", "max_new", "layer", "reserved")],
+                *[(n, C.c_void_p) for n in ("q", "lse", "weights")],
+                *[(n, C.c_uint64) for n in ("q_stride", "seq_stride", "head_stride")],
+                ("slopes", C.c_void_p), ("spans", C.c_void_p),
+                *[(n, C.c_uint32) for n in ("q_heads", "n_slots", "window", "sinks", "max_len")],
+                *[(n, C.c_float) for n in ("scale", "softcap", "decay")],
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+def test_strides_whose_bytes_pass_64_bits_are_refused(lib):
+    """From C: (tokens - 1) * stride * 2 bytes, or a table's, are a multiple of 2^64. Nothing is launched."""
+    c, lens, _, q = case(BF, 1, 1, 64, [1], [20])
+    n = (1 << 25) + 1
+    q, L = q.to(DEV), ints(lens)
+    lse, w = torch.zeros(n, 1, device=DEV), torch.zeros(1, 1, 64, device=DEV)
+    room = torch.zeros(1 << 30, dtype=torch.uint8, device=DEV)
+    d = WeighDesc(table=c.table.data_ptr(), table_stride=c.max_pages, lens=L.data_ptr(), table_pages=c.max_pages, n_seqs=1, n_tokens=n,
+                  q=q.data_ptr(), lse=lse.data_ptr(), weights=w.data_ptr(), q_stride=1 << 38, seq_stride=64, head_stride=64, q_heads=1,
+                  n_slots=64, scale=0.125, decay=1.0, workspace=room.data_ptr(), workspace_bytes=room.numel())
+    before = c.store.stats()["launches"]
+    assert lib.t2i_kv_weigh(c._h, C.byref(d), None) == 1 and "q:" in c.store.last_error()
+    many = 1 << 24
+    lens_of = torch.zeros(many + 1, dtype=torch.int32, device=DEV)
+    d.n_tokens = d.n_seqs = many + 1
+    d.lens, d.table_stride, d.q_stride = lens_of.data_ptr(), 1 << 38, 64
+    assert lib.t2i_kv_weigh(c._h, C.byref(d), None) == 1 and "table" in c.store.last_error()
+    torch.cuda.synchronize()
+    assert c.store.stats()["launches"] == before
