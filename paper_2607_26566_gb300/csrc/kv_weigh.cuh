@@ -57,18 +57,20 @@ struct WeighShape {
     static constexpr uint32_t kQ = N * 128 * NS;                             // a column tile
     static constexpr uint32_t kQs = HOW == Tiles::kMany ? (NS == 1 ? 5 : 3) : N == 16 || NS == 1 ? 4 : 2;
     static constexpr uint32_t kBufs = N > 32 ? 2 : 4;                      // tiles of scores of each half
+    static_assert(N != 128 || kBufs == 2, "a place for each group's scores");
     static constexpr uint32_t kTmem = 2 * kBufs * N;
     static constexpr uint32_t kBytes = 1024 + kHalf * kKeys + kQ * kQs;
-    // The warps that add up come in groups of four: one a half, or two, each with half of the columns. Then a
+    // The warps that add up come in groups of four: one a half, or two, which take tiles (of one tile: units) in turn. Then a
     // loading warp and a product warp for each half (one's products run while the other waits; N = 128 has one loading warp, and
     // one that idles).
     static constexpr int kGroups = N == 128 ? 4 : 2;
-    static constexpr int kCols = 2 * N / kGroups;  // of a group
+    static constexpr int kCols = N;
+    static constexpr int kSpanCols = N < 64 ? N : 64;  // whose spans are held at a time
     static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + 128;
     static constexpr int kRegs = 96, kSumRegs = 104, kOtherRegs = 64;
     static_assert(kGroups != 4 || kSumRegs * kSumWarps * 32 + kOtherRegs * 128 <= kRegs * kThreads, "what a block was launched with");
-    static constexpr int kTiles = HOW == Tiles::kFew ? 2 : 1;  // whose log-sum-exps are held
-    static constexpr uint32_t kFixed = 8192 + kSumWarps * kCols * (8 + 8 * kTiles);  // static shared memory, at most
+    static constexpr int kTiles = 1;
+    static constexpr uint32_t kFixed = 8192 + kSumWarps * (kCols * 8 * kTiles + kSpanCols * 8);  // static shared memory, at most
     static_assert(kBytes + kFixed + 1024 <= 228 * 1024, "an SM's shared memory");
     static constexpr int kChunk = kCols < 32 ? kCols : 32;  // columns that a thread works on at a time
 };
@@ -163,7 +165,7 @@ struct WeighShared {
     uint64_t k_full[12], k_empty[12], q_full[5], q_empty[5];
     uint64_t s_full[2][4], s_empty[2][4];
     uint64_t sum_full[2][2], sum_empty[2][2];  // [half][parity of the unit]
-    float sum[2][2][128];  // of the groups with the second half of the columns
+    float sum[2][2][128];  // of the groups with the odd tiles
     uint64_t unit_full[kWeighUnits], unit_empty[kWeighUnits];
     WeighUnit unit[kWeighUnits];
     uint32_t tmem, dead;
@@ -204,10 +206,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
     __shared__ __align__(16) WeighShared sh;
     constexpr int kThreads = Sh::kThreads, kSumWarps = Sh::kSumWarps, kCols = Sh::kCols;
     // each adding warp's own: of its columns the log-sum-exps in units of log2, negative; spans, slopes
-    constexpr int kTiles = Sh::kTiles;
-    __shared__ __align__(16) float lse_of[kSumWarps][kTiles][kCols];
-    __shared__ __align__(16) int2 span_of[kSumWarps][kCols];
-    __shared__ __align__(16) float slope_of[MOD ? kSumWarps : 1][kTiles][kCols];
+    __shared__ __align__(16) float lse_of[kSumWarps][kCols];
+    __shared__ __align__(16) int2 span_of[kSumWarps][Sh::kSpanCols];
+    __shared__ __align__(16) float slope_of[MOD ? kSumWarps : 1][kCols];
     __shared__ __align__(16) float token_of[MOD ? N : 4];  // a column's token, counted in the tile
     static_assert(sizeof(WeighShared) + N * 4 <= 8192, "kFixed");
     const KvAttend& a = f.w.a;
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         for (uint32_t i = 0; i < Sh::kKeys; ++i) mbar_init(bar(sh.k_full[i]), 1), mbar_init(bar(sh.k_empty[i]), 1);
         for (uint32_t i = 0; i < Sh::kQs; ++i) mbar_init(bar(sh.q_full[i]), 1), mbar_init(bar(sh.q_empty[i]), 2);
         for (uint32_t i = 0; i < Sh::kBufs; ++i)
-            for (int h = 0; h < 2; ++h) mbar_init(bar(sh.s_full[h][i]), 1), mbar_init(bar(sh.s_empty[h][i]), 2 * Sh::kGroups);
+            for (int h = 0; h < 2; ++h) mbar_init(bar(sh.s_full[h][i]), 1), mbar_init(bar(sh.s_empty[h][i]), 4);
         for (uint32_t i = 0; i < kWeighUnits; ++i) mbar_init(bar(sh.unit_full[i]), 1), mbar_init(bar(sh.unit_empty[i]), kSumWarps + 2);
         for (int h = 0; h < 2; ++h)
             for (int i = 0; i < 2; ++i) mbar_init(bar(sh.sum_full[h][i]), 4), mbar_init(bar(sh.sum_empty[h][i]), 4);
@@ -435,7 +436,9 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         const uint64_t kd = smem_desc(ring, 16, 1024, 2), qd = smem_desc(qs, 16, 1024, 2);
         // (One lane issues them all: what stands between two products is short.)
         bool more = lane == 0, ok = true;
-        uint32_t kn = 0, qn = 0, n = 0;
+        // (Where two groups of warps take turns, each has one of the two places for scores, whatever tiles a unit begins and
+        // ends with: a wait names one of two phases, so nobody may wait at a place whose other phase is another's.)
+        uint32_t kn = 0, qn = 0, n = 0, taken[2] = {0, 0};
         auto products = [&](uint64_t k0, uint64_t q0, uint32_t to, auto all) {
 #pragma unroll
             for (uint32_t x = 0; x < 4 * NS; ++x) {
@@ -446,7 +449,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         for (uint32_t u = 0; more && ok; ++u) {
             if (!mbar_wait(bar(sh.unit_full[u % kWeighUnits]), u / kWeighUnits & 1, dead)) break;
             const WeighUnit& o = sh.unit[u % kWeighUnits];
-            const int32_t steps = o.dry ? 0 : o.n;
+            const int32_t steps = o.dry ? 0 : o.n, tile0 = o.tile;
             more = o.more;
             mbar_arrive(bar(sh.unit_empty[u % kWeighUnits]));
             if (!steps) continue;
@@ -454,8 +457,12 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             ok = mbar_wait(bar(sh.k_full[ek]), Sh::phase(half, kn), dead);
             const uint64_t k0 = desc_at(kd, ek * Sh::kHalf);
             for (int32_t i = 0; i < steps && ok; ++i, ++n, ++qn) {
-                const uint32_t eq = qn % Sh::kQs, buf = n % Sh::kBufs;
-                ok = mbar_wait(bar(sh.s_empty[half][buf]), (n / Sh::kBufs & 1) ^ 1, dead) &&
+                const uint32_t turn = HOW == Tiles::kOne ? u & 1 : uint32_t(tile0 + i) & 1;
+                const uint32_t eq = qn % Sh::kQs, buf = Sh::kGroups == 4 ? turn : n % Sh::kBufs;
+                const uint32_t phase = Sh::kGroups == 4 ? (turn ? taken[1] : taken[0]) & 1 : n / Sh::kBufs & 1;
+                if (turn) ++taken[1];
+                else ++taken[0];
+                ok = mbar_wait(bar(sh.s_empty[half][buf]), phase ^ 1, dead) &&
                      mbar_wait(bar(sh.q_full[eq]), qn / Sh::kQs & 1, dead);
                 if (!ok) break;
                 fence_after();
@@ -481,27 +488,31 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
     } else if (busy) {
         // ---------------------------------------------------------- weights
         if (Sh::kGroups == 4) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kSumRegs));
-        const int half = warp / 4 % 2, side = warp / 8;  // which 128 keys, and which columns
+        const int half = warp / 4 % 2, side = warp / 8;  // which 128 keys, and which tiles: the even or the odd ones
+        constexpr bool kTurns = Sh::kGroups == 4, kTileTurns = kTurns && HOW != Tiles::kOne, kUnitTurns = kTurns && HOW == Tiles::kOne;
+        constexpr int kStep = kTileTurns ? 2 : 1;
         const uint32_t key = tid % 128;
-        const uint32_t lanes = tmem + ((warp % 4) << 21) + half * Sh::kBufs * N + side * kCols;
+        const uint32_t lanes = tmem + ((warp % 4) << 21) + half * Sh::kBufs * N;
         const float k2 = a.scale * kLog2e;
         const bool cap = MOD && a.softcap != 0.0f;
         const float cap_in = cap ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
-        const uint64_t k22 = pack2(k2, k2);
         // the lane's columns of a tile: token and head, counted in the tile
         constexpr int kMine = kCols < 32 ? 1 : kCols / 32;
-        int32_t token_at[kMine], head_at[kMine];
-        float next[kMine];  // their log-sum-exps of the next tile
-        bool pad[kMine];        // no column of a complete tile
-        uint32_t offset[kMine];
+        uint32_t place_of[kMine];  // token, and the head above it
+        float next[kMine];         // their log-sum-exps of the next tile
 #pragma unroll
         for (int k = 0; k < kMine; ++k) {
-            const int32_t c = side * kCols + k * 32 + int32_t(lane);
-            token_at[k] = c / f.per_token, head_at[k] = c % f.per_token;
-            if (k * 32 + int32_t(lane) >= kCols) token_at[k] = INT32_MAX;  // none
-            pad[k] = token_at[k] >= f.per_tile;
-            offset[k] = pad[k] ? 0 : uint32_t(token_at[k]) * a.q_heads + uint32_t(head_at[k]);
+            const uint32_t c = k * 32 + lane, t = c / uint32_t(f.per_token);
+            place_of[k] = k * 32 + int32_t(lane) >= kCols ? 0xFFFFu : t | (c - t * uint32_t(f.per_token)) << 16;  // (0xFFFF: none)
         }
+        auto token_at = [&](int k) { return int32_t(place_of[k] & 0xFFFFu); };
+        auto head_at = [&](int k) { return int32_t(place_of[k] >> 16); };
+        // the first token and query of a column tile
+        auto tile_at = [&](int32_t tile) {
+            if (f.slices == 1) return make_int2(tile * f.per_tile, 0);
+            const int32_t t = tile / f.slices;
+            return make_int2(t * f.per_tile, (tile - t * f.slices) * f.per_token);
+        };
         constexpr bool kLean = !kFlat && !MOD;
         const bool lean = f.slices == 1 && !a.spans;
         // of the tile that begins with token t0 and the head's query g0 (first: the sequence's first token)
@@ -509,8 +520,8 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             const float* const at = f.w.lse + uint64_t(uint32_t(first + t0)) * a.q_heads + h * a.group + g0;
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
-                const bool real = token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0;
-                next[k] = at[real ? uint32_t(token_at[k]) * a.q_heads + uint32_t(head_at[k]) : 0];  // (a tile has a first column)
+                const bool real = token_at(k) < min(f.per_tile, m - t0) && head_at(k) < int32_t(a.group) - g0;
+                next[k] = at[real ? uint32_t(token_at(k)) * a.q_heads + uint32_t(head_at(k)) : 0];  // (a tile has a first column)
                 if (!real) next[k] = -INFINITY;
             }
         };
@@ -522,25 +533,33 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         };
         float then = 0.0f;  // ... of the next unit
         bool then_known = false;
-        // ... and what was looked up to the tile's place, with slopes and spans
-        auto put = [&](int in, int32_t first, int32_t h, int32_t m, int32_t t0, int32_t g0) {
+        // ... and what was looked up to its place, with slopes
+        auto put = [&](int32_t h, int32_t m, int32_t t0, int32_t g0) {
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
                 const int32_t c = k * 32 + int32_t(lane);
                 if (kCols < 32 && c >= kCols) break;
-                lse_of[warp][in][c] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
-                if (MOD || a.spans) {
-                    const bool real = token_at[k] < min(f.per_tile, m - t0) && head_at[k] < int32_t(a.group) - g0;
-                    int2 span = make_int2(0, 0);
-                    if (a.spans && real) span = reinterpret_cast<const int2*>(a.spans)[first + t0 + token_at[k]];
-                    if (a.spans) span_of[warp][c] = span;
-                    if (MOD) slope_of[MOD ? warp : 0][in][c] = a.slopes && real ? a.slopes[h * a.group + g0 + head_at[k]] * kLog2e : 0.0f;
+                lse_of[warp][c] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
+                if (MOD) {
+                    const bool real = token_at(k) < min(f.per_tile, m - t0) && head_at(k) < int32_t(a.group) - g0;
+                    slope_of[MOD ? warp : 0][c] = a.slopes && real ? a.slopes[h * a.group + g0 + head_at(k)] * kLog2e : 0.0f;
                 }
             }
         };
+        // spans of kSpanCols columns from c0 on
+        auto put_spans = [&](int c0, int32_t first, int32_t m, int32_t t0, int32_t g0) {
+            __syncwarp();
+            for (int c = int(lane); c < Sh::kSpanCols; c += 32) {
+                const int32_t t = (c0 + c) / f.per_token, g = (c0 + c) % f.per_token;
+                int2 span = make_int2(0, 0);
+                if (t < min(f.per_tile, m - t0) && g < int32_t(a.group) - g0) span = reinterpret_cast<const int2*>(a.spans)[first + t0 + t];
+                span_of[warp][c] = span;
+            }
+            __syncwarp();
+        };
         int32_t had_s = -1, had_h = -1;  // whose log-sum-exps are there (kFlat)
         bool known = false;              // `next` is the next tile's
-        uint32_t n = 0;
+        uint32_t n = 0;  // the group's tiles
         bool more = true;
         for (uint32_t u = 0; more; ++u) {
             const bool got = mbar_wait(bar(sh.unit_full[u % kWeighUnits]), u / kWeighUnits & 1, dead);
@@ -552,7 +571,8 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             const int32_t in_part = rec.part, tile0 = rec.tile;
             more = rec.more;
             if (none) break;
-            const bool mine = side == 0 && slot < len && uint32_t(slot) < f.w.n_slots;
+            const bool turn = !kUnitTurns || int(u & 1) == side;  // this group's unit
+            const bool mine = (kUnitTurns ? turn : side == 0) && slot < len && uint32_t(slot) < f.w.n_slots;
             float* const place = f.w.weights + uint32_t(s) * f.w.seq_stride + uint32_t(h) * f.w.head_stride + slot;
             float held = then;
             if (!kFlat && whole && mine && slot < ctx && f.w.decay != 0.0f) held = *place;
@@ -573,96 +593,96 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             const int32_t all0 = __reduce_max_sync(0xFFFFFFFFu, i0), all1 = a.spans ? 0 : __reduce_min_sync(0xFFFFFFFFu, i1);
             if (slot >= len) i1 = 0;  // (what lies behind the sequence is not written, so it may be added up)
             KvSum sum;
-            float part[4] = {};
-            int32_t t0 = tile0, g0 = 0;
-            if (f.slices > 1) t0 = tile0 / f.slices, g0 = (tile0 - t0 * f.slices) * f.per_token;
-            t0 *= f.per_tile;
-            for (int32_t i = 0; i < steps; ++i, ++n) {
+            for (int32_t i = kTileTurns ? (tile0 ^ side) & 1 : 0; i < steps && turn; i += kStep) {
+                int2 at0 = tile_at(tile0 + i);
                 // (which way a tile goes does not depend on whether its log-sum-exps came early: sums are added up in one order)
-                if (!kFlat && !known) look_up(first, h, m, t0, g0), known = true;
-                if (kLean && lean && t0 >= all0) {
-                    // Tiles that all of the warp's slots see, and the next of which is complete: nothing to decide.
-                    const int32_t last = min(steps - 1, i + (all1 - t0) / f.per_tile - 1);
-                    const uint64_t stride = uint64_t(uint32_t(f.per_tile)) * a.q_heads;
-                    const float* at = f.w.lse + uint64_t(uint32_t(first + t0)) * a.q_heads + h * a.group;
+                if (!kFlat && !known) look_up(first, h, m, at0.x, at0.y), known = true;
+                if (kLean && lean && at0.x >= all0) {
+                    // Tiles that all of the warp's slots see, and the group's next of which is complete: nothing to decide.
+                    const uint64_t stride = uint64_t(uint32_t(f.per_tile)) * (a.q_heads * kStep);
+                    const float* at = f.w.lse + uint64_t(uint32_t(first + at0.x)) * a.q_heads + h * a.group;
+                    uint32_t offset[kMine];
+#pragma unroll
+                    for (int k = 0; k < kMine; ++k)
+                        offset[k] = token_at(k) >= f.per_tile ? 0xFFFFFFFFu : uint32_t(token_at(k)) * a.q_heads + uint32_t(head_at(k));
 #pragma unroll 1
-                    for (; i < last; ++i, ++n, t0 += f.per_tile) {
+                    for (; i + kStep < steps && at0.x + (kStep + 1) * f.per_tile <= all1; i += kStep, at0.x += kStep * f.per_tile) {
                         __syncwarp();
 #pragma unroll
-                        for (int k = 0; k < kMine; ++k) lse_of[warp][0][k * 32 + lane] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
+                        for (int k = 0; k < kMine; ++k) lse_of[warp][k * 32 + lane] = next[k] == -INFINITY ? -INFINITY : -next[k] * kLog2e;
                         __syncwarp();
                         at += stride;
 #pragma unroll
-                        for (int k = 0; k < kMine; ++k) next[k] = pad[k] ? -INFINITY : at[offset[k]];
-                        const uint32_t buf = n % Sh::kBufs;
-                        const bool there = mbar_wait(bar(sh.s_full[half][buf]), n / Sh::kBufs & 1, dead);
+                        for (int k = 0; k < kMine; ++k) next[k] = offset[k] == 0xFFFFFFFFu ? -INFINITY : at[offset[k]];
+                        const uint32_t buf = uint32_t(side);  // (kTileTurns)
+                        const bool there = mbar_wait(bar(sh.s_full[half][buf]), n++ & 1, dead);
                         if (!__all_sync(0xFFFFFFFFu, there)) goto weights_done;
                         fence_after();
-                        float x[kCols];
-#pragma unroll
-                        for (int c = 0; c < kCols; c += 32) tmem_ld32(lanes + buf * N + c, x + c);
-                        wait_ld(x);
-                        fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(bar(sh.s_empty[half][buf]));
                         uint64_t add0 = 0, add1 = 0;
+#pragma unroll 1
+                        for (int c0 = 0; c0 < kCols; c0 += 64) {
+                            float x[64];
 #pragma unroll
-                        for (int c = 0; c < kCols; c += 4) {
-                            const float4 l = *reinterpret_cast<const float4*>(lse_of[warp][0] + c);
-                            add0 = add2(add0, pack2(exp2_approx(fmaf(x[c], k2, l.x)), exp2_approx(fmaf(x[c + 1], k2, l.y))));
-                            add1 = add2(add1, pack2(exp2_approx(fmaf(x[c + 2], k2, l.z)), exp2_approx(fmaf(x[c + 3], k2, l.w))));
+                            for (int c = 0; c < 64; c += 32) tmem_ld32(lanes + buf * N + c0 + c, x + c);
+                            wait_ld(x);
+                            if (c0 + 64 >= kCols) {
+                                fence_before();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(bar(sh.s_empty[half][buf]));
+                            }
+#pragma unroll
+                            for (int c = 0; c < 64; c += 4) {
+                                const float4 l = *reinterpret_cast<const float4*>(lse_of[warp] + c0 + c);
+                                add0 = add2(add0, pack2(exp2_approx(fmaf(x[c], k2, l.x)), exp2_approx(fmaf(x[c + 1], k2, l.y))));
+                                add1 = add2(add1, pack2(exp2_approx(fmaf(x[c + 2], k2, l.z)), exp2_approx(fmaf(x[c + 3], k2, l.w))));
+                            }
                         }
                         float y0, y1;
                         unpack2(add2(add0, add1), y0, y1);
                         sum.add(y0 + y1);
                     }
                 }
-                if (!kFlat) {
-                    known = false;
-                    __syncwarp();
-                    put(0, first, h, m, t0, g0);
-                    __syncwarp();
-                } else if (s != had_s || h != had_h) {  // all tiles of another key head
-                    __syncwarp();
-                    for (int32_t t = 0; t < kTiles && t * f.per_tile < m * f.slices; ++t) {
-                        const int32_t token = f.slices > 1 ? t / f.slices : t * f.per_tile, query = f.slices > 1 ? t % f.slices * f.per_token : 0;
-                        look_up(first, h, m, token, query);
-                        put(t, first, h, m, token, query);
+                const int32_t t0 = at0.x, g0 = at0.y;
+                if (!kFlat || kTileTurns || s != had_s || h != had_h) {
+                    if (kFlat) {
+                        // (a group's tile of a key head is the same for all its units)
+                        if (s != had_s || h != had_h) look_up(first, h, m, t0, g0), had_s = s, had_h = h, known = true;
                     }
-                    __syncwarp();
-                    had_s = s, had_h = h;
+                    if (known) {
+                        known = false;
+                        __syncwarp();
+                        put(h, m, t0, g0);
+                        __syncwarp();
+                    }
                 }
-                const int in = kTiles == 1 ? 0 : tile0 + i;
-                const float* const lse_at = lse_of[warp][in];
-                const float* const slope_at = slope_of[MOD ? warp : 0][in];
                 const float ahead = float(ctx + t0 - slot);
                 const bool plain = t0 >= all0 && t0 + f.per_tile <= all1 && g0 + f.per_token <= int32_t(a.group);
                 // the thread's visible columns [v0, v1), where not all are
                 int32_t v0 = 0, v1 = kCols;
                 if (!plain) {
                     const int32_t cols = min(f.per_tile, m - t0) * min(f.per_token, int32_t(a.group) - g0);
-                    v0 = a.spans ? 0 : min(max(i0 - t0, 0), f.per_tile) * f.per_token - side * kCols;
-                    v1 = (slot >= len ? 0 : a.spans ? cols : min(min(max(i1 - t0, 0), f.per_tile) * f.per_token, cols)) - side * kCols;
+                    v0 = a.spans ? 0 : min(max(i0 - t0, 0), f.per_tile) * f.per_token;
+                    v1 = slot >= len ? 0 : a.spans ? cols : min(min(max(i1 - t0, 0), f.per_tile) * f.per_token, cols);
                 }
-                if (f.slices > 1) {
-                    g0 += f.per_token;
-                    if (g0 >= int32_t(a.group)) g0 = 0, t0 += f.per_tile;
-                } else {
-                    t0 += f.per_tile;
-                }
-                if (!kFlat) {  // the next tile's, on their way while this one is worked on
-                    if (i + 1 < steps) {
-                        look_up(first, h, m, t0, g0), known = true;
+                if (!kFlat) {  // the group's next tile's, on their way while this one is worked on
+                    if (i + kStep < steps) {
+                        const int2 b = tile_at(tile0 + i + kStep);
+                        look_up(first, h, m, b.x, b.y), known = true;
                     } else if (more) {
                         const uint32_t v = u + 1;
                         const WeighUnit& o = sh.unit[v % kWeighUnits];
                         const bool out = mbar_test(bar(sh.unit_full[v % kWeighUnits]), v / kWeighUnits & 1);
-                        if (__all_sync(0xFFFFFFFFu, out) && !o.dry && f.slices == 1)
-                            look_up(o.q.first, o.h, weigh_tokens(a, o.q), o.tile * f.per_tile, 0), known = true;
+                        if (__all_sync(0xFFFFFFFFu, out)) {
+                            const int32_t j = (o.tile ^ side) & 1;
+                            const int2 b = tile_at(o.tile + j);
+                            if (!o.dry && j < o.n) look_up(o.q.first, o.h, weigh_tokens(a, o.q), b.x, b.y), known = true;
+                        }
                     }
                 }
-                const uint32_t buf = n % Sh::kBufs;
-                const bool there = mbar_wait(bar(sh.s_full[half][buf]), n / Sh::kBufs & 1, dead);
+                float part[4] = {};
+                const uint32_t buf = kTurns ? uint32_t(side) : n % Sh::kBufs;
+                const bool there = mbar_wait(bar(sh.s_full[half][buf]), kTurns ? n & 1 : n / Sh::kBufs & 1, dead);
+                ++n;
                 if (!__all_sync(0xFFFFFFFFu, there)) goto weights_done;
                 fence_after();
 #pragma unroll 1
@@ -680,10 +700,10 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
                     // scores, less the log-sum-exp, in units of log2
 #pragma unroll
                     for (int c = 0; c < kChunk; c += 4) {
-                        const float4 l = *reinterpret_cast<const float4*>(lse_at + c0 + c);
+                        const float4 l = *reinterpret_cast<const float4*>(lse_of[warp] + c0 + c);
                         if (MOD) {
-                            const float4 sl = *reinterpret_cast<const float4*>(slope_at + c0 + c);
-                            const float4 tk = *reinterpret_cast<const float4*>(token_of + (MOD ? side * kCols + c0 + c : 0));
+                            const float4 sl = *reinterpret_cast<const float4*>(slope_of[MOD ? warp : 0] + c0 + c);
+                            const float4 tk = *reinterpret_cast<const float4*>(token_of + (MOD ? c0 + c : 0));
                             const float sls[4] = {sl.x, sl.y, sl.z, sl.w}, ls[4] = {l.x, l.y, l.z, l.w}, tks[4] = {tk.x, tk.y, tk.z, tk.w};
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
@@ -699,9 +719,10 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
                     if (!plain) {
                         uint32_t see = 0;
                         if (a.spans) {
+                            if (c0 % Sh::kSpanCols == 0) put_spans(c0, first, m, t0, g0);
 #pragma unroll 4
                             for (int c = 0; c < kChunk; ++c) {
-                                const int2 sp = span_of[warp][c0 + c];
+                                const int2 sp = span_of[warp][c0 % Sh::kSpanCols + c];
                                 see |= uint32_t(slot >= sp.x && slot < sp.y && c0 + c < v1) << c;
                             }
                         } else {
@@ -717,13 +738,11 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
                         for (int k = 0; k < 4; ++k) part[k] += exp2_approx(x[c + k]);
                     }
                 }
-                if (i % 4 == 3 || i + 1 == steps) {
-                    sum.add((part[0] + part[1]) + (part[2] + part[3]));
-                    part[0] = part[1] = part[2] = part[3] = 0.0f;
-                }
+                sum.add((part[0] + part[1]) + (part[2] + part[3]));
             }
             float got_all = sum.value();
-            if (Sh::kGroups == 4) {  // the sums of both halves of the columns meet
+            if (kUnitTurns && !turn) continue;
+            if (kTileTurns) {  // the sums of the even and the odd tiles meet
                 const uint32_t b = u & 1;
                 float* const other = sh.sum[half][b];
                 if (side) {
