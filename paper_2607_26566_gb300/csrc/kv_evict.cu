@@ -104,7 +104,13 @@ __device__ __forceinline__ void select_row(const KvSelect& c, SelShared& sh, uin
             if (pass) __syncthreads();  // (the first one's are zeros from the start)
             // numbers between these have the leading bits (NaN, and what no number has, are not looked for by them)
             const uint32_t lo = known ? prefix << (32 - known) : 0, hi = known ? lo + (0xFFFFFFFFu >> known) : 0xFFFFFFFFu;
-            if (HELD && pass && lo >= kLowest) {
+            if (HELD && pass == 0) {
+#pragma unroll
+                for (int i = 0; i < I; ++i) {
+                    if (i >= mine) break;
+                    if (choice >> i & 1) atomicAdd(&h[order_of(held[HELD ? i : 0]) >> 21], 1u);
+                }
+            } else if (HELD && lo >= kLowest) {
                 const float from = weight_of(lo), upto = weight_of(hi == 0x7FFFFFFFu ? hi - 1 : min(hi, kHighest));
 #pragma unroll
                 for (int i = 0; i < I; ++i) {
@@ -222,8 +228,8 @@ __device__ __forceinline__ void select_row(const KvSelect& c, SelShared& sh, uin
             if (i >= mine) break;
             const bool over = over_bits >> i & 1;
             const uint32_t mo = __ballot_sync(0xFFFFFFFFu, over);
-            const uint32_t to = base + __popc(mo & lower);
             if (over) {
+                const uint32_t to = base + __popc(mo & lower);
                 kept[to] = int32_t(w0 + i * 32 + lane);
                 if (copy) out[to] = held[HELD ? i : 0];
             }

@@ -496,6 +496,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         const float k2 = a.scale * kLog2e;
         const bool cap = MOD && a.softcap != 0.0f;
         const float cap_in = cap ? a.scale / a.softcap : 0.0f, cap2 = a.softcap * kLog2e;
+        const uint64_t k22 = pack2(k2, k2);
         // the lane's columns of a tile: token and head, counted in the tile
         constexpr int kMine = kCols < 32 ? 1 : kCols / 32;
         uint32_t place_of[kMine];  // token, and the head above it
@@ -632,9 +633,12 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
                             }
 #pragma unroll
                             for (int c = 0; c < 64; c += 4) {
-                                const float4 l = *reinterpret_cast<const float4*>(lse_of[warp] + c0 + c);
-                                add0 = add2(add0, pack2(exp2_approx(fmaf(x[c], k2, l.x)), exp2_approx(fmaf(x[c + 1], k2, l.y))));
-                                add1 = add2(add1, pack2(exp2_approx(fmaf(x[c + 2], k2, l.z)), exp2_approx(fmaf(x[c + 3], k2, l.w))));
+                                const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(lse_of[warp] + c0 + c);
+                                float y0, y1, y2, y3;
+                                unpack2(fma2(pack2(x[c], x[c + 1]), k22, l.x), y0, y1);
+                                unpack2(fma2(pack2(x[c + 2], x[c + 3]), k22, l.y), y2, y3);
+                                add0 = add2(add0, pack2(exp2_approx(y0), exp2_approx(y1)));
+                                add1 = add2(add1, pack2(exp2_approx(y2), exp2_approx(y3)));
                             }
                         }
                         float y0, y1;
