@@ -24,7 +24,7 @@
 //
 // Measured: a token each of 64 sequences of up to 16k slots (2.2 GB of keys and values,
 // 32 heads over 8 of 128) 331 us, 6.8 TB/s; of 48 of up to 9k in a window of 4,096, heads
-// of 64, scores capped, 28-29 us; of 192 of 600 slots 85 us (70 at the copy rate); of 256 of
+// of 64, scores capped, 28-29 us; of 64 in a window of 2,048 with 4 sinks 98-99 us (79 at the copy rate); of 192 of 600 slots 85 us (70 at the copy rate); of 256 of
 // 100 slots 41 us, 5 us a segment in each of an SM's two blocks: half of it scores and
 // weights, a quarter the products, a quarter the output; of one sequence of 700 slots 12.4
 // us, of which the two launches and the chain of one tile are all.

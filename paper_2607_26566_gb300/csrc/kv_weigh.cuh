@@ -3,8 +3,8 @@
 //
 // With an attention's log-sum-exp at hand no maximum and no second product is needed: S^T = K Q^T on the tensor cores,
 // 128 keys to the rows of a product and N queries to its columns, so that a thread has one key, adds its row up, and
-// nothing goes from thread to thread. A unit is 256 keys of one key head in two halves, one to each half of the softmax
-// warps: its keys are loaded once (TMA), its queries, 128 columns at a time, once for both halves.
+// nothing goes from thread to thread. A unit is 256 keys of one key head in two halves, one to each half of the warps
+// that add up: its keys are loaded once (TMA), its queries, 128 columns at a time, once for both halves.
 //
 // Two regimes. Where all queries of a key head are one column tile or two (a decoding step, an observation window) the
 // call is bound by reading the keys: each block streams them through a ring. Of more (a prompt) it is bound by the sums
@@ -18,9 +18,10 @@
 // the exponential, score - lse in units of log2, is rounded once in fp32 from a scale that is rounded too: 2e-6 of a
 // weight whose score and lse are 30, 3e-7 of a prompt's sums.
 //
-// Measured, 32 heads over 8 of 128: one token over 700 slots 5.7 us; a token each of 64 sequences of up to 16k slots (1.16
-// GB) 178 us, 6.5 TB/s; a prompt of 8190 tokens 257-268 us, 1.03-1.07 PFLOP/s of what is visible, where the products alone
-// (no sums) took 192; 32 tokens of nine prompts of up to 7k, 28 heads over 4, 24-25 us.
+// Measured, 32 heads over 8 of 128: one token over 700 slots 5.6 us; a token each of 64 sequences of up to 16k slots (1.16
+// GB) 177 us, 6.5 TB/s; a prompt of 8190 tokens 242-261 us, 1.05-1.14 PFLOP/s of what is visible, where products and loads
+// alone (nothing added up) took 193; 32 tokens of nine prompts of up to 7k, 28 heads over 4, 22-24 us. (With half of a
+// tile's columns to each group of warps, in place of tiles in turn, the last two took 257 and 23.5.)
 #pragma once
 
 #include <algorithm>
@@ -40,8 +41,8 @@ constexpr uint32_t kHalfSlot = 16384;  // 128 keys of 64 elements
 constexpr uint32_t kWeighUnits = 8;    // handed out at a time
 constexpr int kPartFloats = kUnitKeys;
 
-// Column tiles of a sequence: one; two, whose log-sum-exps stay, like the one's, while a run is in one key head; or so many
-// that keys stay while they pass, and units are cut where runs end.
+// Column tiles of a sequence: one; two, one to a group of warps, whose log-sum-exps stay, like the one's, while a run is in
+// one key head; or so many that keys stay while they pass, and units are cut where runs end.
 enum class Tiles { kOne, kFew, kMany };
 
 template <int N, int NS, Tiles HOW>
@@ -61,16 +62,15 @@ struct WeighShape {
     static constexpr uint32_t kTmem = 2 * kBufs * N;
     static constexpr uint32_t kBytes = 1024 + kHalf * kKeys + kQ * kQs;
     // The warps that add up come in groups of four: one a half, or two, which take tiles (of one tile: units) in turn. Then a
-    // loading warp and a product warp for each half (one's products run while the other waits; N = 128 has one loading warp, and
-    // one that idles).
+    // loading warp and a product warp for each half (one's products run while the other waits; of many tiles there is one
+    // loading warp, and one that idles).
     static constexpr int kGroups = N == 128 ? 4 : 2;
     static constexpr int kCols = N;
     static constexpr int kSpanCols = N < 64 ? N : 64;  // whose spans are held at a time
     static constexpr int kSumWarps = 4 * kGroups, kThreads = kSumWarps * 32 + 128;
     static constexpr int kRegs = 96, kSumRegs = 104, kOtherRegs = 64;
     static_assert(kGroups != 4 || kSumRegs * kSumWarps * 32 + kOtherRegs * 128 <= kRegs * kThreads, "what a block was launched with");
-    static constexpr int kTiles = 1;
-    static constexpr uint32_t kFixed = 8192 + kSumWarps * (kCols * 8 * kTiles + kSpanCols * 8);  // static shared memory, at most
+    static constexpr uint32_t kFixed = 8192 + kSumWarps * (kCols * 8 + kSpanCols * 8);  // static shared memory, at most
     static_assert(kBytes + kFixed + 1024 <= 228 * 1024, "an SM's shared memory");
     static constexpr int kChunk = kCols < 32 ? kCols : 32;  // columns that a thread works on at a time
 };
@@ -144,8 +144,8 @@ __device__ __forceinline__ int2 unit_tiles(const Weigh& f, const KvSeq& q, uint3
     return make_int2(i0 / f.per_tile * f.slices, int32_t((i1 + f.per_tile - 1) / f.per_tile) * f.slices);
 }
 // What a unit costs where runs are cut: its steps, and so many before them (its keys' way, tiles with a mask, its sums'
-// way out). Measured with 0, 2, 4, 8 and 14: prompts of 4,096 tokens 89, 84, 79, 82, 86 us, of 8,190 284, 273, 265, 262,
-// 266.
+// way out). Measured with 4, 6 and 9: prompts of 4,096 tokens 76, 74, 77 us, of 8,190 252, 246, 246 (before tiles were taken
+// in turn with 0, 2, 4, 8 and 14 284, 273, 265, 262 and 266).
 constexpr int32_t kUnitCost = 6;
 __device__ __forceinline__ int32_t unit_cost(int2 tiles) { return tiles.y > tiles.x ? kUnitCost + tiles.y - tiles.x : 1; }
 
@@ -862,8 +862,8 @@ cudaError_t launch_weigh(const KvWeigh& w, const KvLaunch& l, cudaStream_t strea
         if (rows <= 64) return launch_weigh_n<T, 64, Tiles::kOne>(f, l, stream);
         return launch_weigh_n<T, 128, Tiles::kOne>(f, l, stream);
     }
-    // Two: 32 tokens of nine prompts of up to 7k slots 24 us, as if there were many 33; of one of 3k 10 against 15. (Three
-    // are slower so, 81 against 74 us, but over short contexts.) There is room for one tile's spans.
+    // Two: 32 tokens of nine prompts of up to 7k slots 22 us, as if there were many 33; of one of 3k 10 against 15. (Three
+    // are slower so, 81 against 74 us, but over short contexts.) Spans go with many.
     if (uint64_t(tiles) * f.slices == 2 && !w.a.spans) return launch_weigh_n<T, 128, Tiles::kFew>(f, l, stream);
     return launch_weigh_n<T, 128, Tiles::kMany>(f, l, stream);
 }
