@@ -362,3 +362,30 @@ def test_strides_whose_bytes_pass_64_bits_are_refused(lib):
     assert lib.t2i_kv_weigh(c._h, C.byref(d), None) == 1 and "table" in c.store.last_error()
     torch.cuda.synchronize()
     assert c.store.stats()["launches"] == before
+
+
+@pytest.mark.parametrize("heads,kv,tokens", [(4, 4, 1), (8, 2, 7), (8, 2, 14), (8, 2, 24), (14, 2, 32), (8, 2, 160)])
+def test_units_that_no_token_sees_between_others(heads, kv, tokens):
+    """A window in sequences of many units, and weights that decay everywhere: most units have nothing to add up, in each
+    of the forms (one column tile of 16 to 128 columns, two, many), some of them the first or the last of a block."""
+    new = [tokens, 1, tokens, max(1, tokens // 2)] * 5
+    ctx = [2500, 1300, 700, 2000] * 5
+    c, lens, kvs, q = case(BF, heads, kv, 64, new, ctx, page=262144)
+    check(c, lens, new, kvs, q, decay=0.5, window=200, sinks=3)
+    check(c, lens, new, kvs, q, decay=0.0, window=200, sinks=700)
+
+
+@pytest.mark.parametrize("heads,kv,dim,new,ctx", [(8, 2, 64, [40, 33], [700, 1500]), (8, 2, 128, [24, 31, 2], [600, 90, 800]),
+                                                  (4, 4, 64, [12, 1], [900, 300])])
+@pytest.mark.parametrize("bias", [False, True])
+def test_spans_of_long_contexts(heads, kv, dim, new, ctx, bias):
+    """Two column tiles, one of 128 and one of 16 columns; far units that no token sees."""
+    c, lens, kvs, q = case(HF, heads, kv, dim, new, ctx)
+    rng = np.random.default_rng(dim)
+    spans = []
+    for m, L in zip(new, lens):
+        for i in range(m):
+            a = int(rng.integers(0, 300)) if i % 3 else L - m
+            spans.append((a, min(L, a + int(rng.integers(1, 200)))) if i % 5 else (0, 0))
+    opt = dict(slopes=torch.tensor([2.0 ** (-h - 4) for h in range(heads)]), softcap=30.0) if bias else {}
+    check(c, lens, new, kvs, q, spans=torch.tensor(spans), decay=0.5, **opt)
