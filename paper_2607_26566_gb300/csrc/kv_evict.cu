@@ -296,14 +296,16 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_kernel(const __grid_con
 // each, 8 heads of 128 (2.15 GB): 339 us, 6.3 TB/s.
 constexpr uint32_t kEvictThreads = 256;
 constexpr uint32_t kEvictDeep = 4;  // rows of a thread in a chunk
-constexpr uint32_t kEvictRows = kEvictThreads / 2 * kEvictDeep;  // of a chunk, at most
+// Rows of a chunk, at most: what two columns of threads or more come to. Where a row is one vector (heads of 8) half of the
+// threads only look up; places for all of them would take 32 KiB of shared memory of every other form too.
+constexpr uint32_t kEvictRows = kEvictThreads / 2 * kEvictDeep;
 __global__ void __launch_bounds__(kEvictThreads, 4) evict_kernel(const __grid_constant__ KvEvict c, const uint32_t cols) {
     __shared__ ulonglong2 place[2][kEvictRows];  // a row's key: where it is and where it goes; 0: it stays
     tc::pdl_launch();
     tc::pdl_wait();
     const KvPages& p = c.pages;
     const uint32_t s = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads, layer = p.layer + blockIdx.y;
-    const uint32_t rows = kEvictThreads / cols, chunk = rows * kEvictDeep;
+    const uint32_t rows = min(kEvictThreads / cols, kEvictRows / kEvictDeep), chunk = rows * kEvictDeep;
     const uint32_t r = threadIdx.x / cols, col = blockIdx.z * cols + threadIdx.x % cols;
     const bool mine = r < rows && col * 8 < p.head_dim;
     const uint32_t n = uint32_t(min(max(c.counts[s], 0), int32_t(c.max_kept)));
@@ -380,8 +382,8 @@ cudaError_t launch_kv_select(const KvSelect& c, uint32_t sms, cudaStream_t strea
 cudaError_t launch_kv_evict(const KvEvict& c, uint32_t sms, cudaStream_t stream) {
     const uint32_t vectors = c.pages.head_dim / 8;
     const uint64_t units = uint64_t(c.n_seqs) * c.pages.kv_heads * c.layers;
-    // Fewer units than blocks that an SM's four places take: a block has a share of the columns, of 32 bytes at least. 512
-    // units of 4,096 rows of 256 bytes with 1, 2 and 4 shares: 360, 338, 565 us.
+    // Fewer units than blocks that an SM's four places take: a block has a share of the columns, of 32 bytes at least (or
+    // all of a narrower row). 512 units of 4,096 rows of 256 bytes with 1, 2 and 4 shares: 360, 338, 565 us.
     uint32_t parts = 1;
     while (parts < 8 && units * parts < 4 * sms && vectors / parts >= 4) parts *= 2;
     const uint32_t cols = (vectors + parts - 1) / parts;
