@@ -584,7 +584,8 @@ typedef struct t2i_kv_weigh_desc {
  * decay * weights + sum (decay 0: the sum; weights so far may be anything).
  * Slots of the new tokens: the sum. Others are left as they are. A query
  * whose lse is -infinity (and whose q is finite) counts nothing. Keys may hold anything where no
- * token sees them. Sums are fp32, in an order that does not depend on timing. */
+ * token sees them. Sums are fp32, in an order that does not depend on timing.
+ * Neither weights nor the workspace share a byte with another array.         */
 t2i_status t2i_kv_weigh(t2i_kv* kv, const t2i_kv_weigh_desc* desc, void* cuda_stream);
 
 /* Workspace bytes that t2i_kv_weigh needs for such a batch at most.         */

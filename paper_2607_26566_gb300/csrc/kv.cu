@@ -371,8 +371,21 @@ t2i_status weigh(t2i_kv* kv, const t2i_kv_weigh_desc& d, cudaStream_t stream) {
     c.require(n == 1 || (d.q_stride < (uint64_t(1) << 39) && d.q_stride >= uint64_t(d.q_heads) * kv->layout.head_dim),
               "q: the stride must be at least a token's heads, and below 2^39");
     if (!c.ok()) return T2I_ERR_INVALID;
-    c.require(!overlap(d.weights, bytes, d.lse, n * d.q_heads * 4) &&
-                  !overlap(d.weights, bytes, d.q, c.token_bytes(n, d.q_heads, d.q_stride, 2)), "weights overlap q or lse");
+    // What is read lies apart from what is written: each block cuts the runs by itself, from lens, starts and spans, and the
+    // first ones done write while others have not begun.
+    auto apart = [&](const char* name, const void* p, uint64_t size) {
+        if (!c.ok() || !p) return;
+        if (overlap(p, size, d.weights, bytes)) return c.fail(name, "overlaps weights");
+        if (overlap(p, size, d.workspace, need)) c.fail(name, "overlaps the workspace");
+    };
+    apart("q", d.q, c.token_bytes(n, d.q_heads, d.q_stride, 2));
+    apart("lse", d.lse, n * d.q_heads * 4);
+    apart("lens", d.batch.lens, uint64_t(seqs) * 4);
+    apart("starts", d.batch.starts, (uint64_t(seqs) + 1) * 4);
+    apart("table", d.batch.table, at_most((Wide(seqs - 1) * d.batch.table_stride + d.batch.table_pages) * 4));
+    apart("slopes", d.slopes, uint64_t(d.q_heads) * 4);
+    apart("spans", d.spans, n * 8);
+    c.require(!overlap(d.weights, bytes, d.workspace, need), "weights overlap the workspace");
     if (!c.ok()) return T2I_ERR_INVALID;
     a.pages = pages_of(kv, d.batch.table, d.batch.table_stride, d.batch.table_pages, d.batch.layer);
     a.q = d.q;

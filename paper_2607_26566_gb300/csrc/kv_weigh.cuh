@@ -224,6 +224,7 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
         for (int h = 0; h < 2; ++h)
             for (int i = 0; i < 2; ++i) mbar_init(bar(sh.sum_full[h][i]), 4), mbar_init(bar(sh.sum_empty[h][i]), 4);
         sh.dead = 0;
+        sh.start_seq = -1;
         fence_mbar_init();
         tma_prefetch_map(&map), tma_prefetch_map(&q_map);
     }
@@ -270,11 +271,12 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
     }
     total *= K;
     const int64_t blocks = min(int64_t(gridDim.x), total);
-    const bool busy = blockIdx.x < blocks;
+    bool busy = blockIdx.x < blocks;
     const int64_t run0 = busy ? blockIdx.x * total / blocks : 0, run1 = busy ? (blockIdx.x + 1) * total / blocks : 0;
     if (busy && run0 >= lo * K && run0 < (lo + mine) * K) {
         int64_t p = lo * K;
-        for (uint32_t s = who * per;; ++s) {
+        // (bounded, like the loads' way from sequence to sequence: lengths that change during the call find no end otherwise)
+        for (uint32_t s = who * per; s < min(a.tok.n_seqs, (who + 1) * per); ++s) {
             const int64_t steps = seq_cost<kFlat>(f, kv_seq(a.pages, a.tok, s), s, lane);
             if (run0 < p + steps * K) {
                 if (kFlat || lane == 0) sh.start_seq = int32_t(s), sh.start_rest = run0 - p, sh.start_steps = steps;
@@ -285,6 +287,10 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
     }
     __syncthreads();
     const uint32_t tmem = sh.tmem;
+    if (busy && sh.start_seq < 0) {
+        busy = false;
+        if (tid == 0) sh.dead = 1;
+    }
 
     if (busy && warp >= kSumWarps) {
         if (Sh::kGroups == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
@@ -374,12 +380,15 @@ __global__ void __launch_bounds__(WeighShape<N, NS, HOW>::kThreads, 1)
             __syncwarp();
             if (more) {  // the next unit (the segment ended with this one)
                 unit = at;
-                if (++i == list.n) {
+                if (++i >= list.n) {
                     i = 0;
                     if (++h == int32_t(K)) {
                         h = 0;
                         do {
-                            ++s;
+                            if (++s >= int32_t(a.tok.n_seqs)) {
+                                *dead = 1;
+                                goto loads_done;
+                            }
                             q = kv_seq(a.pages, a.tok, s);
                             list = unit_list(f, q);
                         } while (list.n == 0);
