@@ -446,6 +446,7 @@ t2i_status select(t2i_kv* kv, const t2i_kv_select_desc& d, cudaStream_t stream) 
             c.require(in_place || !overlap(d.weights_out, out, d.weights, in), "weights_out overlaps weights without being them");
             c.require(!overlap(d.weights_out, out, d.kept, kept), "weights_out overlaps kept");
             apart("weights_out", d.weights_out, out);
+            c.require(!overlap(d.weights_out, out, d.counts, per_seq), "weights_out overlaps counts");
         }
         apart("kept", d.kept, kept);
         c.require(!overlap(d.kept, kept, d.counts, per_seq), "kept overlaps counts");

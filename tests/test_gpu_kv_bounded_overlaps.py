@@ -1,5 +1,5 @@
-"""Arrays of weigh and select that share bytes (marked gpu): refused, with nothing launched, wherever a call would read
-what another of its blocks writes; arrays that lie side by side are not."""
+"""Arrays of weigh and select that share bytes (marked gpu): refused, with nothing launched, wherever a block would read or
+write what another writes; arrays that lie side by side are not."""
 import ctypes as C
 
 import pytest
@@ -66,3 +66,16 @@ def test_a_workspace_over_what_a_call_reads_or_writes(lib):
     assert c.store.stats()["launches"] == before
     assert lib.t2i_kv_weigh(c._h, C.byref(WeighDesc(**good, **how)), torch.cuda.current_stream().cuda_stream) == 0
     torch.cuda.synchronize()
+
+
+def test_outputs_of_a_choice_over_one_another():
+    c, lens, _, _ = case(BF, 4, 2, 64, [1, 1], [9, 9])
+    w, kept = torch.rand(2, 2, 20, device=DEV), torch.zeros(2, 2, 5, dtype=torch.int32, device=DEV)
+    room = torch.zeros(1024, device=DEV)
+    out, i = room[:20].view(2, 2, 5), room.view(torch.int32)
+    for at in (0, 7, 19):
+        refused(c, "weights_out overlaps counts",
+                lambda: c.select(w, ints(lens), 5, kept=kept, counts=i[at:at + 2], weights_out=out))
+    refused(c, "weights_out overlaps kept", lambda: c.select(w, ints(lens), 5, kept=i[19:39].view(2, 2, 5), weights_out=out))
+    c.select(w, ints(lens), 5, kept=kept, counts=i[20:22], weights_out=out)          # behind them
+    assert i[20:22].tolist() == [5, 5] and torch.equal(out, torch.gather(w, 2, kept.long()))
