@@ -330,10 +330,13 @@ t2i_status commit(t2i_kv* kv, const t2i_kv_commit_desc& d, cudaStream_t stream) 
     return launch(kv, "kv_commit", [&] { return launch_kv_commit(a, stream); });
 }
 
-// Rows [n_seqs][n_heads][width] of 4 bytes that a call writes lie apart.
+// Rows [n_seqs][n_heads][width] of 4 bytes that a call writes lie apart, those of a sequence or those of a head together.
 void rows_apart(Checks& c, const char* what, uint32_t n_seqs, uint32_t n_heads, uint64_t width, uint64_t seq_stride, uint64_t head_stride) {
-    c.require((n_heads == 1 || (head_stride >= width && head_stride <= kMaxStride)) &&
-                  (n_seqs == 1 || (seq_stride >= (n_heads - 1) * head_stride + width && seq_stride <= kMaxStride)), what);
+    auto nested = [&](uint32_t n_in, uint64_t in, uint32_t n_out, uint64_t out) {
+        return (n_in == 1 || (in >= width && in <= kMaxStride)) &&
+               (n_out == 1 || (out >= Wide(n_in - 1) * in + width && out <= kMaxStride));
+    };
+    c.require(nested(n_heads, head_stride, n_seqs, seq_stride) || nested(n_seqs, seq_stride, n_heads, head_stride), what);
 }
 uint64_t rows_bytes(uint32_t n_seqs, uint32_t n_heads, uint64_t width, uint64_t seq_stride, uint64_t head_stride) {
     return at_most((Wide(n_seqs - 1) * seq_stride + Wide(n_heads - 1) * head_stride + width) * 4);
