@@ -562,14 +562,16 @@ typedef struct t2i_kv_weigh_desc {
     float* weights;         /* device, [n_seqs][kv_heads][n_slots]           */
     uint64_t q_stride;      /* of several tokens q_heads * head_dim or more  */
     uint64_t seq_stride;    /* elements of weights from sequence to sequence, */
-    uint64_t head_stride;   /* and from head to head: rows do not overlap    */
+    uint64_t head_stride;   /* and from head to head: rows do not overlap, and
+                               those of a sequence or a head lie together    */
     const float* slopes;    /* these as in t2i_kv_attend_desc                */
     const int32_t* spans;
     uint32_t q_heads;
     uint32_t n_slots;       /* of a row of weights; others are not counted   */
     uint32_t window;
     uint32_t sinks;
-    uint32_t max_len;
+    uint32_t max_len;       /* likewise; another one may split sums elsewhere
+                               (their last bits)                             */
     float scale;
     float softcap;
     float decay;            /* of the weights so far                         */
@@ -585,7 +587,8 @@ typedef struct t2i_kv_weigh_desc {
  * Slots of the new tokens: the sum. Others are left as they are. A query
  * whose lse is -infinity (and whose q is finite) counts nothing. Keys may hold anything where no
  * token sees them. Sums are fp32, in an order that does not depend on timing.
- * Neither weights nor the workspace share a byte with another array.         */
+ * Neither weights nor the workspace share a byte with another array. A prompt's
+ * chunk and other sequences' single tokens go faster as two calls.           */
 t2i_status t2i_kv_weigh(t2i_kv* kv, const t2i_kv_weigh_desc* desc, void* cuda_stream);
 
 /* Workspace bytes that t2i_kv_weigh needs for such a batch at most.         */
@@ -619,7 +622,8 @@ typedef struct t2i_kv_select_desc {
  * and -0 are equal; NaN is below every number.) kept receives them, ascending;
  * what lies behind n in kept and weights_out is left as it is. A sequence whose
  * lens is negative or above n_slots has no slots. No output shares a byte
- * with another array, but weights_out with weights.                         */
+ * with another array, but weights_out with weights; its rows lie as weights'
+ * do in t2i_kv_weigh.                                                        */
 t2i_status t2i_kv_select(t2i_kv* kv, const t2i_kv_select_desc* desc, void* cuda_stream);
 
 typedef struct t2i_kv_evict_desc {

@@ -33,7 +33,7 @@ constexpr uint32_t kMaxDim = 128;
 constexpr uint32_t kMaxHeads = 1024;
 constexpr uint32_t kMaxLayers = 1024;
 constexpr uint32_t kMinPageTokens = 8;
-constexpr uint32_t kMaxSlots = 0x7FFFFF00u;  // of a sequence (slots are counted in 32 bits with a sign, up to the end of a tile of 128)
+constexpr uint32_t kMaxSlots = 0x7FFFFF00u;  // of a sequence (slots are counted in 32 bits with a sign, up to the end of a unit of 256)
 constexpr uint64_t kMaxStride = uint64_t(1) << 40;
 
 struct DeviceScope {

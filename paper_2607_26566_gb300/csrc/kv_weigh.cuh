@@ -7,8 +7,10 @@
 // that add up: its keys are loaded once (TMA), its queries, 128 columns at a time, once for both halves.
 //
 // Two regimes. Where all queries of a key head are one column tile or two (a decoding step, an observation window) the
-// call is bound by reading the keys: each block streams them through a ring. Of more (a prompt) it is bound by the sums
-// beside the products, an exponential a score; keys stay while column tiles pass.
+// keys stream through a ring: one tile over long contexts is bound by reading them, two by what a unit takes (3.15 us, of
+// which the sums of two steps are 2.1). Of more (a prompt) keys stay while column tiles pass, and the call is bound by
+// shared memory, whose data stage is 90% busy: 51% with threads' reads, in the loop the log-sum-exps, 38% with the products'
+// operands; beside it an exponential a score.
 //
 // Work split: the column tiles (steps) of all units, in order, are cut into equal runs, one to an SM. A unit that lies in
 // several runs is joined by a second kernel, in the order of the runs; with one or two tiles units are not cut. Results do
@@ -19,8 +21,8 @@
 // weight whose score and lse are 30, 3e-7 of a prompt's sums.
 //
 // Measured, 32 heads over 8 of 128: one token over 700 slots 5.6 us; a token each of 64 sequences of up to 16k slots (1.16
-// GB) 177 us, 6.5 TB/s; a prompt of 8190 tokens 242-261 us, 1.05-1.14 PFLOP/s of what is visible, where products and loads
-// alone (nothing added up) took 193; 32 tokens of nine prompts of up to 7k, 28 heads over 4, 22-24 us. (With half of a
+// GB) 178 us, 6.5 TB/s; a prompt of 8190 tokens 244-263 us, 1.05-1.13 PFLOP/s of what is visible, where products and loads
+// alone (nothing added up) took 193; 32 tokens of nine prompts of up to 7k, 28 heads over 4, 23-24 us. (With half of a
 // tile's columns to each group of warps, in place of tiles in turn, the last two took 257 and 23.5.)
 #pragma once
 

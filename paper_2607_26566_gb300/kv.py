@@ -297,7 +297,9 @@ class KVCache:
         has ``decay`` times what it had added (0: nothing, whatever that was);
         the new tokens' slots start with their sum, slots behind them are left as
         they are. The last tokens of a prompt alone, as new tokens, give what an
-        observation window sees."""
+        observation window sees. ``weights`` shares no memory with what the call
+        reads; its heads may lie inside its sequences or around them. A prompt's
+        chunk and other sequences' single tokens go faster as two calls."""
         st = _kv.weigh(self._c, q, lens, lse, weights, starts, max_new, layer, self._scale if scale is None else scale, softcap,
                        slopes, window, sinks, spans, decay, max_len, table, stream)
         if st:
@@ -333,7 +335,7 @@ class KVCache:
         or in all of them. ``kept``: int32 [sequences, kv_heads, any], ascending
         (one list for all heads: ``kept.expand(-1, kv_heads, -1)``). The sequence
         then has counts[s] tokens; a token's position is not its slot any more
-        (``append`` takes ``positions``)."""
+        (``append`` takes ``positions``). Pages behind them stay with the sequence."""
         st = _kv.evict(self._c, kept, counts, 0 if layer is None else layer, self.layers if layer is None else 1, table, stream)
         if st:
             self._done(st)
